@@ -284,6 +284,120 @@ int dv_stream_flush(dv_handle* h, float* out_embeddings, uint8_t* out_masks, flo
 int dv_compact(const uint8_t* masks, int n_frames, int n_tokens, int group_size, int32_t* idx,
                int32_t* pos, int32_t* qoff, int32_t* count, hipStream_t stream);
 
+/* ---- Operators on token rows and their 8-bit cache -----------------------------------------------
+ * For what follows the encoder (a query over a video's tokens: Section 2.1's query engine) and for
+ * streams that hold many references (cached memory compaction, Section 5.2): rotary positions
+ * with a time, a height and a width axis, and a paged cache of keys and values in 8 bits that rows
+ * are written to, read back from and attended over.  Rows are fp32 or bf16 (DV_F32, DV_BF16): row
+ * r, head h, channel c lies at r * stride + h * head_dim + c elements, stride >= heads * head_dim.
+ * All calls are asynchronous on `stream`, allocate nothing, keep no state of their own and take
+ * the current device; calls on different streams do not disturb one another as long as their
+ * buffers differ (workspaces among them).  Rows that belong to no sequence are left as they were. */
+
+/* Rates of rotary positions (host data, held by the caller; dv_rotary_init fills it). */
+#define DV_ROTARY_HALVES 0   /* pair i is channels i and dim/2 + i */
+#define DV_ROTARY_PAIRS 1    /* pair i is channels 2i and 2i + 1 */
+typedef struct dv_rotary_plan {
+    int dim;            /* leading channels of a head that are turned, 2 .. 128: twice the sum below */
+    int section[3];     /* pairs that turn with the time, height and width position, in this order */
+    int layout;         /* DV_ROTARY_HALVES or DV_ROTARY_PAIRS */
+    uint64_t turn[64];  /* 2^64 / (2 pi) times each pair's rate */
+} dv_rotary_plan;
+
+/* Fills *plan.  Pair i turns by its axis's position times base^(-2i/dim) radians, or with per_axis
+ * != 0 times base^(-j/s), j its place among the s pairs of its axis (every axis then covers the
+ * whole range of rates).  Serves the positions of Section 2.3's tokens (time of the frame, row and
+ * column of the patch).  Errors: DV_EINVAL (NULL, a negative section, their sum outside
+ * [1, 64], unknown layout, base not a finite number >= 1). */
+int dv_rotary_init(dv_rotary_plan* plan, const int section[3], int layout, int per_axis, double base);
+
+/* Turns every head of `rows` rows: for each pair (x, y) and its angle w, (x cos w - y sin w,
+ * y cos w + x sin w), computed in fp32 and rounded once; channels past plan->dim are copied.
+ * positions: device int32 [rows, 3], any values (angles are exact to 1e-9 radians at all of them);
+ * negated positions undo the turn, which is also its gradient.  out may be x with the same stride
+ * (in place), and must not overlap it otherwise.  The position part of Section 2.3's attention.
+ * Errors: DV_EINVAL (NULL pointer, bad plan, dtype, rows < 0, heads or head_dim < 1, head_dim odd or
+ * below plan->dim, stride too small, different strides in place, rows of more than 2^24 or in all 2^33
+ * channels or more), DV_EHIP.  rows = 0 does nothing, and the pointers may be NULL then. */
+int dv_rotary(const dv_rotary_plan* plan, int dtype, const void* x, long long x_stride, int rows,
+              int heads, int head_dim, const int32_t* positions, void* out, long long out_stride,
+              hipStream_t stream);
+
+/* A paged cache of keys and values (device buffers of the caller, 16-byte aligned codes).
+ * Codes are OCP e4m3 bytes; a page and head has one scale for its keys and one for its values.
+ * Keys lie [pages, kv_heads, page_tokens, head_dim], values [pages, kv_heads, head_dim,
+ * page_tokens], scales [pages, kv_heads]; a value is its code times its scale.  Neither codes nor
+ * scales need initialising: a page is defined by the first write to its first place. */
+typedef struct dv_cache {
+    uint8_t* k;
+    uint8_t* v;
+    float* k_scale;
+    float* v_scale;
+    int pages;
+    int page_tokens;   /* 16, 32, 64 or 128 */
+    int kv_heads;
+    int head_dim;      /* a multiple of 16, at most 128 */
+} dv_cache;
+
+/* The sequences of a call: place p of sequence s lies in page table[s * table_pages + p /
+ * page_tokens] (device int32; NULL: page s * table_pages + p / page_tokens).  An entry that is no
+ * page of the cache (negative, or >= pages) means that the page is not there: what is written to it
+ * is dropped, it reads as zeros, and attention does not see it; the same goes for places past the
+ * table.  Rows of sequence s: offsets[s] .. offsets[s + 1] - 1 of the call's `rows` rows (device
+ * int32 [n_seqs + 1], not descending; rows from offsets[n_seqs] on are padding), or with offsets
+ * NULL row s alone.  Common errors: DV_EINVAL (NULL pointer, n_seqs or table_pages < 1, rows < 0, rows
+ * < n_seqs without offsets, page_tokens, kv_heads, head_dim or pages out of range, misaligned
+ * codes, table NULL and n_seqs * table_pages > pages, table_pages * page_tokens > 2^30, unknown
+ * dtype, stride too small, sizes past one launch's 2^32 threads), DV_EHIP.  rows = 0 does nothing, and row
+ * pointers may be NULL then. */
+
+/* Writes rows of keys and values to places starts[s] .. of each sequence (device int32 [n_seqs]; a
+ * sequence with a negative start is passed over).  A page and head takes the least power of two
+ * >= 2^-126 of which its largest magnitude is at most 448 times; codes are rounded to nearest
+ * even.  Writing a page's first place starts the page anew; writing further places keeps the
+ * tokens before them and lets the scale grow, which rescales those tokens' codes (each rounded again
+ * only where it falls below 2^-6 of the scale).  Infinities and NaN are stored as NaN and do not
+ * count for the scale.  Places after the last one written are undefined.  With `plan`, keys are
+ * turned by positions[row] (device int32 [rows, 3]) before they are quantised, and q rows (q_heads
+ * heads; NULL for none) are turned into q_out, which may be q with the same stride: one launch for a
+ * decoding step.  No two sequences of a call may write the same page.  (The memory compaction of
+ * Section 5.2, applied to what is kept between calls.)
+ * Errors: the common ones, and DV_EINVAL for q without plan or q_out, q_heads < 1, plan without
+ * positions, plan->dim > head_dim. */
+int dv_cache_write(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
+                   const int32_t* offsets, const int32_t* starts, int dtype, const void* k,
+                   long long k_stride, const void* v, long long v_stride, int rows,
+                   const dv_rotary_plan* plan, const int32_t* positions, const void* q,
+                   long long q_stride, int q_heads, void* q_out, long long q_out_stride,
+                   hipStream_t stream);
+
+/* Reads places starts[s] .. of each sequence into rows of keys and values (code times scale, rounded
+ * to dtype; exact in both), the inverse of dv_cache_write's layout (Section 5.2).  Errors: the common
+ * ones. */
+int dv_cache_read(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
+                  const int32_t* offsets, const int32_t* starts, int dtype, void* k,
+                  long long k_stride, void* v, long long v_stride, int rows, hipStream_t stream);
+
+/* Attention of q_heads heads per row over each sequence's first lengths[s] places (device int32; cut
+ * to the table, negative means 0): out = softmax(scale q k) v in fp32 arithmetic, q_heads a
+ * multiple of kv_heads, query head i reading key/value head i / (q_heads / kv_heads).  causal != 0:
+ * the rows are the sequence's last places, and each sees those up to its own (the i-th of n rows
+ * the first lengths[s] - n + i + 1).  A row that sees nothing gets zeros.  What a row does not see, NaN
+ * and infinities among it, does not reach it.  max_rows: an upper bound of the rows of any sequence, 0 if
+ * unknown; it serves the choice of kernel only.  workspace: device scratch of
+ * dv_cache_attention_workspace bytes for the same arguments (16-byte aligned; NULL where that is 0),
+ * of this call alone until it has run.  (The attention of Section 2.3 for a query engine's reads of
+ * cached tokens.)  Errors: the common ones, and DV_EINVAL for q_heads no multiple of kv_heads,
+ * q_heads * rows >= 2^31, a scale that is not finite and positive, max_rows < 0, out rows that do not
+ * start on four elements, a workspace that is too small or misaligned. */
+int dv_cache_attention_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets,
+                                 int rows, int q_heads, int max_rows, size_t* bytes);
+int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
+                       const int32_t* offsets, const int32_t* lengths, int dtype, const void* q,
+                       long long q_stride, int rows, int q_heads, int max_rows, float scale,
+                       int causal, void* out, long long out_stride, void* workspace,
+                       size_t workspace_bytes, hipStream_t stream);
+
 /* Stage timing (measurement support; the stages are the steps of Sections 2.3 and 3.3) with
  * HIP events recorded on the encode stream around every
  * launch of the selected stages.  stage_mask: bit s selects stage s (0 = off,

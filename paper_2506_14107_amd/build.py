@@ -12,7 +12,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_lib")
 LIB = os.path.join(OUT_DIR, "libdejavu.so")
-SOURCES = ["api.hip", "rowops.hip", "gemm.hip", "attention.hip", "probe.hip"]
+SOURCES = ["api.hip", "rowops.hip", "gemm.hip", "attention.hip", "cache.hip",
+           "cache_attn.hip", "probe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-fno-gpu-rdc",

@@ -51,6 +51,7 @@
 #include <vector>
 
 #include "../../include/dejavu.h"
+#include "cache_plan.h"
 #include "dv_internal.h"
 
 using namespace dv;
@@ -889,6 +890,93 @@ int stream_impl(dv_handle* h, const float* frames, int n, int G, float tau, cons
     return DV_OK;
 }
 
+// ---- operators on rows and the 8-bit cache ------------------------------------------------------
+int check_plan(const dv_rotary_plan* p) {
+    if (!p) return fail(DV_EINVAL, "rotary plan is NULL");
+    if (p->layout != DV_ROTARY_HALVES && p->layout != DV_ROTARY_PAIRS)
+        return fail(DV_EINVAL, "unknown rotary layout %d", p->layout);
+    long long sum = 0;
+    for (int s : p->section) {
+        if (s < 0) return fail(DV_EINVAL, "rotary sections must be >= 0 (got %d)", s);
+        sum += s;
+    }
+    if (sum < 1 || sum > 64) return fail(DV_EINVAL, "rotary sections must sum to 1 .. 64 (got %lld)", sum);
+    if (p->dim != 2 * sum) return fail(DV_EINVAL, "rotary plan is not initialised (dv_rotary_init)");
+    return DV_OK;
+}
+
+RotaryPlan kernel_plan(const dv_rotary_plan* p) {
+    RotaryPlan r{};
+    if (!p) return r;
+    memcpy(r.turn, p->turn, sizeof r.turn);
+    r.dim = p->dim;
+    r.end0 = p->section[0];
+    r.end1 = p->section[0] + p->section[1];
+    r.pairs = p->layout == DV_ROTARY_PAIRS;
+    return r;
+}
+
+int check_dtype(int dtype) {
+    return dtype == DV_F32 || dtype == DV_BF16 ? DV_OK : fail(DV_EINVAL, "unknown dtype %d", dtype);
+}
+
+int check_stride(const char* what, long long stride, long long least) {
+    if (stride < least) return fail(DV_EINVAL, "%s stride %lld is below the row's %lld elements", what, stride, least);
+    if (stride > (1ll << 40)) return fail(DV_EINVAL, "%s stride %lld is too large", what, stride);
+    return DV_OK;
+}
+
+constexpr long long MAX_THREADS = (1ll << 32) - 1;   // of one launch
+
+// Cache and sequences of a call, without what the call reads and writes.
+int check_cache(const dv_cache* c, int n_seqs, const int32_t* table, int table_pages, bool offsets, int rows) {
+    if (!c) return fail(DV_EINVAL, "cache is NULL");
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(DV_EINVAL, "a buffer of the cache is NULL");
+    if ((uintptr_t)c->k % 16 || (uintptr_t)c->v % 16) return fail(DV_EINVAL, "the cache's codes must be 16-byte aligned");
+    if (c->pages < 1 || c->kv_heads < 1) return fail(DV_EINVAL, "cache sizes must be >= 1");
+    if (!page_tokens_ok(c->page_tokens))
+        return fail(DV_EINVAL, "page_tokens must be 16, 32, 64 or 128 (got %d)", c->page_tokens);
+    if (c->head_dim < 16 || c->head_dim > 128 || c->head_dim % 16)
+        return fail(DV_EINVAL, "head dim %d must be a multiple of 16, <= 128", c->head_dim);
+    if (n_seqs < 1 || table_pages < 1) return fail(DV_EINVAL, "n_seqs and table_pages must be >= 1");
+    if ((long long)table_pages * c->page_tokens > (1ll << 30))
+        return fail(DV_EINVAL, "table_pages %d: more than 2^30 tokens a sequence", table_pages);
+    if (!table && (long long)n_seqs * table_pages > c->pages)
+        return fail(DV_EINVAL, "without a table %d sequences of %d pages need more than the cache's %d pages", n_seqs,
+                    table_pages, c->pages);
+    if (rows < 0) return fail(DV_EINVAL, "rows must be >= 0 (got %d)", rows);
+    if (!offsets && rows > 0 && rows < n_seqs)
+        return fail(DV_EINVAL, "without offsets every sequence has a row: %d rows for %d sequences", rows, n_seqs);
+    if (page_slots(offsets ? (const int*)c->k : nullptr, n_seqs, rows, page_shift(c->page_tokens)) * 2 * c->kv_heads *
+            256 > MAX_THREADS)
+        return fail(DV_EINVAL, "%d rows of %d sequences with %d heads are too many for one call", rows, n_seqs,
+                    c->kv_heads);
+    return DV_OK;
+}
+
+CacheView view_of(const dv_cache* c) {
+    return {c->k, c->v, c->k_scale, c->v_scale, c->pages, c->page_tokens, c->kv_heads, c->head_dim};
+}
+
+int device_cus() {
+    int dev = 0, cus = 0;
+    if (hipGetDevice(&dev) != hipSuccess ||
+        hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
+        cus = 0;   // planned as for 256
+    return cus;
+}
+
+int check_queries(const dv_cache* c, int n_seqs, int rows, int q_heads, int max_rows) {
+    if (q_heads < 1 || q_heads % c->kv_heads)
+        return fail(DV_EINVAL, "q_heads %d must be a multiple of the cache's %d heads", q_heads, c->kv_heads);
+    if (max_rows < 0) return fail(DV_EINVAL, "max_rows must be >= 0 (got %d)", max_rows);
+    const long long tiles = (long long)rows * (q_heads / c->kv_heads) + 2ll * n_seqs;
+    if ((long long)rows * q_heads >= (1ll << 31) || tiles * c->kv_heads > (1ll << 31) ||
+        (tiles / 16 + 2ll * n_seqs) * c->kv_heads * 256 > MAX_THREADS)
+        return fail(DV_EINVAL, "%d rows of %d heads are too many for one call", rows, q_heads);
+    return DV_OK;
+}
+
 template <class T>
 T* carve(char*& p, size_t count) {
     T* r = (T*)p;
@@ -1225,6 +1313,168 @@ int dv_compact(const uint8_t* masks, int n_frames, int n_tokens, int group_size,
     launch_scan(qoff, 1, n_frames, 0, qoff, count, stream);
     launch_compact(masks, qoff, n_frames, n_tokens, group_size, idx, pos, nullptr, nullptr,
                    stream);
+    HIP_TRY(hipGetLastError());
+    return DV_OK;
+}
+
+int dv_rotary_init(dv_rotary_plan* plan, const int section[3], int layout, int per_axis, double base) {
+    if (!plan || !section) return fail(DV_EINVAL, "NULL argument");
+    if (!(base >= 1) || std::isinf(base)) return fail(DV_EINVAL, "rotary base must be a finite number >= 1");
+    dv_rotary_plan p{};
+    memcpy(p.section, section, sizeof p.section);
+    p.layout = layout;
+    long long sum = 0;
+    for (int s : p.section) sum += s;
+    p.dim = sum >= 1 && sum <= 64 ? (int)(2 * sum) : 0;
+    const int rc = check_plan(&p);
+    if (rc) return rc;
+    const long double turns = 0x1p64L / 6.283185307179586476925286766559L;   // 2^64 / (2 pi)
+    for (int axis = 0, i = 0; axis < 3; ++axis)
+        for (int j = 0; j < section[axis]; ++j, ++i) {
+            const long double power = per_axis ? (long double)j / section[axis] : 2.0L * i / p.dim;
+            p.turn[i] = (uint64_t)roundl(turns * powl((long double)base, -power));
+        }
+    *plan = p;
+    return DV_OK;
+}
+
+int dv_rotary(const dv_rotary_plan* plan, int dtype, const void* x, long long x_stride, int rows, int heads,
+              int head_dim, const int32_t* positions, void* out, long long out_stride, hipStream_t stream) {
+    int rc = check_plan(plan);
+    if (rc || (rc = check_dtype(dtype))) return rc;
+    if (rows > 0 && (!x || !positions || !out)) return fail(DV_EINVAL, "NULL argument");
+    if (rows < 0 || heads < 1 || head_dim < 1) return fail(DV_EINVAL, "rows must be >= 0, heads and head_dim >= 1");
+    if (plan->dim > head_dim || head_dim % 2)
+        return fail(DV_EINVAL, "head dim %d must be even and hold the %d turned channels", head_dim, plan->dim);
+    const long long wide = (long long)heads * head_dim;
+    if (wide > (1 << 24) || rows * wide >= (1ll << 33)) return fail(DV_EINVAL, "rows of %lld channels: too many for one call", wide);
+    if ((rc = check_stride("x", x_stride, wide)) || (rc = check_stride("out", out_stride, wide))) return rc;
+    if (x && x == out && x_stride != out_stride) return fail(DV_EINVAL, "in place the strides must be the same");
+    if (rows == 0) return DV_OK;
+    RotaryArgs a{};
+    a.x = x;
+    a.out = out;
+    a.x_stride = x_stride;
+    a.out_stride = out_stride;
+    a.rows = rows;
+    a.heads = heads;
+    a.dh = head_dim;
+    a.pos = positions;
+    a.rot = kernel_plan(plan);
+    launch_rotary(dtype == DV_BF16, a, stream);
+    HIP_TRY(hipGetLastError());
+    return DV_OK;
+}
+
+int dv_cache_write(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages, const int32_t* offsets,
+                   const int32_t* starts, int dtype, const void* k, long long k_stride, const void* v,
+                   long long v_stride, int rows, const dv_rotary_plan* plan, const int32_t* positions, const void* q,
+                   long long q_stride, int q_heads, void* q_out, long long q_out_stride, hipStream_t stream) {
+    int rc = check_cache(cache, n_seqs, table, table_pages, offsets != nullptr, rows);
+    if (rc || (rc = check_dtype(dtype))) return rc;
+    if (!starts || (rows > 0 && (!k || !v))) return fail(DV_EINVAL, "NULL argument");
+    const long long wide = (long long)cache->kv_heads * cache->head_dim;
+    if ((rc = check_stride("k", k_stride, wide)) || (rc = check_stride("v", v_stride, wide))) return rc;
+    if (plan) {
+        if ((rc = check_plan(plan))) return rc;
+        if (rows > 0 && !positions) return fail(DV_EINVAL, "rotary positions are NULL");
+        if (plan->dim > cache->head_dim)
+            return fail(DV_EINVAL, "head dim %d does not hold the %d turned channels", cache->head_dim, plan->dim);
+    }
+    if (q) {
+        if (!plan || !q_out) return fail(DV_EINVAL, "q is there to be turned: it needs a rotary plan and q_out");
+        if (q_heads < 1 || (long long)rows * q_heads * cache->head_dim >= (1ll << 32))
+            return fail(DV_EINVAL, "%d rows of %d query heads are too few or too many for one call", rows, q_heads);
+        const long long q_wide = (long long)q_heads * cache->head_dim;
+        if ((rc = check_stride("q", q_stride, q_wide)) || (rc = check_stride("q_out", q_out_stride, q_wide))) return rc;
+        if (q == q_out && q_stride != q_out_stride) return fail(DV_EINVAL, "in place the strides must be the same");
+    }
+    if (rows == 0) return DV_OK;
+    WriteArgs a{};
+    a.c = view_of(cache);
+    a.seq = {n_seqs, table_pages, rows, table, offsets, starts};
+    a.k = k;
+    a.v = v;
+    a.q = q;
+    a.q_out = q_out;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q_stride = q_stride;
+    a.qo_stride = q_out_stride;
+    a.q_heads = q ? q_heads : 0;
+    a.pos = positions;
+    a.rot = kernel_plan(plan);
+    launch_cache_write(dtype == DV_BF16, a, stream);
+    HIP_TRY(hipGetLastError());
+    return DV_OK;
+}
+
+int dv_cache_read(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages, const int32_t* offsets,
+                  const int32_t* starts, int dtype, void* k, long long k_stride, void* v, long long v_stride, int rows,
+                  hipStream_t stream) {
+    int rc = check_cache(cache, n_seqs, table, table_pages, offsets != nullptr, rows);
+    if (rc || (rc = check_dtype(dtype))) return rc;
+    if (!starts || (rows > 0 && (!k || !v))) return fail(DV_EINVAL, "NULL argument");
+    const long long wide = (long long)cache->kv_heads * cache->head_dim;
+    if ((rc = check_stride("k", k_stride, wide)) || (rc = check_stride("v", v_stride, wide))) return rc;
+    if (rows == 0) return DV_OK;
+    ReadArgs a{};
+    a.c = view_of(cache);
+    a.seq = {n_seqs, table_pages, rows, table, offsets, starts};
+    a.k = k;
+    a.v = v;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    launch_cache_read(dtype == DV_BF16, a, stream);
+    HIP_TRY(hipGetLastError());
+    return DV_OK;
+}
+
+int dv_cache_attention_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets, int rows,
+                                 int q_heads, int max_rows, size_t* bytes) {
+    if (!bytes) return fail(DV_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    static const int32_t some = 0;   // the size does not depend on what a table holds
+    int rc = check_cache(cache, n_seqs, &some, table_pages, with_offsets != 0, rows);
+    if (rc || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows))) return rc;
+    *bytes = cache_attn_plan(n_seqs, rows, with_offsets != 0, table_pages, cache->page_tokens, cache->kv_heads,
+                             q_heads, cache->head_dim, device_cus()).bytes;
+    return DV_OK;
+}
+
+int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
+                       const int32_t* offsets, const int32_t* lengths, int dtype, const void* q, long long q_stride,
+                       int rows, int q_heads, int max_rows, float scale, int causal, void* out, long long out_stride,
+                       void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    int rc = check_cache(cache, n_seqs, table, table_pages, offsets != nullptr, rows);
+    if (rc || (rc = check_dtype(dtype)) || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows))) return rc;
+    if (!lengths || (rows > 0 && (!q || !out))) return fail(DV_EINVAL, "NULL argument");
+    if (!(scale > 0) || std::isinf(scale)) return fail(DV_EINVAL, "scale must be finite and positive");
+    const long long wide = (long long)q_heads * cache->head_dim;
+    if ((rc = check_stride("q", q_stride, wide)) || (rc = check_stride("out", out_stride, wide))) return rc;
+    if ((uintptr_t)out % (dtype == DV_BF16 ? 8 : 16) || out_stride % 4)
+        return fail(DV_EINVAL, "out rows must start on four elements");
+    const CacheAttnPlan p = cache_attn_plan(n_seqs, rows, offsets != nullptr, table_pages, cache->page_tokens,
+                                            cache->kv_heads, q_heads, cache->head_dim, device_cus());
+    if (p.bytes && (!workspace || workspace_bytes < p.bytes || (uintptr_t)workspace % 16))
+        return fail(DV_EINVAL, "the call needs a 16-byte aligned workspace of %zu bytes (got %zu)", p.bytes,
+                    workspace ? workspace_bytes : 0);
+    if (rows == 0) return DV_OK;
+    CacheAttnArgs a{};
+    a.c = view_of(cache);
+    a.seq = {n_seqs, table_pages, rows, table, offsets, lengths};
+    a.q = q;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.o_stride = out_stride;
+    a.q_heads = q_heads;
+    a.scale = scale;
+    a.causal = causal;
+    a.chunk = p.chunk;
+    a.splits = p.splits;
+    a.slots = p.slots;
+    a.part = (float*)workspace;
+    launch_cache_attention(dtype == DV_BF16, a, stream);
     HIP_TRY(hipGetLastError());
     return DV_OK;
 }

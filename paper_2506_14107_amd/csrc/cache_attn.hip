@@ -1,0 +1,392 @@
+// Attention of query rows over the paged 8-bit cache.
+//
+// A tile is R packed rows of one sequence and key/value head: packed row r is query row r / G, head
+// h G + r % G, so that the G query heads that share keys share their loads.  As in the encoder's
+// attention every quantity is kept with one query per lane:
+//   S^T = K . Q^T     A = 16 keys, B = 16 queries (MFMA 16x16x32, fp32 accumulate): lane l gets the scores of
+//                     query l % 16 against 4 keys of each 16
+//   O^T += V^T . P^T  the probabilities stay in the lanes that computed them
+// A step takes 64 keys.  Row m of score tile t is key (m / 4) 16 + 4 t + m % 4 of the step, so that lane group
+// g = l / 16 ends up with the scores of the 16 keys 16 g .. 16 g + 15: the order in which the value
+// product contracts them, and 16 bytes of one channel's row of a page.
+// Codes become bf16 exactly (3 fraction bits, power-of-two scales) by v_cvt_scalef32_pk_bf16_fp8, which
+// applies the scale.  The softmax is one pass with a running maximum and sum in fp32; probabilities are
+// rounded to bf16 for the value product, a relative 2^-9 each, as in the encoder.  fp32 queries are three
+// bf16 terms (24 bits), and so are their probabilities: K and V being exact in bf16, three products
+// give fp32 results at the bf16 matrix rate.
+#include "cache_plan.h"
+
+namespace dv {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int TS = 4, TR = 1 << TS;   // packed rows of a tile
+constexpr int STEP = 64;   // keys of a step
+constexpr int WAVES = 4;
+
+// f of the two values that lanes whose numbers differ in one bit (4 or 5) hold, in both: the swap gives
+// one lane's value in its first result and the other's in its second.  (The elements are copied before
+// the bit cast, which takes element 0 of a vector for any.)
+template <int BIT, class F>
+__device__ __forceinline__ float across(float x, F f) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = BIT == 4 ? __builtin_amdgcn_permlane16_swap(u, u, false, false)
+                            : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned a = r[0], b = r[1];
+    return f(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+// maximum and sum over the four 16-lane groups, in every lane
+__device__ __forceinline__ float group_max(float x) {
+    const auto f = [](float a, float b) { return fmaxf(a, b); };
+    return across<5>(across<4>(x, f), f);
+}
+__device__ __forceinline__ float group_sum(float x) {
+    const auto f = [](float a, float b) { return a + b; };
+    return across<5>(across<4>(x, f), f);
+}
+
+// eight codes to bf16, times a power of two
+__device__ __forceinline__ bf16x8 decode8(uint32_t lo, uint32_t hi, float scale) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return (bf16x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// x as T bf16 terms: the first its rounding, each next the rounding of what is left
+template <int T>
+__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&t)[T]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float rest = x[e];
+#pragma unroll
+        for (int k = 0; k < T; ++k) {
+            t[k][e] = (__bf16)rest;
+            if (k + 1 < T) rest -= (float)t[k][e];
+        }
+    }
+}
+// bytes of w that are NaN codes
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+    const uint32_t x = w & 0x7F7F7F7Fu;
+    return (x + 0x01010101u) & 0x80808080u;
+}
+
+template <int SHIFT>
+__device__ __forceinline__ Tile tile_at(const CacheAttnArgs& a, long long u) {
+    const int G = a.q_heads / a.c.kv_heads;
+    const int s = a.seq.offsets ? find_seq(a.seq.offsets, a.seq.n_seqs, G, SHIFT, 1, u)
+                                : (int)(u / ((G + (1 << SHIFT) - 1) >> SHIFT));
+    return tile_of(a.seq, a.c.page_tokens, G, SHIFT, a.causal != 0, s, u);
+}
+
+template <bool BF>
+__device__ __forceinline__ void store4(void* out, size_t at, f32x4 x) {
+    if constexpr (BF) {
+        const bf16x4 r = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+        *(bf16x4*)((uint16_t*)out + at) = r;
+    } else {
+        *(f32x4*)((float*)out + at) = x;
+    }
+}
+
+// partial results: per tile, head and split TR rows of DH fp32, then TR (maximum, sum)
+__host__ __device__ inline size_t part_floats(int dh) { return (size_t)TR * (dh + 2); }
+
+// One tile, head and split of the keys per block; its wavefronts take the steps of the split in turn and
+// join their results through LDS.
+template <int DH, bool BF>
+__global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
+    constexpr int NT = BF ? 1 : 3;             // bf16 terms of queries and probabilities
+    constexpr int KS = (DH + 31) / 32;         // 32-channel steps of S^T
+    constexpr int CT = DH / 16;                // 16-channel tiles of O^T
+    constexpr bool WIDE = DH % 64 == 0;        // 16-byte key loads
+    __shared__ float s_o[WAVES][TR][DH + 4];
+    __shared__ float s_m[WAVES][TR], s_l[WAVES][TR];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int H = a.c.kv_heads, pt = a.c.page_tokens, shift = page_shift(pt);
+    const int h = blockIdx.x % H;
+    const long long u = blockIdx.x / H;
+    const Tile t = tile_at<TS>(a, u);
+    if (t.seq < 0) return;
+    const int k0 = blockIdx.y * a.chunk, k1 = min(t.end, k0 + a.chunk);
+    if (blockIdx.y > 0 && k0 >= k1) return;    // the first split also writes rows that see no key
+    const int G = a.q_heads / H;
+    const int g = lane >> 4, c16 = lane & 15;
+    const float sl2 = a.scale * 1.4426950408889634f;
+
+    // the lane's query: packed row first + c16 (rows past the tile repeat its last one)
+    const int r = t.first + min(c16, t.rows - 1), qi = r / G;
+    const int sees = a.causal ? t.len - t.n + qi + 1 : t.len;
+    const size_t qat = (size_t)(t.row0 + qi) * a.q_stride + (size_t)(h * G + r % G) * DH;
+    bf16x8 qf[KS][NT];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        const int ch = WIDE ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        if (ch < DH) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                x[e] = BF ? bf16_to_f32(((const uint16_t*)a.q)[qat + ch + e]) : ((const float*)a.q)[qat + ch + e];
+        }
+        split8<NT>(x, qf[s]);
+    }
+
+    f32x4 o[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) o[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+
+    for (int kb = k0 + wave * STEP; kb < k1; kb += WAVES * STEP) {
+        // pages: of the key rows that the lane loads (group c16 / 4), and of the group it owns
+        const int kk = kb + (c16 >> 2) * 16, kv = kb + g * 16;
+        const int kp = page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, kk >> shift);
+        const int vp = page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, kv >> shift);
+        const size_t kpage = (size_t)max(kp, 0) * H + h, vpage = (size_t)max(vp, 0) * H + h;
+        const uint8_t* kbase = a.c.k + (kpage * pt + (kk & (pt - 1)) + (c16 & 3)) * DH;
+        const uint8_t* vbase = a.c.v + (vpage * DH + c16) * pt + (kv & (pt - 1));
+        const float ks = a.c.k_scale[kpage];
+        float vs = a.c.v_scale[vpage];
+        uint32_t kw[4][KS][2];
+        u32x4 vw[CT];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint8_t* row = kbase + q * 4 * DH;
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int s = 0; s < KS; s += 2) {
+                    const u32x4 w = *(const u32x4*)(row + s * 32 + g * 16);
+                    kw[q][s][0] = w[0], kw[q][s][1] = w[1], kw[q][s + 1][0] = w[2], kw[q][s + 1][1] = w[3];
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    const int ch = s * 32 + g * 8;
+                    u32x2 w = {0, 0};
+                    if (ch < DH) w = *(const u32x2*)(row + ch);
+                    kw[q][s][0] = w[0], kw[q][s][1] = w[1];
+                }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) vw[c] = *(const u32x4*)(vbase + (size_t)c * 16 * pt);
+
+        float sc[16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bf16x8 kf = decode8(kw[q][s][0], kw[q][s][1], ks);
+#pragma unroll
+                for (int n = NT - 1; n >= 0; --n)
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[s][n], acc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[q * 4 + e] = acc[e];
+        }
+        // keys kv .. kv + 15 belong to the lane; those it does not see, and those of pages that are
+        // not there, get -inf
+        const int live = vp >= 0 ? min(sees, k1) - kv : 0;
+        const bool some = __any(live < 16);
+        uint32_t nans = 0;
+        if (some) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[e] = e < live ? sc[e] : -INFINITY;
+            // values that no row of the tile sees may hold anything, NaN among them, and so may the
+            // scale of a page that has none else: 0
+            const int there = vp >= 0 ? k1 - kv : 0;
+            if (there <= 0) vs = 1.f;
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int b = there - 4 * w;
+                    vw[c][w] &= b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << 8 * b) - 1;
+                    nans |= nan_bytes(vw[c][w]);
+                }
+        }
+        float top = sc[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, sc[e]);
+        top = group_max(top);
+        const float mn = fmaxf(m, top);
+        const float ref = mn == -INFINITY ? 0.f : mn;      // no key seen yet: all probabilities 0
+        const float alpha = __builtin_amdgcn_exp2f((m - ref) * sl2);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) o[c] *= alpha;
+        float p[2][8];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            p[e >> 3][e & 7] = __builtin_amdgcn_exp2f((sc[e] - ref) * sl2);
+            l += p[e >> 3][e & 7];
+        }
+        bf16x8 pf[2][NT];
+        split8<NT>(p[0], pf[0]);
+        split8<NT>(p[1], pf[1]);
+        if (!(some && __any(nans != 0))) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const bf16x8 vf = decode8(vw[c][2 * k], vw[c][2 * k + 1], vs);
+#pragma unroll
+                    for (int n = NT - 1; n >= 0; --n)
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k][n], o[c], 0, 0, 0);
+                }
+        } else {
+            // A NaN value among keys that only some rows see: its products with the other rows'
+            // zero probabilities would be NaN.  The product runs without it, and a product of
+            // indicators tells which outputs it reaches.
+            bf16x8 seen[2];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) seen[e >> 3][e & 7] = (__bf16)(e < live ? 1.f : 0.f);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                f32x4 hit = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t n0 = nan_bytes(vw[c][2 * k]), n1 = nan_bytes(vw[c][2 * k + 1]);
+                    const bf16x8 vf = decode8(vw[c][2 * k] & ~((n0 >> 7) * 255u), vw[c][2 * k + 1] & ~((n1 >> 7) * 255u), vs);
+                    const bf16x8 nf = decode8((n0 >> 7) * 0x38u, (n1 >> 7) * 0x38u, 1.f);   // 0x38: 1
+#pragma unroll
+                    for (int n = NT - 1; n >= 0; --n)
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k][n], o[c], 0, 0, 0);
+                    hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf, seen[k], hit, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[c][e] = hit[e] > 0.f ? __builtin_nanf("") : o[c][e];
+            }
+        }
+    }
+
+    // join the wavefronts
+    l = group_sum(l);
+    if (g == 0) s_m[wave][c16] = m, s_l[wave][c16] = l;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) *(f32x4*)&s_o[wave][c16][c * 16 + g * 4] = o[c];
+    __syncthreads();
+    const bool whole = t.end <= a.chunk;      // no other split has keys
+    float* part = a.part + (((size_t)u * H + h) * a.splits + blockIdx.y) * part_floats(DH);
+    for (int i = tid; i < TR * (DH / 4); i += 256) {
+        const int row = i / (DH / 4), ch = i % (DH / 4) * 4;
+        if (row >= t.rows) break;
+        float top = s_m[0][row];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_m[w][row]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = __builtin_amdgcn_exp2f((s_m[w][row] - ref) * sl2);
+            sum += s_l[w][row] * f;
+            x += *(const f32x4*)&s_o[w][row][ch] * f;
+        }
+        if (whole) {
+            const int pr = t.first + row;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            store4<BF>(a.out, (size_t)(t.row0 + pr / G) * a.o_stride + (size_t)(h * G + pr % G) * DH + ch, x * inv);
+        } else {
+            *(f32x4*)(part + row * DH + ch) = x;
+            if (ch == 0) part[TR * DH + row] = top, part[TR * DH + TR + row] = sum;
+        }
+    }
+}
+
+// Joins the splits of one row: lanes over the channels, groups of lanes over the splits.
+template <bool BF>
+__global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
+    __shared__ f32x4 s_x[256];
+    __shared__ float s_l[256];
+    const int tid = threadIdx.x;
+    const int H = a.c.kv_heads, DH = a.c.head_dim, row = blockIdx.y;
+    const int h = blockIdx.x % H;
+    const long long u = blockIdx.x / H;
+    const Tile t = tile_at<TS>(a, u);
+    if (t.seq < 0 || row >= t.rows || t.end <= a.chunk) return;
+    const int splits = (t.end + a.chunk - 1) / a.chunk;
+    const int lanes = DH / 4, groups = 256 / lanes;
+    const int ch = tid % lanes * 4, grp = tid / lanes;
+    const float sl2 = a.scale * 1.4426950408889634f;
+    const size_t per = part_floats(DH);
+    const float* part = a.part + (((size_t)u * H + h) * a.splits) * per;
+    float top = -INFINITY;
+    for (int s = 0; s < splits; ++s) top = fmaxf(top, part[s * per + TR * DH + row]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    if (grp < groups)
+        for (int s = grp; s < splits; s += groups) {
+            const float* p = part + s * per;
+            const float f = __builtin_amdgcn_exp2f((p[TR * DH + row] - ref) * sl2);
+            sum += p[TR * DH + TR + row] * f;
+            x += *(const f32x4*)(p + row * DH + ch) * f;
+        }
+    s_x[tid] = x;
+    s_l[tid] = sum;
+    __syncthreads();
+    if (grp == 0) {
+        for (int k = 1; k < groups; ++k) x += s_x[k * lanes + tid], sum += s_l[k * lanes + tid];
+        const int G = a.q_heads / H, pr = t.first + row;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        store4<BF>(a.out, (size_t)(t.row0 + pr / G) * a.o_stride + (size_t)(h * G + pr % G) * DH + ch, x * inv);
+    }
+}
+
+template <int DH>
+void launch_dh(bool bf, const CacheAttnArgs& a, dim3 grid, hipStream_t s) {
+    if (bf) cache_attn_k<DH, true><<<grid, 256, 0, s>>>(a);
+    else cache_attn_k<DH, false><<<grid, 256, 0, s>>>(a);
+}
+
+}  // namespace
+
+CacheAttnPlan cache_attn_plan(int n_seqs, int rows, bool offsets, int table_pages, int page_tokens, int kv_heads,
+                              int q_heads, int head_dim, int cus) {
+    CacheAttnPlan p;
+    const int G = q_heads / kv_heads;
+    p.slots = tile_slots(offsets, n_seqs, rows, G, TS);
+    // splits of equal length, so that a ragged batch's long sequences spread over the chip: about four
+    // blocks a compute unit if every sequence is as long as its table, but no less than 256 keys each
+    const long long keys = (long long)table_pages * page_tokens;   // at most 2^30
+    const long long blocks = std::max(1ll, 4ll * (cus > 0 ? cus : 256) / std::max(1ll, p.slots * kv_heads));
+    long long chunk = (keys + blocks - 1) / blocks;
+    chunk = std::max(256ll, (chunk + 255) / 256 * 256);
+    p.chunk = (int)chunk;
+    p.splits = (int)std::max(1ll, (keys + p.chunk - 1) / p.chunk);
+    p.bytes = p.splits > 1 ? (size_t)p.slots * kv_heads * p.splits * part_floats(head_dim) * sizeof(float) : 0;
+    return p;
+}
+
+void launch_cache_attention(bool bf, const CacheAttnArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)(a.slots * a.c.kv_heads), (unsigned)a.splits);
+    switch (a.c.head_dim) {
+        case 16: launch_dh<16>(bf, a, grid, s); break;
+        case 32: launch_dh<32>(bf, a, grid, s); break;
+        case 48: launch_dh<48>(bf, a, grid, s); break;
+        case 64: launch_dh<64>(bf, a, grid, s); break;
+        case 80: launch_dh<80>(bf, a, grid, s); break;
+        case 96: launch_dh<96>(bf, a, grid, s); break;
+        case 112: launch_dh<112>(bf, a, grid, s); break;
+        default: launch_dh<128>(bf, a, grid, s); break;
+    }
+    if (a.splits > 1) {
+        const dim3 join((unsigned)(a.slots * a.c.kv_heads), TR);
+        if (bf) cache_join_k<true><<<join, 256, 0, s>>>(a);
+        else cache_join_k<false><<<join, 256, 0, s>>>(a);
+    }
+}
+
+}  // namespace dv

@@ -1,0 +1,128 @@
+// Where tokens lie in the paged 8-bit cache and how the launches of its operators are cut: functions of
+// sizes and of the sequences' offsets alone, used by host code and kernels alike.
+#pragma once
+#include <algorithm>
+
+#include "dv_internal.h"
+
+namespace dv {
+
+// ---- pages ---------------------------------------------------------------------------------------
+// A page holds `pt` tokens (16, 32, 64 or 128) of every key/value head.  Keys lie token by token
+// [page, head, token, channel], values channel by channel [page, head, channel, token]: a lane of a
+// score product reads channels of one key, a lane of the value product tokens of one channel, both
+// 8 or 16 bytes at once and with no transposition.
+inline bool page_tokens_ok(int pt) { return pt == 16 || pt == 32 || pt == 64 || pt == 128; }
+__host__ __device__ inline int page_shift(int pt) { return pt == 16 ? 4 : pt == 32 ? 5 : pt == 64 ? 6 : 7; }
+
+// Page of a sequence's j-th stretch of pt tokens, or -1: past the table, or no page of the cache.
+__host__ __device__ inline int page_of(const int* table, int table_pages, int pages, int s, int j) {
+    if (j < 0 || j >= table_pages) return -1;
+    const long long at = (long long)s * table_pages + j;
+    const long long p = table ? (long long)table[at] : at;
+    return p >= 0 && p < pages ? (int)p : -1;
+}
+
+// ---- rows of a call ------------------------------------------------------------------------------
+// Rows of sequence s: offsets[s] .. offsets[s + 1] - 1, cut to the rows there are; without offsets
+// sequence s has row s.
+struct Span {
+    int row0, n;
+};
+__host__ __device__ inline Span rows_of(const int* offsets, int rows, int s) {
+    if (!offsets) return {s, s < rows ? 1 : 0};
+    const int a = offsets[s] < 0 ? 0 : offsets[s], b = offsets[s + 1] < rows ? offsets[s + 1] : rows;
+    return {a, b > a ? b - a : 0};
+}
+
+// Kernels deal blocks to slots: sequence s owns the slots from slot_base(s), and a slot finds its
+// sequence by comparing bases, so that a ragged batch needs no list made on the host.
+//   pages that n rows touch, from any start: at most n / pt + 2 (floor), so base = offset / pt + 2 s
+//   tiles of R packed rows (row x query heads of a key head, `mul`): at most n mul / R + 1 (floor)
+__host__ __device__ inline long long slot_base(int offset, int mul, int shift, int add, int s) {
+    return ((long long)offset * mul >> shift) + (long long)add * s;
+}
+__host__ __device__ inline long long page_slots(const int* offsets, int n_seqs, int rows, int shift) {
+    return offsets ? slot_base(rows, 1, shift, 2, n_seqs) : n_seqs;
+}
+
+// One page of one sequence that a call's rows touch.
+struct PagePart {
+    int page;       // -1: the cache does not have it
+    int row0;       // row of its first token
+    int slot0, n;   // its places slot0 .. slot0 + n - 1; n = 0: nothing
+};
+// ... slot u, of sequence s
+__host__ __device__ inline PagePart part_at(const SeqArgs& q, int pt, int pages, int s, long long u) {
+    PagePart p = {-1, 0, 0, 0};
+    if (s < 0 || s >= q.n_seqs) return p;
+    const int shift = page_shift(pt);
+    const Span sp = rows_of(q.offsets, q.rows, s);
+    const int start = q.at[s];
+    if (sp.n == 0 || start < 0) return p;
+    const long long j = q.offsets ? u - slot_base(q.offsets[s], 1, shift, 2, s) : 0;
+    const long long page = ((long long)start >> shift) + j;     // of the sequence
+    const long long end = (long long)start + sp.n, next = (page + 1) << shift;
+    const long long a = start > page << shift ? start : page << shift, b = end < next ? end : next;
+    if (a >= b) return p;
+    p.page = page < q.table_pages ? page_of(q.table, q.table_pages, pages, s, (int)page) : -1;
+    p.row0 = sp.row0 + (int)(a - start);
+    p.slot0 = (int)(a - (page << shift));
+    p.n = (int)(b - a);
+    return p;
+}
+
+// A tile of at most R = 2^shift packed rows of one sequence.
+struct Tile {
+    int seq;     // -1: none
+    int row0;    // the sequence's first row
+    int n;       // its rows
+    int first;   // the tile's first packed row
+    int rows;    // packed rows of the tile
+    int len;     // keys of the sequence
+    int end;     // keys that the tile's last row sees
+};
+__host__ __device__ inline long long tile_slots(bool offsets, int n_seqs, int rows, int group, int shift) {
+    return offsets ? slot_base(rows, group, shift, 1, n_seqs)
+                   : (long long)n_seqs * ((group + (1 << shift) - 1) >> shift);
+}
+// ... slot u, of sequence s (without offsets: of sequence u / tiles of a row)
+__host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int shift, bool causal, int s, long long u) {
+    Tile t = {-1, 0, 0, 0, 0, 0, 0};
+    if (s < 0 || s >= q.n_seqs) return t;
+    const Span sp = rows_of(q.offsets, q.rows, s);
+    const long long j = q.offsets ? u - slot_base(q.offsets[s], group, shift, 1, s)
+                                  : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
+    const long long first = j << shift, left = (long long)sp.n * group - first;
+    if (left <= 0) return t;
+    t.seq = s;
+    t.row0 = sp.row0;
+    t.n = sp.n;
+    t.first = (int)first;
+    t.rows = (int)(left < (1 << shift) ? left : 1 << shift);
+    const int most = q.table_pages * pt, len = q.at[s] < most ? q.at[s] : most;
+    t.len = len > 0 ? len : 0;
+    t.end = t.len;
+    if (causal) {
+        const long long e = (long long)t.len - sp.n + (t.first + t.rows - 1) / group + 1;
+        t.end = e > 0 ? (int)e : 0;
+    }
+    return t;
+}
+
+#ifdef __HIPCC__
+// The sequence whose slots hold slot u, or -1 (every lane of a wavefront calls, with the same u).
+__device__ __forceinline__ int find_seq(const int* offsets, int n_seqs, int mul, int shift, int add, long long u) {
+    int found = 0;
+    for (int b = 0; b < n_seqs; b += 64) {
+        const int s = b + (threadIdx.x & 63);
+        const bool before = s < n_seqs && slot_base(offsets[s], mul, shift, add, s) <= u;
+        const int k = __popcll(__ballot(before));
+        found += k;
+        if (k < 64) break;
+    }
+    return found - 1;
+}
+#endif
+
+}  // namespace dv

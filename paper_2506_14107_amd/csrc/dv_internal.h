@@ -274,4 +274,79 @@ void launch_resolve(const uint8_t* cur, const uint8_t* src, int F, int N, int G,
 void launch_final_ln(const float* x, int F, int N, int D, const float* g, const float* b,
                      float* emb, hipStream_t s);
 
+// ---- rotary positions and the 8-bit cache --------------------------------------------------------
+// Rates of rotary positions: pair i (i < dim/2) turns by turn[i] / 2^64 of a full turn per unit of its
+// axis's position; pairs below end0 take axis 0, below end1 axis 1, the others axis 2.
+struct RotaryPlan {
+    uint64_t turn[64];
+    int dim, end0, end1, pairs;   // pairs: channels 2i and 2i + 1 (else i and i + dim/2)
+};
+struct RotaryArgs {
+    const void* x;           // row r, head h, channel c: x[r * x_stride + h * dh + c]
+    void* out;               // may be x
+    long long x_stride, out_stride;
+    int rows, heads, dh;
+    const int* rows_dev;     // device row count (nullptr: rows)
+    const int* pos;          // [.., 3]
+    const int* pos_idx;      // row r takes position pos_idx[r] % pos_mod (nullptr: r)
+    int pos_mod;
+    RotaryPlan rot;
+};
+void launch_rotary(bool bf16, const RotaryArgs& a, hipStream_t s);
+
+struct CacheView {
+    uint8_t *k, *v;            // e4m3 codes: [pages, heads, tokens, channels], [pages, heads, channels, tokens]
+    float *k_scale, *v_scale;  // [pages, heads], powers of two
+    int pages, page_tokens, kv_heads, head_dim;
+};
+struct SeqArgs {
+    int n_seqs, table_pages, rows;
+    const int* table;      // [n_seqs, table_pages] (nullptr: sequence s has pages s * table_pages ..)
+    const int* offsets;    // [n_seqs + 1] first row of each sequence (nullptr: one row each)
+    const int* at;         // [n_seqs] write, read: place of the first row; attention: keys
+};
+struct WriteArgs {
+    CacheView c;
+    SeqArgs seq;
+    const void *k, *v, *q;     // q (or nullptr): turned into q_out
+    void* q_out;
+    long long k_stride, v_stride, q_stride, qo_stride;
+    int q_heads;
+    const int* pos;            // [rows, 3]; unused where rot.dim is 0
+    RotaryPlan rot;
+    int slots, vec;            // set by the launcher
+};
+void launch_cache_write(bool bf16, WriteArgs a, hipStream_t s);
+struct ReadArgs {
+    CacheView c;
+    SeqArgs seq;
+    void *k, *v;
+    long long k_stride, v_stride;
+    int vec;                   // set by the launcher
+};
+void launch_cache_read(bool bf16, ReadArgs a, hipStream_t s);
+
+struct CacheAttnArgs {
+    CacheView c;
+    SeqArgs seq;
+    const void* q;
+    void* out;
+    long long q_stride, o_stride;
+    int q_heads;
+    float scale;
+    int causal;
+    int chunk, splits;         // keys of a split, splits of the longest sequence the table holds
+    long long slots;           // row tiles dealt
+    float* part;               // partial results, where splits > 1
+};
+// How a call is cut, from its sizes; the same rule sizes the workspace.
+struct CacheAttnPlan {
+    int chunk, splits;
+    long long slots;
+    size_t bytes;              // workspace
+};
+CacheAttnPlan cache_attn_plan(int n_seqs, int rows, bool offsets, int table_pages, int page_tokens, int kv_heads,
+                              int q_heads, int head_dim, int cus);
+void launch_cache_attention(bool bf16, const CacheAttnArgs& a, hipStream_t s);
+
 }  // namespace dv

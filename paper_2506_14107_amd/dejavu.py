@@ -21,12 +21,25 @@ STAGES = ["patch", "gate", "compact", "ln1", "qkv", "attn", "oproj", "ln2", "fc1
 DV_FLAG_RESTORE = 1
 DV_FLAG_DECISION = 2
 DV_FLAG_REORDER = 4
+DV_ROTARY_HALVES, DV_ROTARY_PAIRS = 0, 1
 
 
 class DejaVuError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"dejavu error {code}: {msg}")
         self.code = code
+
+
+class dv_rotary_plan(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int), ("section", ctypes.c_int * 3), ("layout", ctypes.c_int),
+                ("turn", ctypes.c_uint64 * 64)]
+
+
+class dv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int),
+                ("page_tokens", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int)]
 
 
 class dv_config(ctypes.Structure):
@@ -38,6 +51,7 @@ class dv_config(ctypes.Structure):
 
 _lib = None
 _P = ctypes.c_void_p
+_I64 = ctypes.c_longlong
 
 
 def load(path=None):
@@ -70,6 +84,24 @@ def load(path=None):
         "dv_stream_reset": (ctypes.c_int, [_P]),
         "dv_stream_held": (ctypes.c_int, [_P, ctypes.POINTER(ctypes.c_int)]),
         "dv_stream_flush": (ctypes.c_int, [_P, _P, _P, _P, _P]),
+        "dv_rotary_init": (ctypes.c_int, [ctypes.POINTER(dv_rotary_plan),
+                                          ctypes.POINTER(ctypes.c_int * 3), ctypes.c_int,
+                                          ctypes.c_int, ctypes.c_double]),
+        "dv_rotary": (ctypes.c_int, [_P, ctypes.c_int, _P, _I64, ctypes.c_int, ctypes.c_int,
+                                     ctypes.c_int, _P, _P, _I64, _P]),
+        "dv_cache_write": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P, ctypes.c_int,
+                                          _P, _I64, _P, _I64, ctypes.c_int, _P, _P, _P, _I64,
+                                          ctypes.c_int, _P, _I64, _P]),
+        "dv_cache_read": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P, ctypes.c_int,
+                                         _P, _I64, _P, _I64, ctypes.c_int, _P]),
+        "dv_cache_attention_workspace": (ctypes.c_int, [_P, ctypes.c_int, ctypes.c_int,
+                                                        ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                                        ctypes.c_int,
+                                                        ctypes.POINTER(ctypes.c_size_t)]),
+        "dv_cache_attention": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P,
+                                              ctypes.c_int, _P, _I64, ctypes.c_int, ctypes.c_int,
+                                              ctypes.c_int, ctypes.c_float, ctypes.c_int, _P, _I64,
+                                              _P, ctypes.c_size_t, _P]),
         "dv_mfma_probe": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, _P,
                                          ctypes.POINTER(ctypes.c_double), _P]),
         "dv_profile": (ctypes.c_int, [_P, ctypes.c_uint]),
@@ -170,6 +202,50 @@ def dv_stream_flush(handle, out_embeddings, out_masks, out_tokens, stream):
 def dv_compact(masks, n_frames, n_tokens, group_size, idx, pos, qoff, count, stream):
     _check(load().dv_compact(masks, n_frames, n_tokens, group_size, idx, pos, qoff, count,
                              stream))
+
+
+def dv_rotary_init(section, layout, per_axis, base):
+    """Returns the filled dv_rotary_plan."""
+    plan = dv_rotary_plan()
+    sec = (ctypes.c_int * 3)(*section)
+    _check(load().dv_rotary_init(ctypes.byref(plan), ctypes.byref(sec), layout, int(per_axis),
+                                 float(base)))
+    return plan
+
+
+# In the calls below `plan` and `cache` are addresses (ctypes.addressof) of the structures.
+def dv_rotary(plan, dtype, x, x_stride, rows, heads, head_dim, positions, out, out_stride, stream):
+    _check(load().dv_rotary(plan, dtype, x, x_stride, rows, heads, head_dim, positions, out,
+                            out_stride, stream))
+
+
+def dv_cache_write(cache, n_seqs, table, table_pages, offsets, starts, dtype, k, k_stride, v,
+                   v_stride, rows, plan, positions, q, q_stride, q_heads, q_out, q_out_stride,
+                   stream):
+    _check(load().dv_cache_write(cache, n_seqs, table, table_pages, offsets, starts, dtype, k,
+                                 k_stride, v, v_stride, rows, plan, positions, q, q_stride,
+                                 q_heads, q_out, q_out_stride, stream))
+
+
+def dv_cache_read(cache, n_seqs, table, table_pages, offsets, starts, dtype, k, k_stride, v,
+                  v_stride, rows, stream):
+    _check(load().dv_cache_read(cache, n_seqs, table, table_pages, offsets, starts, dtype, k,
+                                k_stride, v, v_stride, rows, stream))
+
+
+def dv_cache_attention_workspace(cache, n_seqs, table_pages, with_offsets, rows, q_heads, max_rows):
+    n = ctypes.c_size_t()
+    _check(load().dv_cache_attention_workspace(cache, n_seqs, table_pages, int(with_offsets), rows,
+                                               q_heads, max_rows, ctypes.byref(n)))
+    return n.value
+
+
+def dv_cache_attention(cache, n_seqs, table, table_pages, offsets, lengths, dtype, q, q_stride,
+                       rows, q_heads, max_rows, scale, causal, out, out_stride, workspace,
+                       workspace_bytes, stream):
+    _check(load().dv_cache_attention(cache, n_seqs, table, table_pages, offsets, lengths, dtype, q,
+                                     q_stride, rows, q_heads, max_rows, scale, int(causal), out,
+                                     out_stride, workspace, workspace_bytes, stream))
 
 
 def dv_mfma_probe(blocks, iters, sink, stream):
@@ -334,3 +410,223 @@ def compact(masks, group_size, stream=None):
     dv_compact(_ptr(masks.contiguous()), F, N, group_size, _ptr(idx), _ptr(pos), _ptr(qoff),
                _ptr(cnt), _stream(stream))
     return idx, pos, qoff, cnt
+
+
+# ---- token rows and their 8-bit cache -----------------------------------------------------------
+def _dtype(t):
+    import torch
+    if t.dtype is torch.bfloat16:
+        return DV_BF16
+    if t.dtype is torch.float32:
+        return DV_F32
+    raise ValueError(f"rows must be bf16 or fp32 (got {t.dtype})")
+
+
+def _rows(name, t, device, heads=None, head_dim=None, rows=None, dtype=None):
+    """Checks a row tensor [rows, heads, head_dim] whose heads lie side by side; returns its row
+    stride."""
+    if t.dim() != 3 or t.device != device:
+        raise ValueError(f"{name} must be a tensor [rows, heads, head_dim] on {device}")
+    n, h, d = t.shape
+    if ((heads is not None and h != heads) or (head_dim is not None and d != head_dim)
+            or (rows is not None and n != rows) or (dtype is not None and t.dtype is not dtype)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)} and type {t.dtype}, which does not fit "
+                         "the other arguments")
+    sr, sh, sd = t.stride()
+    if (d > 1 and sd != 1) or (h > 1 and sh != d):
+        raise ValueError(f"the heads of a row of {name} must lie side by side")
+    return sr if n > 1 else max(sr, h * d)
+
+
+def _ints(name, t, device, shape):
+    import torch
+    if (t.dtype is not torch.int32 or t.device != device or tuple(t.shape) != tuple(shape)
+            or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+    return t.data_ptr()
+
+
+class _On:
+    """The device and stream a call runs on: makes the device current where it is not, and a given
+    stream current where it is another than the device's own (so that what the call allocates
+    belongs to it)."""
+
+    def __init__(self, device, stream):
+        import torch
+        if device.type != "cuda":
+            raise ValueError("tensors must be on a HIP device")
+        self.stack = []
+        if torch.cuda.current_device() != device.index:
+            self.stack.append(torch.cuda.device(device))
+        if stream is not None:
+            self.stack.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        import torch
+        for c in self.stack:
+            c.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *e):
+        for c in reversed(self.stack):
+            c.__exit__(*e)
+
+
+class Rotary:
+    """Rates of rotary positions with a time, a height and a width axis: `sections` pairs of channels
+    turn with each.  layout "halves" (channels i and i + dim/2) or "pairs" (2i and 2i + 1); per_axis:
+    every axis takes the whole range of rates."""
+
+    def __init__(self, sections, layout="halves", per_axis=False, base=10000.0):
+        code = {"halves": DV_ROTARY_HALVES, "pairs": DV_ROTARY_PAIRS}.get(layout)
+        if code is None:
+            raise ValueError(f"unknown rotary layout {layout!r}")
+        if len(sections) != 3:
+            raise ValueError("sections are the pairs of three axes")
+        self.plan = dv_rotary_init(sections, code, per_axis, base)
+        self.dim = self.plan.dim
+        self.address = ctypes.addressof(self.plan)
+
+
+def rotary(x, positions, rot, out=None, stream=None):
+    """Rows x [rows, heads, head_dim] with their heads turned by `positions` (int32 [rows, 3]) at the
+    rates of `rot` (Rotary), into `out` (which may be x) or a new tensor."""
+    import torch
+    device = x.device
+    with _On(device, stream) as s:
+        n, h, d = x.shape
+        xs = _rows("x", x, device)
+        if out is None:
+            out = torch.empty((n, h, d), dtype=x.dtype, device=device)
+            os = h * d
+        else:
+            os = _rows("out", out, device, h, d, n, x.dtype)
+        dv_rotary(rot.address, _dtype(x), x.data_ptr(), xs, n, h, d,
+                  _ints("positions", positions, device, (n, 3)), out.data_ptr(), os, s)
+    return out
+
+
+class TokenCache:
+    """A paged cache of keys and values in 8 bits (float8_e4m3fn codes, a power-of-two scale for each
+    page and head): `pages` pages of `page_tokens` tokens of `kv_heads` heads.
+
+    A sequence's places lie in the pages of its row of `table` (int32 [n_seqs, table_pages]; None:
+    sequence s has the table_pages = pages // n_seqs pages from s * table_pages on).  `offsets`
+    (int32 [n_seqs + 1]) cuts a call's rows into sequences; None: one row each.
+
+    buffers: (k, v, k_scale, v_scale) to use instead of new ones: float8_e4m3fn [pages, kv_heads,
+    page_tokens, head_dim] and [pages, kv_heads, head_dim, page_tokens], fp32 [pages, kv_heads].
+    """
+
+    def __init__(self, pages, kv_heads, head_dim, page_tokens=64, device=None, buffers=None):
+        import torch
+        shapes = [(pages, kv_heads, page_tokens, head_dim), (pages, kv_heads, head_dim, page_tokens),
+                  (pages, kv_heads), (pages, kv_heads)]
+        types = [torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32]
+        if buffers is None:
+            device = device or torch.device("cuda", torch.cuda.current_device())
+            buffers = [torch.empty(s, dtype=t, device=device) for s, t in zip(shapes, types)]
+        for b, s, t in zip(buffers, shapes, types):
+            if (tuple(b.shape) != s or b.dtype is not t or not b.is_contiguous()
+                    or b.device != buffers[0].device):
+                raise ValueError(f"a cache buffer must be a contiguous {t} tensor {list(s)}")
+        self.k, self.v, self.k_scale, self.v_scale = buffers
+        self.device = self.k.device
+        self.pages, self.kv_heads = pages, kv_heads
+        self.head_dim, self.page_tokens = head_dim, page_tokens
+        self.desc = dv_cache(*(b.data_ptr() for b in buffers), pages, page_tokens, kv_heads,
+                             head_dim)
+        self.address = ctypes.addressof(self.desc)
+
+    def _seqs(self, at, name, offsets, table):
+        """(n_seqs, table, table_pages, offsets, at) as the entry points take them."""
+        n = at.shape[0]
+        if table is None:
+            t, tp = 0, self.pages // max(n, 1)
+        else:
+            tp = table.shape[1] if table.dim() == 2 else -1
+            t = _ints("table", table, self.device, (n, tp))
+        o = 0 if offsets is None else _ints("offsets", offsets, self.device, (n + 1,))
+        return n, t, tp, o, _ints(name, at, self.device, (n,))
+
+    def write(self, k, v, starts, offsets=None, table=None, rotary=None, positions=None, q=None,
+              q_out=None, stream=None):
+        """Quantises rows k and v [rows, kv_heads, head_dim] into places starts[s] .. of each
+        sequence.  With `rotary` and `positions` the keys are turned first, and the rows of q
+        [rows, heads, head_dim] into `q_out` (which may be q) or a new tensor, which is returned."""
+        import torch
+        dev = self.device
+        with _On(dev, stream) as s:
+            n, t, tp, o, at = self._seqs(starts, "starts", offsets, table)
+            ks = _rows("k", k, dev, self.kv_heads, self.head_dim)
+            rows = k.shape[0]
+            vs = _rows("v", v, dev, self.kv_heads, self.head_dim, rows, k.dtype)
+            if (rotary is None) != (positions is None):
+                raise ValueError("rotary and positions come together")
+            qs = qos = heads = 0
+            if q is not None:
+                qs = _rows("q", q, dev, None, self.head_dim, rows, k.dtype)
+                heads = q.shape[1]
+                if q_out is None:
+                    q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+                qos = _rows("q_out", q_out, dev, heads, self.head_dim, rows, k.dtype)
+            elif q_out is not None:
+                raise ValueError("q_out without q")
+            dv_cache_write(self.address, n, t, tp, o, at, _dtype(k), k.data_ptr(), ks,
+                           v.data_ptr(), vs, rows, 0 if rotary is None else rotary.address,
+                           0 if rotary is None else _ints("positions", positions, dev, (rows, 3)),
+                           _ptr(q), qs, heads, _ptr(q_out), qos, s)
+        return q_out
+
+    def read(self, starts, offsets=None, table=None, rows=None, dtype=None, out=None, stream=None):
+        """Keys and values [rows, kv_heads, head_dim] of places starts[s] .. of each sequence, into
+        `out` (a pair of tensors) or new tensors of `rows` rows and `dtype` (bf16)."""
+        import torch
+        dev = self.device
+        with _On(dev, stream) as s:
+            n, t, tp, o, at = self._seqs(starts, "starts", offsets, table)
+            if out is None:
+                shape = (n if rows is None else rows, self.kv_heads, self.head_dim)
+                out = [torch.empty(shape, dtype=dtype or torch.bfloat16, device=dev)
+                       for _ in range(2)]
+            k, v = out
+            ks = _rows("k", k, dev, self.kv_heads, self.head_dim)
+            vs = _rows("v", v, dev, self.kv_heads, self.head_dim, k.shape[0], k.dtype)
+            dv_cache_read(self.address, n, t, tp, o, at, _dtype(k), k.data_ptr(), ks, v.data_ptr(),
+                          vs, k.shape[0], s)
+        return out
+
+    def attention(self, q, lengths, offsets=None, table=None, causal=True, scale=None, max_rows=0,
+                  out=None, workspace=None, stream=None):
+        """Attention of rows q [rows, heads, head_dim] over the first lengths[s] places of their
+        sequences, into `out` or a new tensor.  causal: the rows are the sequence's last places and
+        see no later ones.  max_rows: an upper bound of any sequence's rows, if known.  workspace: a
+        uint8 tensor to use (see attention_workspace) instead of one of the call's own."""
+        import torch
+        dev = self.device
+        with _On(dev, stream) as s:
+            n, t, tp, o, at = self._seqs(lengths, "lengths", offsets, table)
+            qs = _rows("q", q, dev, None, self.head_dim)
+            rows, heads, d = q.shape
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+                os = heads * d
+            else:
+                os = _rows("out", out, dev, heads, d, rows, q.dtype)
+            if workspace is None:
+                need = dv_cache_attention_workspace(self.address, n, tp, o != 0, rows, heads,
+                                                    max_rows)
+                if need:
+                    workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+            dv_cache_attention(self.address, n, t, tp, o, at, _dtype(q), q.data_ptr(), qs, rows,
+                               heads, max_rows, d ** -0.5 if scale is None else scale, causal,
+                               out.data_ptr(), os, _ptr(workspace),
+                               0 if workspace is None else workspace.numel(), s)
+        return out
+
+    def attention_workspace(self, n_seqs, rows, heads, table_pages=None, with_offsets=True,
+                            max_rows=0):
+        """Bytes of scratch that `attention` needs for such a call."""
+        tp = self.pages // max(n_seqs, 1) if table_pages is None else table_pages
+        return dv_cache_attention_workspace(self.address, n_seqs, tp, with_offsets, rows, heads,
+                                            max_rows)
