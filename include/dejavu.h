@@ -80,7 +80,8 @@ typedef struct dv_config {
     int mlp;               /* Dm: MLP hidden width */
     int dtype;             /* DV_F32 or DV_BF16 */
     int max_batch_frames;  /* frames per internal batch (rounded down to whole groups per call) */
-    unsigned flags;        /* DV_FLAG_RESTORE, DV_FLAG_DECISION, DV_FLAG_REORDER or 0 */
+    unsigned flags;        /* DV_FLAG_RESTORE, DV_FLAG_DECISION, DV_FLAG_REORDER, DV_FLAG_ROTARY,
+                            * DV_FLAG_CACHE8 or 0 */
 } dv_config;
 
 /* Restoration layer on reused tokens (Section 3.3): after each layer, a reused token i of a
@@ -124,6 +125,22 @@ typedef struct dv_config {
  * input's difference to the source's input); the group size is then at most 60 (chains of
  * sources up to 16 long).  No extra weights. */
 #define DV_FLAG_REORDER 4u
+
+/* Rotary positions in the encoder's attention, beside the position table (Section 2.3's tokens): the
+ * first half of the pairs of every query and key head turns with the patch's row + 1, the other with its
+ * column + 1 (rates DV_ROTARY_BASE^(-j/s) for the j-th of an axis's s pairs, layout DV_ROTARY_HALVES;
+ * dv_rotary's arithmetic); the class token is not turned.  A token has the same place in every
+ * frame, so a reused key keeps its turn.  No extra weights. */
+#define DV_FLAG_ROTARY 16u
+#define DV_ROTARY_BASE 100.0
+
+/* The stream's cached reference holds its keys and values in 8 bits, as dv_cache_write quantises
+ * them (pages of 64 tokens), for half (bf16) or a quarter (fp32) of their memory: a server holds one
+ * handle per stream (Section 5.2's memory compaction).  Frames whose reference came in an earlier call
+ * attend to the quantised keys and values of their reused tokens; the others are not affected, so a
+ * stream's results depend on where its calls are cut, by the rounding to 8 bits.  Encode calls
+ * outside streams do not change. */
+#define DV_FLAG_CACHE8 32u
 
 typedef struct dv_handle dv_handle;
 
@@ -230,8 +247,9 @@ int dv_encode_tokens(dv_handle* h, const float* frames, int n_frames, int group_
  * dv_stream_encode calls g = 0, 1, ... since the last dv_stream_reset (or creation); frame g's
  * reference is frame G * floor(g / G), which may have come in an earlier call: the handle then
  * keeps that reference's per-layer input rows and keys/values in a cache ((L+1) N D fp32 plus
- * L N 2D dtype elements, part of the workspace dv_create allocates) instead of recomputing it.  Results
- * are those of one dv_encode_tokens call over all frames of the stream.  frames, masks (NULL:
+ * L N 2D dtype elements, or 8-bit ones with DV_FLAG_CACHE8, part of the workspace dv_create allocates)
+ * instead of recomputing it.  Results are those of one dv_encode_tokens call over all frames of the
+ * stream (with DV_FLAG_CACHE8 up to that cache's rounding).  frames, masks (NULL:
  * gate mode with tau), out_embeddings, out_masks and out_tokens (both may be NULL) cover this
  * call's frames, with the layouts of dv_encode_tokens.  group_size must stay the same until the
  * next reset.

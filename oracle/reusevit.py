@@ -63,6 +63,12 @@ What it computes, following the paper's model description (Section 3):
   that gave it (the past one on a tie); the decision MLP's type cue is the
   frame's own type.
 
+* Rotary positions, when the configuration enables them (``cfg["rotary"]``):
+  before attention the channels of every query and key head are turned in
+  pairs (i, i + dh/2), the first half of the pairs by the patch's row + 1, the
+  other by its column + 1, times 100^(-j/s) for the j-th of an axis's s pairs; the
+  class token is not turned.
+
 Modes: gate mode (``tau``) and mask-injection mode (``masks`` given; class
 token and reference-frame entries are forced to 0).  ``tau = -inf`` turns
 reuse off (dense), ``tau = +inf`` reuses every non-class token of every
@@ -79,6 +85,7 @@ LN_EPS = 1e-5
 COS_EPS = 1e-8
 RESTORE_HIDDEN = 128   # hidden width of the restoration MLP (Section 3.3)
 DECISION_HIDDEN = 64   # hidden width of the decision MLP (Section 3.3 gives none)
+ROTARY_BASE = 100.0    # rotary positions of the encoder's attention
 FRAME_TYPES = ("I", "P", "B_dist2", "B_dist1")   # reference-type cue r (Section 3.3)
 
 
@@ -120,6 +127,9 @@ def unpack_blob(blob, cfg, dtype=np.float64):
         for lay in W["layers"]:
             lay["W_d1"], lay["b_d1"] = take(Hd, 2 + len(FRAME_TYPES)), take(Hd)
             lay["W_d2"], lay["b_d2"] = take(1, Hd), take(1)
+    if cfg.get("rotary"):
+        for lay in W["layers"]:
+            lay["rotary"] = (cfg["heads"], cfg["image_size"] // p)
     if off != blob.size:
         raise ValueError(f"weight blob has {blob.size} floats, layout needs {off}")
     return W
@@ -259,9 +269,45 @@ def decision_gate(d, tau):
     return d > tau
 
 
-def qkv_rows(x_rows, P):
+def turn_rows(rows, tokens, heads, side):
+    """Rotary positions of query or key rows [n, D] of the given tokens (module docstring)."""
+    n, D = rows.shape
+    dh = D // heads
+    s = dh // 4                                           # pairs of each axis
+    patch = np.asarray(tokens) - 1
+    at = np.where(patch < 0, 0, np.stack([patch // side + 1, patch % side + 1]))
+    rate = ROTARY_BASE ** (-np.arange(s) / s)
+    w = np.concatenate([at[0][:, None] * rate, at[1][:, None] * rate], axis=1)[:, None]
+    t = rows.reshape(n, heads, dh)
+    a, b = t[..., :dh // 2], t[..., dh // 2:]
+    return np.concatenate([a * np.cos(w) - b * np.sin(w), b * np.cos(w) + a * np.sin(w)],
+                          axis=2).reshape(n, D).astype(rows.dtype)
+
+
+def eight_bits(rows, heads):
+    """Key or value rows [N, D] of one frame as the 8-bit reference cache holds them: per 64
+    tokens and head the least power of two of which the largest magnitude is at most 448 times,
+    and values of 3 fraction bits (4 significant ones; 2^-9 the least) of it, ties to even."""
+    out = np.empty_like(rows)
+    dh = rows.shape[1] // heads
+    for a in range(0, len(rows), 64):
+        for h in range(heads):
+            s = (slice(a, a + 64), slice(h * dh, (h + 1) * dh))
+            x = rows[s]
+            scale = 2.0 ** np.ceil(np.log2(np.abs(x).max() / 448))
+            step = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(x) / scale, 2.0 ** -6))) - 3) * scale
+            out[s] = np.round(x / step) * step
+    return out
+
+
+def qkv_rows(x_rows, P, tokens=None):
+    """Queries, keys and values of rows; tokens: their token numbers (None: 0, 1, ...)."""
     D = x_rows.shape[1]
     t = layer_norm(x_rows, P["ln1_g"], P["ln1_b"]) @ P["W_qkv"].T + P["b_qkv"]
+    if "rotary" in P:
+        i = np.arange(len(t)) if tokens is None else tokens
+        t = np.concatenate([turn_rows(t[:, :D], i, *P["rotary"]),
+                            turn_rows(t[:, D:2 * D], i, *P["rotary"]), t[:, 2 * D:]], axis=1)
     return t[:, :D], t[:, D:2 * D], t[:, 2 * D:]
 
 
@@ -323,7 +369,7 @@ def reordered_layer(x, P, cfg, G, l, tau, masks, sources, t_cls, rec):
         C, R = np.flatnonzero(~m), np.flatnonzero(m)
         src = np.where(np.concatenate([[False], from_fut]), fut if fut is not None else past,
                        past)[R]                             # reference of each reused token
-        q_c, k_c, v_c = qkv_rows(x[f, C], P)
+        q_c, k_c, v_c = qkv_rows(x[f, C], P, C)
         k_t, v_t = np.empty((N, D)), np.empty((N, D))
         k_t[C], v_t[C] = k_c, v_c                           # fresh keys/values ...
         k_t[R], v_t[R] = k_eff[src, R], v_eff[src, R]       # ... and the reference's
@@ -337,7 +383,7 @@ def reordered_layer(x, P, cfg, G, l, tau, masks, sources, t_cls, rec):
 
 
 def encode(frames, blob, cfg, group_size, tau=None, masks=None, dtype=np.float64,
-           return_layers=False, sources=None):
+           return_layers=False, sources=None, cached8=None):
     """Reuse-aware encoder forward over ``frames`` [F, 3, S, S].
 
     Returns a dict with
@@ -353,6 +399,9 @@ def encode(frames, blob, cfg, group_size, tau=None, masks=None, dtype=np.float64
       cos_past, cos_fut  [F, L, N]  the two cosines (reorder; NaN where absent)
       tokens [F, N, D]   output of the last layer
       layers (optional)  list of the L+1 token buffers x^0..x^L
+
+    cached8 (optional, bool [F], not with cfg["reorder"]): frames whose reference came in an earlier
+    call of a stream that holds its keys and values in 8 bits.
     """
     if (tau is None) == (masks is None):
         raise ValueError("give exactly one of tau (gate mode) and masks (injection mode)")
@@ -413,8 +462,10 @@ def encode(frames, blob, cfg, group_size, tau=None, masks=None, dtype=np.float64
                 m = np.concatenate([[False], reuse])          # class token never reused
                 out_m[f, l] = m
                 C = np.flatnonzero(~m)                        # recompute tokens (C[0] = class)
-                q_c, k_c, v_c = qkv_rows(x[f, C], P)
+                q_c, k_c, v_c = qkv_rows(x[f, C], P, C)
                 k_t, v_t = k_r.copy(), v_r.copy()             # keys/values: reference ...
+                if cached8 is not None and cached8[f]:        # ... as the 8-bit cache holds it
+                    k_t, v_t = eight_bits(k_r, H), eight_bits(v_r, H)
                 k_t[C], v_t[C] = k_c, v_c                     # ... overwritten by fresh rows
                 o_c, p_c = attention(q_c, k_t, v_t, H, first_probs=True)
                 y_c = finish_rows(x[f, C], o_c, P)

@@ -134,6 +134,8 @@ struct Dims {
     bool restore;   // DV_FLAG_RESTORE
     bool decision;  // DV_FLAG_DECISION
     bool reorder;   // DV_FLAG_REORDER
+    bool rotary;    // DV_FLAG_ROTARY
+    bool cache8;    // DV_FLAG_CACHE8
     int Bw;         // frames of workspace: B, plus one look-ahead frame with reordering
 };
 
@@ -146,7 +148,7 @@ int check_config(const dv_config* c, Dims* d) {
         c->mlp < 1 || c->max_batch_frames < 1)
         return fail(DV_EINVAL, "config sizes must be >= 1");
     if (c->dtype != DV_F32 && c->dtype != DV_BF16) return fail(DV_EINVAL, "unknown dtype %d", c->dtype);
-    if (c->flags & ~(DV_FLAG_RESTORE | DV_FLAG_DECISION | DV_FLAG_REORDER))
+    if (c->flags & ~(DV_FLAG_RESTORE | DV_FLAG_DECISION | DV_FLAG_REORDER | DV_FLAG_ROTARY | DV_FLAG_CACHE8))
         return fail(DV_EUNSUPPORTED, "unknown flag bits 0x%x", c->flags);
     if (c->image_size % c->patch) return fail(DV_EUNSUPPORTED, "image_size %% patch != 0");
     if (c->width % c->heads) return fail(DV_EUNSUPPORTED, "width %% heads != 0");
@@ -172,6 +174,8 @@ int check_config(const dv_config* c, Dims* d) {
     d->restore = (c->flags & DV_FLAG_RESTORE) != 0;
     d->decision = (c->flags & DV_FLAG_DECISION) != 0;
     d->reorder = (c->flags & DV_FLAG_REORDER) != 0;
+    d->rotary = (c->flags & DV_FLAG_ROTARY) != 0;
+    d->cache8 = (c->flags & DV_FLAG_CACHE8) != 0;
     d->Bw = d->B + (d->reorder ? 1 : 0);
     if (!attention_supported(bf, d->N, dh))
         return fail(DV_EUNSUPPORTED, "attention for N=%d tokens, head dim %d is not supported "
@@ -204,6 +208,9 @@ size_t blob_floats(const Dims& d) {
     return D * 3 * p * p + D + D + N * D + (size_t)d.L * per_layer + 2 * D + restore + decision;
 }
 
+constexpr int REF_PAGE = 64;   // tokens a page of a stream's 8-bit reference cache
+size_t ref_pages(const Dims& d) { return (d.N + REF_PAGE - 1) / REF_PAGE; }
+
 // Workspace of one internal batch size: the buffers every launch of an encode reads and writes.
 // A handle carves one from its own allocation (with the stream state); dv_encode_noalloc carves
 // one from the static scratch array.
@@ -228,10 +235,13 @@ struct Work {
     int* rslot = nullptr;       // [T] reordered restoration: a reused token's slot in ridx
     float* rbuf = nullptr;      // [Tp, D] reordered restoration: restoration outputs
     // stream state (handles only): the cached reference's layer inputs x^0 .. x^L [L+1, N, D]
-    // fp32 and keys/values [L, N, 2D] elem; under reordering the held frames' pixels
+    // fp32 and keys/values [L, N, 2D] elem, or with DV_FLAG_CACHE8 a paged 8-bit cache of one
+    // sequence a layer (kvc: its keys' codes, then its values'); under reordering the held frames' pixels
     // [3, 3, S, S], their maps [3, L, N] and a staging area for a batch's maps [B, L, N]
     float* xc = nullptr;
     void* kvc = nullptr;
+    float* kv_scale = nullptr;   // DV_FLAG_CACHE8: keys' scales, then values' [2, L * pages, H]
+    int* zero = nullptr;         // a 0: the place of a reference's first token in its sequence
     float* hold = nullptr;
     uint8_t* holdm = nullptr;
     uint8_t* injs = nullptr;
@@ -283,7 +293,14 @@ size_t carve_work(const Dims& d, char* base, Work* out, bool stream) {
     }
     if (stream) {
         w.xc = (float*)take((L + 1) * N * D * 4);
-        w.kvc = take(L * N * 2 * D * el);
+        if (d.cache8) {
+            const size_t pages = L * ref_pages(d);
+            w.kvc = take(pages * 2 * REF_PAGE * D);
+            w.kv_scale = (float*)take(pages * 2 * d.H * 4);
+            w.zero = (int*)take(4);
+        } else {
+            w.kvc = take(L * N * 2 * D * el);
+        }
         if (d.reorder) {
             w.hold = (float*)take((size_t)3 * 3 * d.S * d.S * 4);
             w.holdm = (uint8_t*)take(3 * L * N);
@@ -296,6 +313,14 @@ size_t carve_work(const Dims& d, char* base, Work* out, bool stream) {
 
 // Bytes of workspace a handle of these dimensions allocates.
 size_t workspace_need(const Dims& d) { return carve_work(d, nullptr, nullptr, true); }
+
+// Layer l's pages of a stream's 8-bit reference cache.
+CacheView ref_cache(const Dims& d, const Work& w, int l) {
+    const size_t P = ref_pages(d), codes = P * REF_PAGE * d.D, scales = P * d.H;
+    uint8_t* k = (uint8_t*)w.kvc + 2 * l * codes;
+    float* ks = w.kv_scale + 2 * l * scales;
+    return {k, k + codes, ks, ks + scales, (int)P, REF_PAGE, d.H, d.D / d.H};
+}
 
 struct Stage {
     double ms = 0;
@@ -315,6 +340,8 @@ struct dv_handle {
     // weights
     const void* W_pe;
     const float *b_pe, *cls, *pos, *lnf_g, *lnf_b;
+    const int* rot_pos = nullptr;   // DV_FLAG_ROTARY: [N, 3] positions of a frame's tokens
+    RotaryPlan rot{};
     std::vector<LayerW> layers;
     Work w;                 // views into ws
     // stream state: frames seen since the last reset, their group size, and the cached
@@ -546,13 +573,50 @@ int run_batch(dv_handle* h, Work& wk, const float* frames, int F, int G, int mod
             g.out = wk.qkv;
             launch_gemm(Epi::Qkv, bf, g, s);
         }
-        if (skip > 0)   // the cached reference's keys and values, at packed rows ext_row ..
-            HIP_TRY(hipMemcpy2DAsync((char*)wk.qkv + ((size_t)wk.ext_row * 3 * D + D) * el,
-                                     3 * D * el, (const char*)wk.kvc + (size_t)l * kv_bytes,
+        if (d.rotary) {   // queries and keys of the packed rows, before any of them is cached or read
+            Scope sc(h, DV_STAGE_QKV, s);
+            RotaryArgs ra{};
+            ra.x = wk.qkv;
+            ra.out = wk.qkv;
+            ra.x_stride = ra.out_stride = 3ll * D;
+            ra.rows = T;
+            ra.rows_dev = Mdev;
+            ra.heads = 2 * d.H;
+            ra.dh = D / d.H;
+            ra.pos = h->rot_pos;
+            ra.pos_idx = idx;
+            ra.pos_mod = N;
+            ra.rot = h->rot;
+            launch_rotary(bf, ra, s);
+        }
+        char* ext = (char*)wk.qkv + ((size_t)wk.ext_row * 3 * D + D) * el;   // keys of row ext_row
+        if (skip > 0 && d.cache8) {   // the cached reference's keys and values, at packed rows ext_row ..
+            ReadArgs ra{};
+            ra.c = ref_cache(d, wk, l);
+            ra.seq = {1, (int)ref_pages(d), N, nullptr, nullptr, wk.zero};
+            ra.seq.one = 1;
+            ra.k = ext;
+            ra.v = ext + (size_t)D * el;
+            ra.k_stride = ra.v_stride = 3ll * D;
+            launch_cache_read(bf, ra, s);
+        } else if (skip > 0) {
+            HIP_TRY(hipMemcpy2DAsync(ext, 3 * D * el, (const char*)wk.kvc + (size_t)l * kv_bytes,
                                      2 * D * el, 2 * D * el, N, hipMemcpyDeviceToDevice, s));
-        if (fill >= 0)
+        }
+        if (fill >= 0 && d.cache8) {
+            WriteArgs wa{};
+            wa.c = ref_cache(d, wk, l);
+            wa.seq = {1, (int)ref_pages(d), N, nullptr, nullptr, wk.zero};
+            wa.seq.one = 1;
+            wa.k = (const char*)wk.qkv + (size_t)D * el;
+            wa.v = (const char*)wk.qkv + (size_t)2 * D * el;
+            wa.k_stride = wa.v_stride = 3ll * D;
+            wa.row_idx = pos + (size_t)fill * N;
+            launch_cache_write(bf, wa, s);
+        } else if (fill >= 0) {
             launch_copy_ref_kv(wk.qkv, pos, fill, N, D, (int)el,
                                (char*)wk.kvc + (size_t)l * kv_bytes, s);
+        }
         g.a_idx = nullptr;
         AttnArgs at{};
         at.qkv = wk.qkv;
@@ -947,7 +1011,7 @@ int check_cache(const dv_cache* c, int n_seqs, const int32_t* table, int table_p
     if (rows < 0) return fail(DV_EINVAL, "rows must be >= 0 (got %d)", rows);
     if (!offsets && rows > 0 && rows < n_seqs)
         return fail(DV_EINVAL, "without offsets every sequence has a row: %d rows for %d sequences", rows, n_seqs);
-    if (page_slots(offsets ? (const int*)c->k : nullptr, n_seqs, rows, page_shift(c->page_tokens)) * 2 * c->kv_heads *
+    if (page_slots(offsets, n_seqs, rows, page_shift(c->page_tokens)) * 2 * c->kv_heads *
             256 > MAX_THREADS)
         return fail(DV_EINVAL, "%d rows of %d sequences with %d heads are too many for one call", rows, n_seqs,
                     c->kv_heads);
@@ -1053,6 +1117,7 @@ int dv_create(const dv_config* cfg, const float* weights, size_t weights_bytes, 
     }
     std::vector<size_t> dco(d.decision ? L : 0);
     for (auto& o : dco) o = reserve(DEC_FLOATS * 4);
+    const size_t o_rot = d.rotary ? reserve(N * 3 * 4) : 0;
     // an optional cap on the device memory a handle may take (weights and workspace), checked
     // before any device call: DV_MAX_DEVICE_BYTES in the environment
     if (const char* cap = getenv("DV_MAX_DEVICE_BYTES")) {
@@ -1108,9 +1173,21 @@ int dv_create(const dv_config* cfg, const float* weights, size_t weights_bytes, 
     }
     for (auto o : dco) put_vec(o, DEC_FLOATS);   // W_d1, b_d1, W_d2, b_d2 as the kernel reads them
 
+    dv_rotary_plan plan{};
+    if (d.rotary) {   // the class token stays; the patch of row r and column c is at (0, r + 1, c + 1)
+        const int q = d.D / d.H / 4, section[3] = {0, q, q}, side = d.S / d.p;
+        if ((rc = dv_rotary_init(&plan, section, DV_ROTARY_HALVES, 1, DV_ROTARY_BASE))) return rc;
+        int* at = (int*)(host.data() + o_rot);
+        for (int i = 0; i < d.P; ++i) {
+            at[3 * (i + 1) + 1] = i / side + 1;
+            at[3 * (i + 1) + 2] = i % side + 1;
+        }
+    }
+
     dv_handle* h = new (std::nothrow) dv_handle();
     if (!h) return fail(DV_ENOMEM, "handle");
     h->d = d;
+    h->rot = kernel_plan(d.rotary ? &plan : nullptr);
     auto cleanup = [&](int code) {
         if (h->wmem) (void)hipFree(h->wmem);
         if (h->ws) (void)hipFree(h->ws);
@@ -1140,6 +1217,7 @@ int dv_create(const dv_config* cfg, const float* weights, size_t weights_bytes, 
     h->pos = (const float*)(wb + o_pos);
     h->lnf_g = (const float*)(wb + o_lnf_g);
     h->lnf_b = (const float*)(wb + o_lnf_b);
+    if (d.rotary) h->rot_pos = (const int*)(wb + o_rot);
     h->layers.resize(L);
     for (size_t l = 0; l < L; ++l) {
         LayerW& w = h->layers[l];

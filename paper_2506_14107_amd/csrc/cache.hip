@@ -187,7 +187,7 @@ __device__ __forceinline__ float wave_max(float v) {
 
 // The part of a page that slot u stands for.
 __device__ __forceinline__ PagePart page_part(const SeqArgs& q, int pt, int pages, int u) {
-    const int s = q.offsets ? find_seq(q.offsets, q.n_seqs, 1, page_shift(pt), 2, u) : u;
+    const int s = q.one ? 0 : q.offsets ? find_seq(q.offsets, q.n_seqs, 1, page_shift(pt), 2, u) : u;
     return part_at(q, pt, pages, s, u);
 }
 
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256) void cache_write_k(WriteArgs a) {
         const int i = tid + k * 256;
         if (i >= items) break;
         const int t = i / per_tok, c = i % per_tok, row = p.row0 + t;
-        const size_t at = (size_t)row * stride + (size_t)h * dh;
+        const size_t at = (size_t)(a.row_idx ? a.row_idx[row] : row) * stride + (size_t)h * dh;
         const int* pos = a.pos + (size_t)row * 3;
         if (a.vec == 8) {
             float u[8], w[8];
@@ -423,7 +423,7 @@ void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
     bool wide = a.rot.dim % 16 == 0 && aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el);
     if (a.q) wide = wide && aligned16(a.q, a.q_stride, el) && aligned16(a.q_out, a.qo_stride, el);
     a.vec = wide ? 8 : 1;
-    a.slots = (int)page_slots(a.seq.offsets, a.seq.n_seqs, a.seq.rows, page_shift(a.c.page_tokens));
+    a.slots = (int)page_slots(a.seq.offsets || a.seq.one, a.seq.n_seqs, a.seq.rows, page_shift(a.c.page_tokens));
     const long long q_items = a.q ? (long long)a.seq.rows * a.q_heads * (a.c.head_dim / (2 * a.vec)) : 0;
     const dim3 grid((unsigned)((long long)a.slots * 2 * a.c.kv_heads + (q_items + 255) / 256));
     const size_t lds = (size_t)a.c.page_tokens * (a.c.head_dim + 4);
@@ -434,7 +434,8 @@ void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
 void launch_cache_read(bool bf, ReadArgs a, hipStream_t s) {
     const size_t el = bf ? 2 : 4;
     a.vec = aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el) ? 8 : 1;
-    const long long slots = page_slots(a.seq.offsets, a.seq.n_seqs, a.seq.rows, page_shift(a.c.page_tokens));
+    const long long slots = page_slots(a.seq.offsets || a.seq.one, a.seq.n_seqs, a.seq.rows,
+                                       page_shift(a.c.page_tokens));
     const dim3 grid((unsigned)(slots * 2 * a.c.kv_heads));
     const size_t lds = (size_t)a.c.head_dim * (a.c.page_tokens + 4);
     if (bf) cache_read_k<true><<<grid, 256, lds, s>>>(a);

@@ -25,13 +25,14 @@ __host__ __device__ inline int page_of(const int* table, int table_pages, int pa
 
 // ---- rows of a call ------------------------------------------------------------------------------
 // Rows of sequence s: offsets[s] .. offsets[s + 1] - 1, cut to the rows there are; without offsets
-// sequence s has row s.
+// sequence s has row s (or the call's one sequence has them all).
 struct Span {
     int row0, n;
 };
-__host__ __device__ inline Span rows_of(const int* offsets, int rows, int s) {
-    if (!offsets) return {s, s < rows ? 1 : 0};
-    const int a = offsets[s] < 0 ? 0 : offsets[s], b = offsets[s + 1] < rows ? offsets[s + 1] : rows;
+__host__ __device__ inline Span rows_of(const SeqArgs& q, int s) {
+    if (q.one) return {0, q.rows};
+    if (!q.offsets) return {s, s < q.rows ? 1 : 0};
+    const int a = q.offsets[s] < 0 ? 0 : q.offsets[s], b = q.offsets[s + 1] < q.rows ? q.offsets[s + 1] : q.rows;
     return {a, b > a ? b - a : 0};
 }
 
@@ -42,7 +43,7 @@ __host__ __device__ inline Span rows_of(const int* offsets, int rows, int s) {
 __host__ __device__ inline long long slot_base(int offset, int mul, int shift, int add, int s) {
     return ((long long)offset * mul >> shift) + (long long)add * s;
 }
-__host__ __device__ inline long long page_slots(const int* offsets, int n_seqs, int rows, int shift) {
+__host__ __device__ inline long long page_slots(bool offsets, int n_seqs, int rows, int shift) {
     return offsets ? slot_base(rows, 1, shift, 2, n_seqs) : n_seqs;
 }
 
@@ -57,10 +58,10 @@ __host__ __device__ inline PagePart part_at(const SeqArgs& q, int pt, int pages,
     PagePart p = {-1, 0, 0, 0};
     if (s < 0 || s >= q.n_seqs) return p;
     const int shift = page_shift(pt);
-    const Span sp = rows_of(q.offsets, q.rows, s);
+    const Span sp = rows_of(q, s);
     const int start = q.at[s];
     if (sp.n == 0 || start < 0) return p;
-    const long long j = q.offsets ? u - slot_base(q.offsets[s], 1, shift, 2, s) : 0;
+    const long long j = q.one ? u : q.offsets ? u - slot_base(q.offsets[s], 1, shift, 2, s) : 0;
     const long long page = ((long long)start >> shift) + j;     // of the sequence
     const long long end = (long long)start + sp.n, next = (page + 1) << shift;
     const long long a = start > page << shift ? start : page << shift, b = end < next ? end : next;
@@ -90,7 +91,7 @@ __host__ __device__ inline long long tile_slots(bool offsets, int n_seqs, int ro
 __host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int shift, bool causal, int s, long long u) {
     Tile t = {-1, 0, 0, 0, 0, 0, 0};
     if (s < 0 || s >= q.n_seqs) return t;
-    const Span sp = rows_of(q.offsets, q.rows, s);
+    const Span sp = rows_of(q, s);
     const long long j = q.offsets ? u - slot_base(q.offsets[s], group, shift, 1, s)
                                   : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
     const long long first = j << shift, left = (long long)sp.n * group - first;

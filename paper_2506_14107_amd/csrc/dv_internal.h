@@ -304,6 +304,7 @@ struct SeqArgs {
     const int* table;      // [n_seqs, table_pages] (nullptr: sequence s has pages s * table_pages ..)
     const int* offsets;    // [n_seqs + 1] first row of each sequence (nullptr: one row each)
     const int* at;         // [n_seqs] write, read: place of the first row; attention: keys
+    int one;               // one sequence that all rows belong to (offsets nullptr)
 };
 struct WriteArgs {
     CacheView c;
@@ -313,6 +314,7 @@ struct WriteArgs {
     long long k_stride, v_stride, q_stride, qo_stride;
     int q_heads;
     const int* pos;            // [rows, 3]; unused where rot.dim is 0
+    const int* row_idx;        // row r of the call is row row_idx[r] of k and v (nullptr: r)
     RotaryPlan rot;
     int slots, vec;            // set by the launcher
 };

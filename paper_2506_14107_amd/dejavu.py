@@ -21,6 +21,8 @@ STAGES = ["patch", "gate", "compact", "ln1", "qkv", "attn", "oproj", "ln2", "fc1
 DV_FLAG_RESTORE = 1
 DV_FLAG_DECISION = 2
 DV_FLAG_REORDER = 4
+DV_FLAG_ROTARY = 16
+DV_FLAG_CACHE8 = 32
 DV_ROTARY_HALVES, DV_ROTARY_PAIRS = 0, 1
 
 
@@ -286,7 +288,9 @@ class Encoder:
         self.model = m
         flags = (DV_FLAG_RESTORE if getattr(m, "restore", False) else 0) | \
             (DV_FLAG_DECISION if getattr(m, "decision", False) else 0) | \
-            (DV_FLAG_REORDER if getattr(m, "reorder", False) else 0)
+            (DV_FLAG_REORDER if getattr(m, "reorder", False) else 0) | \
+            (DV_FLAG_ROTARY if getattr(m, "rotary", False) else 0) | \
+            (DV_FLAG_CACHE8 if getattr(m, "cache8", False) else 0)
         self.cfg = make_config(m.image_size, m.patch, m.depth, m.width, m.heads, m.mlp, m.dtype,
                                max_batch_frames, flags)
         self.handle = dv_create(self.cfg, weights)

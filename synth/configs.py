@@ -27,6 +27,8 @@ class ModelConfig:
     restore: bool = False   # per-layer restoration MLP on reused tokens (hidden RESTORE_HIDDEN)
     decision: bool = False  # per-layer learned decision MLP as the gate (hidden DECISION_HIDDEN)
     reorder: bool = False   # I/P/B referencing with past and future references (no weights)
+    rotary: bool = False    # queries and keys turned by their patch's row and column (no weights)
+    cache8: bool = False    # a stream's cached reference keys and values in 8 bits
 
     @property
     def n_patches(self) -> int:
@@ -43,7 +45,8 @@ class ModelConfig:
     def as_dict(self):
         return dict(image_size=self.image_size, patch=self.patch, depth=self.depth,
                     width=self.width, heads=self.heads, mlp=self.mlp, dtype=self.dtype,
-                    restore=self.restore, decision=self.decision, reorder=self.reorder)
+                    restore=self.restore, decision=self.decision, reorder=self.reorder,
+                    rotary=self.rotary, cache8=self.cache8)
 
 
 @dataclass(frozen=True)

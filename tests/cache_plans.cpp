@@ -11,7 +11,7 @@ extern "C" {
 int t_page_parts(const int* table, int table_pages, int pages, const int* offsets, int n_seqs, int rows,
                  const int* starts, int pt, int* out) {
     const SeqArgs q = {n_seqs, table_pages, rows, table, offsets, starts};
-    const int slots = (int)page_slots(offsets, n_seqs, rows, page_shift(pt));
+    const int slots = (int)page_slots(offsets != nullptr, n_seqs, rows, page_shift(pt));
     for (int u = 0; u < slots; ++u) {
         int s = offsets ? -1 : u;
         if (offsets)
