@@ -417,63 +417,89 @@ def compact(masks, group_size, stream=None):
 
 
 # ---- token rows and their 8-bit cache -----------------------------------------------------------
-def _dtype(t):
+# Small calls are bound by what the host does, so the checks below read few attributes.
+def _torch():
     import torch
-    if t.dtype is torch.bfloat16:
+    return torch
+
+
+def _dtype(t):
+    d = t.dtype
+    torch = _torch()
+    if d is torch.bfloat16:
         return DV_BF16
-    if t.dtype is torch.float32:
+    if d is torch.float32:
         return DV_F32
-    raise ValueError(f"rows must be bf16 or fp32 (got {t.dtype})")
+    raise ValueError(f"rows must be bf16 or fp32 (got {d})")
 
 
-def _rows(name, t, device, heads=None, head_dim=None, rows=None, dtype=None):
-    """Checks a row tensor [rows, heads, head_dim] whose heads lie side by side; returns its row
-    stride."""
-    if t.dim() != 3 or t.device != device:
-        raise ValueError(f"{name} must be a tensor [rows, heads, head_dim] on {device}")
+def _misfit(name, t):
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, type {t.dtype} and device {t.device}, which "
+                     "do not fit the other arguments")
+
+
+def _stride(name, t):
+    """Row stride of a tensor [rows, heads, head_dim] whose heads lie side by side."""
     n, h, d = t.shape
-    if ((heads is not None and h != heads) or (head_dim is not None and d != head_dim)
-            or (rows is not None and n != rows) or (dtype is not None and t.dtype is not dtype)):
-        raise ValueError(f"{name} has shape {tuple(t.shape)} and type {t.dtype}, which does not fit "
-                         "the other arguments")
     sr, sh, sd = t.stride()
-    if (d > 1 and sd != 1) or (h > 1 and sh != d):
+    if (sd != 1 and d > 1) or (sh != d and h > 1):
         raise ValueError(f"the heads of a row of {name} must lie side by side")
     return sr if n > 1 else max(sr, h * d)
 
 
-def _ints(name, t, device, shape):
-    import torch
-    if (t.dtype is not torch.int32 or t.device != device or tuple(t.shape) != tuple(shape)
+def _rows(name, t, shape, dtype, index):
+    """Checks a row tensor against what it has to be; returns its row stride."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        _misfit(name, t)
+    return _stride(name, t)
+
+
+def _ints(name, t, index, shape):
+    if (t.dtype is not _torch().int32 or t.get_device() != index or t.shape != shape
             or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on device {index}")
     return t.data_ptr()
 
 
-class _On:
-    """The device and stream a call runs on: makes the device current where it is not, and a given
-    stream current where it is another than the device's own (so that what the call allocates
-    belongs to it)."""
+class _Away:
+    """Makes a device current where it is not, and a given stream where there is one, so that what
+    the call allocates belongs to it."""
 
-    def __init__(self, device, stream):
-        import torch
-        if device.type != "cuda":
-            raise ValueError("tensors must be on a HIP device")
-        self.stack = []
-        if torch.cuda.current_device() != device.index:
-            self.stack.append(torch.cuda.device(device))
-        if stream is not None:
-            self.stack.append(torch.cuda.stream(stream))
+    def __init__(self, index, stream):
+        torch = _torch()
+        self.stack = [torch.cuda.device(index)] + ([torch.cuda.stream(stream)] if stream else [])
 
     def __enter__(self):
-        import torch
         for c in self.stack:
             c.__enter__()
-        return torch.cuda.current_stream().cuda_stream
 
     def __exit__(self, *e):
         for c in reversed(self.stack):
             c.__exit__(*e)
+
+
+class _Here:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *e):
+        pass
+
+
+_HERE = _Here()
+
+
+def _on(index, stream):
+    """Context of a call on device `index` and on `stream` (None: the device's current one)."""
+    if index < 0:
+        raise ValueError("tensors must be on a HIP device")
+    if stream is None and _torch().cuda.current_device() == index:
+        return _HERE
+    return _Away(index, stream)
+
+
+def _raw_stream(index):
+    return _torch()._C._cuda_getCurrentRawStream(index)
 
 
 class Rotary:
@@ -495,18 +521,21 @@ class Rotary:
 def rotary(x, positions, rot, out=None, stream=None):
     """Rows x [rows, heads, head_dim] with their heads turned by `positions` (int32 [rows, 3]) at the
     rates of `rot` (Rotary), into `out` (which may be x) or a new tensor."""
-    import torch
-    device = x.device
-    with _On(device, stream) as s:
-        n, h, d = x.shape
-        xs = _rows("x", x, device)
+    index = x.get_device()
+    if x.dim() != 3:
+        _misfit("x", x)
+    with _on(index, stream):
+        shape = n, h, d = x.shape
+        dtype = _dtype(x)
+        xs = _stride("x", x)
         if out is None:
-            out = torch.empty((n, h, d), dtype=x.dtype, device=device)
+            out = _torch().empty(shape, dtype=x.dtype, device=x.device)
             os = h * d
         else:
-            os = _rows("out", out, device, h, d, n, x.dtype)
-        dv_rotary(rot.address, _dtype(x), x.data_ptr(), xs, n, h, d,
-                  _ints("positions", positions, device, (n, 3)), out.data_ptr(), os, s)
+            os = xs if out is x else _rows("out", out, shape, x.dtype, index)
+        dv_rotary(rot.address, dtype, x.data_ptr(), xs, n, h, d,
+                  _ints("positions", positions, index, (n, 3)), out.data_ptr(), os,
+                  _raw_stream(index))
     return out
 
 
@@ -523,7 +552,7 @@ class TokenCache:
     """
 
     def __init__(self, pages, kv_heads, head_dim, page_tokens=64, device=None, buffers=None):
-        import torch
+        torch = _torch()
         shapes = [(pages, kv_heads, page_tokens, head_dim), (pages, kv_heads, head_dim, page_tokens),
                   (pages, kv_heads), (pages, kv_heads)]
         types = [torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32]
@@ -535,7 +564,7 @@ class TokenCache:
                     or b.device != buffers[0].device):
                 raise ValueError(f"a cache buffer must be a contiguous {t} tensor {list(s)}")
         self.k, self.v, self.k_scale, self.v_scale = buffers
-        self.device = self.k.device
+        self.device, self.index = self.k.device, self.k.get_device()
         self.pages, self.kv_heads = pages, kv_heads
         self.head_dim, self.page_tokens = head_dim, page_tokens
         self.desc = dv_cache(*(b.data_ptr() for b in buffers), pages, page_tokens, kv_heads,
@@ -544,60 +573,68 @@ class TokenCache:
 
     def _seqs(self, at, name, offsets, table):
         """(n_seqs, table, table_pages, offsets, at) as the entry points take them."""
-        n = at.shape[0]
+        index = self.index
+        n = at.shape[0] if at.dim() == 1 else -1
         if table is None:
             t, tp = 0, self.pages // max(n, 1)
         else:
             tp = table.shape[1] if table.dim() == 2 else -1
-            t = _ints("table", table, self.device, (n, tp))
-        o = 0 if offsets is None else _ints("offsets", offsets, self.device, (n + 1,))
-        return n, t, tp, o, _ints(name, at, self.device, (n,))
+            t = _ints("table", table, index, (n, tp))
+        o = 0 if offsets is None else _ints("offsets", offsets, index, (n + 1,))
+        return n, t, tp, o, _ints(name, at, index, (n,))
 
     def write(self, k, v, starts, offsets=None, table=None, rotary=None, positions=None, q=None,
               q_out=None, stream=None):
         """Quantises rows k and v [rows, kv_heads, head_dim] into places starts[s] .. of each
         sequence.  With `rotary` and `positions` the keys are turned first, and the rows of q
         [rows, heads, head_dim] into `q_out` (which may be q) or a new tensor, which is returned."""
-        import torch
-        dev = self.device
-        with _On(dev, stream) as s:
+        index = self.index
+        with _on(index, stream):
             n, t, tp, o, at = self._seqs(starts, "starts", offsets, table)
-            ks = _rows("k", k, dev, self.kv_heads, self.head_dim)
-            rows = k.shape[0]
-            vs = _rows("v", v, dev, self.kv_heads, self.head_dim, rows, k.dtype)
-            if (rotary is None) != (positions is None):
+            rows, dt = k.shape[0], k.dtype
+            dtype = _dtype(k)
+            shape = (rows, self.kv_heads, self.head_dim)
+            ks = _rows("k", k, shape, dt, index)
+            vs = _rows("v", v, shape, dt, index)
+            plan = pos = qp = qs = qop = qos = heads = 0
+            if rotary is not None and positions is not None:
+                plan, pos = rotary.address, _ints("positions", positions, index, (rows, 3))
+            elif rotary is not None or positions is not None:
                 raise ValueError("rotary and positions come together")
-            qs = qos = heads = 0
             if q is not None:
-                qs = _rows("q", q, dev, None, self.head_dim, rows, k.dtype)
+                if q.dim() != 3:
+                    _misfit("q", q)
                 heads = q.shape[1]
+                shape = (rows, heads, self.head_dim)
+                qs = _rows("q", q, shape, dt, index)
                 if q_out is None:
-                    q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-                qos = _rows("q_out", q_out, dev, heads, self.head_dim, rows, k.dtype)
+                    q_out = _torch().empty(shape, dtype=dt, device=q.device)
+                qos = _rows("q_out", q_out, shape, dt, index)
+                qp, qop = q.data_ptr(), q_out.data_ptr()
             elif q_out is not None:
                 raise ValueError("q_out without q")
-            dv_cache_write(self.address, n, t, tp, o, at, _dtype(k), k.data_ptr(), ks,
-                           v.data_ptr(), vs, rows, 0 if rotary is None else rotary.address,
-                           0 if rotary is None else _ints("positions", positions, dev, (rows, 3)),
-                           _ptr(q), qs, heads, _ptr(q_out), qos, s)
+            dv_cache_write(self.address, n, t, tp, o, at, dtype, k.data_ptr(), ks, v.data_ptr(), vs,
+                           rows, plan, pos, qp, qs, heads, qop, qos, _raw_stream(index))
         return q_out
 
     def read(self, starts, offsets=None, table=None, rows=None, dtype=None, out=None, stream=None):
         """Keys and values [rows, kv_heads, head_dim] of places starts[s] .. of each sequence, into
         `out` (a pair of tensors) or new tensors of `rows` rows and `dtype` (bf16)."""
-        import torch
-        dev = self.device
-        with _On(dev, stream) as s:
+        index = self.index
+        with _on(index, stream):
             n, t, tp, o, at = self._seqs(starts, "starts", offsets, table)
             if out is None:
+                torch = _torch()
                 shape = (n if rows is None else rows, self.kv_heads, self.head_dim)
-                out = [torch.empty(shape, dtype=dtype or torch.bfloat16, device=dev)
+                out = [torch.empty(shape, dtype=dtype or torch.bfloat16, device=self.device)
                        for _ in range(2)]
             k, v = out
-            ks = _rows("k", k, dev, self.kv_heads, self.head_dim)
-            vs = _rows("v", v, dev, self.kv_heads, self.head_dim, k.shape[0], k.dtype)
+            rows, dt = k.shape[0], k.dtype
+            shape = (rows, self.kv_heads, self.head_dim)
+            ks = _rows("k", k, shape, dt, index)
+            vs = _rows("v", v, shape, dt, index)
             dv_cache_read(self.address, n, t, tp, o, at, _dtype(k), k.data_ptr(), ks, v.data_ptr(),
-                          vs, k.shape[0], s)
+                          vs, rows, _raw_stream(index))
         return out
 
     def attention(self, q, lengths, offsets=None, table=None, causal=True, scale=None, max_rows=0,
@@ -606,26 +643,32 @@ class TokenCache:
         sequences, into `out` or a new tensor.  causal: the rows are the sequence's last places and
         see no later ones.  max_rows: an upper bound of any sequence's rows, if known.  workspace: a
         uint8 tensor to use (see attention_workspace) instead of one of the call's own."""
-        import torch
-        dev = self.device
-        with _On(dev, stream) as s:
+        index = self.index
+        with _on(index, stream):
             n, t, tp, o, at = self._seqs(lengths, "lengths", offsets, table)
-            qs = _rows("q", q, dev, None, self.head_dim)
+            if q.dim() != 3:
+                _misfit("q", q)
             rows, heads, d = q.shape
+            shape = (rows, heads, self.head_dim)
+            qs = _rows("q", q, shape, q.dtype, index)
+            dtype = _dtype(q)
             if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+                out = _torch().empty(shape, dtype=q.dtype, device=q.device)
                 os = heads * d
             else:
-                os = _rows("out", out, dev, heads, d, rows, q.dtype)
+                os = _rows("out", out, shape, q.dtype, index)
             if workspace is None:
                 need = dv_cache_attention_workspace(self.address, n, tp, o != 0, rows, heads,
                                                     max_rows)
                 if need:
-                    workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-            dv_cache_attention(self.address, n, t, tp, o, at, _dtype(q), q.data_ptr(), qs, rows,
-                               heads, max_rows, d ** -0.5 if scale is None else scale, causal,
+                    torch = _torch()
+                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            elif workspace.get_device() != index or workspace.dtype is not _torch().uint8:
+                _misfit("workspace", workspace)
+            dv_cache_attention(self.address, n, t, tp, o, at, dtype, q.data_ptr(), qs, rows, heads,
+                               max_rows, d ** -0.5 if scale is None else scale, causal,
                                out.data_ptr(), os, _ptr(workspace),
-                               0 if workspace is None else workspace.numel(), s)
+                               0 if workspace is None else workspace.numel(), _raw_stream(index))
         return out
 
     def attention_workspace(self, n_seqs, rows, heads, table_pages=None, with_offsets=True,
