@@ -30,6 +30,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int TS = 4, TR = 1 << TS;   // packed rows of a tile
 constexpr int STEP = 64;   // keys of a step
 constexpr int WAVES = 4;
+constexpr int MAX_SPLITS = 512;
 
 // f of the two values that lanes whose numbers differ in one bit (4 or 5) hold, in both: the swap gives
 // one lane's value in its first result and the other's in its second.  (The elements are copied before
@@ -121,6 +122,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     const int G = a.q_heads / H;
     const int g = lane >> 4, c16 = lane & 15;
     const float sl2 = a.scale * 1.4426950408889634f;
+    const float lazy = 8.f / sl2;
 
     // the lane's query: packed row first + c16 (rows past the tile repeat its last one)
     const int r = t.first + min(c16, t.rows - 1), qi = r / G;
@@ -146,21 +148,25 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     for (int c = 0; c < CT; ++c) o[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
 
-    for (int kb = k0 + wave * STEP; kb < k1; kb += WAVES * STEP) {
-        // pages: of the key rows that the lane loads (group c16 / 4), and of the group it owns
-        const int kk = kb + (c16 >> 2) * 16, kv = kb + g * 16;
-        const int kp = page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, kk >> shift);
-        const int vp = page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, kv >> shift);
-        const size_t kpage = (size_t)max(kp, 0) * H + h, vpage = (size_t)max(vp, 0) * H + h;
-        const uint8_t* kbase = a.c.k + (kpage * pt + (kk & (pt - 1)) + (c16 & 3)) * DH;
-        const uint8_t* vbase = a.c.v + (vpage * DH + c16) * pt + (kv & (pt - 1));
-        const float ks = a.c.k_scale[kpage];
-        float vs = a.c.v_scale[vpage];
-        uint32_t kw[4][KS][2];
-        u32x4 vw[CT];
+    // pages of the step at kb: of the key rows that the lane loads (group c16 / 4), and of the group it owns
+    struct Pages {
+        int k, v;
+    };
+    auto pages = [&](int kb) {
+        return Pages{page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, (kb + (c16 >> 2) * 16) >> shift),
+                     page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, (kb + g * 16) >> shift)};
+    };
+    uint32_t kw[4][KS][2];
+    u32x4 vw[CT];
+    float ks, vs;
+    auto load_keys = [&](int kb, const Pages& pg) {
+        const int kk = kb + (c16 >> 2) * 16;
+        const size_t page = (size_t)max(pg.k, 0) * H + h;
+        const uint8_t* base = a.c.k + (page * pt + (kk & (pt - 1)) + (c16 & 3)) * DH;
+        ks = a.c.k_scale[page];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const uint8_t* row = kbase + q * 4 * DH;
+            const uint8_t* row = base + q * 4 * DH;
             if constexpr (WIDE) {
 #pragma unroll
                 for (int s = 0; s < KS; s += 2) {
@@ -177,9 +183,29 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
                 }
             }
         }
+    };
+    auto load_values = [&](int kb, const Pages& pg) {
+        const int kv = kb + g * 16;
+        const size_t page = (size_t)max(pg.v, 0) * H + h;
+        const uint8_t* base = a.c.v + (page * DH + c16) * pt + (kv & (pt - 1));
+        vs = a.c.v_scale[page];
 #pragma unroll
-        for (int c = 0; c < CT; ++c) vw[c] = *(const u32x4*)(vbase + (size_t)c * 16 * pt);
+        for (int c = 0; c < CT; ++c) vw[c] = *(const u32x4*)(base + (size_t)c * 16 * pt);
+    };
 
+    // The wavefront's steps.  The registers of a step's keys take the next step's codes as soon as its scores
+    // are computed, those of its values when their product is; the pages of the step after that are
+    // asked for between the two, because loads are waited for in order.
+    constexpr int NEXT = WAVES * STEP;
+    int kb = k0 + wave * STEP;
+    Pages now = pages(kb), next = pages(kb + NEXT);
+    if (kb < k1) {
+        load_keys(kb, now);
+        load_values(kb, now);
+    }
+    for (; kb < k1; kb += NEXT) {
+        const bool more = kb + NEXT < k1, present = now.v >= 0;
+        const int kv = kb + g * 16;
         float sc[16];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -194,9 +220,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) sc[q * 4 + e] = acc[e];
         }
+        __builtin_amdgcn_sched_barrier(0);
+        Pages after = next;
+        if (more) {
+            load_keys(kb + NEXT, next);
+            after = pages(kb + 2 * NEXT);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         // keys kv .. kv + 15 belong to the lane; those it does not see, and those of pages that are
         // not there, get -inf
-        const int live = vp >= 0 ? min(sees, k1) - kv : 0;
+        const int live = present ? min(sees, k1) - kv : 0;
         const bool some = __any(live < 16);
         uint32_t nans = 0;
         if (some) {
@@ -204,7 +237,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
             for (int e = 0; e < 16; ++e) sc[e] = e < live ? sc[e] : -INFINITY;
             // values that no row of the tile sees may hold anything, NaN among them, and so may the
             // scale of a page that has none else: 0
-            const int there = vp >= 0 ? k1 - kv : 0;
+            const int there = present ? k1 - kv : 0;
             if (there <= 0) vs = 1.f;
 #pragma unroll
             for (int c = 0; c < CT; ++c)
@@ -219,17 +252,21 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
 #pragma unroll
         for (int e = 1; e < 16; ++e) top = fmaxf(top, sc[e]);
         top = group_max(top);
-        const float mn = fmaxf(m, top);
-        const float ref = mn == -INFINITY ? 0.f : mn;      // no key seen yet: all probabilities 0
-        const float alpha = __builtin_amdgcn_exp2f((m - ref) * sl2);
-        m = mn;
-        l *= alpha;
+        // rescale only when some row's maximum has grown by more than 2^8: probabilities stay far
+        // inside the range of fp32 and bf16
+        if (__any(top > m + lazy)) {
+            const float mn = fmaxf(m, top);
+            const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * sl2);
+            m = mn;
+            l *= alpha;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) o[c] *= alpha;
+            for (int c = 0; c < CT; ++c) o[c] *= alpha;
+        }
+        const float off = m == -INFINITY ? 0.f : -m * sl2;      // no key seen yet: all probabilities 0
         float p[2][8];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            p[e >> 3][e & 7] = __builtin_amdgcn_exp2f((sc[e] - ref) * sl2);
+            p[e >> 3][e & 7] = __builtin_amdgcn_exp2f(fmaf(sc[e], sl2, off));
             l += p[e >> 3][e & 7];
         }
         bf16x8 pf[2][NT];
@@ -257,9 +294,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
                 f32x4 hit = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const uint32_t n0 = nan_bytes(vw[c][2 * k]), n1 = nan_bytes(vw[c][2 * k + 1]);
-                    const bf16x8 vf = decode8(vw[c][2 * k] & ~((n0 >> 7) * 255u), vw[c][2 * k + 1] & ~((n1 >> 7) * 255u), vs);
-                    const bf16x8 nf = decode8((n0 >> 7) * 0x38u, (n1 >> 7) * 0x38u, 1.f);   // 0x38: 1
+                    const uint32_t w0 = vw[c][2 * k], w1 = vw[c][2 * k + 1];
+                    const uint32_t n0 = nan_bytes(w0) >> 7, n1 = nan_bytes(w1) >> 7;
+                    const bf16x8 vf = decode8(w0 & ~(n0 * 255u), w1 & ~(n1 * 255u), vs);
+                    const bf16x8 nf = decode8(n0 * 0x38u, n1 * 0x38u, 1.f);   // 0x38: 1
 #pragma unroll
                     for (int n = NT - 1; n >= 0; --n)
                         o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k][n], o[c], 0, 0, 0);
@@ -269,6 +307,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
                 for (int e = 0; e < 4; ++e) o[c][e] = hit[e] > 0.f ? __builtin_nanf("") : o[c][e];
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) load_values(kb + NEXT, next);
+        __builtin_amdgcn_sched_barrier(0);
+        now = next;
+        next = after;
     }
 
     // join the wavefronts
@@ -305,43 +348,67 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     }
 }
 
-// Joins the splits of one row: lanes over the channels, groups of lanes over the splits.
+// Joins the splits of one row: the maxima and sums first, one split a thread, whose weights go to LDS; then
+// lanes over the channels, groups of lanes over the splits.
 template <bool BF>
 __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
+    __shared__ float s_w[MAX_SPLITS];
     __shared__ f32x4 s_x[256];
-    __shared__ float s_l[256];
+    __shared__ float s_r[2][4];
     const int tid = threadIdx.x;
-    const int H = a.c.kv_heads, DH = a.c.head_dim, row = blockIdx.y;
+    const int H = a.c.kv_heads, DH = a.c.head_dim;
     const int h = blockIdx.x % H;
     const long long u = blockIdx.x / H;
     const Tile t = tile_at<TS>(a, u);
-    if (t.seq < 0 || row >= t.rows || t.end <= a.chunk) return;
+    if (t.seq < 0 || t.end <= a.chunk) return;
     const int splits = (t.end + a.chunk - 1) / a.chunk;
-    const int lanes = DH / 4, groups = 256 / lanes;
-    const int ch = tid % lanes * 4, grp = tid / lanes;
     const float sl2 = a.scale * 1.4426950408889634f;
     const size_t per = part_floats(DH);
     const float* part = a.part + (((size_t)u * H + h) * a.splits) * per;
-    float top = -INFINITY;
-    for (int s = 0; s < splits; ++s) top = fmaxf(top, part[s * per + TR * DH + row]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    if (grp < groups)
-        for (int s = grp; s < splits; s += groups) {
-            const float* p = part + s * per;
-            const float f = __builtin_amdgcn_exp2f((p[TR * DH + row] - ref) * sl2);
-            sum += p[TR * DH + TR + row] * f;
-            x += *(const f32x4*)(p + row * DH + ch) * f;
+    for (int row = blockIdx.y; row < t.rows; row += gridDim.y) {   // one row a block, as a rule
+        float mx[MAX_SPLITS / 256], top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < MAX_SPLITS / 256; ++k) {
+            const int s = tid + k * 256;
+            mx[k] = s < splits ? part[s * per + TR * DH + row] : -INFINITY;
+            top = fmaxf(top, mx[k]);
         }
-    s_x[tid] = x;
-    s_l[tid] = sum;
-    __syncthreads();
-    if (grp == 0) {
-        for (int k = 1; k < groups; ++k) x += s_x[k * lanes + tid], sum += s_l[k * lanes + tid];
-        const int G = a.q_heads / H, pr = t.first + row;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        store4<BF>(a.out, (size_t)(t.row0 + pr / G) * a.o_stride + (size_t)(h * G + pr % G) * DH + ch, x * inv);
+        auto block = [&](float x, float (&r)[4], auto f) {
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1) x = f(x, __shfl_xor(x, o, 64));
+            if ((tid & 63) == 0) r[tid >> 6] = x;
+            __syncthreads();
+            return f(f(r[0], r[1]), f(r[2], r[3]));
+        };
+        top = block(top, s_r[0], [](float x, float y) { return fmaxf(x, y); });
+        const float ref = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < MAX_SPLITS / 256; ++k) {
+            const int s = tid + k * 256;
+            if (s < splits) {
+                const float w = __builtin_amdgcn_exp2f((mx[k] - ref) * sl2);
+                s_w[s] = w;
+                sum += part[s * per + TR * DH + TR + row] * w;
+            }
+        }
+        sum = block(sum, s_r[1], [](float x, float y) { return x + y; });
+        const int lanes = DH / 4, groups = 256 / lanes;
+        const int ch = tid % lanes * 4, grp = tid / lanes;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if (grp < groups) {
+#pragma unroll 4
+            for (int s = grp; s < splits; s += groups) x += *(const f32x4*)(part + s * per + row * DH + ch) * s_w[s];
+        }
+        s_x[tid] = x;
+        __syncthreads();
+        if (grp == 0) {
+            for (int k = 1; k < groups; ++k) x += s_x[k * lanes + tid];
+            const int G = a.q_heads / H, pr = t.first + row;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            store4<BF>(a.out, (size_t)(t.row0 + pr / G) * a.o_stride + (size_t)(h * G + pr % G) * DH + ch, x * inv);
+        }
+        __syncthreads();
     }
 }
 
@@ -353,19 +420,25 @@ void launch_dh(bool bf, const CacheAttnArgs& a, dim3 grid, hipStream_t s) {
 
 }  // namespace
 
-CacheAttnPlan cache_attn_plan(int n_seqs, int rows, bool offsets, int table_pages, int page_tokens, int kv_heads,
-                              int q_heads, int head_dim, int cus) {
+CacheAttnPlan cache_attn_plan(int n_seqs, int rows, bool offsets, int max_rows, int table_pages, int page_tokens,
+                              int kv_heads, int q_heads, int head_dim, int cus) {
     CacheAttnPlan p;
     const int G = q_heads / kv_heads;
     p.slots = tile_slots(offsets, n_seqs, rows, G, TS);
-    // splits of equal length, so that a ragged batch's long sequences spread over the chip: about four
-    // blocks a compute unit if every sequence is as long as its table, but no less than 256 keys each
+    // Splits of equal length.  One sequence: as many as are resident at once, two blocks a compute unit (one
+    // query over 200,001 keys of 8 heads of 128, us with 32 / 64 / 98 / 126 splits: 85 / 77 / 87 / 82).
+    // Several may have any lengths up to the table's: splits of 2048 keys at most, so that the long ones
+    // spread over the chip (64 sequences of 1 to 12,000 keys, us with splits of 1024 / 2048 / 3136 /
+    // 6272 / 12,032 keys: 171 / 161 / 167 / 180 / 182) unless there are many tiles anyway.  512 keys and fewer are not split: the join costs more.
     const long long keys = (long long)table_pages * page_tokens;   // at most 2^30
-    const long long blocks = std::max(1ll, 4ll * (cus > 0 ? cus : 256) / std::max(1ll, p.slots * kv_heads));
-    long long chunk = (keys + blocks - 1) / blocks;
-    chunk = std::max(256ll, (chunk + 255) / 256 * 256);
-    p.chunk = (int)chunk;
+    const long long units = std::max(1ll, p.slots * kv_heads);
+    const long long most = std::min<long long>(MAX_SPLITS, std::max(1ll, 2ll * (cus > 0 ? cus : 256) / units));
+    long long chunk = (keys + most - 1) / most;
+    if (n_seqs > 1 && units < 16ll * (cus > 0 ? cus : 256)) chunk = std::min(chunk, 2048ll);
+    chunk = std::max({chunk, 512ll, (keys + MAX_SPLITS - 1) / MAX_SPLITS});
+    p.chunk = (int)((chunk + 255) / 256 * 256);
     p.splits = (int)std::max(1ll, (keys + p.chunk - 1) / p.chunk);
+    p.tile_rows = (int)std::min<long long>(TR, (long long)(max_rows > 0 ? std::min(max_rows, rows) : rows) * G);
     p.bytes = p.splits > 1 ? (size_t)p.slots * kv_heads * p.splits * part_floats(head_dim) * sizeof(float) : 0;
     return p;
 }
@@ -383,7 +456,7 @@ void launch_cache_attention(bool bf, const CacheAttnArgs& a, hipStream_t s) {
         default: launch_dh<128>(bf, a, grid, s); break;
     }
     if (a.splits > 1) {
-        const dim3 join((unsigned)(a.slots * a.c.kv_heads), TR);
+        const dim3 join((unsigned)(a.slots * a.c.kv_heads), (unsigned)a.tile_rows);
         if (bf) cache_join_k<true><<<join, 256, 0, s>>>(a);
         else cache_join_k<false><<<join, 256, 0, s>>>(a);
     }

@@ -338,17 +338,19 @@ struct CacheAttnArgs {
     float scale;
     int causal;
     int chunk, splits;         // keys of a split, splits of the longest sequence the table holds
+    int tile_rows;             // packed rows of any tile, at most
     long long slots;           // row tiles dealt
     float* part;               // partial results, where splits > 1
 };
 // How a call is cut, from its sizes; the same rule sizes the workspace.
 struct CacheAttnPlan {
     int chunk, splits;
+    int tile_rows;             // packed rows of any tile, at most
     long long slots;
     size_t bytes;              // workspace
 };
-CacheAttnPlan cache_attn_plan(int n_seqs, int rows, bool offsets, int table_pages, int page_tokens, int kv_heads,
-                              int q_heads, int head_dim, int cus);
+CacheAttnPlan cache_attn_plan(int n_seqs, int rows, bool offsets, int max_rows, int table_pages, int page_tokens,
+                              int kv_heads, int q_heads, int head_dim, int cus);
 void launch_cache_attention(bool bf16, const CacheAttnArgs& a, hipStream_t s);
 
 }  // namespace dv
