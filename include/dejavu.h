@@ -409,7 +409,7 @@ int dv_cache_read(const dv_cache* cache, int n_seqs, const int32_t* table, int t
  * q_heads * rows >= 2^31, a scale that is not finite and positive, max_rows < 0, out rows that do not
  * start on four elements, a workspace that is too small or misaligned. */
 int dv_cache_attention_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets,
-                                 int rows, int q_heads, int max_rows, size_t* bytes);
+                                 int dtype, int rows, int q_heads, int max_rows, size_t* bytes);
 int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
                        const int32_t* offsets, const int32_t* lengths, int dtype, const void* q,
                        long long q_stride, int rows, int q_heads, int max_rows, float scale,

@@ -1508,15 +1508,15 @@ int dv_cache_read(const dv_cache* cache, int n_seqs, const int32_t* table, int t
     return DV_OK;
 }
 
-int dv_cache_attention_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets, int rows,
-                                 int q_heads, int max_rows, size_t* bytes) {
+int dv_cache_attention_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets, int dtype,
+                                 int rows, int q_heads, int max_rows, size_t* bytes) {
     if (!bytes) return fail(DV_EINVAL, "bytes is NULL");
     *bytes = 0;
     static const int32_t some = 0;   // the size does not depend on what a table holds
     int rc = check_cache(cache, n_seqs, &some, table_pages, with_offsets != 0, rows);
-    if (rc || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows))) return rc;
-    *bytes = cache_attn_plan(n_seqs, rows, with_offsets != 0, max_rows, table_pages, cache->page_tokens, cache->kv_heads,
-                             q_heads, cache->head_dim, device_cus()).bytes;
+    if (rc || (rc = check_dtype(dtype)) || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows))) return rc;
+    *bytes = cache_attn_plan(dtype == DV_BF16, n_seqs, rows, with_offsets != 0, max_rows, table_pages,
+                             cache->page_tokens, cache->kv_heads, q_heads, cache->head_dim, device_cus()).bytes;
     return DV_OK;
 }
 
@@ -1532,8 +1532,9 @@ int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, 
     if ((rc = check_stride("q", q_stride, wide)) || (rc = check_stride("out", out_stride, wide))) return rc;
     if ((uintptr_t)out % (dtype == DV_BF16 ? 8 : 16) || out_stride % 4)
         return fail(DV_EINVAL, "out rows must start on four elements");
-    const CacheAttnPlan p = cache_attn_plan(n_seqs, rows, offsets != nullptr, max_rows, table_pages,
-                                            cache->page_tokens, cache->kv_heads, q_heads, cache->head_dim, device_cus());
+    const CacheAttnPlan p = cache_attn_plan(dtype == DV_BF16, n_seqs, rows, offsets != nullptr, max_rows, table_pages,
+                                            cache->page_tokens, cache->kv_heads, q_heads, cache->head_dim,
+                                            device_cus());
     if (p.bytes && (!workspace || workspace_bytes < p.bytes || (uintptr_t)workspace % 16))
         return fail(DV_EINVAL, "the call needs a 16-byte aligned workspace of %zu bytes (got %zu)", p.bytes,
                     workspace ? workspace_bytes : 0);
@@ -1548,12 +1549,7 @@ int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, 
     a.q_heads = q_heads;
     a.scale = scale;
     a.causal = causal;
-    a.chunk = p.chunk;
-    a.splits = p.splits;
-    a.tile_rows = p.tile_rows;
-    a.slots = p.slots;
-    a.part = (float*)workspace;
-    launch_cache_attention(dtype == DV_BF16, a, stream);
+    launch_cache_attention(dtype == DV_BF16, a, p, (float*)workspace, stream);
     HIP_TRY(hipGetLastError());
     return DV_OK;
 }

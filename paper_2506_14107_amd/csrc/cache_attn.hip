@@ -21,6 +21,7 @@ namespace dv {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -28,6 +29,8 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int TS = 4, TR = 1 << TS;   // packed rows of a tile
+constexpr int LS = 7, LR = 1 << LS;   // packed rows of a large tile
+constexpr int FEW = 32;    // packed rows of a sequence up to which small tiles take it
 constexpr int STEP = 64;   // keys of a step
 constexpr int WAVES = 4;
 constexpr int MAX_SPLITS = 512;
@@ -74,10 +77,33 @@ __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&t)[T]) {
         }
     }
 }
-// bytes of w that are NaN codes
+// bytes of w that are NaN codes, as 0xFF
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-    const uint32_t x = w & 0x7F7F7F7Fu;
-    return (x + 0x01010101u) & 0x80808080u;
+    return (((w & 0x7F7F7F7Fu) + 0x01010101u & 0x80808080u) >> 7) * 255u;
+}
+
+// A NaN among values that only some rows of a tile see: its products with the other rows' zero
+// probabilities would be NaN too.  Steps that not all rows see in full take such codes as 0 and say so; if
+// one did, each lane looks through the values that its row sees in those steps.  (Products of indicators on
+// the matrix units instead, within the step, cost every step registers.)
+// Keys first .. last - 1 of sequence s, key/value head h: bit i tells of the lane's i-th channel, base +
+// stride (i / 4) + i % 4 (those below DH).
+__device__ __forceinline__ uint64_t find_nan(const CacheAttnArgs& a, int s, int h, int first, int last, int stride,
+                                             int base) {
+    const int pt = a.c.page_tokens, shift = page_shift(pt), DH = a.c.head_dim;
+    uint64_t found = 0;
+#pragma unroll 1
+    for (int key = first; key < last; ++key) {
+        const int page = page_of(a.seq.table, a.seq.table_pages, a.c.pages, s, key >> shift);
+        if (page < 0) continue;
+        const uint8_t* v = a.c.v + ((size_t)page * a.c.kv_heads + h) * DH * pt + (key & (pt - 1));
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i) {
+            const int ch = base + stride * (i >> 2) + (i & 3);
+            if (ch < DH && (v[(size_t)ch * pt] & 0x7F) == 0x7F) found |= 1ull << i;
+        }
+    }
+    return found;
 }
 
 template <int SHIFT>
@@ -85,7 +111,10 @@ __device__ __forceinline__ Tile tile_at(const CacheAttnArgs& a, long long u) {
     const int G = a.q_heads / a.c.kv_heads;
     const int s = a.seq.offsets ? find_seq(a.seq.offsets, a.seq.n_seqs, G, SHIFT, 1, u)
                                 : (int)(u / ((G + (1 << SHIFT) - 1) >> SHIFT));
-    return tile_of(a.seq, a.c.page_tokens, G, SHIFT, a.causal != 0, s, u);
+    Tile t = tile_of(a.seq, a.c.page_tokens, G, SHIFT, a.causal != 0, s, u);
+    // a mixed batch: short sequences go to the kernel of single tokens, the others to that of tiles
+    if (a.route == ATTN_BOTH && ((long long)t.n * G > FEW) != (SHIFT == LS)) t.seq = -1;
+    return t;
 }
 
 template <bool BF>
@@ -98,8 +127,8 @@ __device__ __forceinline__ void store4(void* out, size_t at, f32x4 x) {
     }
 }
 
-// partial results: per tile, head and split TR rows of DH fp32, then TR (maximum, sum)
-__host__ __device__ inline size_t part_floats(int dh) { return (size_t)TR * (dh + 2); }
+// partial results: per tile of R rows, head and split R rows of DH fp32, R maxima, R sums
+__host__ __device__ inline size_t part_floats(int R, int dh) { return (size_t)R * (dh + 2); }
 
 // One tile, head and split of the keys per block; its wavefronts take the steps of the split in turn and
 // join their results through LDS.
@@ -117,7 +146,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     const long long u = blockIdx.x / H;
     const Tile t = tile_at<TS>(a, u);
     if (t.seq < 0) return;
-    const int k0 = blockIdx.y * a.chunk, k1 = min(t.end, k0 + a.chunk);
+    const int k0 = blockIdx.y * a.few.chunk, k1 = min(t.end, k0 + a.few.chunk);
     if (blockIdx.y > 0 && k0 >= k1) return;    // the first split also writes rows that see no key
     const int G = a.q_heads / H;
     const int g = lane >> 4, c16 = lane & 15;
@@ -197,6 +226,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     // are computed, those of its values when their product is; the pages of the step after that are
     // asked for between the two, because loads are waited for in order.
     constexpr int NEXT = WAVES * STEP;
+    uint32_t nans = 0;
     int kb = k0 + wave * STEP;
     Pages now = pages(kb), next = pages(kb + NEXT);
     if (kb < k1) {
@@ -231,12 +261,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
         // not there, get -inf
         const int live = present ? min(sees, k1) - kv : 0;
         const bool some = __any(live < 16);
-        uint32_t nans = 0;
         if (some) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[e] = e < live ? sc[e] : -INFINITY;
-            // values that no row of the tile sees may hold anything, NaN among them, and so may the
-            // scale of a page that has none else: 0
+            // values that no row of the tile sees may hold anything, and so may the scale of a page
+            // that has none else: 0
             const int there = present ? k1 - kv : 0;
             if (there <= 0) vs = 1.f;
 #pragma unroll
@@ -245,7 +274,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
                 for (int w = 0; w < 4; ++w) {
                     const int b = there - 4 * w;
                     vw[c][w] &= b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << 8 * b) - 1;
-                    nans |= nan_bytes(vw[c][w]);
+                    const uint32_t bad = nan_bytes(vw[c][w]);
+                    nans |= bad;
+                    vw[c][w] &= ~bad;
                 }
         }
         float top = sc[0];
@@ -272,46 +303,30 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
         bf16x8 pf[2][NT];
         split8<NT>(p[0], pf[0]);
         split8<NT>(p[1], pf[1]);
-        if (!(some && __any(nans != 0))) {
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
+        for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const bf16x8 vf = decode8(vw[c][2 * k], vw[c][2 * k + 1], vs);
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 vf = decode8(vw[c][2 * k], vw[c][2 * k + 1], vs);
 #pragma unroll
-                    for (int n = NT - 1; n >= 0; --n)
-                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k][n], o[c], 0, 0, 0);
-                }
-        } else {
-            // A NaN value among keys that only some rows see: its products with the other rows'
-            // zero probabilities would be NaN.  The product runs without it, and a product of
-            // indicators tells which outputs it reaches.
-            bf16x8 seen[2];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) seen[e >> 3][e & 7] = (__bf16)(e < live ? 1.f : 0.f);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                f32x4 hit = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t w0 = vw[c][2 * k], w1 = vw[c][2 * k + 1];
-                    const uint32_t n0 = nan_bytes(w0) >> 7, n1 = nan_bytes(w1) >> 7;
-                    const bf16x8 vf = decode8(w0 & ~(n0 * 255u), w1 & ~(n1 * 255u), vs);
-                    const bf16x8 nf = decode8(n0 * 0x38u, n1 * 0x38u, 1.f);   // 0x38: 1
-#pragma unroll
-                    for (int n = NT - 1; n >= 0; --n)
-                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k][n], o[c], 0, 0, 0);
-                    hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf, seen[k], hit, 0, 0, 0);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[c][e] = hit[e] > 0.f ? __builtin_nanf("") : o[c][e];
+                for (int n = NT - 1; n >= 0; --n)
+                    o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k][n], o[c], 0, 0, 0);
             }
-        }
         __builtin_amdgcn_sched_barrier(0);
         if (more) load_values(kb + NEXT, next);
         __builtin_amdgcn_sched_barrier(0);
         now = next;
         next = after;
+    }
+
+    if (__any(nans != 0)) {
+        uint64_t found = 0;
+        for (kb = k0 + wave * STEP; kb < k1; kb += NEXT)
+            found |= find_nan(a, t.seq, h, kb, min(min(kb + STEP, k1), sees), 16, g * 4);
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][e] = found >> (c * 4 + e) & 1 ? __builtin_nanf("") : o[c][e];
     }
 
     // join the wavefronts
@@ -320,8 +335,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) *(f32x4*)&s_o[wave][c16][c * 16 + g * 4] = o[c];
     __syncthreads();
-    const bool whole = t.end <= a.chunk;      // no other split has keys
-    float* part = a.part + (((size_t)u * H + h) * a.splits + blockIdx.y) * part_floats(DH);
+    const bool whole = t.end <= a.few.chunk;      // no other split has keys
+    float* part = a.few.part + (((size_t)u * H + h) * a.few.splits + blockIdx.y) * part_floats(TR, DH);
     for (int i = tid; i < TR * (DH / 4); i += 256) {
         const int row = i / (DH / 4), ch = i % (DH / 4) * 4;
         if (row >= t.rows) break;
@@ -348,10 +363,260 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     }
 }
 
+// ---- large tiles -----------------------------------------------------------------------------------
+// 128 packed rows per block, 32 per wavefront (MFMA 32x32x16, queries in registers); the 64 keys of a step are
+// decoded to bf16 once per block into one of two LDS buffers, while the other is read: a
+// wavefront's matrix work on a step (1024 clocks of a SIMD at 128 channels) needs 32 KB of it.
+// Row m of a 32-key score block is key m with bits 2 and 3 exchanged, so that lane half hl ends up with
+// keys 16 j + 8 hl .. + 7 of each 16: the order in which the value product takes them.  Keys
+// lie in LDS at the exchanged rows.
+template <int DH>
+struct Lds {
+    static constexpr int KLD = DH * 2 + 16, VLD = STEP * 2 + 16;   // row strides: 8 rows on distinct banks
+    uint8_t k[2][STEP * KLD];
+    uint8_t v[2][DH * VLD];
+    uint8_t there[2][4];   // whether a step's four 16-key groups have a page
+    int nan;               // a step that not all rows see holds a NaN value
+};
+
+template <int DH>
+__global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
+    constexpr int KS = DH / 16;                      // 16-channel steps of S^T
+    constexpr int CB = (DH + 31) / 32;               // 32-channel blocks of O^T
+    constexpr int PARTS = DH / 16;                   // 16-byte parts of a key
+    constexpr int NL = (STEP * PARTS + 255) / 256;   // parts a thread copies of each of keys and values
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    Lds<DH>& lds = *(Lds<DH>*)smem;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hl = lane >> 5, lr = lane & 31;
+    const int H = a.c.kv_heads, pt = a.c.page_tokens, shift = page_shift(pt);
+    const int h = blockIdx.x % H;
+    const long long u = a.many.slots - 1 - blockIdx.x / H;   // a sequence's last rows, with the most keys, first
+    const Tile t = tile_at<LS>(a, u);
+    if (t.seq < 0) return;
+    const int k0 = blockIdx.y * a.many.chunk, k1 = min(t.end, k0 + a.many.chunk);
+    if (blockIdx.y > 0 && k0 >= k1) return;
+    const int G = a.q_heads / H;
+    const float sl2 = a.scale * 1.4426950408889634f, lazy = 8.f / sl2;
+
+    const int mine = t.first + wave * 32;                    // the wavefront's first packed row
+    const int r = min(mine + lr, t.first + t.rows - 1), qi = r / G;
+    const int sees = a.causal ? t.len - t.n + qi + 1 : t.len;
+    // keys that the wavefront's last row sees, and that all its rows see
+    const int wlast = min(mine + 31, t.first + t.rows - 1) / G, wfirst = min(mine, t.first + t.rows - 1) / G;
+    const int wend = mine < t.first + t.rows ? min(k1, a.causal ? t.len - t.n + wlast + 1 : t.len) : 0;
+    const int wall = a.causal ? t.len - t.n + wfirst + 1 : t.len;
+    const int ball = a.causal ? t.len - t.n + t.first / G + 1 : t.len;   // ... all of the block's
+    bf16x8 qf[KS];
+    {
+        const uint16_t* q = (const uint16_t*)a.q + (size_t)(t.row0 + qi) * a.q_stride + (size_t)(h * G + r % G) * DH;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            uint16_t x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = q[s * 16 + hl * 8 + e];
+            qf[s] = __builtin_bit_cast(bf16x8, x);
+        }
+    }
+
+    // Codes of a step: part i of the keys is 16 channels of key i / PARTS, of the values 16 keys (group
+    // i % 4) of channel i / 4.  The pages of a step are asked for a step before its codes.
+    struct Pages {
+        int k[NL], v;
+    };
+    auto pages = [&](int kb) {
+        Pages p;
+#pragma unroll
+        for (int n = 0; n < NL; ++n)
+            p.k[n] = page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, (kb + (tid + n * 256) / PARTS) >> shift);
+        p.v = page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, (kb + tid % 4 * 16) >> shift);
+        return p;
+    };
+    u32x4 kc[NL], vc[NL];
+    float ksc[NL], vsc;
+    bool vin;
+    auto load = [&](int kb, const Pages& p) {
+        const int tok = kb + tid % 4 * 16;
+        const size_t vpage = (size_t)max(p.v, 0) * H + h;
+        const uint8_t* vbase = a.c.v + vpage * DH * pt + (tok & (pt - 1));
+        vsc = a.c.v_scale[vpage];
+        vin = p.v >= 0;
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            const int i = tid + n * 256;
+            if (STEP * PARTS % 256 && i >= STEP * PARTS) break;
+            const size_t kpage = (size_t)max(p.k[n], 0) * H + h;
+            kc[n] = *(const u32x4*)(a.c.k + (kpage * pt + ((kb + i / PARTS) & (pt - 1))) * DH + i % PARTS * 16);
+            ksc[n] = a.c.k_scale[kpage];
+            vc[n] = *(const u32x4*)(vbase + i / 4 * pt);
+        }
+    };
+    auto store = [&](int kb, int buf) {
+        if (tid < 4) lds.there[buf][tid] = vin;   // the four groups of the first channel
+        // values past the keys that anyone sees, and of pages that are not there, are 0
+        const int there = vin ? k1 - kb - tid % 4 * 16 : 0;
+        if (there <= 0) vsc = 1.f;
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            const int i = tid + n * 256;
+            if (STEP * PARTS % 256 && i >= STEP * PARTS) break;
+            const int key = i / PARTS, row = (key & ~12) | (key & 4) << 1 | (key & 8) >> 1;
+            u32x4* k = (u32x4*)(lds.k[buf] + row * Lds<DH>::KLD + i % PARTS * 32);
+            k[0] = __builtin_bit_cast(u32x4, decode8(kc[n][0], kc[n][1], ksc[n]));
+            k[1] = __builtin_bit_cast(u32x4, decode8(kc[n][2], kc[n][3], ksc[n]));
+            if (kb + STEP > min(ball, k1) || !vin) {
+                uint32_t bad = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int b = there - 4 * w;
+                    vc[n][w] &= b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << 8 * b) - 1;
+                    const uint32_t x = nan_bytes(vc[n][w]);
+                    bad |= x;
+                    vc[n][w] &= ~x;
+                }
+                if (bad) lds.nan = 1;
+            }
+            u32x4* v = (u32x4*)(lds.v[buf] + i / 4 * Lds<DH>::VLD + i % 4 * 32);
+            v[0] = __builtin_bit_cast(u32x4, decode8(vc[n][0], vc[n][1], vsc));
+            v[1] = __builtin_bit_cast(u32x4, decode8(vc[n][2], vc[n][3], vsc));
+        }
+    };
+
+    f32x16 o[CB];
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    auto step = [&](int kb, int buf) {
+        f32x16 sc[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
+        const uint8_t* krow = lds.k[buf] + lr * Lds<DH>::KLD + hl * 16;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)   // two chains
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(krow + b * 32 * Lds<DH>::KLD + s * 32),
+                                                                qf[s], sc[b], 0, 0, 0);
+        // element e of block b is key kb + 32 b + 16 (e / 8) + 8 hl + e % 8
+        const uint32_t there = *(const uint32_t*)lds.there[buf];
+        const bool some = kb + STEP > min(wall, k1) || there != 0x01010101u;
+        if (some) {
+            const int live = min(sees, k1) - kb - 8 * hl;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int j = 2 * b + (e >> 3);
+                    sc[b][e] = 16 * j + (e & 7) < live && (there >> 8 * j & 1) ? sc[b][e] : -INFINITY;
+                }
+        }
+        float mx[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mx[e] = fmaxf(sc[0][e], sc[1][e]);
+#pragma unroll
+        for (int w = 8; w >= 1; w >>= 1)
+#pragma unroll
+            for (int e = 0; e < w; ++e) mx[e] = fmaxf(mx[e], mx[e + w]);
+        const float top = across<5>(mx[0], [](float x, float y) { return fmaxf(x, y); });
+        if (__any(top > m + lazy)) {
+            const float mn = fmaxf(m, top);
+            const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * sl2);
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[c][e] *= alpha;
+        }
+        const float off = m == -INFINITY ? 0.f : -m * sl2;
+        bf16x8 pf[4];
+        float sum[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[0][e], sl2, off));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[1][e], sl2, off));
+            sum[e] = p0 + p1;
+            pf[e >> 3][e & 7] = (__bf16)p0;
+            pf[2 + (e >> 3)][e & 7] = (__bf16)p1;
+        }
+#pragma unroll
+        for (int w = 8; w >= 1; w >>= 1)
+#pragma unroll
+            for (int e = 0; e < w; ++e) sum[e] += sum[e + w];
+        l += sum[0];
+        const uint8_t* vrow = lds.v[buf] + lr * Lds<DH>::VLD + hl * 16;
+        // (channels past DH take those 16 before: they are not stored)
+        auto at = [&](int c, int j) {
+            const int back = DH % 32 && c == CB - 1 ? (lr & 16) * Lds<DH>::VLD : 0;
+            return *(const bf16x8*)(vrow + c * 32 * Lds<DH>::VLD - back + j * 32);
+        };
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+                o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at(c, j), pf[j], o[c], 0, 0, 0);
+    };
+
+    if (tid == 0) lds.nan = 0;
+    Pages next = pages(k0);
+    if (k0 < k1) load(k0, next);
+    next = pages(k0 + STEP);
+    __syncthreads();
+    if (k0 < k1) store(k0, 0);
+    __syncthreads();
+    int buf = 0;
+    for (int kb = k0; kb < k1; kb += STEP, buf ^= 1) {
+        const bool more = kb + STEP < k1;
+        if (more) {
+            const Pages after = pages(kb + 2 * STEP);   // first: loads are waited for in order
+            load(kb + STEP, next);
+            next = after;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (kb < wend) step(kb, buf);
+        if (more) store(kb + STEP, buf ^ 1);
+        __syncthreads();
+    }
+
+    if (lds.nan) {
+        const int first = max(k0, k0 + (min(ball, k1) - k0) / STEP * STEP);   // the first step not seen in full
+        const uint64_t found = find_nan(a, t.seq, h, first, min(sees, k1), 8, hl * 4);
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[c][e] = found >> (c * 16 + e) & 1 ? __builtin_nanf("") : o[c][e];
+    }
+    l = across<5>(l, [](float x, float y) { return x + y; });
+    const int row = mine + lr - t.first;
+    if (row >= t.rows) return;
+    const bool whole = t.end <= a.many.chunk;
+    float* part = a.many.part + (((size_t)u * H + h) * a.many.splits + blockIdx.y) * part_floats(LR, DH);
+    const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int ch = c * 32 + e * 8 + hl * 4;
+            if (ch >= DH) break;
+            const f32x4 x = (f32x4){o[c][e * 4], o[c][e * 4 + 1], o[c][e * 4 + 2], o[c][e * 4 + 3]} * inv;
+            if (whole)
+                store4<true>(a.out, (size_t)(t.row0 + qi) * a.o_stride + (size_t)(h * G + r % G) * DH + ch, x);
+            else
+                *(f32x4*)(part + row * DH + ch) = x;
+        }
+    if (!whole && hl == 0) part[LR * DH + row] = m, part[LR * DH + LR + row] = l;
+}
+
 // Joins the splits of one row: the maxima and sums first, one split a thread, whose weights go to LDS; then
 // lanes over the channels, groups of lanes over the splits.
-template <bool BF>
+template <bool BF, int SHIFT>
 __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
+    constexpr int R = 1 << SHIFT;
+    const CacheAttnCut& cut = SHIFT == TS ? a.few : a.many;
     __shared__ float s_w[MAX_SPLITS];
     __shared__ f32x4 s_x[256];
     __shared__ float s_r[2][4];
@@ -359,18 +624,18 @@ __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
     const int H = a.c.kv_heads, DH = a.c.head_dim;
     const int h = blockIdx.x % H;
     const long long u = blockIdx.x / H;
-    const Tile t = tile_at<TS>(a, u);
-    if (t.seq < 0 || t.end <= a.chunk) return;
-    const int splits = (t.end + a.chunk - 1) / a.chunk;
+    const Tile t = tile_at<SHIFT>(a, u);
+    if (t.seq < 0 || t.end <= cut.chunk) return;
+    const int splits = (t.end + cut.chunk - 1) / cut.chunk;
     const float sl2 = a.scale * 1.4426950408889634f;
-    const size_t per = part_floats(DH);
-    const float* part = a.part + (((size_t)u * H + h) * a.splits) * per;
+    const size_t per = part_floats(R, DH);
+    const float* part = cut.part + (((size_t)u * H + h) * cut.splits) * per;
     for (int row = blockIdx.y; row < t.rows; row += gridDim.y) {   // one row a block, as a rule
         float mx[MAX_SPLITS / 256], top = -INFINITY;
 #pragma unroll
         for (int k = 0; k < MAX_SPLITS / 256; ++k) {
             const int s = tid + k * 256;
-            mx[k] = s < splits ? part[s * per + TR * DH + row] : -INFINITY;
+            mx[k] = s < splits ? part[s * per + R * DH + row] : -INFINITY;
             top = fmaxf(top, mx[k]);
         }
         auto block = [&](float x, float (&r)[4], auto f) {
@@ -389,7 +654,7 @@ __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
             if (s < splits) {
                 const float w = __builtin_amdgcn_exp2f((mx[k] - ref) * sl2);
                 s_w[s] = w;
-                sum += part[s * per + TR * DH + TR + row] * w;
+                sum += part[s * per + R * DH + R + row] * w;
             }
         }
         sum = block(sum, s_r[1], [](float x, float y) { return x + y; });
@@ -413,52 +678,84 @@ __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
 }
 
 template <int DH>
-void launch_dh(bool bf, const CacheAttnArgs& a, dim3 grid, hipStream_t s) {
-    if (bf) cache_attn_k<DH, true><<<grid, 256, 0, s>>>(a);
-    else cache_attn_k<DH, false><<<grid, 256, 0, s>>>(a);
+void launch_dh(bool bf, const CacheAttnArgs& a, hipStream_t s) {
+    if (a.route != ATTN_MANY) {
+        const dim3 grid((unsigned)(a.few.slots * a.c.kv_heads), (unsigned)a.few.splits);
+        if (bf) cache_attn_k<DH, true><<<grid, 256, 0, s>>>(a);
+        else cache_attn_k<DH, false><<<grid, 256, 0, s>>>(a);
+    }
+    if (a.route != ATTN_FEW) {
+        static const bool ok = allow_lds((const void*)cache_attn_tile_k<DH>, sizeof(Lds<DH>));
+        (void)ok;
+        const dim3 grid((unsigned)(a.many.slots * a.c.kv_heads), (unsigned)a.many.splits);
+        cache_attn_tile_k<DH><<<grid, 256, sizeof(Lds<DH>), s>>>(a);
+    }
 }
 
 }  // namespace
 
-CacheAttnPlan cache_attn_plan(int n_seqs, int rows, bool offsets, int max_rows, int table_pages, int page_tokens,
-                              int kv_heads, int q_heads, int head_dim, int cus) {
-    CacheAttnPlan p;
+CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets, int max_rows, int table_pages,
+                              int page_tokens, int kv_heads, int q_heads, int head_dim, int cus) {
+    CacheAttnPlan p{};
     const int G = q_heads / kv_heads;
-    p.slots = tile_slots(offsets, n_seqs, rows, G, TS);
+    const long long unit = cus > 0 ? cus : 256;
+    const long long keys = (long long)table_pages * page_tokens;   // at most 2^30
+    const long long most_rows = std::min<long long>(rows, !offsets ? 1 : max_rows > 0 ? max_rows : rows);
+    // Large tiles (bf16) take sequences of more than FEW packed rows.  Where some may have fewer, both kernels
+    // run, each on its own sequences: they need not if no sequence can have more, if there is one
+    // sequence, or if all have as many as the longest.
+    const bool alike = n_seqs == 1 || (max_rows > 0 && (long long)n_seqs * max_rows == rows);
+    p.route = !bf || most_rows * G <= FEW ? ATTN_FEW : alike ? ATTN_MANY : ATTN_BOTH;
+
     // Splits of equal length.  One sequence: as many as are resident at once, two blocks a compute unit (one
     // query over 200,001 keys of 8 heads of 128, us with 32 / 64 / 98 / 126 splits: 85 / 77 / 87 / 82).
     // Several may have any lengths up to the table's: splits of 2048 keys at most, so that the long ones
     // spread over the chip (64 sequences of 1 to 12,000 keys, us with splits of 1024 / 2048 / 3136 /
-    // 6272 / 12,032 keys: 171 / 161 / 167 / 180 / 182) unless there are many tiles anyway.  512 keys and fewer are not split: the join costs more.
-    const long long keys = (long long)table_pages * page_tokens;   // at most 2^30
-    const long long units = std::max(1ll, p.slots * kv_heads);
-    const long long most = std::min<long long>(MAX_SPLITS, std::max(1ll, 2ll * (cus > 0 ? cus : 256) / units));
-    long long chunk = (keys + most - 1) / most;
-    if (n_seqs > 1 && units < 16ll * (cus > 0 ? cus : 256)) chunk = std::min(chunk, 2048ll);
-    chunk = std::max({chunk, 512ll, (keys + MAX_SPLITS - 1) / MAX_SPLITS});
-    p.chunk = (int)((chunk + 255) / 256 * 256);
-    p.splits = (int)std::max(1ll, (keys + p.chunk - 1) / p.chunk);
-    p.tile_rows = (int)std::min<long long>(TR, (long long)(max_rows > 0 ? std::min(max_rows, rows) : rows) * G);
-    p.bytes = p.splits > 1 ? (size_t)p.slots * kv_heads * p.splits * part_floats(head_dim) * sizeof(float) : 0;
+    // 6272 / 12,032 keys: 171 / 161 / 167 / 180 / 182) unless there are many tiles anyway.  512 keys and fewer
+    // are not split: the join costs more.
+    auto cut = [&](CacheAttnCut& c, int shift, long long cap) {
+        c.slots = tile_slots(offsets, n_seqs, rows, G, shift);
+        const long long units = std::max(1ll, c.slots * kv_heads);
+        const long long most = std::min<long long>(MAX_SPLITS, std::max(1ll, 2 * unit / units));
+        long long chunk = (keys + most - 1) / most;
+        if (n_seqs > 1 && units < 16 * unit) chunk = std::min(chunk, cap);
+        chunk = std::max({chunk, 512ll, (keys + MAX_SPLITS - 1) / MAX_SPLITS});
+        c.chunk = (int)((chunk + 255) / 256 * 256);
+        c.splits = (int)std::max(1ll, (keys + c.chunk - 1) / c.chunk);
+        c.tile_rows = (int)std::min<long long>(1 << shift, std::max(1ll, most_rows * G));
+        return c.splits > 1 ? (size_t)c.slots * kv_heads * c.splits * part_floats(1 << shift, head_dim) : 0;
+    };
+    if (p.route != ATTN_MANY) p.few_floats = cut(p.few, TS, 2048);
+    size_t many = 0;
+    if (p.route != ATTN_FEW) many = cut(p.many, LS, keys);
+    p.bytes = (p.few_floats + many) * sizeof(float);
     return p;
 }
 
-void launch_cache_attention(bool bf, const CacheAttnArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)(a.slots * a.c.kv_heads), (unsigned)a.splits);
+void launch_cache_attention(bool bf, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s) {
+    a.route = p.route;
+    a.few = p.few;
+    a.many = p.many;
+    a.few.part = workspace;
+    a.many.part = workspace + p.few_floats;
     switch (a.c.head_dim) {
-        case 16: launch_dh<16>(bf, a, grid, s); break;
-        case 32: launch_dh<32>(bf, a, grid, s); break;
-        case 48: launch_dh<48>(bf, a, grid, s); break;
-        case 64: launch_dh<64>(bf, a, grid, s); break;
-        case 80: launch_dh<80>(bf, a, grid, s); break;
-        case 96: launch_dh<96>(bf, a, grid, s); break;
-        case 112: launch_dh<112>(bf, a, grid, s); break;
-        default: launch_dh<128>(bf, a, grid, s); break;
+        case 16: launch_dh<16>(bf, a, s); break;
+        case 32: launch_dh<32>(bf, a, s); break;
+        case 48: launch_dh<48>(bf, a, s); break;
+        case 64: launch_dh<64>(bf, a, s); break;
+        case 80: launch_dh<80>(bf, a, s); break;
+        case 96: launch_dh<96>(bf, a, s); break;
+        case 112: launch_dh<112>(bf, a, s); break;
+        default: launch_dh<128>(bf, a, s); break;
     }
-    if (a.splits > 1) {
-        const dim3 join((unsigned)(a.slots * a.c.kv_heads), (unsigned)a.tile_rows);
-        if (bf) cache_join_k<true><<<join, 256, 0, s>>>(a);
-        else cache_join_k<false><<<join, 256, 0, s>>>(a);
+    if (a.route != ATTN_MANY && a.few.splits > 1) {
+        const dim3 join((unsigned)(a.few.slots * a.c.kv_heads), (unsigned)a.few.tile_rows);
+        if (bf) cache_join_k<true, TS><<<join, 256, 0, s>>>(a);
+        else cache_join_k<false, TS><<<join, 256, 0, s>>>(a);
+    }
+    if (a.route != ATTN_FEW && a.many.splits > 1) {
+        const dim3 join((unsigned)(a.many.slots * a.c.kv_heads), (unsigned)a.many.tile_rows);
+        cache_join_k<true, LS><<<join, 256, 0, s>>>(a);
     }
 }
 

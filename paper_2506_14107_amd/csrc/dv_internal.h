@@ -328,6 +328,15 @@ struct ReadArgs {
 };
 void launch_cache_read(bool bf16, ReadArgs a, hipStream_t s);
 
+// How a call's tiles of one size are cut: splits of `chunk` keys, `splits` of them for the longest
+// sequence the table holds, `slots` row tiles dealt, of at most tile_rows packed rows; part: the partial
+// results, where there are several splits.
+struct CacheAttnCut {
+    int chunk, splits, tile_rows;
+    long long slots;
+    float* part;
+};
+enum CacheAttnRoute : int { ATTN_FEW = 0, ATTN_MANY = 1, ATTN_BOTH = 2 };   // small tiles, large tiles, by sequence
 struct CacheAttnArgs {
     CacheView c;
     SeqArgs seq;
@@ -337,20 +346,19 @@ struct CacheAttnArgs {
     int q_heads;
     float scale;
     int causal;
-    int chunk, splits;         // keys of a split, splits of the longest sequence the table holds
-    int tile_rows;             // packed rows of any tile, at most
-    long long slots;           // row tiles dealt
-    float* part;               // partial results, where splits > 1
+    // set by the launcher
+    int route;
+    CacheAttnCut few, many;
 };
-// How a call is cut, from its sizes; the same rule sizes the workspace.
+// What a call takes, from its sizes: the same rule sizes the workspace.
 struct CacheAttnPlan {
-    int chunk, splits;
-    int tile_rows;             // packed rows of any tile, at most
-    long long slots;
-    size_t bytes;              // workspace
+    int route;
+    CacheAttnCut few, many;
+    size_t few_floats;         // workspace: small tiles' partial results, then large ones'
+    size_t bytes;
 };
-CacheAttnPlan cache_attn_plan(int n_seqs, int rows, bool offsets, int max_rows, int table_pages, int page_tokens,
-                              int kv_heads, int q_heads, int head_dim, int cus);
-void launch_cache_attention(bool bf16, const CacheAttnArgs& a, hipStream_t s);
+CacheAttnPlan cache_attn_plan(bool bf16, int n_seqs, int rows, bool offsets, int max_rows, int table_pages,
+                              int page_tokens, int kv_heads, int q_heads, int head_dim, int cus);
+void launch_cache_attention(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);
 
 }  // namespace dv

@@ -98,7 +98,7 @@ def load(path=None):
                                          _P, _I64, _P, _I64, ctypes.c_int, _P]),
         "dv_cache_attention_workspace": (ctypes.c_int, [_P, ctypes.c_int, ctypes.c_int,
                                                         ctypes.c_int, ctypes.c_int, ctypes.c_int,
-                                                        ctypes.c_int,
+                                                        ctypes.c_int, ctypes.c_int,
                                                         ctypes.POINTER(ctypes.c_size_t)]),
         "dv_cache_attention": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P,
                                               ctypes.c_int, _P, _I64, ctypes.c_int, ctypes.c_int,
@@ -235,10 +235,11 @@ def dv_cache_read(cache, n_seqs, table, table_pages, offsets, starts, dtype, k, 
                                 k_stride, v, v_stride, rows, stream))
 
 
-def dv_cache_attention_workspace(cache, n_seqs, table_pages, with_offsets, rows, q_heads, max_rows):
+def dv_cache_attention_workspace(cache, n_seqs, table_pages, with_offsets, dtype, rows, q_heads,
+                                 max_rows):
     n = ctypes.c_size_t()
-    _check(load().dv_cache_attention_workspace(cache, n_seqs, table_pages, int(with_offsets), rows,
-                                               q_heads, max_rows, ctypes.byref(n)))
+    _check(load().dv_cache_attention_workspace(cache, n_seqs, table_pages, int(with_offsets), dtype,
+                                               rows, q_heads, max_rows, ctypes.byref(n)))
     return n.value
 
 
@@ -658,8 +659,8 @@ class TokenCache:
             else:
                 os = _rows("out", out, shape, q.dtype, index)
             if workspace is None:
-                need = dv_cache_attention_workspace(self.address, n, tp, o != 0, rows, heads,
-                                                    max_rows)
+                need = dv_cache_attention_workspace(self.address, n, tp, o != 0, dtype, rows,
+                                                    heads, max_rows)
                 if need:
                     torch = _torch()
                     workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
@@ -672,8 +673,10 @@ class TokenCache:
         return out
 
     def attention_workspace(self, n_seqs, rows, heads, table_pages=None, with_offsets=True,
-                            max_rows=0):
-        """Bytes of scratch that `attention` needs for such a call."""
+                            max_rows=0, dtype=None):
+        """Bytes of scratch that `attention` needs for such a call (of rows of `dtype`; bf16)."""
+        torch = _torch()
         tp = self.pages // max(n_seqs, 1) if table_pages is None else table_pages
-        return dv_cache_attention_workspace(self.address, n_seqs, tp, with_offsets, rows, heads,
-                                            max_rows)
+        return dv_cache_attention_workspace(self.address, n_seqs, tp, with_offsets,
+                                            DV_F32 if dtype is torch.float32 else DV_BF16, rows,
+                                            heads, max_rows)

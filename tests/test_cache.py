@@ -153,7 +153,7 @@ def test_attention_refuses_a_workspace_that_is_too_small():
     """A long table splits its keys over blocks, which meet in the workspace."""
     desc = cache(pages=4096)
     at = ctypes.addressof(desc)
-    need = dj.dv_cache_attention_workspace(at, 4, 1024, True, 4, 16, 1)
+    need = dj.dv_cache_attention_workspace(at, 4, 1024, True, dj.DV_BF16, 4, 16, 1)
     assert need > 0
     kw = dict(c=dict(pages=4096), rows=4, table_pages=1024, max_rows=1)
     for bad in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=FAKE + 4)):
@@ -170,9 +170,10 @@ def test_calls_without_rows_do_nothing():
 def test_workspace_refuses():
     desc = cache()
     at, lib, n = ctypes.addressof(desc), dj.load(), ctypes.c_size_t(7)
-    assert lib.dv_cache_attention_workspace(at, 4, 8, 1, 9, 16, 0, None) == dj.DV_EINVAL
-    assert lib.dv_cache_attention_workspace(at, 4, 8, 1, 9, 12, 0, ctypes.byref(n)) == dj.DV_EINVAL
-    assert lib.dv_cache_attention_workspace(None, 4, 8, 1, 9, 16, 0, ctypes.byref(n)) == dj.DV_EINVAL
+    assert lib.dv_cache_attention_workspace(at, 4, 8, 1, 1, 9, 16, 0, None) == dj.DV_EINVAL
+    assert lib.dv_cache_attention_workspace(at, 4, 8, 1, 1, 9, 12, 0, ctypes.byref(n)) == dj.DV_EINVAL
+    assert lib.dv_cache_attention_workspace(None, 4, 8, 1, 1, 9, 16, 0, ctypes.byref(n)) == dj.DV_EINVAL
+    assert lib.dv_cache_attention_workspace(at, 4, 8, 1, 2, 9, 16, 0, ctypes.byref(n)) == dj.DV_EINVAL
     assert n.value == 0
 
 
