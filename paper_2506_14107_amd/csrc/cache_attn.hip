@@ -14,6 +14,8 @@
 // rounded to bf16 for the value product, a relative 2^-9 each, as in the encoder.  fp32 queries are three
 // bf16 terms (24 bits), and so are their probabilities: K and V being exact in bf16, three products
 // give fp32 results at the bf16 matrix rate.
+#include <type_traits>
+
 #include "cache_plan.h"
 
 namespace dv {
@@ -76,6 +78,20 @@ __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&t)[T]) {
             if (k + 1 < T) rest -= (float)t[k][e];
         }
     }
+}
+// Waits for the queries here: left to their first use, the wait would stand in the loop of steps, where
+// it waits for the loads of the next step at every turn.
+template <int K, int T>
+__device__ __forceinline__ void settle(bf16x8 (&q)[K][T]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int n = 0; n < T; ++n) asm volatile("" : "+v"(q[k][n]));
+}
+template <int K>
+__device__ __forceinline__ void settle(bf16x8 (&q)[K]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) asm volatile("" : "+v"(q[k]));
 }
 // bytes of w that are NaN codes, as 0xFF
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
@@ -171,6 +187,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
         }
         split8<NT>(x, qf[s]);
     }
+    settle(qf);
 
     f32x4 o[CT];
 #pragma unroll
@@ -182,15 +199,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
         int k, v;
     };
     auto pages = [&](int kb) {
-        return Pages{page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, (kb + (c16 >> 2) * 16) >> shift),
-                     page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, (kb + g * 16) >> shift)};
+        return Pages{entry_of(a.seq, t.seq, (kb + (c16 >> 2) * 16) >> shift),
+                     entry_of(a.seq, t.seq, (kb + g * 16) >> shift)};
     };
     uint32_t kw[4][KS][2];
     u32x4 vw[CT];
     float ks, vs;
+    bool present = false;   // the lane's group of the step has a page
     auto load_keys = [&](int kb, const Pages& pg) {
         const int kk = kb + (c16 >> 2) * 16;
-        const size_t page = (size_t)max(pg.k, 0) * H + h;
+        const size_t page = (size_t)max(page_from(a.seq, a.c.pages, pg.k, t.seq, kk >> shift), 0) * H + h;
         const uint8_t* base = a.c.k + (page * pt + (kk & (pt - 1)) + (c16 & 3)) * DH;
         ks = a.c.k_scale[page];
 #pragma unroll
@@ -215,7 +233,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     };
     auto load_values = [&](int kb, const Pages& pg) {
         const int kv = kb + g * 16;
-        const size_t page = (size_t)max(pg.v, 0) * H + h;
+        const int p = page_from(a.seq, a.c.pages, pg.v, t.seq, kv >> shift);
+        present = p >= 0;
+        const size_t page = (size_t)max(p, 0) * H + h;
         const uint8_t* base = a.c.v + (page * DH + c16) * pt + (kv & (pt - 1));
         vs = a.c.v_scale[page];
 #pragma unroll
@@ -228,13 +248,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     constexpr int NEXT = WAVES * STEP;
     uint32_t nans = 0;
     int kb = k0 + wave * STEP;
-    Pages now = pages(kb), next = pages(kb + NEXT);
+    Pages next = pages(kb);
     if (kb < k1) {
-        load_keys(kb, now);
-        load_values(kb, now);
+        load_keys(kb, next);
+        load_values(kb, next);
     }
-    for (; kb < k1; kb += NEXT) {
-        const bool more = kb + NEXT < k1, present = now.v >= 0;
+    next = pages(kb + NEXT);
+    auto step = [&](auto last) {   // the last one loads nothing: no wait in the others stands behind a branch
+        constexpr bool more = !decltype(last)::value;
         const int kv = kb + g * 16;
         float sc[16];
 #pragma unroll
@@ -252,7 +273,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
         }
         __builtin_amdgcn_sched_barrier(0);
         Pages after = next;
-        if (more) {
+        if constexpr (more) {
             load_keys(kb + NEXT, next);
             after = pages(kb + 2 * NEXT);
         }
@@ -313,10 +334,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
                     o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k][n], o[c], 0, 0, 0);
             }
         __builtin_amdgcn_sched_barrier(0);
-        if (more) load_values(kb + NEXT, next);
+        if constexpr (more) load_values(kb + NEXT, next);
         __builtin_amdgcn_sched_barrier(0);
-        now = next;
         next = after;
+    };
+    if (kb < k1) {
+        for (; kb + NEXT < k1; kb += NEXT) step(std::false_type());
+        step(std::true_type());
     }
 
     if (__any(nans != 0)) {
@@ -416,6 +440,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
             for (int e = 0; e < 8; ++e) x[e] = q[s * 16 + hl * 8 + e];
             qf[s] = __builtin_bit_cast(bf16x8, x);
         }
+        settle(qf);
     }
 
     // Codes of a step: part i of the keys is 16 channels of key i / PARTS, of the values 16 keys (group
@@ -427,8 +452,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
         Pages p;
 #pragma unroll
         for (int n = 0; n < NL; ++n)
-            p.k[n] = page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, (kb + (tid + n * 256) / PARTS) >> shift);
-        p.v = page_of(a.seq.table, a.seq.table_pages, a.c.pages, t.seq, (kb + tid % 4 * 16) >> shift);
+            p.k[n] = entry_of(a.seq, t.seq, (kb + (tid + n * 256) / PARTS) >> shift);
+        p.v = entry_of(a.seq, t.seq, (kb + tid % 4 * 16) >> shift);
         return p;
     };
     u32x4 kc[NL], vc[NL];
@@ -436,15 +461,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
     bool vin;
     auto load = [&](int kb, const Pages& p) {
         const int tok = kb + tid % 4 * 16;
-        const size_t vpage = (size_t)max(p.v, 0) * H + h;
+        const int vp = page_from(a.seq, a.c.pages, p.v, t.seq, tok >> shift);
+        vin = vp >= 0;
+        const size_t vpage = (size_t)max(vp, 0) * H + h;
         const uint8_t* vbase = a.c.v + vpage * DH * pt + (tok & (pt - 1));
         vsc = a.c.v_scale[vpage];
-        vin = p.v >= 0;
 #pragma unroll
         for (int n = 0; n < NL; ++n) {
             const int i = tid + n * 256;
             if (STEP * PARTS % 256 && i >= STEP * PARTS) break;
-            const size_t kpage = (size_t)max(p.k[n], 0) * H + h;
+            const size_t kpage = (size_t)max(page_from(a.seq, a.c.pages, p.k[n], t.seq, (kb + i / PARTS) >> shift), 0) * H + h;
             kc[n] = *(const u32x4*)(a.c.k + (kpage * pt + ((kb + i / PARTS) & (pt - 1))) * DH + i % PARTS * 16);
             ksc[n] = a.c.k_scale[kpage];
             vc[n] = *(const u32x4*)(vbase + i / 4 * pt);
@@ -495,12 +521,23 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
         const uint8_t* krow = lds.k[buf] + lr * Lds<DH>::KLD + hl * 16;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int s = 0; s < KS; ++s)   // two chains
 #pragma unroll
             for (int b = 0; b < 2; ++b)
                 sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(krow + b * 32 * Lds<DH>::KLD + s * 32),
                                                                 qf[s], sc[b], 0, 0, 0);
+        // the LDS reads run AHEAD matrix instructions ahead
+        constexpr int AHEAD = KS < 3 ? 2 * KS : 6;
+        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+        for (int s = 0; s < 2 * KS - AHEAD; ++s) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
+        __builtin_amdgcn_sched_barrier(0);
         // element e of block b is key kb + 32 b + 16 (e / 8) + 8 hl + e % 8
         const uint32_t there = *(const uint32_t*)lds.there[buf];
         const bool some = kb + STEP > min(wall, k1) || there != 0x01010101u;
@@ -569,18 +606,17 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
     if (k0 < k1) store(k0, 0);
     __syncthreads();
     int buf = 0;
-    for (int kb = k0; kb < k1; kb += STEP, buf ^= 1) {
-        const bool more = kb + STEP < k1;
-        if (more) {
-            const Pages after = pages(kb + 2 * STEP);   // first: loads are waited for in order
-            load(kb + STEP, next);
-            next = after;
-        }
+    int kb = k0;
+    for (; kb + STEP < k1; kb += STEP, buf ^= 1) {
+        const Pages after = pages(kb + 2 * STEP);   // first: loads are waited for in order
+        load(kb + STEP, next);
+        next = after;
         __builtin_amdgcn_sched_barrier(0);
         if (kb < wend) step(kb, buf);
-        if (more) store(kb + STEP, buf ^ 1);
+        store(kb + STEP, buf ^ 1);
         __syncthreads();
     }
+    if (kb < wend) step(kb, buf);
 
     if (lds.nan) {
         const int first = max(k0, k0 + (min(ball, k1) - k0) / STEP * STEP);   // the first step not seen in full

@@ -23,6 +23,19 @@ __host__ __device__ inline int page_of(const int* table, int table_pages, int pa
     return p >= 0 && p < pages ? (int)p : -1;
 }
 
+// The same in two steps, for kernels that ask for a page well before they need it: a table entry (of the
+// table's last stretch, past it; without a table any int), and the page or -1.  The load takes no branch,
+// so that the wait for it need not be for all loads.
+__host__ __device__ inline int entry_of(const SeqArgs& q, int s, int j) {
+    const long long at = (long long)s * q.table_pages + (j < q.table_pages ? j : q.table_pages - 1);
+    const int* p = q.table ? q.table + at : q.at;
+    return *p;
+}
+__host__ __device__ inline int page_from(const SeqArgs& q, int pages, int entry, int s, int j) {
+    const int e = q.table ? entry : (int)((long long)s * q.table_pages + j);
+    return j < q.table_pages && (unsigned)e < (unsigned)pages ? e : -1;
+}
+
 // ---- rows of a call ------------------------------------------------------------------------------
 // Rows of sequence s: offsets[s] .. offsets[s + 1] - 1, cut to the rows there are; without offsets
 // sequence s has row s (or the call's one sequence has them all).
