@@ -249,11 +249,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     uint32_t nans = 0;
     int kb = k0 + wave * STEP;
     Pages next = pages(kb);
-    if (kb < k1) {
+    if (kb < k1) {   // in the order of the loop, whose waits count on it
         load_keys(kb, next);
+        __builtin_amdgcn_sched_barrier(0);
+        const Pages after = pages(kb + NEXT);
+        __builtin_amdgcn_sched_barrier(0);
         load_values(kb, next);
+        next = after;
     }
-    next = pages(kb + NEXT);
     auto step = [&](auto last) {   // the last one loads nothing: no wait in the others stands behind a branch
         constexpr bool more = !decltype(last)::value;
         const int kv = kb + g * 16;
@@ -647,17 +650,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
     if (!whole && hl == 0) part[LR * DH + row] = m, part[LR * DH + LR + row] = l;
 }
 
-// Joins the splits of one row: the maxima and sums first, one split a thread, whose weights go to LDS; then
-// lanes over the channels, groups of lanes over the splits.
-template <bool BF, int SHIFT>
+// Joins the splits of a tile's rows.  A row takes W wavefronts of a block (1, or 4 where it has many
+// splits); every lane weighs one split in 64, then lanes go over the channels and groups of lanes over the
+// splits.
+template <bool BF, int SHIFT, int W>
 __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
-    constexpr int R = 1 << SHIFT;
-    const CacheAttnCut& cut = SHIFT == TS ? a.few : a.many;
-    __shared__ float s_w[MAX_SPLITS];
+    constexpr int R = 1 << SHIFT, ROWS = 4 / W;
     __shared__ f32x4 s_x[256];
-    __shared__ float s_r[2][4];
-    const int tid = threadIdx.x;
-    const int H = a.c.kv_heads, DH = a.c.head_dim;
+    const CacheAttnCut& cut = SHIFT == TS ? a.few : a.many;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int H = a.c.kv_heads, DH = a.c.head_dim, G = a.q_heads / H;
     const int h = blockIdx.x % H;
     const long long u = blockIdx.x / H;
     const Tile t = tile_at<SHIFT>(a, u);
@@ -666,51 +668,60 @@ __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
     const float sl2 = a.scale * 1.4426950408889634f;
     const size_t per = part_floats(R, DH);
     const float* part = cut.part + (((size_t)u * H + h) * cut.splits) * per;
-    for (int row = blockIdx.y; row < t.rows; row += gridDim.y) {   // one row a block, as a rule
-        float mx[MAX_SPLITS / 256], top = -INFINITY;
+    const int lanes = DH / 4, groups = 64 / lanes;        // of a wavefront
+    const int ch = lane % lanes * 4, grp = lane / lanes;
+    // one round, unless a sequence has more rows than it was said to have
+    for (int row0 = blockIdx.y * ROWS; row0 < t.rows; row0 += gridDim.y * ROWS) {
+        const int row = min(row0 + wave / W, t.rows - 1);
+        float mx[MAX_SPLITS / 64], top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < MAX_SPLITS / 256; ++k) {
-            const int s = tid + k * 256;
+        for (int k = 0; k < (W == 1 ? 1 : MAX_SPLITS / 64); ++k) {
+            const int s = lane + k * 64;
             mx[k] = s < splits ? part[s * per + R * DH + row] : -INFINITY;
             top = fmaxf(top, mx[k]);
         }
-        auto block = [&](float x, float (&r)[4], auto f) {
 #pragma unroll
-            for (int o = 32; o >= 1; o >>= 1) x = f(x, __shfl_xor(x, o, 64));
-            if ((tid & 63) == 0) r[tid >> 6] = x;
-            __syncthreads();
-            return f(f(r[0], r[1]), f(r[2], r[3]));
-        };
-        top = block(top, s_r[0], [](float x, float y) { return fmaxf(x, y); });
+        for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
         const float ref = top == -INFINITY ? 0.f : top;
         float sum = 0.f;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < MAX_SPLITS / 256; ++k) {
-            const int s = tid + k * 256;
+        for (int k = 0; k < (W == 1 ? 1 : MAX_SPLITS / 64); ++k) {
+            const int s = lane + k * 64, n = min(64, splits - k * 64);
+            float w = 0.f;
             if (s < splits) {
-                const float w = __builtin_amdgcn_exp2f((mx[k] - ref) * sl2);
-                s_w[s] = w;
+                w = __builtin_amdgcn_exp2f((mx[k] - ref) * sl2);
                 sum += part[s * per + R * DH + R + row] * w;
             }
-        }
-        sum = block(sum, s_r[1], [](float x, float y) { return x + y; });
-        const int lanes = DH / 4, groups = 256 / lanes;
-        const int ch = tid % lanes * 4, grp = tid / lanes;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        if (grp < groups) {
+            const float* p = part + (size_t)k * 64 * per + row * DH + ch;
 #pragma unroll 4
-            for (int s = grp; s < splits; s += groups) x += *(const f32x4*)(part + s * per + row * DH + ch) * s_w[s];
+            for (int i = wave % W * groups; i < n; i += W * groups) {
+                const int j = i + grp;
+                const float wj = __shfl(w, j & 63, 64);
+                if (grp < groups && j < n) x += *(const f32x4*)(p + (size_t)j * per) * wj;
+            }
         }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
         s_x[tid] = x;
         __syncthreads();
-        if (grp == 0) {
-            for (int k = 1; k < groups; ++k) x += s_x[k * lanes + tid];
-            const int G = a.q_heads / H, pr = t.first + row;
+        if (wave % W == 0 && grp == 0 && row0 + wave / W < t.rows) {
+            for (int v = 0; v < W; ++v)
+                for (int k = v == 0; k < groups; ++k) x += s_x[(wave + v) * 64 + k * lanes + lane];
+            const int pr = t.first + row;
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
             store4<BF>(a.out, (size_t)(t.row0 + pr / G) * a.o_stride + (size_t)(h * G + pr % G) * DH + ch, x * inv);
         }
         __syncthreads();
     }
+}
+
+template <bool BF, int SHIFT>
+void launch_join(const CacheAttnArgs& a, const CacheAttnCut& c, hipStream_t s) {
+    const bool few = c.splits <= 16;   // us of 8 tiles of 4 rows in 61 splits: 15 with one wavefront a row, 6 with four; of 640 in 6: 6, 10
+    const dim3 grid((unsigned)(c.slots * a.c.kv_heads), (unsigned)(few ? (c.tile_rows + 3) / 4 : c.tile_rows));
+    if (few) cache_join_k<BF, SHIFT, 1><<<grid, 256, 0, s>>>(a);
+    else cache_join_k<BF, SHIFT, 4><<<grid, 256, 0, s>>>(a);
 }
 
 template <int DH>
@@ -784,15 +795,8 @@ void launch_cache_attention(bool bf, CacheAttnArgs a, const CacheAttnPlan& p, fl
         case 112: launch_dh<112>(bf, a, s); break;
         default: launch_dh<128>(bf, a, s); break;
     }
-    if (a.route != ATTN_MANY && a.few.splits > 1) {
-        const dim3 join((unsigned)(a.few.slots * a.c.kv_heads), (unsigned)a.few.tile_rows);
-        if (bf) cache_join_k<true, TS><<<join, 256, 0, s>>>(a);
-        else cache_join_k<false, TS><<<join, 256, 0, s>>>(a);
-    }
-    if (a.route != ATTN_FEW && a.many.splits > 1) {
-        const dim3 join((unsigned)(a.many.slots * a.c.kv_heads), (unsigned)a.many.tile_rows);
-        cache_join_k<true, LS><<<join, 256, 0, s>>>(a);
-    }
+    if (a.route != ATTN_MANY && a.few.splits > 1) bf ? launch_join<true, TS>(a, a.few, s) : launch_join<false, TS>(a, a.few, s);
+    if (a.route != ATTN_FEW && a.many.splits > 1) launch_join<true, LS>(a, a.many, s);
 }
 
 }  // namespace dv
