@@ -11,6 +11,9 @@
 // gains nothing from a finer scale, and a power of two can grow with a page that fills over several
 // calls while codes away from the format's underflow (2^-6 of a scale) stay exact.  Scales and sums are
 // fp32.
+#include <algorithm>
+#include <type_traits>
+
 #include "cache_plan.h"
 
 namespace dv {
@@ -19,6 +22,7 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -88,13 +92,10 @@ __device__ __forceinline__ void turn_cos_sin(int pos, uint64_t turn, float& c, f
     if (q == 1 || q == 2) c = -c;
     if (q >= 2) s = -s;
 }
-__device__ __forceinline__ int axis_of(const RotaryPlan& r, int pair) {
-    return pair < r.end0 ? 0 : pair < r.end1 ? 1 : 2;
-}
-
 // An item is two groups of V channels of one row and head that the rotation mixes (or, past the turned
 // channels, leaves): items of the `dim` turned channels first.
 //   halves: channels o .. o + V - 1 with o + dim/2 ..; pairs (V = 8): 16 channels in a row, (V = 1): 2
+// Either way the i-th item turns the V pairs from V i on.
 struct Item {
     int o0, o1;
     bool turned;
@@ -102,57 +103,93 @@ struct Item {
 template <int V>
 __device__ __forceinline__ Item item_at(int dim, bool pairs, int i) {
     const int turned = dim / (2 * V);
-    if (i >= turned) return {i * 2 * V, i * 2 * V + V, false};
-    if (pairs) return {i * 2 * V, i * 2 * V + V, true};
+    if (i >= turned || pairs) return {i * 2 * V, i * 2 * V + V, i < turned};
     return {i * V, i * V + dim / 2, true};
 }
 template <int V>
-__device__ __forceinline__ void turn_item(const RotaryPlan& r, const Item& it, const int* pos, float (&a)[V],
-                                          float (&b)[V]) {
-    if (!it.turned) return;
-    int p3[3];
+__device__ __forceinline__ void turn_item(bool pairs, const float* cos, const float* sin, float (&a)[V], float (&b)[V]) {
+    float c[V], s[V];
+    if constexpr (V == 8) {
 #pragma unroll
-    for (int x = 0; x < 3; ++x) p3[x] = pos[x];
-    auto rotate = [&](int pair, float& x, float& y) {
-        const int ax = axis_of(r, pair);
-        float c, s;
-        turn_cos_sin(ax == 0 ? p3[0] : ax == 1 ? p3[1] : p3[2], r.turn[pair], c, s);
-        const float u = x * c - y * s;
-        y = fmaf(x, s, y * c);
+        for (int i = 0; i < 2; ++i) {
+            const f32x4 x = *(const f32x4*)(cos + 4 * i), y = *(const f32x4*)(sin + 4 * i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[4 * i + e] = x[e], s[4 * i + e] = y[e];
+        }
+    } else {
+        c[0] = *cos, s[0] = *sin;
+    }
+    auto rotate = [&](int i, float& x, float& y) {
+        const float u = x * c[i] - y * s[i];
+        y = fmaf(x, s[i], y * c[i]);
         x = u;
     };
-    if (V == 1 || !r.pairs) {
-        const int first = r.pairs ? it.o0 / 2 : it.o0;
+    if (V == 1 || !pairs) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) rotate(first + i, a[i], b[i]);
+        for (int i = 0; i < V; ++i) rotate(i, a[i], b[i]);
     } else if constexpr (V > 1) {
 #pragma unroll
         for (int i = 0; i < V; i += 2) {
-            rotate((it.o0 + i) / 2, a[i], a[i + 1]);
-            rotate((it.o1 + i) / 2, b[i], b[i + 1]);
+            rotate(i / 2, a[i], a[i + 1]);
+            rotate(V / 2 + i / 2, b[i], b[i + 1]);
         }
     }
 }
 
-// out row = the row with its heads turned.  One item per thread.
+// The cosines and sines of n rows' angles (row(r): the positions of the r-th), into cos and sin [n][ld]: a lane
+// keeps its pair.  NT threads.
+template <int NT, class Row>
+__device__ __forceinline__ void angles_of(const RotaryPlan& rot, int n, float* cos, float* sin, int ld, Row row) {
+    const int lane = threadIdx.x & 63, half = rot.dim / 2, rows = 64 / half;   // of a wavefront at once
+    const int pair = lane % half, sub = lane / half;
+    if (sub >= rows) return;
+    const uint64_t turn = rot.turn[pair];
+    const int axis = pair < rot.end0 ? 0 : pair < rot.end1 ? 1 : 2;
+    for (int r = (threadIdx.x >> 6) * rows + sub; r < n; r += NT / 64 * rows) {
+        float c, s;
+        turn_cos_sin(row(r)[axis], turn, c, s);
+        cos[r * ld + pair] = c;
+        sin[r * ld + pair] = s;
+    }
+}
+
+// Rows row0 .. row0 + n - 1 of x, heads turned, to out (a block; n at most ROT_ROWS).  Each angle is computed
+// once, into LDS, and used by all heads (16,448 rows of 32 heads of 80 channels, bf16: 36 us, with every head
+// computing its own 51).
+constexpr int ROT_ROWS = 16, ROT_LDS = ROT_ROWS * 64 * 2;
+template <bool BF, int V, int NT>
+__device__ __forceinline__ void turn_rows(const RowsArgs& a, const RotaryPlan& rot, int row0, int n, float* lds) {
+    const int tid = threadIdx.x, half = rot.dim / 2, ld = (half + 3) & ~3;
+    float *cos = lds, *sin = lds + ROT_ROWS * 64;
+    angles_of<NT>(rot, n, cos, sin, ld, [&](int r) {
+        return a.pos + (size_t)(a.pos_idx ? a.pos_idx[row0 + r] % a.pos_mod : row0 + r) * 3;
+    });
+    __syncthreads();
+    const int per_head = a.dh / (2 * V), per_row = per_head * a.heads;
+    for (int i = tid; i < n * per_row; i += NT) {
+        const int r = i / per_row, rest = i % per_row, h = rest / per_head, c = rest % per_head;
+        const Item it = item_at<V>(rot.dim, rot.pairs, c);
+        float x[V], y[V];
+        const size_t at = (size_t)(row0 + r) * a.x_stride + (size_t)h * a.dh;
+        load_ch<BF, V>(a.x, at + it.o0, x);
+        load_ch<BF, V>(a.x, at + it.o1, y);
+        if (it.turned) turn_item<V>(rot.pairs, cos + r * ld + c * V, sin + r * ld + c * V, x, y);
+        const size_t to = (size_t)(row0 + r) * a.out_stride + (size_t)h * a.dh;
+        store_ch<BF, V>(a.out, to + it.o0, x);
+        store_ch<BF, V>(a.out, to + it.o1, y);
+    }
+}
+// Rows a block takes: about four items a thread.
+int rows_a_block(int heads, int dh, int vec) {
+    return std::max(1, std::min(ROT_ROWS, 1024 / std::max(1, heads * (dh / (2 * vec)))));
+}
+
 template <bool BF, int V>
 __global__ __launch_bounds__(256) void rotary_k(RotaryArgs a) {
-    const int per_head = a.dh / (2 * V), per_row = per_head * a.heads;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int row = (int)(i / per_row);
-    const int rows = a.rows_dev ? *a.rows_dev : a.rows;
-    if (row >= rows) return;
-    const int rest = (int)(i % per_row), h = rest / per_head;
-    const Item it = item_at<V>(a.rot.dim, a.rot.pairs, rest % per_head);
-    const int* pos = a.pos + (size_t)(a.pos_idx ? a.pos_idx[row] % a.pos_mod : row) * 3;
-    float x[V], y[V];
-    const size_t at = (size_t)row * a.x_stride + (size_t)h * a.dh;
-    load_ch<BF, V>(a.x, at + it.o0, x);
-    load_ch<BF, V>(a.x, at + it.o1, y);
-    turn_item<V>(a.rot, it, pos, x, y);
-    const size_t to = (size_t)row * a.out_stride + (size_t)h * a.dh;
-    store_ch<BF, V>(a.out, to + it.o0, x);
-    store_ch<BF, V>(a.out, to + it.o1, y);
+    __shared__ __attribute__((aligned(16))) float lds[ROT_LDS];
+    const int row0 = blockIdx.x * a.per_block;
+    const int n = min(a.rows_dev ? *a.rows_dev : a.rows, a.rows) - row0;
+    if (n > 0) turn_rows<BF, V, 256>(a, a.rot, row0, min(n, a.per_block), lds);
 }
 
 // ---- codes -----------------------------------------------------------------------------------------
@@ -165,9 +202,12 @@ __device__ __forceinline__ void decode4(uint32_t w, float s, float (&x)[4]) {
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     x[0] = a[0] * s, x[1] = a[1] * s, x[2] = b[0] * s, x[3] = b[1] * s;
 }
-// Infinities are stored as NaN: the format has none, and a largest finite value would hide them.
-__device__ __forceinline__ float storable(float x) {
-    return fabsf(x) <= 3.4028235e38f ? x : __builtin_nanf("");
+// four dwords of bytes, transposed
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), b = __builtin_amdgcn_perm(w[3], w[2], 0x05010400);
+    const uint32_t c = __builtin_amdgcn_perm(w[1], w[0], 0x07030602), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+    w[0] = __builtin_amdgcn_perm(b, a, 0x05040100), w[1] = __builtin_amdgcn_perm(b, a, 0x07060302);
+    w[2] = __builtin_amdgcn_perm(d, c, 0x05040100), w[3] = __builtin_amdgcn_perm(d, c, 0x07060302);
 }
 // The least power of two >= 2^-126 with most <= 448 of it: 448 = 1.75 * 2^8, so the exponent of `most` goes up
 // by one where its fraction passes 0.75.
@@ -179,223 +219,262 @@ __device__ __forceinline__ float scale_for(float most) {
 __device__ __forceinline__ float inverse(float s) {
     return __builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, s));
 }
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
-}
-
 // The part of a page that slot u stands for.
 __device__ __forceinline__ PagePart page_part(const SeqArgs& q, int pt, int pages, int u) {
-    const int s = q.one ? 0 : q.offsets ? find_seq(q.offsets, q.n_seqs, 1, page_shift(pt), 2, u) : u;
-    return part_at(q, pt, pages, s, u);
+    return part_at(q, pt, pages, q.offsets ? find_seq(q, 1, page_shift(pt), 2, u) : seq_of(q, q.one ? 0 : u), u);
 }
 
 // ---- write -----------------------------------------------------------------------------------------
-// A block quantises the new tokens of one page and key/value head, keys or values, and owns that page: it
-// alone reads and writes its codes and its scale.  Further blocks turn the query rows.
-constexpr int MAX_ITEMS = 4;   // items of 16 channels per thread: 128 tokens of 128 channels over 256 threads
-
-template <bool BF, int V>
-__device__ __forceinline__ void load_item(const void* src, size_t at, const Item& it, const RotaryPlan& r,
-                                          const int* pos, float (&x)[V], float (&y)[V]) {
-    load_ch<BF, V>(src, at + it.o0, x);
-    load_ch<BF, V>(src, at + it.o1, y);
-    turn_item<V>(r, it, pos, x, y);
-}
-
-template <bool BF>
-__global__ __launch_bounds__(256) void cache_write_k(WriteArgs a) {
-    __shared__ float s_most[4];
-    extern __shared__ __attribute__((aligned(16))) uint8_t tile[];   // values: codes [token][channel + 4]
+// A block quantises the new tokens of one page, keys or values, of a few heads, and owns those: it alone reads and
+// writes their codes and scales.  Its loads are all asked for together: 32 bytes or more a thread.
+// Further blocks turn the query rows.
+constexpr int MAX_ITEMS = 2;                    // items of 16 channels a thread and pass
+constexpr int MAX_HEADS = 16;                   // heads of a block
+// WT threads a block: 256, or 512 where a page and head have more than 512 items (more than 64 tokens of
+// 128 channels).
+template <bool BF, int V, int WT>
+__global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
+    constexpr int PASS = MAX_ITEMS * WT;      // items of a pass: one head's, or more heads'
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    __shared__ uint32_t s_most[MAX_HEADS];
+    __shared__ float s_scale[MAX_HEADS], s_old[MAX_HEADS];
     const int tid = threadIdx.x;
     const int dh = a.c.head_dim, pt = a.c.page_tokens, H = a.c.kv_heads;
-    const long long kv_blocks = (long long)a.slots * 2 * H;
-    if (blockIdx.x >= kv_blocks) {   // queries: one item of 2 x 8 (or 2 x 1) channels per thread
-        const int V = a.vec;
-        const int per_head = dh / (2 * V), per_row = per_head * a.q_heads;
-        const long long i = ((long long)blockIdx.x - kv_blocks) * 256 + tid;
-        const int row = (int)(i / per_row);
+    if (blockIdx.x >= (unsigned)a.kv_blocks) {   // queries
+        const RowsArgs q = {a.q, a.q_out, a.q_stride, a.qo_stride, a.q_heads, dh, a.pos, nullptr, 0};
+        const int row0 = (blockIdx.x - a.kv_blocks) * a.q_rows;
         const int live = a.seq.offsets ? min(a.seq.offsets[a.seq.n_seqs], a.seq.rows) : min(a.seq.n_seqs, a.seq.rows);
-        if (row >= live) return;
-        const int rest = (int)(i % per_row), h = rest / per_head;
-        const size_t at = (size_t)row * a.q_stride + (size_t)h * dh, to = (size_t)row * a.qo_stride + (size_t)h * dh;
-        auto go = [&](auto v) {
-            constexpr int W = decltype(v)::value;
-            const Item it = item_at<W>(a.rot.dim, a.rot.pairs, rest % per_head);
-            float x[W], y[W];
-            load_item<BF, W>(a.q, at, it, a.rot, a.pos + (size_t)row * 3, x, y);
-            store_ch<BF, W>(a.q_out, to + it.o0, x);
-            store_ch<BF, W>(a.q_out, to + it.o1, y);
-        };
-        if (V == 8) go(std::integral_constant<int, 8>());
-        else go(std::integral_constant<int, 1>());
+        if (live > row0) turn_rows<BF, V, WT>(q, a.rot, row0, min(live - row0, a.q_rows), (float*)lds);
         return;
     }
-    const int h = blockIdx.x % H;
-    const bool values = blockIdx.x / H & 1;
-    const PagePart p = page_part(a.seq, pt, a.c.pages, blockIdx.x / (2 * H));
+    const int groups = (H + a.heads - 1) / a.heads, hg = blockIdx.x % groups;
+    const bool values = blockIdx.x / groups & 1;
+    const PagePart p = page_part(a.seq, pt, a.c.pages, blockIdx.x / (2 * groups));
     if (p.page < 0 || p.n == 0) return;
     const void* src = values ? a.v : a.k;
     const size_t stride = values ? a.v_stride : a.k_stride;
-    float* scales = (values ? a.c.v_scale : a.c.k_scale) + (size_t)p.page * H + h;
-    uint8_t* codes = (values ? a.c.v : a.c.k) + ((size_t)p.page * H + h) * pt * dh;
     const int dim = values ? 0 : a.rot.dim;   // channels that are turned
+    const int per_tok = dh / 16, per_head = p.n * per_tok, keep = p.slot0;
+    const int end = min(H, (hg + 1) * a.heads);
+    // keys: cosines and sines [token][pair], once for all heads; values: codes [head][token][channel + 4]
+    const int ald = (dim / 2 + 3) & ~3, ld = dh + 4;
+    float *cos = (float*)lds, *sin = cos + p.n * ald;
+    uint8_t* tile = lds;
+    if (dim) angles_of<WT>(a.rot, p.n, cos, sin, ald, [&](int r) { return a.pos + (size_t)(p.row0 + r) * 3; });
+    // i / per_head for i < 2^10, per_head <= 2^10 (the error of the factor, below per_head, times i is below 2^20)
+    const uint32_t by_head = ((1u << 20) + per_head - 1) / per_head;
 
-    // all new values of the page and head in registers: 16 (or 2) channels an item
-    const int per_tok = dh / 16, items = p.n * per_tok;
-    float x[MAX_ITEMS][16];
-    float most = 0.f;
+    for (int h0 = hg * a.heads, hn; h0 < end; h0 += hn) {
+        hn = max(1, min(end - h0, PASS / per_head));
+        float* scales = (values ? a.c.v_scale : a.c.k_scale) + (size_t)p.page * H + h0;
+        uint8_t* codes = (values ? a.c.v : a.c.k) + ((size_t)p.page * H + h0) * pt * dh;
+        float old = 0.f;
+        if (tid < hn) {
+            s_most[tid] = 0;
+            if (keep > 0) old = scales[tid];
+        }
+        // the pass's new values in registers
+        float x[MAX_ITEMS][16];
+        int hh[MAX_ITEMS], tt[MAX_ITEMS], cc[MAX_ITEMS];
 #pragma unroll
-    for (int k = 0; k < MAX_ITEMS; ++k) {
-        const int i = tid + k * 256;
-        if (i >= items) break;
-        const int t = i / per_tok, c = i % per_tok, row = p.row0 + t;
-        const size_t at = (size_t)(a.row_idx ? a.row_idx[row] : row) * stride + (size_t)h * dh;
-        const int* pos = a.pos + (size_t)row * 3;
-        if (a.vec == 8) {
-            float u[8], w[8];
-            load_item<BF, 8>(src, at, item_at<8>(dim, a.rot.pairs, c), a.rot, pos, u, w);
+        for (int k = 0; k < MAX_ITEMS; ++k) {
+            const int i = tid + k * WT;
+            hh[k] = (int)(i * by_head >> 20);
+            const int rest = i - hh[k] * per_head;
+            tt[k] = div_by(rest, a.by_tok), cc[k] = rest - tt[k] * per_tok;
+            if (hh[k] >= hn) continue;
+            const int row = p.row0 + tt[k];
+            const size_t at = (size_t)(a.row_idx ? a.row_idx[row] : row) * stride + (size_t)(h0 + hh[k]) * dh;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[k][e] = u[e], x[k][8 + e] = w[e];
-        } else {
+            for (int e = 0; e < 8 / V; ++e) {
+                const Item it = item_at<V>(dim, a.rot.pairs, cc[k] * (8 / V) + e);
+                float u[V], w[V];
+                load_ch<BF, V>(src, at + it.o0, u);
+                load_ch<BF, V>(src, at + it.o1, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float u[1], w[1];
-                load_item<BF, 1>(src, at, item_at<1>(dim, a.rot.pairs, c * 8 + e), a.rot, pos, u, w);
-                x[k][e] = u[0], x[k][8 + e] = w[0];
+                for (int f = 0; f < V; ++f) x[k][e * V + f] = u[f], x[k][8 + e * V + f] = w[f];
             }
         }
+        __syncthreads();   // s_most is cleared, the angles are there
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            x[k][e] = storable(x[k][e]);
-            most = fmaxf(most, fabsf(x[k][e]));   // a NaN does not count
+        for (int k = 0; k < MAX_ITEMS; ++k) {
+            if (hh[k] >= hn) continue;
+#pragma unroll
+            for (int e = 0; e < 8 / V; ++e) {
+                const int c = cc[k] * (8 / V) + e, at = tt[k] * ald + c * V;
+                if (c * 2 * V >= dim) continue;
+                float u[V], w[V];
+#pragma unroll
+                for (int f = 0; f < V; ++f) u[f] = x[k][e * V + f], w[f] = x[k][8 + e * V + f];
+                turn_item<V>(a.rot.pairs, cos + at, sin + at, u, w);
+#pragma unroll
+                for (int f = 0; f < V; ++f) x[k][e * V + f] = u[f], x[k][8 + e * V + f] = w[f];
+            }
+            float most = 0.f;   // a NaN does not count
+#pragma unroll
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf(x[k][e]));
+            if (most > 3.4028235e38f) {   // infinities become NaN: the format has none, and 448 would hide them
+                most = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    x[k][e] = fabsf(x[k][e]) <= 3.4028235e38f ? x[k][e] : __builtin_nanf("");
+                    most = fmaxf(most, fabsf(x[k][e]));
+                }
+            }
+            atomicMax(&s_most[hh[k]], __builtin_bit_cast(uint32_t, most));   // (of LDS; the order does not matter)
         }
-    }
-    most = wave_max(most);
-    if ((tid & 63) == 0) s_most[tid >> 6] = most;
-    __syncthreads();
-    most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
-    const int keep = p.slot0;
-    const float old = keep > 0 ? *scales : 0.f;
-    const float scale = fmaxf(old, scale_for(most)), inv = inverse(scale);
-    if (keep > 0 && old < scale) {   // the tokens that the page held
-        const float f = old * inv;
-        auto again = [&](uint32_t w) {
-            float v[4];
-            decode4(w, f, v);
-            return code4(v[0], v[1], v[2], v[3]);
-        };
-        if (!values) {
-            for (int i = tid; i < keep * dh / 4; i += 256) ((uint32_t*)codes)[i] = again(((uint32_t*)codes)[i]);
-        } else {
-            const int words = (keep + 3) / 4;   // of each channel; the last may hold places that stay as they are
-            for (int i = tid; i < words * dh; i += 256) {
-                uint32_t* at = (uint32_t*)(codes + (size_t)(i / words) * pt) + i % words;
-                const int live = min(4, keep - i % words * 4);
-                const uint32_t mask = live == 4 ? 0xFFFFFFFFu : (1u << 8 * live) - 1;
-                *at = (again(*at) & mask) | (*at & ~mask);
+        __syncthreads();
+        if (tid < hn) {
+            const float scale = fmaxf(old, scale_for(__builtin_bit_cast(float, s_most[tid])));
+            s_old[tid] = keep > 0 ? old : scale;
+            s_scale[tid] = scale;
+            scales[tid] = scale;
+        }
+        __syncthreads();
+        for (int j = 0; keep > 0 && j < hn; ++j) {   // the tokens that the page held, where the scale has grown
+            if (!(s_old[j] < s_scale[j])) continue;
+            const float f = s_old[j] * inverse(s_scale[j]);
+            uint8_t* base = codes + (size_t)j * pt * dh;
+            auto again = [&](uint32_t w) {
+                float v[4];
+                decode4(w, f, v);
+                return code4(v[0], v[1], v[2], v[3]);
+            };
+            if (!values) {
+                for (int i = tid; i < keep * dh / 4; i += WT) ((uint32_t*)base)[i] = again(((uint32_t*)base)[i]);
+            } else {
+                const int words = (keep + 3) / 4;   // of each channel; the last may hold places that stay as they are
+                for (int i = tid; i < words * dh; i += WT) {
+                    uint32_t* at = (uint32_t*)(base + (size_t)(i / words) * pt) + i % words;
+                    const int live = min(4, keep - i % words * 4);
+                    const uint32_t mask = live == 4 ? 0xFFFFFFFFu : (1u << 8 * live) - 1, w = *at;
+                    *at = (again(w) & mask) | (w & ~mask);
+                }
             }
         }
-    }
-    // codes: keys go to their place; values into LDS, token by token
-    const int ld = dh + 4;
+        // codes: keys go to their place; values into LDS, token by token
 #pragma unroll
-    for (int k = 0; k < MAX_ITEMS; ++k) {
-        const int i = tid + k * 256;
-        if (i >= items) break;
-        const int t = i / per_tok, c = i % per_tok;
-        uint32_t w[4];
+        for (int k = 0; k < MAX_ITEMS; ++k) {
+            if (hh[k] >= hn) continue;
+            const float inv = inverse(s_scale[hh[k]]);
+            uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            w[e] = code4(x[k][4 * e] * inv, x[k][4 * e + 1] * inv, x[k][4 * e + 2] * inv, x[k][4 * e + 3] * inv);
-        uint8_t* to = values ? tile + t * ld : codes + (size_t)(p.slot0 + t) * dh;
-        if (a.vec == 8) {
-            const Item it = item_at<8>(dim, a.rot.pairs, c);
-            ((uint32_t*)(to + it.o0))[0] = w[0];
-            ((uint32_t*)(to + it.o0))[1] = w[1];
-            ((uint32_t*)(to + it.o1))[0] = w[2];
-            ((uint32_t*)(to + it.o1))[1] = w[3];
-        } else {
+            for (int e = 0; e < 4; ++e)
+                w[e] = code4(x[k][4 * e] * inv, x[k][4 * e + 1] * inv, x[k][4 * e + 2] * inv, x[k][4 * e + 3] * inv);
+            if constexpr (V == 8) {
+                const Item it = item_at<8>(dim, a.rot.pairs, cc[k]);
+                if (values) {
+                    uint32_t* to = (uint32_t*)(tile + (hh[k] * p.n + tt[k]) * ld + it.o0);   // (o1 = o0 + 8)
+                    to[0] = w[0], to[1] = w[1], to[2] = w[2], to[3] = w[3];
+                } else {
+                    uint8_t* to = codes + ((size_t)hh[k] * pt + p.slot0 + tt[k]) * dh;
+                    *(u32x2*)(to + it.o0) = (u32x2){w[0], w[1]};
+                    *(u32x2*)(to + it.o1) = (u32x2){w[2], w[3]};
+                }
+            } else {
+                uint8_t* to = values ? tile + (hh[k] * p.n + tt[k]) * ld
+                                     : codes + ((size_t)hh[k] * pt + p.slot0 + tt[k]) * dh;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const Item it = item_at<1>(dim, a.rot.pairs, c * 8 + e);
-                to[it.o0] = (uint8_t)(w[e >> 2] >> 8 * (e & 3));
-                to[it.o1] = (uint8_t)(w[2 + (e >> 2)] >> 8 * (e & 3));
+                for (int e = 0; e < 8; ++e) {
+                    const Item it = item_at<1>(dim, a.rot.pairs, cc[k] * 8 + e);
+                    to[it.o0] = (uint8_t)(w[e >> 2] >> 8 * (e & 3));
+                    to[it.o1] = (uint8_t)(w[2 + (e >> 2)] >> 8 * (e & 3));
+                }
             }
         }
-    }
-    __syncthreads();   // the rescaled words and the tile are complete
-    if (values) {
-        for (int i = tid; i < p.n * dh; i += 256) {
-            const int ch = i / p.n, t = i % p.n;
-            codes[(size_t)ch * pt + p.slot0 + t] = tile[t * ld + ch];
+        if (values) {
+            __syncthreads();   // the rescaled words and the tile are complete
+            // four channels of 16 tokens at once, neighbouring lanes on a channel's neighbouring tokens; where
+            // the new tokens fill fewer, byte by byte
+            const int first = keep >> 4, chunks = ((keep + p.n + 15) >> 4) - first, quads = dh / 4;
+            for (int i = tid; i < hn * quads * chunks; i += WT) {
+                const int row = i / chunks, j = first + i - row * chunks;           // row: head and four channels
+                const int hd = row / quads, c4 = row - hd * quads, t0 = j * 16 - keep;   // t0: token of the first byte
+                const uint8_t* from = tile + (hd * p.n + t0) * ld + c4 * 4;
+                uint8_t* to = codes + ((size_t)hd * dh + c4 * 4) * pt + j * 16;
+                if (t0 >= 0 && t0 + 16 <= p.n) {
+                    u32x4 w[4];
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        uint32_t q[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) q[e] = *(const uint32_t*)(from + (4 * g + e) * ld);
+                        transpose4(q);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e][g] = q[e];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) *(u32x4*)(to + (size_t)e * pt) = w[e];
+                } else {
+                    for (int t = max(0, -t0); t < min(16, p.n - t0); ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) to[e * pt + t] = from[t * ld + e];
+                }
+            }
         }
+        __syncthreads();   // the next pass takes the tile and the scales' places again
     }
-    if (tid == 0) *scales = scale;
 }
 
 // ---- read ------------------------------------------------------------------------------------------
+// four codes to bf16 (v_cvt_scalef32_pk_bf16_fp8 applies the scale, exactly)
+__device__ __forceinline__ u32x2 decode_bf16(uint32_t w, float scale) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true);
+    return (u32x2){__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+}
+// Four codes of one row to its channels `to` ..
+template <bool BF, bool WIDE>
+__device__ __forceinline__ void store_codes(void* dst, size_t to, uint32_t w, float scale) {
+    if constexpr (BF) {
+        const u32x2 r = decode_bf16(w, scale);
+        uint16_t* p = (uint16_t*)dst + to;
+        if constexpr (WIDE) *(u32x2*)p = r;
+        else p[0] = r[0] & 0xFFFF, p[1] = r[0] >> 16, p[2] = r[1] & 0xFFFF, p[3] = r[1] >> 16;
+    } else {
+        float x[4];
+        decode4(w, scale, x);
+        float* p = (float*)dst + to;
+        if constexpr (WIDE) *(f32x4*)p = (f32x4){x[0], x[1], x[2], x[3]};
+        else p[0] = x[0], p[1] = x[1], p[2] = x[2], p[3] = x[3];
+    }
+}
+
 // One block per page part, head, and keys or values.  A page that the cache does not have reads as zeros.
-template <bool BF>
+template <bool BF, bool WIDE>
 __global__ __launch_bounds__(256) void cache_read_k(ReadArgs a) {
-    extern __shared__ __attribute__((aligned(16))) uint8_t tile[];   // values: codes [channel][token + 4]
     const int tid = threadIdx.x;
     const int dh = a.c.head_dim, pt = a.c.page_tokens, H = a.c.kv_heads;
     const int h = blockIdx.x % H;
     const bool values = blockIdx.x / H & 1;
     const PagePart p = page_part(a.seq, pt, a.c.pages, blockIdx.x / (2 * H));
     if (p.n == 0) return;
-    void* dst = values ? a.v : a.k;
-    const size_t stride = values ? a.v_stride : a.k_stride;
-    const int per_tok = dh / 16, items = p.n * per_tok;
     const bool there = p.page >= 0;
-    const size_t at = ((size_t)max(p.page, 0) * H + h);
+    const size_t at = (size_t)max(p.page, 0) * H + h;
     const uint8_t* codes = (values ? a.c.v : a.c.k) + at * pt * dh;
-    const float scale = there ? (values ? a.c.v_scale : a.c.k_scale)[at] : 0.f;
-    const int ld = pt + 4;
-    if (values) {
-        const int words = pt / 4;
-        for (int i = tid; i < words * dh; i += 256)
-            *(uint32_t*)(tile + i / words * ld + i % words * 4) = ((const uint32_t*)codes)[i];
-        __syncthreads();
-    }
-    for (int i = tid; i < items; i += 256) {
-        const int t = i / per_tok, c = i % per_tok * 16;
-        uint32_t w[4];
-        if (values) {
+    const float scale = there ? (values ? a.c.v_scale : a.c.k_scale)[at] : 1.f;
+    const uint32_t keep = there ? 0xFFFFFFFFu : 0u;
+    const int quads = dh / 4;
+    if (!values) {   // four channels of a token, neighbouring lanes on neighbouring channels
+        char* dst = (char*)a.k;
+        for (int i = tid; i < p.n * quads; i += 256) {
+            const int t = div_by(i, a.by_quad), c = (i - t * quads) * 4;
+            const uint32_t w = *(const uint32_t*)(codes + (size_t)(p.slot0 + t) * dh + c) & keep;
+            store_codes<BF, WIDE>(dst, (size_t)(p.row0 + t) * a.k_stride + (size_t)h * dh + c, w, scale);
+        }
+    } else {         // four channels of four tokens
+        const int first = p.slot0 >> 2, groups = ((p.slot0 + p.n + 3) >> 2) - first;
+        for (int i = tid; i < groups * quads; i += 256) {
+            const int j = div_by(i, a.by_quad), c = (i - j * quads) * 4, tok = (first + j) * 4;
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = *(const uint32_t*)(codes + (size_t)(c + e) * pt + tok) & keep;
+            transpose4(w);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                w[e] = 0;
-#pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    w[e] |= (uint32_t)tile[(c + 4 * e + b) * ld + p.slot0 + t] << 8 * b;
-            }
-        } else {
-            const u32x4 r = *(const u32x4*)(codes + (size_t)(p.slot0 + t) * dh + c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = r[e];
-        }
-        float x[16];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float v[4];
-            decode4(w[e], scale, v);
-#pragma unroll
-            for (int b = 0; b < 4; ++b) x[4 * e + b] = there ? v[b] : 0.f;
-        }
-        const size_t to = (size_t)(p.row0 + t) * stride + (size_t)h * dh + c;
-        if (a.vec == 8) {
-            float u[8], v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = x[e], v[e] = x[8 + e];
-            store_ch<BF, 8>(dst, to, u);
-            store_ch<BF, 8>(dst, to + 8, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                float u[1] = {x[e]};
-                store_ch<BF, 1>(dst, to + e, u);
+                const int t = tok + e - p.slot0;
+                if (t >= 0 && t < p.n)
+                    store_codes<BF, WIDE>(a.v, (size_t)(p.row0 + t) * a.v_stride + (size_t)h * dh + c, w[e], scale);
             }
         }
     }
@@ -405,13 +484,13 @@ bool aligned16(const void* p, size_t stride, size_t el) { return (uintptr_t)p % 
 
 }  // namespace
 
-void launch_rotary(bool bf, const RotaryArgs& a, hipStream_t s) {
+void launch_rotary(bool bf, RotaryArgs a, hipStream_t s) {
     const size_t el = bf ? 2 : 4;
     // eight channels at once where rows and heads start on 16 bytes and both halves of a turned pair do
     const bool wide = a.dh % 16 == 0 && a.rot.dim % 16 == 0 && aligned16(a.x, a.x_stride, el) &&
                       aligned16(a.out, a.out_stride, el);
-    const long long items = (long long)a.rows * a.heads * (a.dh / (wide ? 16 : 2));
-    const dim3 grid((unsigned)((items + 255) / 256));
+    a.per_block = rows_a_block(a.heads, a.dh, wide ? 8 : 1);
+    const dim3 grid((unsigned)(((long long)a.rows + a.per_block - 1) / a.per_block));
     if (bf && wide) rotary_k<true, 8><<<grid, 256, 0, s>>>(a);
     else if (bf) rotary_k<true, 1><<<grid, 256, 0, s>>>(a);
     else if (wide) rotary_k<false, 8><<<grid, 256, 0, s>>>(a);
@@ -420,26 +499,49 @@ void launch_rotary(bool bf, const RotaryArgs& a, hipStream_t s) {
 
 void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
     const size_t el = bf ? 2 : 4;
+    const CacheView& c = a.c;
     bool wide = a.rot.dim % 16 == 0 && aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el);
     if (a.q) wide = wide && aligned16(a.q, a.q_stride, el) && aligned16(a.q_out, a.qo_stride, el);
-    a.vec = wide ? 8 : 1;
-    a.slots = (int)page_slots(a.seq.offsets || a.seq.one, a.seq.n_seqs, a.seq.rows, page_shift(a.c.page_tokens));
-    const long long q_items = a.q ? (long long)a.seq.rows * a.q_heads * (a.c.head_dim / (2 * a.vec)) : 0;
-    const dim3 grid((unsigned)((long long)a.slots * 2 * a.c.kv_heads + (q_items + 255) / 256));
-    const size_t lds = (size_t)a.c.page_tokens * (a.c.head_dim + 4);
-    if (bf) cache_write_k<true><<<grid, 256, lds, s>>>(a);
-    else cache_write_k<false><<<grid, 256, lds, s>>>(a);
+    const int threads = c.page_tokens * (c.head_dim / 16) <= 512 ? 256 : 512, pass = MAX_ITEMS * threads;
+    // heads of a block: as many as fill its threads if a page gets as many tokens as an average sequence has,
+    // fewer where that leaves compute units without a block
+    const bool ragged = a.seq.offsets || a.seq.one;
+    const long long slots = page_slots(ragged, a.seq.n_seqs, a.seq.rows, page_shift(c.page_tokens));
+    const int tokens = ragged ? std::max(1, std::min(c.page_tokens, a.seq.rows / a.seq.n_seqs)) : 1;
+    a.heads = std::max(1, std::min({MAX_HEADS, c.kv_heads, pass / (tokens * (c.head_dim / 16))}));
+    while (a.heads > 1 && slots * 2 * ((c.kv_heads + a.heads - 1) / a.heads) < 512) a.heads = (a.heads + 1) / 2;
+    a.kv_blocks = (int)(slots * 2 * ((c.kv_heads + a.heads - 1) / a.heads));
+    a.q_rows = rows_a_block(std::max(1, a.q_heads), c.head_dim, wide ? 8 : 1);
+    const dim3 grid((unsigned)(a.kv_blocks + (a.q ? ((long long)a.seq.rows + a.q_rows - 1) / a.q_rows : 0)));
+    a.by_tok = div_magic(c.head_dim / 16);
+    // a pass's codes, rows padded by 4 bytes (16 channels: a row an item); the angles of a page, or of q_rows rows
+    const size_t lds = std::max({(size_t)pass * 20, (size_t)c.page_tokens * ((a.rot.dim / 2 + 3) & ~3) * 2 * sizeof(float),
+                                 ROT_LDS * sizeof(float)});   // 64 KB at most
+    auto go = [&](auto f, auto v) {
+        constexpr bool B = decltype(f)::value;
+        constexpr int V = decltype(v)::value;
+        if (threads == 256) cache_write_k<B, V, 256><<<grid, 256, lds, s>>>(a);
+        else cache_write_k<B, V, 512><<<grid, 512, lds, s>>>(a);
+    };
+    using W8 = std::integral_constant<int, 8>;
+    using W1 = std::integral_constant<int, 1>;
+    if (bf && wide) go(std::true_type(), W8());
+    else if (bf) go(std::true_type(), W1());
+    else if (wide) go(std::false_type(), W8());
+    else go(std::false_type(), W1());
 }
 
 void launch_cache_read(bool bf, ReadArgs a, hipStream_t s) {
     const size_t el = bf ? 2 : 4;
-    a.vec = aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el) ? 8 : 1;
+    const bool wide = aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el);
     const long long slots = page_slots(a.seq.offsets || a.seq.one, a.seq.n_seqs, a.seq.rows,
                                        page_shift(a.c.page_tokens));
+    a.by_quad = div_magic(a.c.head_dim / 4);
     const dim3 grid((unsigned)(slots * 2 * a.c.kv_heads));
-    const size_t lds = (size_t)a.c.head_dim * (a.c.page_tokens + 4);
-    if (bf) cache_read_k<true><<<grid, 256, lds, s>>>(a);
-    else cache_read_k<false><<<grid, 256, lds, s>>>(a);
+    if (bf && wide) cache_read_k<true, true><<<grid, 256, 0, s>>>(a);
+    else if (bf) cache_read_k<true, false><<<grid, 256, 0, s>>>(a);
+    else if (wide) cache_read_k<false, true><<<grid, 256, 0, s>>>(a);
+    else cache_read_k<false, false><<<grid, 256, 0, s>>>(a);
 }
 
 }  // namespace dv

@@ -39,14 +39,21 @@ __host__ __device__ inline int page_from(const SeqArgs& q, int pages, int entry,
 // ---- rows of a call ------------------------------------------------------------------------------
 // Rows of sequence s: offsets[s] .. offsets[s + 1] - 1, cut to the rows there are; without offsets
 // sequence s has row s (or the call's one sequence has them all).
-struct Span {
-    int row0, n;
+struct Seq {
+    int s;          // -1: none
+    int off;        // its first row as the call says
+    int row0, n;    // its rows
+    int at;         // q.at[s]
 };
-__host__ __device__ inline Span rows_of(const SeqArgs& q, int s) {
-    if (q.one) return {0, q.rows};
-    if (!q.offsets) return {s, s < q.rows ? 1 : 0};
-    const int a = q.offsets[s] < 0 ? 0 : q.offsets[s], b = q.offsets[s + 1] < q.rows ? q.offsets[s + 1] : q.rows;
-    return {a, b > a ? b - a : 0};
+__host__ __device__ inline Seq seq_from(const SeqArgs& q, int s, int off, int next, int at) {
+    const int a = off < 0 ? 0 : off, b = next < q.rows ? next : q.rows;
+    return {s, off, a, b > a ? b - a : 0, at};
+}
+__host__ __device__ inline Seq seq_of(const SeqArgs& q, int s) {
+    if (s < 0 || s >= q.n_seqs) return {-1, 0, 0, 0, 0};
+    if (q.one) return {s, 0, 0, q.rows, q.at[s]};
+    if (!q.offsets) return {s, s, s, s < q.rows ? 1 : 0, q.at[s]};
+    return seq_from(q, s, q.offsets[s], q.offsets[s + 1], q.at[s]);
 }
 
 // Kernels deal blocks to slots: sequence s owns the slots from slot_base(s), and a slot finds its
@@ -67,14 +74,11 @@ struct PagePart {
     int slot0, n;   // its places slot0 .. slot0 + n - 1; n = 0: nothing
 };
 // ... slot u, of sequence s
-__host__ __device__ inline PagePart part_at(const SeqArgs& q, int pt, int pages, int s, long long u) {
+__host__ __device__ inline PagePart part_at(const SeqArgs& q, int pt, int pages, const Seq& sp, long long u) {
     PagePart p = {-1, 0, 0, 0};
-    if (s < 0 || s >= q.n_seqs) return p;
-    const int shift = page_shift(pt);
-    const Span sp = rows_of(q, s);
-    const int start = q.at[s];
-    if (sp.n == 0 || start < 0) return p;
-    const long long j = q.one ? u : q.offsets ? u - slot_base(q.offsets[s], 1, shift, 2, s) : 0;
+    const int shift = page_shift(pt), s = sp.s, start = sp.at;
+    if (s < 0 || sp.n == 0 || start < 0) return p;
+    const long long j = q.one ? u : q.offsets ? u - slot_base(sp.off, 1, shift, 2, s) : 0;
     const long long page = ((long long)start >> shift) + j;     // of the sequence
     const long long end = (long long)start + sp.n, next = (page + 1) << shift;
     const long long a = start > page << shift ? start : page << shift, b = end < next ? end : next;
@@ -101,11 +105,12 @@ __host__ __device__ inline long long tile_slots(bool offsets, int n_seqs, int ro
                    : (long long)n_seqs * ((group + (1 << shift) - 1) >> shift);
 }
 // ... slot u, of sequence s (without offsets: of sequence u / tiles of a row)
-__host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int shift, bool causal, int s, long long u) {
+__host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int shift, bool causal, const Seq& sp,
+                                        long long u) {
     Tile t = {-1, 0, 0, 0, 0, 0, 0};
-    if (s < 0 || s >= q.n_seqs) return t;
-    const Span sp = rows_of(q, s);
-    const long long j = q.offsets ? u - slot_base(q.offsets[s], group, shift, 1, s)
+    const int s = sp.s;
+    if (s < 0) return t;
+    const long long j = q.offsets ? u - slot_base(sp.off, group, shift, 1, s)
                                   : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
     const long long first = j << shift, left = (long long)sp.n * group - first;
     if (left <= 0) return t;
@@ -114,7 +119,7 @@ __host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int
     t.n = sp.n;
     t.first = (int)first;
     t.rows = (int)(left < (1 << shift) ? left : 1 << shift);
-    const int most = q.table_pages * pt, len = q.at[s] < most ? q.at[s] : most;
+    const int most = q.table_pages * pt, len = sp.at < most ? sp.at : most;
     t.len = len > 0 ? len : 0;
     t.end = t.len;
     if (causal) {
@@ -125,17 +130,21 @@ __host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int
 }
 
 #ifdef __HIPCC__
-// The sequence whose slots hold slot u, or -1 (every lane of a wavefront calls, with the same u).
-__device__ __forceinline__ int find_seq(const int* offsets, int n_seqs, int mul, int shift, int add, long long u) {
-    int found = 0;
-    for (int b = 0; b < n_seqs; b += 64) {
-        const int s = b + (threadIdx.x & 63);
-        const bool before = s < n_seqs && slot_base(offsets[s], mul, shift, add, s) <= u;
-        const int k = __popcll(__ballot(before));
-        found += k;
-        if (k < 64) break;
+// The sequence whose slots hold slot u (every lane of a wavefront calls, with the same u).  Its offsets and
+// place are loaded along with the search: a chain of loads is what small calls wait for.
+__device__ __forceinline__ Seq find_seq(const SeqArgs& q, int mul, int shift, int add, long long u) {
+    Seq r = {-1, 0, 0, 0, 0};
+    for (int b = 0; b < q.n_seqs; b += 64) {
+        const int s = b + (threadIdx.x & 63), c = s < q.n_seqs ? s : q.n_seqs - 1;
+        const int off = q.offsets[c], next = q.offsets[c + 1], at = q.at[c];
+        const unsigned long long before = __ballot(s < q.n_seqs && slot_base(off, mul, shift, add, s) <= u);
+        if (!before) break;
+        const int k = __popcll(before) - 1;
+        r = seq_from(q, b + k, __builtin_amdgcn_readlane(off, k), __builtin_amdgcn_readlane(next, k),
+                     __builtin_amdgcn_readlane(at, k));
+        if (k < 63) break;
     }
-    return found - 1;
+    return r;
 }
 #endif
 

@@ -281,18 +281,22 @@ struct RotaryPlan {
     uint64_t turn[64];
     int dim, end0, end1, pairs;   // pairs: channels 2i and 2i + 1 (else i and i + dim/2)
 };
-struct RotaryArgs {
+struct RowsArgs {
     const void* x;           // row r, head h, channel c: x[r * x_stride + h * dh + c]
     void* out;               // may be x
     long long x_stride, out_stride;
-    int rows, heads, dh;
-    const int* rows_dev;     // device row count (nullptr: rows)
+    int heads, dh;
     const int* pos;          // [.., 3]
     const int* pos_idx;      // row r takes position pos_idx[r] % pos_mod (nullptr: r)
     int pos_mod;
-    RotaryPlan rot;
 };
-void launch_rotary(bool bf16, const RotaryArgs& a, hipStream_t s);
+struct RotaryArgs : RowsArgs {
+    int rows;
+    const int* rows_dev;     // device row count, at most rows (nullptr: rows)
+    RotaryPlan rot;
+    int per_block;           // set by the launcher
+};
+void launch_rotary(bool bf16, RotaryArgs a, hipStream_t s);
 
 struct CacheView {
     uint8_t *k, *v;            // e4m3 codes: [pages, heads, tokens, channels], [pages, heads, channels, tokens]
@@ -316,7 +320,8 @@ struct WriteArgs {
     const int* pos;            // [rows, 3]; unused where rot.dim is 0
     const int* row_idx;        // row r of the call is row row_idx[r] of k and v (nullptr: r)
     RotaryPlan rot;
-    int slots, vec;            // set by the launcher
+    int heads, kv_blocks, q_rows;   // set by the launcher
+    uint32_t by_tok;
 };
 void launch_cache_write(bool bf16, WriteArgs a, hipStream_t s);
 struct ReadArgs {
@@ -324,7 +329,7 @@ struct ReadArgs {
     SeqArgs seq;
     void *k, *v;
     long long k_stride, v_stride;
-    int vec;                   // set by the launcher
+    uint32_t by_quad;          // set by the launcher
 };
 void launch_cache_read(bool bf16, ReadArgs a, hipStream_t s);
 

@@ -16,7 +16,7 @@ int t_page_parts(const int* table, int table_pages, int pages, const int* offset
         int s = offsets ? -1 : u;
         if (offsets)
             while (s + 1 < n_seqs && slot_base(offsets[s + 1], 1, page_shift(pt), 2, s + 1) <= u) ++s;
-        const PagePart p = part_at(q, pt, pages, s, u);
+        const PagePart p = part_at(q, pt, pages, seq_of(q, s), u);
         const int v[] = {s, p.page, p.row0, p.slot0, p.n};
         for (int i = 0; i < 5; ++i) out[5 * u + i] = v[i];
     }
@@ -33,7 +33,7 @@ int t_tiles(int table_pages, const int* offsets, int n_seqs, int rows, const int
         int s = offsets ? -1 : u / ((group + (1 << shift) - 1) >> shift);
         if (offsets)
             while (s + 1 < n_seqs && slot_base(offsets[s + 1], group, shift, 1, s + 1) <= u) ++s;
-        const Tile t = tile_of(q, pt, group, shift, causal != 0, s, u);
+        const Tile t = tile_of(q, pt, group, shift, causal != 0, seq_of(q, s), u);
         const int v[] = {t.seq, t.row0, t.first, t.rows, t.len, t.end};
         for (int i = 0; i < 6; ++i) out[6 * u + i] = v[i];
     }
