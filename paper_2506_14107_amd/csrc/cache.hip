@@ -423,26 +423,41 @@ __device__ __forceinline__ u32x2 decode_bf16(uint32_t w, float scale) {
     const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true);
     return (u32x2){__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
 }
-// Four codes of one row to its channels `to` ..
+// Eight codes of one row to its channels `to` ..
 template <bool BF, bool WIDE>
-__device__ __forceinline__ void store_codes(void* dst, size_t to, uint32_t w, float scale) {
+__device__ __forceinline__ void store_codes(void* dst, size_t to, uint32_t lo, uint32_t hi, float scale) {
     if constexpr (BF) {
-        const u32x2 r = decode_bf16(w, scale);
+        const u32x2 a = decode_bf16(lo, scale), b = decode_bf16(hi, scale);
+        const u32x4 r = {a[0], a[1], b[0], b[1]};
         uint16_t* p = (uint16_t*)dst + to;
-        if constexpr (WIDE) *(u32x2*)p = r;
-        else p[0] = r[0] & 0xFFFF, p[1] = r[0] >> 16, p[2] = r[1] & 0xFFFF, p[3] = r[1] >> 16;
+        if constexpr (WIDE) {
+            *(u32x4*)p = r;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = (uint16_t)(r[e >> 1] >> 16 * (e & 1));
+        }
     } else {
-        float x[4];
-        decode4(w, scale, x);
+        float x[4], y[4];
+        decode4(lo, scale, x);
+        decode4(hi, scale, y);
         float* p = (float*)dst + to;
-        if constexpr (WIDE) *(f32x4*)p = (f32x4){x[0], x[1], x[2], x[3]};
-        else p[0] = x[0], p[1] = x[1], p[2] = x[2], p[3] = x[3];
+        if constexpr (WIDE) {
+            *(f32x4*)p = (f32x4){x[0], x[1], x[2], x[3]};
+            *(f32x4*)(p + 4) = (f32x4){y[0], y[1], y[2], y[3]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = x[e], p[4 + e] = y[e];
+        }
     }
 }
 
-// One block per page part, head, and keys or values.  A page that the cache does not have reads as zeros.
+// One block per page part, head, and keys or values.  A page that the cache does not have reads as zeros.  A
+// lane stores eight channels of a token, neighbouring lanes neighbouring channels; values pass through
+// LDS, where a lane takes eight channels of four tokens (100,003 tokens of 8 heads of 128, us: 155 with those
+// dwords from memory, 173 byte by byte from LDS).
 template <bool BF, bool WIDE>
 __global__ __launch_bounds__(256) void cache_read_k(ReadArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t tile[];   // values: codes [channel][token + 4]
     const int tid = threadIdx.x;
     const int dh = a.c.head_dim, pt = a.c.page_tokens, H = a.c.kv_heads;
     const int h = blockIdx.x % H;
@@ -454,28 +469,38 @@ __global__ __launch_bounds__(256) void cache_read_k(ReadArgs a) {
     const uint8_t* codes = (values ? a.c.v : a.c.k) + at * pt * dh;
     const float scale = there ? (values ? a.c.v_scale : a.c.k_scale)[at] : 1.f;
     const uint32_t keep = there ? 0xFFFFFFFFu : 0u;
-    const int quads = dh / 4;
-    if (!values) {   // four channels of a token, neighbouring lanes on neighbouring channels
-        char* dst = (char*)a.k;
-        for (int i = tid; i < p.n * quads; i += 256) {
-            const int t = div_by(i, a.by_quad), c = (i - t * quads) * 4;
-            const uint32_t w = *(const uint32_t*)(codes + (size_t)(p.slot0 + t) * dh + c) & keep;
-            store_codes<BF, WIDE>(dst, (size_t)(p.row0 + t) * a.k_stride + (size_t)h * dh + c, w, scale);
+    const int oct = dh / 8;
+    if (!values) {
+        for (int i = tid; i < p.n * oct; i += 256) {
+            const int t = div_by(i, a.by_oct), c = (i - t * oct) * 8;
+            const u32x2 w = *(const u32x2*)(codes + (size_t)(p.slot0 + t) * dh + c);
+            store_codes<BF, WIDE>(a.k, (size_t)(p.row0 + t) * a.k_stride + (size_t)h * dh + c, w[0] & keep, w[1] & keep,
+                                  scale);
         }
-    } else {         // four channels of four tokens
-        const int first = p.slot0 >> 2, groups = ((p.slot0 + p.n + 3) >> 2) - first;
-        for (int i = tid; i < groups * quads; i += 256) {
-            const int j = div_by(i, a.by_quad), c = (i - j * quads) * 4, tok = (first + j) * 4;
-            uint32_t w[4];
+        return;
+    }
+    const int ld = pt + 4, shift = page_shift(pt) - 4;
+    for (int i = tid; i < dh << shift; i += 256) {   // 16 tokens of a channel
+        const u32x4 w = ((const u32x4*)codes)[i];
+        uint32_t* to = (uint32_t*)(tile + (i >> shift) * ld + (i & ((1 << shift) - 1)) * 16);
+        to[0] = w[0], to[1] = w[1], to[2] = w[2], to[3] = w[3];
+    }
+    __syncthreads();
+    const int first = p.slot0 >> 2, groups = ((p.slot0 + p.n + 3) >> 2) - first;
+    for (int i = tid; i < groups * oct; i += 256) {
+        const int j = div_by(i, a.by_oct), c = (i - j * oct) * 8, tok = (first + j) * 4;
+        uint32_t w[2][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = *(const uint32_t*)(codes + (size_t)(c + e) * pt + tok) & keep;
-            transpose4(w);
+        for (int g = 0; g < 2; ++g) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int t = tok + e - p.slot0;
-                if (t >= 0 && t < p.n)
-                    store_codes<BF, WIDE>(a.v, (size_t)(p.row0 + t) * a.v_stride + (size_t)h * dh + c, w[e], scale);
-            }
+            for (int e = 0; e < 4; ++e) w[g][e] = *(const uint32_t*)(tile + (c + 4 * g + e) * ld + tok) & keep;
+            transpose4(w[g]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int t = tok + e - p.slot0;
+            if (t >= 0 && t < p.n)
+                store_codes<BF, WIDE>(a.v, (size_t)(p.row0 + t) * a.v_stride + (size_t)h * dh + c, w[0][e], w[1][e], scale);
         }
     }
 }
@@ -536,12 +561,13 @@ void launch_cache_read(bool bf, ReadArgs a, hipStream_t s) {
     const bool wide = aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el);
     const long long slots = page_slots(a.seq.offsets || a.seq.one, a.seq.n_seqs, a.seq.rows,
                                        page_shift(a.c.page_tokens));
-    a.by_quad = div_magic(a.c.head_dim / 4);
+    a.by_oct = div_magic(a.c.head_dim / 8);
+    const size_t lds = (size_t)a.c.head_dim * (a.c.page_tokens + 4);
     const dim3 grid((unsigned)(slots * 2 * a.c.kv_heads));
-    if (bf && wide) cache_read_k<true, true><<<grid, 256, 0, s>>>(a);
-    else if (bf) cache_read_k<true, false><<<grid, 256, 0, s>>>(a);
-    else if (wide) cache_read_k<false, true><<<grid, 256, 0, s>>>(a);
-    else cache_read_k<false, false><<<grid, 256, 0, s>>>(a);
+    if (bf && wide) cache_read_k<true, true><<<grid, 256, lds, s>>>(a);
+    else if (bf) cache_read_k<true, false><<<grid, 256, lds, s>>>(a);
+    else if (wide) cache_read_k<false, true><<<grid, 256, lds, s>>>(a);
+    else cache_read_k<false, false><<<grid, 256, lds, s>>>(a);
 }
 
 }  // namespace dv

@@ -329,7 +329,7 @@ struct ReadArgs {
     SeqArgs seq;
     void *k, *v;
     long long k_stride, v_stride;
-    uint32_t by_quad;          // set by the launcher
+    uint32_t by_oct;           // set by the launcher
 };
 void launch_cache_read(bool bf16, ReadArgs a, hipStream_t s);
 
