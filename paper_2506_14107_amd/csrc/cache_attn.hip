@@ -66,6 +66,12 @@ __device__ __forceinline__ bf16x8 decode8(uint32_t lo, uint32_t hi, float scale)
     const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     return (bf16x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+// the largest of three, a NaN aside (without the quieting of its operands that fmaxf asks for)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
 // x as T bf16 terms: the first its rounding, each next the rounding of what is left
 template <int T>
 __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&t)[T]) {
@@ -303,10 +309,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
                     vw[c][w] &= ~bad;
                 }
         }
-        float top = sc[0];
+        float top = max3(sc[0], sc[1], sc[2]), top2 = max3(sc[3], sc[4], sc[5]);
 #pragma unroll
-        for (int e = 1; e < 16; ++e) top = fmaxf(top, sc[e]);
-        top = group_max(top);
+        for (int e = 6; e < 14; e += 4) top = max3(top, sc[e], sc[e + 1]), top2 = max3(top2, sc[e + 2], sc[e + 3]);
+        top = group_max(max3(max3(top, sc[14], sc[15]), top2, top2));
         // rescale only when some row's maximum has grown by more than 2^8: probabilities stay far
         // inside the range of fp32 and bf16
         if (__any(top > m + lazy)) {
@@ -406,7 +412,8 @@ struct Lds {
     int nan;               // a step that not all rows see holds a NaN value
 };
 
-template <int DH>
+// ONE: a step lies in one page (64 or 128 tokens), whose address is scalar then.
+template <int DH, bool ONE>
 __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
     constexpr int KS = DH / 16;                      // 16-channel steps of S^T
     constexpr int CB = (DH + 31) / 32;               // 32-channel blocks of O^T
@@ -453,6 +460,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
     };
     auto pages = [&](int kb) {
         Pages p;
+        if constexpr (ONE) {
+            p.v = entry_of(a.seq, t.seq, kb >> shift);
+            return p;
+        }
 #pragma unroll
         for (int n = 0; n < NL; ++n)
             p.k[n] = entry_of(a.seq, t.seq, (kb + (tid + n * 256) / PARTS) >> shift);
@@ -462,7 +473,24 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
     u32x4 kc[NL], vc[NL];
     float ksc[NL], vsc;
     bool vin;
+    const uint32_t kat = tid * 16, vat = tid / 4 * pt + tid % 4 * 16;   // ONE: of part tid, in the page
     auto load = [&](int kb, const Pages& p) {
+        if constexpr (ONE) {
+            const int page = page_from(a.seq, a.c.pages, __builtin_amdgcn_readfirstlane(p.v), t.seq, kb >> shift);
+            const size_t at = (size_t)max(page, 0) * H + h;
+            const uint8_t* kbase = a.c.k + (at * pt + (kb & (pt - 1))) * DH;
+            const uint8_t* vbase = a.c.v + at * DH * pt + (kb & (pt - 1));
+            vin = page >= 0;
+#pragma unroll
+            for (int n = 0; n < NL; ++n) {
+                if (STEP * PARTS % 256 && tid + n * 256 >= STEP * PARTS) break;
+                kc[n] = *(const u32x4*)(kbase + kat + n * 4096u);
+                vc[n] = *(const u32x4*)(vbase + vat + n * 64u * pt);
+                ksc[n] = a.c.k_scale[at];
+            }
+            vsc = a.c.v_scale[at];
+            return;
+        }
         const int tok = kb + tid % 4 * 16;
         const int vp = page_from(a.seq, a.c.pages, p.v, t.seq, tok >> shift);
         vin = vp >= 0;
@@ -554,13 +582,15 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
                     sc[b][e] = 16 * j + (e & 7) < live && (there >> 8 * j & 1) ? sc[b][e] : -INFINITY;
                 }
         }
-        float mx[16];
+        float mx[5];   // five chains
 #pragma unroll
-        for (int e = 0; e < 16; ++e) mx[e] = fmaxf(sc[0][e], sc[1][e]);
+        for (int e = 0; e < 5; ++e) mx[e] = max3(sc[0][3 * e], sc[0][3 * e + 1], sc[0][3 * e + 2]);
 #pragma unroll
-        for (int w = 8; w >= 1; w >>= 1)
+        for (int e = 0; e < 5; ++e) mx[e] = max3(mx[e], sc[1][3 * e], sc[1][3 * e + 1]);
 #pragma unroll
-            for (int e = 0; e < w; ++e) mx[e] = fmaxf(mx[e], mx[e + w]);
+        for (int e = 0; e < 5; ++e) mx[e] = e < 4 ? max3(mx[e], sc[1][3 * e + 2], mx[e]) : max3(mx[e], sc[0][15], sc[1][15]);
+        mx[0] = max3(mx[0], mx[1], sc[1][14]);
+        mx[0] = max3(mx[0], mx[2], max3(mx[3], mx[4], mx[4]));
         const float top = across<5>(mx[0], [](float x, float y) { return fmaxf(x, y); });
         if (__any(top > m + lazy)) {
             const float mn = fmaxf(m, top);
@@ -732,10 +762,15 @@ void launch_dh(bool bf, const CacheAttnArgs& a, hipStream_t s) {
         else cache_attn_k<DH, false><<<grid, 256, 0, s>>>(a);
     }
     if (a.route != ATTN_FEW) {
-        static const bool ok = allow_lds((const void*)cache_attn_tile_k<DH>, sizeof(Lds<DH>));
-        (void)ok;
         const dim3 grid((unsigned)(a.many.slots * a.c.kv_heads), (unsigned)a.many.splits);
-        cache_attn_tile_k<DH><<<grid, 256, sizeof(Lds<DH>), s>>>(a);
+        auto go = [&](auto one) {
+            constexpr auto k = cache_attn_tile_k<DH, decltype(one)::value>;
+            static const bool ok = allow_lds((const void*)k, sizeof(Lds<DH>));
+            (void)ok;
+            k<<<grid, 256, sizeof(Lds<DH>), s>>>(a);
+        };
+        if (a.c.page_tokens >= STEP) go(std::true_type());
+        else go(std::false_type());
     }
 }
 
