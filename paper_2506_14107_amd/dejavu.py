@@ -418,15 +418,20 @@ def compact(masks, group_size, stream=None):
 
 
 # ---- token rows and their 8-bit cache -----------------------------------------------------------
-# Small calls are bound by what the host does, so the checks below read few attributes.
-def _torch():
-    import torch
-    return torch
+# Small calls are bound by what the host does: the checks below read few attributes, and torch is
+# looked up once (by the first Rotary or TokenCache).
+torch = None
+
+
+def _need_torch():
+    global torch
+    if torch is None:
+        import torch as t
+        torch = t
 
 
 def _dtype(t):
     d = t.dtype
-    torch = _torch()
     if d is torch.bfloat16:
         return DV_BF16
     if d is torch.float32:
@@ -456,18 +461,22 @@ def _rows(name, t, shape, dtype, index):
 
 
 def _ints(name, t, index, shape):
-    if (t.dtype is not _torch().int32 or t.get_device() != index or t.shape != shape
+    if (t.dtype is not torch.int32 or t.get_device() != index or t.shape != shape
             or not t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on device {index}")
     return t.data_ptr()
 
 
-class _Away:
-    """Makes a device current where it is not, and a given stream where there is one, so that what
-    the call allocates belongs to it."""
+def _elsewhere(index, stream):
+    """Whether a call on device `index` and `stream` (None: the device's current one) needs another
+    device or stream current, so that what it allocates belongs there (_Away)."""
+    if index < 0:
+        raise ValueError("tensors must be on a HIP device")
+    return stream is not None or torch.cuda.current_device() != index
 
+
+class _Away:
     def __init__(self, index, stream):
-        torch = _torch()
         self.stack = [torch.cuda.device(index)] + ([torch.cuda.stream(stream)] if stream else [])
 
     def __enter__(self):
@@ -479,28 +488,8 @@ class _Away:
             c.__exit__(*e)
 
 
-class _Here:
-    def __enter__(self):
-        pass
-
-    def __exit__(self, *e):
-        pass
-
-
-_HERE = _Here()
-
-
-def _on(index, stream):
-    """Context of a call on device `index` and on `stream` (None: the device's current one)."""
-    if index < 0:
-        raise ValueError("tensors must be on a HIP device")
-    if stream is None and _torch().cuda.current_device() == index:
-        return _HERE
-    return _Away(index, stream)
-
-
 def _raw_stream(index):
-    return _torch()._C._cuda_getCurrentRawStream(index)
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 class Rotary:
@@ -509,6 +498,7 @@ class Rotary:
     every axis takes the whole range of rates."""
 
     def __init__(self, sections, layout="halves", per_axis=False, base=10000.0):
+        _need_torch()
         code = {"halves": DV_ROTARY_HALVES, "pairs": DV_ROTARY_PAIRS}.get(layout)
         if code is None:
             raise ValueError(f"unknown rotary layout {layout!r}")
@@ -523,20 +513,22 @@ def rotary(x, positions, rot, out=None, stream=None):
     """Rows x [rows, heads, head_dim] with their heads turned by `positions` (int32 [rows, 3]) at the
     rates of `rot` (Rotary), into `out` (which may be x) or a new tensor."""
     index = x.get_device()
-    if x.dim() != 3:
+    if _elsewhere(index, stream):
+        with _Away(index, stream):
+            return rotary(x, positions, rot, out)
+    shape = x.shape
+    if len(shape) != 3:
         _misfit("x", x)
-    with _on(index, stream):
-        shape = n, h, d = x.shape
-        dtype = _dtype(x)
-        xs = _stride("x", x)
-        if out is None:
-            out = _torch().empty(shape, dtype=x.dtype, device=x.device)
-            os = h * d
-        else:
-            os = xs if out is x else _rows("out", out, shape, x.dtype, index)
-        dv_rotary(rot.address, dtype, x.data_ptr(), xs, n, h, d,
-                  _ints("positions", positions, index, (n, 3)), out.data_ptr(), os,
-                  _raw_stream(index))
+    n, h, d = shape
+    dtype = _dtype(x)
+    xs = _stride("x", x)
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        os = h * d
+    else:
+        os = xs if out is x else _rows("out", out, shape, x.dtype, index)
+    dv_rotary(rot.address, dtype, x.data_ptr(), xs, n, h, d,
+              _ints("positions", positions, index, (n, 3)), out.data_ptr(), os, _raw_stream(index))
     return out
 
 
@@ -553,7 +545,7 @@ class TokenCache:
     """
 
     def __init__(self, pages, kv_heads, head_dim, page_tokens=64, device=None, buffers=None):
-        torch = _torch()
+        _need_torch()
         shapes = [(pages, kv_heads, page_tokens, head_dim), (pages, kv_heads, head_dim, page_tokens),
                   (pages, kv_heads), (pages, kv_heads)]
         types = [torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32]
@@ -571,6 +563,7 @@ class TokenCache:
         self.desc = dv_cache(*(b.data_ptr() for b in buffers), pages, page_tokens, kv_heads,
                              head_dim)
         self.address = ctypes.addressof(self.desc)
+        self.scratch = {}   # workspace bytes by the sizes they depend on
 
     def _seqs(self, at, name, offsets, table):
         """(n_seqs, table, table_pages, offsets, at) as the entry points take them."""
@@ -590,52 +583,55 @@ class TokenCache:
         sequence.  With `rotary` and `positions` the keys are turned first, and the rows of q
         [rows, heads, head_dim] into `q_out` (which may be q) or a new tensor, which is returned."""
         index = self.index
-        with _on(index, stream):
-            n, t, tp, o, at = self._seqs(starts, "starts", offsets, table)
-            rows, dt = k.shape[0], k.dtype
-            dtype = _dtype(k)
-            shape = (rows, self.kv_heads, self.head_dim)
-            ks = _rows("k", k, shape, dt, index)
-            vs = _rows("v", v, shape, dt, index)
-            plan = pos = qp = qs = qop = qos = heads = 0
-            if rotary is not None and positions is not None:
-                plan, pos = rotary.address, _ints("positions", positions, index, (rows, 3))
-            elif rotary is not None or positions is not None:
-                raise ValueError("rotary and positions come together")
-            if q is not None:
-                if q.dim() != 3:
-                    _misfit("q", q)
-                heads = q.shape[1]
-                shape = (rows, heads, self.head_dim)
-                qs = _rows("q", q, shape, dt, index)
-                if q_out is None:
-                    q_out = _torch().empty(shape, dtype=dt, device=q.device)
-                qos = _rows("q_out", q_out, shape, dt, index)
-                qp, qop = q.data_ptr(), q_out.data_ptr()
-            elif q_out is not None:
-                raise ValueError("q_out without q")
-            dv_cache_write(self.address, n, t, tp, o, at, dtype, k.data_ptr(), ks, v.data_ptr(), vs,
-                           rows, plan, pos, qp, qs, heads, qop, qos, _raw_stream(index))
+        if _elsewhere(index, stream):
+            with _Away(index, stream):
+                return self.write(k, v, starts, offsets, table, rotary, positions, q, q_out)
+        n, t, tp, o, at = self._seqs(starts, "starts", offsets, table)
+        rows, dt = k.shape[0], k.dtype
+        dtype = _dtype(k)
+        shape = (rows, self.kv_heads, self.head_dim)
+        ks = _rows("k", k, shape, dt, index)
+        vs = _rows("v", v, shape, dt, index)
+        plan = pos = qp = qs = qop = qos = heads = 0
+        if rotary is not None and positions is not None:
+            plan, pos = rotary.address, _ints("positions", positions, index, (rows, 3))
+        elif rotary is not None or positions is not None:
+            raise ValueError("rotary and positions come together")
+        if q is not None:
+            if q.dim() != 3:
+                _misfit("q", q)
+            heads = q.shape[1]
+            shape = (rows, heads, self.head_dim)
+            qs = _rows("q", q, shape, dt, index)
+            if q_out is None:
+                q_out = torch.empty(shape, dtype=dt, device=q.device)
+            qos = _rows("q_out", q_out, shape, dt, index)
+            qp, qop = q.data_ptr(), q_out.data_ptr()
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        dv_cache_write(self.address, n, t, tp, o, at, dtype, k.data_ptr(), ks, v.data_ptr(), vs, rows,
+                       plan, pos, qp, qs, heads, qop, qos, _raw_stream(index))
         return q_out
 
     def read(self, starts, offsets=None, table=None, rows=None, dtype=None, out=None, stream=None):
         """Keys and values [rows, kv_heads, head_dim] of places starts[s] .. of each sequence, into
         `out` (a pair of tensors) or new tensors of `rows` rows and `dtype` (bf16)."""
         index = self.index
-        with _on(index, stream):
-            n, t, tp, o, at = self._seqs(starts, "starts", offsets, table)
-            if out is None:
-                torch = _torch()
-                shape = (n if rows is None else rows, self.kv_heads, self.head_dim)
-                out = [torch.empty(shape, dtype=dtype or torch.bfloat16, device=self.device)
-                       for _ in range(2)]
-            k, v = out
-            rows, dt = k.shape[0], k.dtype
-            shape = (rows, self.kv_heads, self.head_dim)
-            ks = _rows("k", k, shape, dt, index)
-            vs = _rows("v", v, shape, dt, index)
-            dv_cache_read(self.address, n, t, tp, o, at, _dtype(k), k.data_ptr(), ks, v.data_ptr(),
-                          vs, rows, _raw_stream(index))
+        if _elsewhere(index, stream):
+            with _Away(index, stream):
+                return self.read(starts, offsets, table, rows, dtype, out)
+        n, t, tp, o, at = self._seqs(starts, "starts", offsets, table)
+        if out is None:
+            shape = (n if rows is None else rows, self.kv_heads, self.head_dim)
+            out = [torch.empty(shape, dtype=dtype or torch.bfloat16, device=self.device)
+                   for _ in range(2)]
+        k, v = out
+        rows, dt = k.shape[0], k.dtype
+        shape = (rows, self.kv_heads, self.head_dim)
+        ks = _rows("k", k, shape, dt, index)
+        vs = _rows("v", v, shape, dt, index)
+        dv_cache_read(self.address, n, t, tp, o, at, _dtype(k), k.data_ptr(), ks, v.data_ptr(), vs,
+                      rows, _raw_stream(index))
         return out
 
     def attention(self, q, lengths, offsets=None, table=None, causal=True, scale=None, max_rows=0,
@@ -645,37 +641,46 @@ class TokenCache:
         see no later ones.  max_rows: an upper bound of any sequence's rows, if known.  workspace: a
         uint8 tensor to use (see attention_workspace) instead of one of the call's own."""
         index = self.index
-        with _on(index, stream):
-            n, t, tp, o, at = self._seqs(lengths, "lengths", offsets, table)
-            if q.dim() != 3:
-                _misfit("q", q)
-            rows, heads, d = q.shape
-            shape = (rows, heads, self.head_dim)
-            qs = _rows("q", q, shape, q.dtype, index)
-            dtype = _dtype(q)
-            if out is None:
-                out = _torch().empty(shape, dtype=q.dtype, device=q.device)
-                os = heads * d
-            else:
-                os = _rows("out", out, shape, q.dtype, index)
-            if workspace is None:
-                need = dv_cache_attention_workspace(self.address, n, tp, o != 0, dtype, rows,
-                                                    heads, max_rows)
-                if need:
-                    torch = _torch()
-                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            elif workspace.get_device() != index or workspace.dtype is not _torch().uint8:
+        if _elsewhere(index, stream):
+            with _Away(index, stream):
+                return self.attention(q, lengths, offsets, table, causal, scale, max_rows, out,
+                                      workspace)
+        n, t, tp, o, at = self._seqs(lengths, "lengths", offsets, table)
+        if q.dim() != 3:
+            _misfit("q", q)
+        rows, heads, d = q.shape
+        shape = (rows, heads, self.head_dim)
+        qs = _rows("q", q, shape, q.dtype, index)
+        dtype = _dtype(q)
+        if out is None:
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+            os = heads * d
+        else:
+            os = _rows("out", out, shape, q.dtype, index)
+        ws = size = 0
+        if workspace is None:
+            key = (n, tp, o != 0, dtype, rows, heads, max_rows)
+            size = self.scratch.get(key)
+            if size is None:
+                size = dv_cache_attention_workspace(self.address, *key)
+                if len(self.scratch) >= 1024:
+                    self.scratch.clear()
+                self.scratch[key] = size
+            if size:
+                workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+                ws = workspace.data_ptr()
+        else:
+            if workspace.get_device() != index or workspace.dtype is not torch.uint8:
                 _misfit("workspace", workspace)
-            dv_cache_attention(self.address, n, t, tp, o, at, dtype, q.data_ptr(), qs, rows, heads,
-                               max_rows, d ** -0.5 if scale is None else scale, causal,
-                               out.data_ptr(), os, _ptr(workspace),
-                               0 if workspace is None else workspace.numel(), _raw_stream(index))
+            ws, size = workspace.data_ptr(), workspace.numel()
+        dv_cache_attention(self.address, n, t, tp, o, at, dtype, q.data_ptr(), qs, rows, heads,
+                           max_rows, d ** -0.5 if scale is None else scale, causal, out.data_ptr(), os,
+                           ws, size, _raw_stream(index))
         return out
 
     def attention_workspace(self, n_seqs, rows, heads, table_pages=None, with_offsets=True,
                             max_rows=0, dtype=None):
         """Bytes of scratch that `attention` needs for such a call (of rows of `dtype`; bf16)."""
-        torch = _torch()
         tp = self.pages // max(n_seqs, 1) if table_pages is None else table_pages
         return dv_cache_attention_workspace(self.address, n_seqs, tp, with_offsets,
                                             DV_F32 if dtype is torch.float32 else DV_BF16, rows,
