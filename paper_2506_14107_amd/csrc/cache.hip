@@ -4,7 +4,7 @@
 // Rotary positions: pair i of a row is turned by pos[axis(i)] * f_i radians.  The angle is kept in turns:
 // f_i / 2 pi as a 64-bit fraction (RotaryPlan::turn), so that the product with a 32-bit position, taken
 // modulo 2^64, is the turn's fraction to 2^-33 at any position; fp32 angles are off by 2^-24 of the whole
-// angle, 64 radians at position 2^30.  Sine and cosine are polynomials on an eighth of a turn, in fp32.
+// angle, 64 radians at position 2^30.
 //
 // Codes are e4m3 (1 sign, 4 exponent, 3 fraction bits; largest 448), rounded to nearest even by
 // v_cvt_pk_fp8_f32.  Scales are powers of two, the least with every |x| <= 448 scale: a floating code
@@ -74,24 +74,32 @@ __device__ __forceinline__ void store_ch(void* base, size_t at, const float (&x)
 }
 
 // ---- rotary positions ------------------------------------------------------------------------------
-// cos and sin of 2 pi pos turn / 2^64.  The low 64 bits of the product hold the fraction of a turn; its
-// high half, rounded by the half of its low half, is a signed 32-bit fraction f.  The nearest eighth of a turn
-// is taken off (|r| <= pi/4 after the nearest quarter), then the Taylor polynomials of degree 9 and 8:
-// remainders (pi/4)^11 / 11! = 1.8e-9 and (pi/4)^10 / 10! = 2.5e-8, below half a step of fp32.
+// cos and sin of 2 pi pos turn / 2^64, rounded to fp32 from fp64: keys are quantised from turned values, and
+// every error there moves values across a code's border.  The low 64 bits of the product hold the fraction of
+// a turn.  The nearest quarter is taken off (|r| <= pi/4), then the Taylor polynomials of degree 11 and
+// 10: remainders (pi/4)^13 / 13! = 7e-12 and (pi/4)^12 / 12! = 1.2e-10, far below half a step of fp32.
 __device__ __forceinline__ void turn_cos_sin(int pos, uint64_t turn, float& c, float& s) {
     const uint64_t p = (uint64_t)(int64_t)pos * turn;
-    const uint32_t f = (uint32_t)((p + 0x80000000ull) >> 32);
-    const uint32_t q = (f + 0x20000000u) >> 30;                 // nearest quarter, modulo 4
-    const float r = (float)(int32_t)(f - (q << 30)) * 1.4629180792671596e-09f;   // 2 pi / 2^32
-    const float r2 = r * r;
-    const float sn = fmaf(fmaf(fmaf(fmaf(2.7557319e-6f, r2, -1.9841270e-4f), r2, 8.3333333e-3f), r2, -1.6666667e-1f),
-                          r2 * r, r);
-    const float cs = fmaf(fmaf(fmaf(fmaf(2.4801587e-5f, r2, -1.3888889e-3f), r2, 4.1666667e-2f), r2, -0.5f), r2, 1.0f);
+    const uint32_t q = (uint32_t)((p + (1ull << 61)) >> 62);    // nearest quarter, modulo 4
+    const int64_t f = (int64_t)(p - ((uint64_t)q << 62));
+    const double r = fma((double)(int32_t)(f >> 32), 4294967296.0, (double)(uint32_t)f) * 3.4061215800865545e-19;   // 2 pi / 2^64
+    const double r2 = r * r;
+    double u = fma(-2.505210838544172e-08, r2, 2.7557319223985893e-06);
+    u = fma(u, r2, -1.984126984126984e-04);
+    u = fma(u, r2, 8.333333333333333e-03);
+    u = fma(u, r2, -1.6666666666666666e-01);
+    const float sn = (float)fma(u * r2, r, r);
+    double v = fma(-2.755731922398589e-07, r2, 2.48015873015873e-05);
+    v = fma(v, r2, -1.388888888888889e-03);
+    v = fma(v, r2, 4.1666666666666664e-02);
+    v = fma(v, r2, -0.5);
+    const float cs = (float)fma(v, r2, 1.0);
     c = q & 1 ? sn : cs;
     s = q & 1 ? cs : sn;
     if (q == 1 || q == 2) c = -c;
     if (q >= 2) s = -s;
 }
+
 // An item is two groups of V channels of one row and head that the rotation mixes (or, past the turned
 // channels, leaves): items of the `dim` turned channels first.
 //   halves: channels o .. o + V - 1 with o + dim/2 ..; pairs (V = 8): 16 channels in a row, (V = 1): 2
