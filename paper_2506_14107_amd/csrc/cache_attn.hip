@@ -26,8 +26,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x2 __attribute__((ext_vector_type(2)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -100,15 +98,6 @@ template <int K>
 __device__ __forceinline__ void settle(bf16x8 (&q)[K]) {
 #pragma unroll
     for (int k = 0; k < K; ++k) asm volatile("" : "+v"(q[k]));
-}
-// l plus the sum of eight probabilities as the value product takes them: what rounding to bf16 does to a large one,
-// it does to the sum that divides it too
-__device__ __forceinline__ float add8(const bf16x8& p, float l) {
-    const s16x8 q = __builtin_bit_cast(s16x8, p);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        l = __builtin_amdgcn_fdot2_f32_bf16((s16x2){q[2 * e], q[2 * e + 1]}, (s16x2){0x3F80, 0x3F80}, l, false);
-    return l;
 }
 // bytes of w that are NaN codes, as 0xFF
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
@@ -339,12 +328,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             p[e >> 3][e & 7] = __builtin_amdgcn_exp2f(fmaf(sc[e], sl2, off));
-            if (!BF) l += p[e >> 3][e & 7];
+            l += p[e >> 3][e & 7];
         }
         bf16x8 pf[2][NT];
         split8<NT>(p[0], pf[0]);
         split8<NT>(p[1], pf[1]);
-        if (BF) l = add8(pf[1][0], add8(pf[0][0], l));
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
@@ -555,7 +543,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
     for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
-    float m = -INFINITY, l4[4] = {0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
 
     auto step = [&](int kb, int buf) {
         f32x16 sc[2];
@@ -608,8 +596,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
             const float mn = fmaxf(m, top);
             const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * sl2);
             m = mn;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) l4[j] *= alpha;
+            l *= alpha;
 #pragma unroll
             for (int c = 0; c < CB; ++c)
 #pragma unroll
@@ -617,13 +604,22 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
         }
         const float off = m == -INFINITY ? 0.f : -m * sl2;
         bf16x8 pf[4];
+        // (v_dot2_f32_bf16 would add two of the rounded ones at once, but loses low bits of a long sum: outputs over
+        // 5000 keys 0.0023 off, relative, instead of 0.0019)
+        float sum[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            pf[e >> 3][e & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[0][e], sl2, off));
-            pf[2 + (e >> 3)][e & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[1][e], sl2, off));
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[0][e], sl2, off));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[1][e], sl2, off));
+            sum[e] = p0 + p1;
+            pf[e >> 3][e & 7] = (__bf16)p0;
+            pf[2 + (e >> 3)][e & 7] = (__bf16)p1;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) l4[j] = add8(pf[j], l4[j]);
+        for (int w = 8; w >= 1; w >>= 1)
+#pragma unroll
+            for (int e = 0; e < w; ++e) sum[e] += sum[e + w];
+        l += sum[0];
         const uint8_t* vrow = lds.v[buf] + lr * Lds<DH>::VLD + hl * 16;
         // (channels past DH take those 16 before: they are not stored)
         auto at = [&](int c, int j) {
@@ -665,7 +661,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[c][e] = found >> (c * 16 + e) & 1 ? __builtin_nanf("") : o[c][e];
     }
-    const float l = across<5>((l4[0] + l4[1]) + (l4[2] + l4[3]), [](float x, float y) { return x + y; });
+    l = across<5>(l, [](float x, float y) { return x + y; });
     const int row = mine + lr - t.first;
     if (row >= t.rows) return;
     const bool whole = t.end <= a.many.chunk;
