@@ -30,12 +30,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int TS = 4, TR = 1 << TS;   // packed rows of a tile
-constexpr int LS = 7, LR = 1 << LS;   // packed rows of a large tile
-constexpr int FEW = 32;    // packed rows of a sequence up to which small tiles take it
-constexpr int STEP = 64;   // keys of a step
+constexpr int TR = 1 << TS, LR = 1 << LS;   // packed rows of a tile
+constexpr int STEP = 64;                    // keys of a step
 constexpr int WAVES = 4;
-constexpr int MAX_SPLITS = 512;
 
 // f of the two values that lanes whose numbers differ in one bit (4 or 5) hold, in both: the swap gives
 // one lane's value in its first result and the other's in its second.  (The elements are copied before
@@ -149,8 +146,6 @@ __device__ __forceinline__ void store4(void* out, size_t at, f32x4 x) {
     }
 }
 
-// partial results: per tile of R rows, head and split R rows of DH fp32, R maxima, R sums
-__host__ __device__ inline size_t part_floats(int R, int dh) { return (size_t)R * (dh + 2); }
 
 // One tile, head and split of the keys per block; its wavefronts take the steps of the split in turn and
 // join their results through LDS.
@@ -726,7 +721,6 @@ __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
                 sum += part[s * per + R * DH + R + row] * w;
             }
             const float* p = part + (size_t)k * 64 * per + row * DH + ch;
-#pragma unroll 4
             for (int i = wave % W * groups; i < n; i += W * groups) {
                 const int j = i + grp;
                 const float wj = __shfl(w, j & 63, 64);
@@ -777,44 +771,6 @@ void launch_dh(bool bf, const CacheAttnArgs& a, hipStream_t s) {
 }
 
 }  // namespace
-
-CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets, int max_rows, int table_pages,
-                              int page_tokens, int kv_heads, int q_heads, int head_dim, int cus) {
-    CacheAttnPlan p{};
-    const int G = q_heads / kv_heads;
-    const long long unit = cus > 0 ? cus : 256;
-    const long long keys = (long long)table_pages * page_tokens;   // at most 2^30
-    const long long most_rows = std::min<long long>(rows, !offsets ? 1 : max_rows > 0 ? max_rows : rows);
-    // Large tiles (bf16) take sequences of more than FEW packed rows.  Where some may have fewer, both kernels
-    // run, each on its own sequences: they need not if no sequence can have more, if there is one
-    // sequence, or if all have as many as the longest.
-    const bool alike = n_seqs == 1 || (max_rows > 0 && (long long)n_seqs * max_rows == rows);
-    p.route = !bf || most_rows * G <= FEW ? ATTN_FEW : alike ? ATTN_MANY : ATTN_BOTH;
-
-    // Splits of equal length.  One sequence: as many as are resident at once, two blocks a compute unit (one
-    // query over 200,001 keys of 8 heads of 128, us with 32 / 64 / 98 / 126 splits: 85 / 77 / 87 / 82).
-    // Several may have any lengths up to the table's: splits of 2048 keys at most, so that the long ones
-    // spread over the chip (64 sequences of 1 to 12,000 keys, us with splits of 1024 / 2048 / 3136 /
-    // 6272 / 12,032 keys: 171 / 161 / 167 / 180 / 182) unless there are many tiles anyway.  512 keys and fewer
-    // are not split: the join costs more.
-    auto cut = [&](CacheAttnCut& c, int shift, long long cap) {
-        c.slots = tile_slots(offsets, n_seqs, rows, G, shift);
-        const long long units = std::max(1ll, c.slots * kv_heads);
-        const long long most = std::min<long long>(MAX_SPLITS, std::max(1ll, 2 * unit / units));
-        long long chunk = (keys + most - 1) / most;
-        if (n_seqs > 1 && units < 16 * unit) chunk = std::min(chunk, cap);
-        chunk = std::max({chunk, 512ll, (keys + MAX_SPLITS - 1) / MAX_SPLITS});
-        c.chunk = (int)((chunk + 255) / 256 * 256);
-        c.splits = (int)std::max(1ll, (keys + c.chunk - 1) / c.chunk);
-        c.tile_rows = (int)std::min<long long>(1 << shift, std::max(1ll, most_rows * G));
-        return c.splits > 1 ? (size_t)c.slots * kv_heads * c.splits * part_floats(1 << shift, head_dim) : 0;
-    };
-    if (p.route != ATTN_MANY) p.few_floats = cut(p.few, TS, 2048);
-    size_t many = 0;
-    if (p.route != ATTN_FEW) many = cut(p.many, LS, keys);
-    p.bytes = (p.few_floats + many) * sizeof(float);
-    return p;
-}
 
 void launch_cache_attention(bool bf, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s) {
     a.route = p.route;

@@ -355,15 +355,13 @@ struct CacheAttnArgs {
     int route;
     CacheAttnCut few, many;
 };
-// What a call takes, from its sizes: the same rule sizes the workspace.
+// What a call takes, from its sizes (cache_plan.h): the same rule sizes the workspace.
 struct CacheAttnPlan {
     int route;
     CacheAttnCut few, many;
     size_t few_floats;         // workspace: small tiles' partial results, then large ones'
     size_t bytes;
 };
-CacheAttnPlan cache_attn_plan(bool bf16, int n_seqs, int rows, bool offsets, int max_rows, int table_pages,
-                              int page_tokens, int kv_heads, int q_heads, int head_dim, int cus);
 void launch_cache_attention(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);
 
 }  // namespace dv

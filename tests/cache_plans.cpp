@@ -40,4 +40,15 @@ int t_tiles(int table_pages, const int* offsets, int n_seqs, int rows, const int
     return slots;
 }
 
+// An attention call's plan: route; out: small tiles' chunk, splits, slots, then large ones', workspace bytes.
+int t_attn_plan(int bf16, int n_seqs, int rows, int offsets, int max_rows, int table_pages, int page_tokens,
+                int kv_heads, int q_heads, int head_dim, int cus, long long* out) {
+    const CacheAttnPlan p = cache_attn_plan(bf16 != 0, n_seqs, rows, offsets != 0, max_rows, table_pages,
+                                            page_tokens, kv_heads, q_heads, head_dim, cus);
+    const long long v[] = {p.few.chunk, p.few.splits, p.few.slots, p.many.chunk, p.many.splits, p.many.slots,
+                           (long long)p.bytes};
+    for (int i = 0; i < 7; ++i) out[i] = v[i];
+    return p.route;
+}
+
 }  // extern "C"

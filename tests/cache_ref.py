@@ -152,7 +152,9 @@ def attention_tolerance(out, mass, size, dtype, dh, keys):
     factor, the exponential itself twice: (3 * 40 + 4) 2^-24.  A probability is rounded to bf16 (fp32: 2^-24),
     its products are summed in fp32 over the keys, and so are the sums that divide them, joined over
     wavefronts and splits: (2 keys + 20) 2^-23 at worst, 2 sqrt(keys) of these in any real sum but not
-    here.  The score's error counts twice, in the probability and in the sum."""
+    here.  The score's error counts twice, in the probability and in the sum.
+    A probability below 2^-126 of the largest is 0 in fp32 (a score 88 below the maximum), which takes away
+    at most that times its value (below 2^6 in these tests) for each key: 64-bit results of 1e-62 come out 0."""
     e = 2 * (dh * 2.0 ** -23 * size[..., None] + 124 * 2.0 ** -24) + (2 * keys + 20) * 2.0 ** -23
-    t = mass * (e + HALF[dtype])
+    t = mass * (e + HALF[dtype]) + keys * 2.0 ** -120
     return t + HALF[dtype] * (np.abs(out) + t)

@@ -12,6 +12,8 @@ import pytest
 
 from paper_2506_14107_amd import dejavu as dj
 
+from . import test_gpu_cache as on_gpu
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "..", "paper_2506_14107_amd", "csrc")
 FAKE = 1 << 20   # an aligned address that nothing may touch
@@ -285,3 +287,59 @@ def test_every_packed_row_has_one_tile(lib, shift, group, causal):
     slots = lib.t_tiles(4, None, 6, 6, sp, 16, group, shift, causal, out.ctypes.data_as(ctypes.c_void_p))
     assert sorted((q, i) for q, _, f, k, _, _ in out[:slots] for i in range(f, f + k)) == \
         [(q, i) for q in range(6) for i in range(group)]
+
+
+# ---- how attention is cut ------------------------------------------------------------------------
+FEW, MANY, BOTH = range(3)
+
+
+def plan(lib, bf16, n, rows, offsets, max_rows, table_pages, pt, heads, q_heads, dh, cus=256):
+    out = (ctypes.c_longlong * 7)()
+    route = lib.t_attn_plan(bf16, n, rows, offsets, max_rows, table_pages, pt, heads, q_heads, dh, cus, out)
+    return (route, *out)
+
+
+def test_attention_routes_of_the_gpu_tests(lib):
+    """The cases that test large tiles take them, alone or for the longer sequences; the others small
+    ones; some batches of each split their keys."""
+    split = set()
+    for cases, large in ((on_gpu.ATTENTION, False), (on_gpu.LARGE, True)):
+        for name, (heads, group, dh, pt, counts, lengths, pad) in cases.items():
+            tp = max(1, max(-(-x // pt) for x in lengths))
+            for most in (0, max(counts)):
+                p = plan(lib, 1, len(counts), sum(counts) + pad, 1, most, tp, pt, heads, heads * group, dh)
+                if not large:
+                    assert p[0] == FEW, name
+                elif len(counts) > 1 and not (most and len(set(counts)) == 1 and pad == 0):
+                    assert p[0] == BOTH, name
+                else:
+                    assert p[0] == MANY, name
+                split |= {(w, p[i] > 1) for w, i in (("few", 2), ("many", 5)) if p[i]}
+            assert plan(lib, 0, len(counts), sum(counts) + pad, 1, 0, tp, pt, heads, heads * group, dh)[0] == FEW
+    assert split == {(w, s) for w in ("few", "many") for s in (False, True)}, split
+
+
+@pytest.mark.parametrize("bf16", [0, 1])
+def test_attention_cuts_cover_the_table(lib, bf16):
+    """Splits cover every key that a table can hold, in the range the kernels take; the workspace holds a
+    partial result for every tile, head and split; launches stay within 2^32 threads."""
+    rng = random.Random(4)
+    for _ in range(3000):
+        n, heads, group = rng.choice([1, 2, 3, 64, 300]), rng.choice([1, 2, 8, 40]), rng.choice([1, 4, 7, 16])
+        pt, dh = rng.choice([16, 32, 64, 128]), rng.choice([16, 64, 128])
+        tp = min((1 << 30) // pt, int(2 ** rng.uniform(0, 26)))
+        offsets = rng.random() < 0.7
+        rows = n if not offsets else rng.choice([n, 5 * n, int(2 ** rng.uniform(0, 18))])
+        most = rng.choice([0, 1, rows])
+        p = plan(lib, bf16, n, rows, int(offsets), most, tp, pt, heads, heads * group, dh, rng.choice([0, 256, 304]))
+        need = 0
+        for chunk, splits, slots, rows_a_tile in ((*p[1:4], 16), (*p[4:7], 128)):
+            if not splits:
+                continue
+            assert chunk % 256 == 0 and 1 <= splits <= 512
+            assert chunk * splits >= tp * pt > chunk * (splits - 1)
+            assert slots * heads * splits * 256 < 1 << 32
+            if splits > 1:
+                need += slots * heads * splits * rows_a_tile * (dh + 2) * 4
+        # 64 blocks a unit of 16 rows; splits of large tiles only where two blocks a unit leave room
+        assert p[7] == need and need <= 304 * (64 * 16 + 4 * 128) * (dh + 2) * 4 + (1 << 24)

@@ -446,13 +446,38 @@ ATTENTION = {
     "prompt-128": (1, 4, 128, 32, [150], [333], 4),
     "prompt-mixed": (2, 4, 80, 16, [1, 140, 2, 0, 33], [400, 140, 90, 10, 500], 0),
 }
+# bf16 batches that take large tiles: all of them, or (with several lengths) the longer sequences
+LARGE = {
+    "one": (16, 4, 64, 64, [141], [300], 3),
+    "page-128": (17, 2, 128, 128, [250], [250], 0),
+    "page-16": (18, 1, 80, 16, [460], [463], 0),
+    "32": (24, 1, 32, 32, [350], [400], 1),
+    "16": (32, 1, 16, 64, [257], [1100], 0),
+    "48": (32, 1, 48, 64, [257], [64], 0),
+    "96": (33, 2, 96, 16, [129], [150], 0),
+    "112": (34, 1, 112, 128, [241], [300], 0),
+    "group-20": (2, 20, 64, 64, [210], [700], 0),
+    "alike": (16, 2, 64, 64, [100, 100, 100], [100, 400, 1], 2),
+    "mixed": (16, 4, 64, 32, [1, 120, 17, 0, 16, 3], [900, 130, 17, 4, 600, 2], 0),
+    "mixed-128": (8, 4, 128, 64, [20, 1, 260, 2], [40, 3000, 260, 0], 0),
+    "split": (4, 8, 64, 64, [300], [5000], 0),
+}
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("name", LARGE)
+def test_attention_large_tiles(name, causal):
+    attention_case(*LARGE[name], name, "bf16", causal)
 
 
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("name", ATTENTION)
 def test_attention(name, dtype, causal):
-    heads, group, dh, pt, counts, lengths, pad = ATTENTION[name]
+    attention_case(*ATTENTION[name], name, dtype, causal)
+
+
+def attention_case(heads, group, dh, pt, counts, lengths, pad, name, dtype, causal):
     rng = np.random.default_rng(11)
     p, table = filled(rng, heads, dh, pt, lengths)
     offs = np.concatenate([[0], np.cumsum(counts)])
@@ -470,12 +495,12 @@ def test_attention(name, dtype, causal):
         check_attention(p, table, q, q64, lengths, offs, causal, dtype, got, f"{name} without offsets")
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [1, 40])
-def test_attention_extremes(rows, dtype):
+@pytest.mark.parametrize("dtype,rows,heads", [("f32", 1, 2), ("bf16", 1, 2), ("f32", 40, 2), ("bf16", 40, 2),
+                                              ("bf16", 80, 18)])
+def test_attention_extremes(rows, dtype, heads):
     """Scores far apart and a scale of the caller's; missing pages; lengths past the table and below zero;
     NaN and infinities among keys and values that a row does not see."""
-    heads, group, dh, pt, length = 2, 2, 64, 16, 150
+    group, dh, pt, length = 2, 64, 16, 150
     rng = np.random.default_rng(12)
     p, table = filled(rng, heads, dh, pt, [length] * 3, size=20.0)
     offs = np.arange(4) * rows
@@ -515,19 +540,19 @@ def test_attention_extremes(rows, dtype):
 
 
 def test_attention_of_nan_queries_stays_in_its_rows():
-    heads, dh = 2, 64
+    dh = 64
     rng = np.random.default_rng(13)
-    p, table = filled(rng, heads, dh, 16, [90])
-    for dtype in ("bf16", "f32"):
-        q, q64 = normal(rng, (20, heads, dh), dtype)
+    for dtype, heads, rows in (("bf16", 2, 20), ("f32", 2, 20), ("bf16", 100, 80)):   # the last: large tiles
+        p, table = filled(rng, heads, dh, 16, [90])
+        q, q64 = normal(rng, (rows, heads, dh), dtype)
         q[4, 1, 9], q64[4, 1, 9] = float("nan"), np.nan
-        got = values(p.c.attention(q, ints([90]), ints([0, 20]), ints(table)))
+        got = values(p.c.attention(q, ints([90]), ints([0, rows]), ints(table)))
         assert np.isnan(got[4, 1]).all() and np.isnan(got).sum() == dh
         want = q64.copy()
         want[4, 1] = 0
         got[4, 1] = 0
         k, v, _ = p.m.history(table.tolist(), 0, 90)
-        sees = np.arange(90)[None] <= (70 + np.arange(20))[:, None]
+        sees = np.arange(90)[None] <= (90 - rows + np.arange(rows))[:, None]
         out, mass, size = ref.attention(want, k, v, sees, dh ** -0.5)
         out[4, 1] = 0
         close(got, out, ref.attention_tolerance(out, mass, size, dtype, dh, 90), "others")
