@@ -335,8 +335,8 @@ int dv_rotary_init(dv_rotary_plan* plan, const int section[3], int layout, int p
  * negated positions undo the turn, which is also its gradient.  out may be x with the same stride
  * (in place), and must not overlap it otherwise.  The position part of Section 2.3's attention.
  * Errors: DV_EINVAL (NULL pointer, bad plan, dtype, rows < 0, heads or head_dim < 1, head_dim odd or
- * below plan->dim, stride too small, different strides in place, rows of more than 2^24 or in all 2^33
- * channels or more), DV_EHIP.  rows = 0 does nothing, and the pointers may be NULL then. */
+ * below plan->dim, stride too small, different strides in place, more than 2^27 rows, rows of more than 2^24
+ * or in all 2^33 channels or more), DV_EHIP.  rows = 0 does nothing, and the pointers may be NULL then. */
 int dv_rotary(const dv_rotary_plan* plan, int dtype, const void* x, long long x_stride, int rows,
               int heads, int head_dim, const int32_t* positions, void* out, long long out_stride,
               hipStream_t stream);
@@ -362,8 +362,8 @@ typedef struct dv_cache {
  * page of the cache (negative, or >= pages) means that the page is not there: what is written to it
  * is dropped, it reads as zeros, and attention does not see it; the same goes for places past the
  * table.  Rows of sequence s: offsets[s] .. offsets[s + 1] - 1 of the call's `rows` rows (device
- * int32 [n_seqs + 1], not descending; rows from offsets[n_seqs] on are padding), or with offsets
- * NULL row s alone.  Common errors: DV_EINVAL (NULL pointer, n_seqs or table_pages < 1, rows < 0, rows
+ * int32 [n_seqs + 1], not descending; rows before offsets[0] and from offsets[n_seqs] on are
+ * padding), or with offsets NULL row s alone.  Common errors: DV_EINVAL (NULL pointer, n_seqs or table_pages < 1, rows < 0, rows
  * < n_seqs without offsets, page_tokens, kv_heads, head_dim or pages out of range, misaligned
  * codes, table NULL and n_seqs * table_pages > pages, table_pages * page_tokens > 2^30, unknown
  * dtype, stride too small, sizes past one launch's 2^32 threads), DV_EHIP.  rows = 0 does nothing, and row
@@ -375,7 +375,7 @@ typedef struct dv_cache {
  * even.  Writing a page's first place starts the page anew; writing further places keeps the
  * tokens before them and lets the scale grow, which rescales those tokens' codes (each rounded again
  * only where it falls below 2^-6 of the scale).  Infinities and NaN are stored as NaN and do not
- * count for the scale.  Places after the last one written are undefined.  With `plan`, keys are
+ * count for the scale; what rounds past fp32 (above 1.9375 * 2^127) reads as infinity.  Places after the last one written are undefined.  With `plan`, keys are
  * turned by positions[row] (device int32 [rows, 3]) before they are quantised, and q rows (q_heads
  * heads; NULL for none) are turned into q_out, which may be q with the same stride: one launch for a
  * decoding step.  No two sequences of a call may write the same page.  (The memory compaction of
@@ -389,8 +389,8 @@ int dv_cache_write(const dv_cache* cache, int n_seqs, const int32_t* table, int 
                    long long q_stride, int q_heads, void* q_out, long long q_out_stride,
                    hipStream_t stream);
 
-/* Reads places starts[s] .. of each sequence into rows of keys and values (code times scale, rounded
- * to dtype; exact in both), the inverse of dv_cache_write's layout (Section 5.2).  Errors: the common
+/* Reads places starts[s] .. of each sequence into rows of keys and values (code times scale; exact,
+ * in bf16 below 2^-126 aside), the inverse of dv_cache_write's layout (Section 5.2).  Errors: the common
  * ones. */
 int dv_cache_read(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
                   const int32_t* offsets, const int32_t* starts, int dtype, void* k,
@@ -404,10 +404,12 @@ int dv_cache_read(const dv_cache* cache, int n_seqs, const int32_t* table, int t
  * and infinities among it, does not reach it.  max_rows: an upper bound of the rows of any sequence, 0 if
  * unknown; it serves the choice of kernel only.  workspace: device scratch of
  * dv_cache_attention_workspace bytes for the same arguments (16-byte aligned; NULL where that is 0),
- * of this call alone until it has run.  (The attention of Section 2.3 for a query engine's reads of
+ * of this call alone until it has run.  out may be q with the same stride (in place), and must not
+ * overlap it otherwise.  (The attention of Section 2.3 for a query engine's reads of
  * cached tokens.)  Errors: the common ones, and DV_EINVAL for q_heads no multiple of kv_heads,
  * q_heads * rows >= 2^31, a scale that is not finite and positive, max_rows < 0, out rows that do not
- * start on four elements, a workspace that is too small or misaligned. */
+ * start on four elements, q and out the same with different strides, a workspace that is too small or
+ * misaligned. */
 int dv_cache_attention_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets,
                                  int dtype, int rows, int q_heads, int max_rows, size_t* bytes);
 int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,

@@ -1425,7 +1425,8 @@ int dv_rotary(const dv_rotary_plan* plan, int dtype, const void* x, long long x_
     if (plan->dim > head_dim || head_dim % 2)
         return fail(DV_EINVAL, "head dim %d must be even and hold the %d turned channels", head_dim, plan->dim);
     const long long wide = (long long)heads * head_dim;
-    if (wide > (1 << 24) || rows * wide >= (1ll << 33)) return fail(DV_EINVAL, "rows of %lld channels: too many for one call", wide);
+    if (wide > (1 << 24) || rows * wide >= (1ll << 33) || rows > (1 << 27))   // blocks of up to 16 rows, 256 threads
+        return fail(DV_EINVAL, "%d rows of %lld channels: too many for one call", rows, wide);
     if ((rc = check_stride("x", x_stride, wide)) || (rc = check_stride("out", out_stride, wide))) return rc;
     if (x && x == out && x_stride != out_stride) return fail(DV_EINVAL, "in place the strides must be the same");
     if (rows == 0) return DV_OK;
@@ -1467,6 +1468,9 @@ int dv_cache_write(const dv_cache* cache, int n_seqs, const int32_t* table, int 
         if ((rc = check_stride("q", q_stride, q_wide)) || (rc = check_stride("q_out", q_out_stride, q_wide))) return rc;
         if (q == q_out && q_stride != q_out_stride) return fail(DV_EINVAL, "in place the strides must be the same");
     }
+    if (cache_write_threads(cache->page_tokens, cache->head_dim, cache->kv_heads, n_seqs, rows, offsets != nullptr,
+                            q ? q_heads : 0) > MAX_THREADS)
+        return fail(DV_EINVAL, "%d rows of %d sequences are too many for one call", rows, n_seqs);
     if (rows == 0) return DV_OK;
     WriteArgs a{};
     a.c = view_of(cache);
@@ -1530,6 +1534,7 @@ int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, 
     if (!(scale > 0) || std::isinf(scale)) return fail(DV_EINVAL, "scale must be finite and positive");
     const long long wide = (long long)q_heads * cache->head_dim;
     if ((rc = check_stride("q", q_stride, wide)) || (rc = check_stride("out", out_stride, wide))) return rc;
+    if (q && q == out && q_stride != out_stride) return fail(DV_EINVAL, "in place the strides must be the same");
     if ((uintptr_t)out % (dtype == DV_BF16 ? 8 : 16) || out_stride % 4)
         return fail(DV_EINVAL, "out rows must start on four elements");
     const CacheAttnPlan p = cache_attn_plan(dtype == DV_BF16, n_seqs, rows, offsets != nullptr, max_rows, table_pages,

@@ -127,8 +127,8 @@ __device__ __forceinline__ void turn_item(bool pairs, const float* cos, const fl
     } else {
         c[0] = *cos, s[0] = *sin;
     }
-    auto rotate = [&](int i, float& x, float& y) {
-        const float u = x * c[i] - y * s[i];
+    auto rotate = [&](int i, float& x, float& y) {   // the same roundings however rows are aligned
+        const float u = fmaf(x, c[i], -(y * s[i]));
         y = fmaf(x, s[i], y * c[i]);
         x = u;
     };
@@ -164,7 +164,7 @@ __device__ __forceinline__ void angles_of(const RotaryPlan& rot, int n, float* c
 // Rows row0 .. row0 + n - 1 of x, heads turned, to out (a block; n at most ROT_ROWS).  Each angle is computed
 // once, into LDS, and used by all heads (16,448 rows of 32 heads of 80 channels, bf16: 36 us, with every head
 // computing its own 51).
-constexpr int ROT_ROWS = 16, ROT_LDS = ROT_ROWS * 64 * 2;
+constexpr int ROT_LDS = ROT_ROWS * 64 * 2;
 template <bool BF, int V, int NT>
 __device__ __forceinline__ void turn_rows(const RowsArgs& a, const RotaryPlan& rot, int row0, int n, float* lds) {
     const int tid = threadIdx.x, half = rot.dim / 2, ld = (half + 3) & ~3;
@@ -186,10 +186,6 @@ __device__ __forceinline__ void turn_rows(const RowsArgs& a, const RotaryPlan& r
         store_ch<BF, V>(a.out, to + it.o0, x);
         store_ch<BF, V>(a.out, to + it.o1, y);
     }
-}
-// Rows a block takes: about four items a thread.
-int rows_a_block(int heads, int dh, int vec) {
-    return std::max(1, std::min(ROT_ROWS, 1024 / std::max(1, heads * (dh / (2 * vec)))));
 }
 
 template <bool BF, int V>
@@ -238,8 +234,7 @@ __device__ __forceinline__ PagePart page_part(const SeqArgs& q, int pt, int page
 // Further blocks turn the query rows.
 constexpr int MAX_ITEMS = 2;                    // items of 16 channels a thread and pass
 constexpr int MAX_HEADS = 16;                   // heads of a block
-// WT threads a block: 256, or 512 where a page and head have more than 512 items (more than 64 tokens of
-// 128 channels).
+// WT threads a block (write_threads).
 template <bool BF, int V, int WT>
 __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
     constexpr int PASS = MAX_ITEMS * WT;      // items of a pass: one head's, or more heads'
@@ -250,9 +245,11 @@ __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
     const int dh = a.c.head_dim, pt = a.c.page_tokens, H = a.c.kv_heads;
     if (blockIdx.x >= (unsigned)a.kv_blocks) {   // queries
         const RowsArgs q = {a.q, a.q_out, a.q_stride, a.qo_stride, a.q_heads, dh, a.pos, nullptr, 0};
-        const int row0 = (blockIdx.x - a.kv_blocks) * a.q_rows;
+        const int b = (blockIdx.x - a.kv_blocks) * a.q_rows;
+        const int row0 = a.seq.offsets ? max(a.seq.offsets[0], b) : b;   // rows before it are no sequence's
         const int live = a.seq.offsets ? min(a.seq.offsets[a.seq.n_seqs], a.seq.rows) : min(a.seq.n_seqs, a.seq.rows);
-        if (live > row0) turn_rows<BF, V, WT>(q, a.rot, row0, min(live - row0, a.q_rows), (float*)lds);
+        const int n = min(live, b + a.q_rows) - row0;
+        if (n > 0) turn_rows<BF, V, WT>(q, a.rot, row0, n, (float*)lds);
         return;
     }
     const int groups = (H + a.heads - 1) / a.heads, hg = blockIdx.x % groups;
@@ -535,7 +532,7 @@ void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
     const CacheView& c = a.c;
     bool wide = a.rot.dim % 16 == 0 && aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el);
     if (a.q) wide = wide && aligned16(a.q, a.q_stride, el) && aligned16(a.q_out, a.qo_stride, el);
-    const int threads = c.page_tokens * (c.head_dim / 16) <= 512 ? 256 : 512, pass = MAX_ITEMS * threads;
+    const int threads = write_threads(c.page_tokens, c.head_dim), pass = MAX_ITEMS * threads;
     // heads of a block: as many as fill its threads if a page gets as many tokens as an average sequence has,
     // fewer where that leaves compute units without a block
     const bool ragged = a.seq.offsets || a.seq.one;
@@ -553,8 +550,13 @@ void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
     auto go = [&](auto f, auto v) {
         constexpr bool B = decltype(f)::value;
         constexpr int V = decltype(v)::value;
-        if (threads == 256) cache_write_k<B, V, 256><<<grid, 256, lds, s>>>(a);
-        else cache_write_k<B, V, 512><<<grid, 512, lds, s>>>(a);
+        if (threads == 256) {
+            cache_write_k<B, V, 256><<<grid, 256, lds, s>>>(a);
+        } else {   // 64 KB beside the kernel's own
+            static const bool ok = allow_lds((const void*)cache_write_k<B, V, 512>, 64 << 10);
+            (void)ok;
+            cache_write_k<B, V, 512><<<grid, 512, lds, s>>>(a);
+        }
     };
     using W8 = std::integral_constant<int, 8>;
     using W1 = std::integral_constant<int, 1>;

@@ -129,6 +129,22 @@ __host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int
     return t;
 }
 
+// ---- launches of rotary positions and of a write --------------------------------------------------
+constexpr int ROT_ROWS = 16;   // rows a block turns at most
+// Rows a block turns: about four items of 2 `vec` channels a thread.
+inline int rows_a_block(int heads, int dh, int vec) {
+    return std::max(1, std::min(ROT_ROWS, 1024 / std::max(1, heads * (dh / (2 * vec)))));
+}
+// A block of a write has 512 threads where a page and head have more than 512 items of 16 channels (more than
+// 64 tokens of 128 channels), else 256.
+inline int write_threads(int pt, int dh) { return pt * (dh / 16) <= 512 ? 256 : 512; }
+// Threads that a write launches at most: a block per page, head and keys or values, and those of the queries.
+inline long long cache_write_threads(int pt, int dh, int kv_heads, int n_seqs, int rows, bool offsets, int q_heads) {
+    const int per = q_heads ? rows_a_block(q_heads, dh, 1) : 1;
+    return (page_slots(offsets, n_seqs, rows, page_shift(pt)) * 2 * kv_heads + (q_heads ? ((long long)rows + per - 1) / per : 0)) *
+           write_threads(pt, dh);
+}
+
 // ---- how an attention call is cut ----------------------------------------------------------------
 constexpr int TS = 4, LS = 7;      // small tiles of 16 packed rows, large ones of 128
 constexpr int FEW = 64;            // packed rows of a sequence up to which small tiles take it

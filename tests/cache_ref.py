@@ -33,12 +33,11 @@ def turn(x, pos, sections, layout="halves", per_axis=False, base=1e4):
     return y, size
 
 
-# fp32 arithmetic of one turned channel, relative to |x| + |y|: the reduced angle is rounded twice (2^-24 of at
-# most pi/4 each: 1.6), sine and cosine are polynomials off by 0.43 (2.5e-8) and rounded at most
-# three times with weight on the result (3), a product and a fused product-sum round twice (2): 7.03 halves of
-# a step of 2^-23; angles of 2^31 units are off by 2^31 * 2^-64 turns (0.0001) and the fp64 reference's
-# own by 2^-53 of the angle (2^30 radians: 2^-23 = 2; at 2^16 positions 2^-13 of that)
-TURN = 8 * 2.0 ** -24
+# One turned channel, relative to |x| + |y|, in halves of a step of fp32: sine and cosine are fp64 (off by
+# 1.3e-10, 0.002) rounded to fp32 (1), two products (1, the second perhaps fused) and their sum (1): 3, and
+# 2^-23 of that for errors of errors; angles of 2^31 units are off by 2^31 * 2^-64 turns (0.02).  The fp64
+# reference's own are off by 2^-53 of the angle, which turn_tolerance adds.
+TURN = 3.03 * 2.0 ** -24
 
 
 def turn_tolerance(y, size, dtype, far=0):

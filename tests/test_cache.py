@@ -81,6 +81,15 @@ def test_rotary_refuses(kw):
     assert call_rotary(**kw) == dj.DV_EINVAL and dj.dv_last_error()
 
 
+def test_launches_past_2_to_32_threads_are_refused():
+    tiny = dj.Rotary((1, 0, 0))
+    assert call_rotary(plan=tiny.address, heads=1, head_dim=2, x_stride=2, out_stride=2,
+                       rows=(1 << 27) + 1) == dj.DV_EINVAL
+    # a page of 128 tokens of 128 channels takes blocks of 512 threads
+    big = dict(c=dict(page_tokens=128, head_dim=128), wide=1 << 14, n_seqs=600000, rows=600000, offsets=None)
+    assert refused("dv_cache_write", WRITE, big) == dj.DV_EINVAL and "600000" in dj.dv_last_error()
+
+
 def test_rotary_of_no_rows():
     assert call_rotary(rows=0) == dj.DV_OK
 
@@ -146,7 +155,7 @@ ATTEND = dict(cache=0, n_seqs=4, table=FAKE, table_pages=8, offsets=FAKE, at=FAK
     dict(q=None), dict(out=None), dict(q_stride=1023), dict(out_stride=1020), dict(out_stride=1026),
     dict(out=FAKE + 4), dict(q_heads=0), dict(q_heads=12), dict(max_rows=-1), dict(scale=0.0),
     dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(rows=1 << 28, wide=1024),
-    dict(dtype=dj.DV_F32, out=FAKE + 8)])
+    dict(dtype=dj.DV_F32, out=FAKE + 8), dict(out_stride=2048)])
 def test_attention_refuses(kw):
     assert refused("dv_cache_attention", ATTEND, kw) == dj.DV_EINVAL and dj.dv_last_error()
 
@@ -248,6 +257,17 @@ def test_places_without_offsets_and_table(lib):
     out = np.zeros((4, 5), np.int32)
     assert lib.t_page_parts(None, 2, 8, None, 4, 4, sp, 16, out.ctypes.data_as(ctypes.c_void_p)) == 4
     assert out.tolist() == [[0, 0, 0, 0, 1], [1, 3, 1, 1, 1], [2, 5, 2, 15, 1], [3, -1, 3, 0, 1]]
+
+
+def test_rows_before_the_first_offset_have_no_place(lib):
+    (o, op), (s, sp) = ints([5, 40, 40, 57]), ints([3, 0, 20])
+    out = np.zeros((64, 5), np.int32)
+    slots = lib.t_page_parts(None, 8, 24, op, 3, 60, sp, 16, out.ctypes.data_as(ctypes.c_void_p))
+    assert sorted(r0 + i for _, _, r0, _, k in out[:slots] for i in range(k)) == list(range(5, 57))
+    tiles = np.zeros((64, 6), np.int32)
+    slots = lib.t_tiles(8, op, 3, 60, sp, 16, 3, 4, 1, tiles.ctypes.data_as(ctypes.c_void_p))
+    rows = sorted((q, first + i) for q, _, first, n, _, _ in tiles[:slots] if q >= 0 for i in range(n))
+    assert rows == [(0, i) for i in range(35 * 3)] + [(2, i) for i in range(17 * 3)]
 
 
 def test_offsets_past_the_rows_are_cut(lib):

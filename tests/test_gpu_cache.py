@@ -298,6 +298,109 @@ def test_write_turns_keys_and_queries():
                 assert all(z[h] in (near[0][h], near[1][h], near[2][h]) for h in range(heads))
 
 
+@pytest.mark.parametrize("first", [0, 1])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_write_turns_whole_heads_on_long_pages(dtype, first):
+    """All of 128 channels turned on pages of 128 tokens (the most angles a block holds), with rows that
+    start on 16 bytes and rows that do not."""
+    rng = np.random.default_rng(19)
+    heads, dh, pt, rows, sec = 2, 128, 128, 200, (24, 20, 20)
+    p = Pair(2, heads, dh, pt)
+    flat, flat64 = normal(rng, first + 2 * rows * heads * dh, dtype)
+    k, v = flat[first:].view(2, rows, heads, dh)
+    k64, v64 = flat64[first:].reshape(2, rows, heads, dh)
+    q, q64 = normal(rng, (rows, 3, dh), dtype)
+    pos = rng.integers(0, 5000, (rows, 3))
+    q_out = p.c.write(k, v, ints([0]), ints([0, rows]), None, dj.Rotary(sec), ints(pos), q)
+    want, size = ref.turn(q64, pos, sec)
+    close(q_out, want, ref.turn_tolerance(want, size, dtype, 5000), "q")
+    want, size = ref.turn(k64, pos, sec)
+    err = ref.turn_tolerance(want, size, "f32", 5000)
+    got, z = p.decoded(), values(p.c.k_scale)
+    for i in range(rows):
+        x, zi = want[i], z[i // pt][:, None]
+        close(got[0][i // pt, :, i % pt], x, err[i] + np.maximum(2.0 ** -4 * (np.abs(x) + err[i]), 2.0 ** -10 * zi), "k")
+    p.m.write([[0, 1]], [0, rows], [0], k64, v64)
+    assert np.array_equal(values(p.c.v_scale), p.m.scale[1])
+    assert np.array_equal(got[1][0], p.m.x[1][0]) and np.array_equal(got[1][1, :, :rows - pt], p.m.x[1][1, :, :rows - pt])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_start_on_odd_elements(dtype):
+    """Rows off 16 bytes, an odd number of elements apart, write the same codes, scales and queries, read the
+    same values and attend alike."""
+    torch = require_gpu()
+    heads, dh, pt, rows = 3, 80, 32, 70
+    rng = np.random.default_rng(20)
+    whole = [normal(rng, (rows, h, dh), dtype)[0] for h in (heads, heads, 2 * heads)]
+
+    def odd(x):
+        flat = torch.zeros(1 + rows * (x[0].numel() + 1), dtype=x.dtype, device="cuda")
+        y = flat.as_strided(x.shape, (x[0].numel() + 1, dh, 1), 1)
+        y.copy_(x)
+        return y
+
+    offs, table, rot = ints([0, 30, 70]), ints([[4, 1], [0, 3]]), dj.Rotary((8, 8, 8))
+    pos, starts, lengths = ints(rng.integers(0, 5000, (rows, 3))), ints([0, 0]), ints([30, 40])
+    got = []
+    for move in (lambda x: x, odd):
+        p = Pair(5, heads, dh, pt)
+        k, v, q = [move(x) for x in whole]
+        q_out = move(torch.zeros_like(whole[2]))
+        p.c.write(k, v, starts, offs, table, rot, pos, q, q_out)
+        rows_out = [move(torch.zeros_like(x)) for x in whole[:2]]
+        p.c.read(starts, offs, table, out=rows_out)
+        got.append([p.bytes(), p.c.k_scale, p.c.v_scale, q_out, *rows_out,
+                    p.c.attention(q_out, lengths, offs, table)])
+    for a, b in zip(got[0][0], got[1][0]):
+        assert np.array_equal(a, b)
+    for a, b in zip(got[0][1:], got[1][1:]):
+        assert np.array_equal(values(a), values(b), equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_before_the_first_sequence_are_left_alone(dtype):
+    torch = require_gpu()
+    heads, dh, pt, lead, n = 2, 64, 16, 5, 20
+    rng = np.random.default_rng(21)
+    rows = lead + n + 2
+    k, v = [normal(rng, (rows, heads, dh), dtype)[0] for _ in range(2)]
+    q, _ = normal(rng, (rows, 2 * heads, dh), dtype)
+    rot, pos = dj.Rotary((8, 12, 12)), ints(rng.integers(0, 500, (rows, 3)))
+    starts, lengths = ints([0, 0]), ints([13, 7])
+    got = []
+    for a, b, offs in ((0, rows, [lead, lead + 13, lead + n]), (lead, lead + n, [0, 13, n])):
+        p = Pair(4, heads, dh, pt)
+        q_out = torch.full_like(q, 3.0)
+        p.c.write(k[a:b], v[a:b], starts, ints(offs), None, rot, pos[a:b], q[a:b], q_out[a:b])
+        out = [torch.full_like(x, 5.0) for x in (k, v, q)]
+        p.c.read(starts, ints(offs), out=(out[0][a:b], out[1][a:b]))
+        p.c.attention(q_out[a:b], lengths, ints(offs), out=out[2][a:b])
+        for x, fill in ((q_out, 3.0), (out[0], 5.0), (out[1], 5.0), (out[2], 5.0)):
+            assert (x[:lead] == fill).all() and (x[lead + n:] == fill).all()
+        got.append([p.c.k, p.c.v, q_out, *out])
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(*got))
+
+
+def test_the_smallest_scale():
+    """All codes at 2^-126 and 2^-120: fp32 holds code times scale exactly, bf16 where it is no smaller than
+    2^-126; below that it may be off by its step there, 2^-133."""
+    torch = require_gpu()
+    c = dj.TokenCache(2, 1, 128, 16)
+    for t in (c.k, c.v):
+        t.view(torch.uint8).copy_(torch.from_numpy(np.resize(np.arange(256), t.shape).astype(np.uint8)))
+    for s in (c.k_scale, c.v_scale):
+        s.copy_(torch.tensor([[2.0 ** -126], [2.0 ** -120]]))
+    lut = ref.codes_table()
+    want = [lut[t.view(torch.uint8).cpu().numpy()] * values(s)[:, :, None, None]
+            for t, s in ((c.k, c.k_scale), (c.v, c.v_scale))]
+    want[1] = want[1].transpose(0, 1, 3, 2)
+    for dtype, tol in (("f32", 0.0), ("bf16", 2.0 ** -133)):
+        for w, got in enumerate(c.read(ints([0, 0]), ints([0, 16, 32]), rows=32, dtype=types(torch)[dtype])):
+            x = want[w].transpose(0, 2, 1, 3).reshape(32, 1, 128)
+            close(got, x, np.where(np.abs(x) < 2.0 ** -126, tol, 0.0), dtype)
+
+
 def test_write_keeps_nan_and_ignores_it_for_the_scale():
     torch = require_gpu()
     heads, dh, pt = 2, 32, 16
@@ -717,6 +820,41 @@ def test_on_a_stream_of_the_callers():
     side.synchronize()
     assert torch.equal(got_q, want_q) and torch.equal(got, want) and torch.equal(got_x, want_x)
     assert all(torch.equal(a, b) for a, b in zip(got_rows, want_rows))
+
+
+@pytest.mark.parametrize("name", ["prompt-mixed", "long", "group-20"])
+def test_attention_in_place(name):
+    """out = q, with one split and several, in both kernels."""
+    torch = require_gpu()
+    for heads, group, dh, pt, counts, lengths, _ in (ATTENTION[name], LARGE["mixed-128"]):
+        rng = np.random.default_rng(22)
+        p, table = filled(rng, heads, dh, pt, lengths)
+        q, _ = normal(rng, (sum(counts), heads * group, dh), "bf16")
+        offs = ints(np.concatenate([[0], np.cumsum(counts)]))
+        want = p.c.attention(q, ints(lengths), offs, ints(table))
+        assert p.c.attention(q, ints(lengths), offs, ints(table), out=q) is q
+        assert torch.equal(q, want)
+
+
+def test_two_streams_at_once():
+    """Calls whose splits meet in workspaces of their own, on two streams in turn."""
+    torch = require_gpu()
+    rng = np.random.default_rng(23)
+    p, table = filled(rng, 2, 128, 64, [9000, 100, 8000])
+    t, lengths, offs = ints(table), ints([9000, 100, 8000]), ints([0, 1, 2, 3])
+    qs = [normal(rng, (3, 8, 128), "bf16")[0] for _ in range(2)]
+    want = [p.c.attention(q, lengths, offs, t, max_rows=1) for q in qs]
+    need = p.c.attention_workspace(3, 3, 8, table.shape[1], True, 1)
+    assert need > 0
+    ws = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in qs]
+    out = [torch.empty_like(q) for q in qs]
+    side = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i, s in enumerate(side):
+            p.c.attention(qs[i], lengths, offs, t, max_rows=1, workspace=ws[i], out=out[i], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
 
 
 def test_a_workspace_of_the_callers():
