@@ -390,7 +390,8 @@ __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
         if (values) {
             __syncthreads();   // the rescaled words and the tile are complete
             // four channels of 16 tokens at once, neighbouring lanes on a channel's neighbouring tokens; where
-            // the new tokens fill fewer, byte by byte
+            // the new tokens fill fewer, by fours and byte by byte (300 sequences of 30 tokens of 16 heads of 64: 57
+            // us with bytes alone, 38 so)
             const int first = keep >> 4, chunks = ((keep + p.n + 15) >> 4) - first, quads = dh / 4;
             for (int i = tid; i < hn * quads * chunks; i += WT) {
                 const int row = i / chunks, j = first + i - row * chunks;           // row: head and four channels
@@ -410,10 +411,22 @@ __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) *(u32x4*)(to + (size_t)e * pt) = w[e];
-                } else {
-                    for (int t = max(0, -t0); t < min(16, p.n - t0); ++t)
+                    continue;
+                }
+                for (int t = max(0, -t0); t < min(16, p.n - t0);) {
+                    if ((t & 3) == 0 && t0 + t + 4 <= p.n) {
+                        uint32_t q[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) q[e] = *(const uint32_t*)(from + (t + e) * ld);
+                        transpose4(q);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) *(uint32_t*)(to + e * pt + t) = q[e];
+                        t += 4;
+                    } else {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) to[e * pt + t] = from[t * ld + e];
+                        ++t;
+                    }
                 }
             }
         }
@@ -533,12 +546,12 @@ void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
     bool wide = a.rot.dim % 16 == 0 && aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el);
     if (a.q) wide = wide && aligned16(a.q, a.q_stride, el) && aligned16(a.q_out, a.qo_stride, el);
     const int threads = write_threads(c.page_tokens, c.head_dim), pass = MAX_ITEMS * threads;
-    // heads of a block: as many as fill its threads if a page gets as many tokens as an average sequence has,
-    // fewer where that leaves compute units without a block
+    // heads of a block: as many as leave two blocks a compute unit, which share the angles of their tokens and the
+    // search for their page (us, with the heads that fill the block's threads once / as many as that: 9232 tokens of
+    // 16 heads of 64 28.5 / 22.7, 100,000 of 8 heads of 128 607 / 425; 9232 with one block a unit 30)
     const bool ragged = a.seq.offsets || a.seq.one;
     const long long slots = page_slots(ragged, a.seq.n_seqs, a.seq.rows, page_shift(c.page_tokens));
-    const int tokens = ragged ? std::max(1, std::min(c.page_tokens, a.seq.rows / a.seq.n_seqs)) : 1;
-    a.heads = std::max(1, std::min({MAX_HEADS, c.kv_heads, pass / (tokens * (c.head_dim / 16))}));
+    a.heads = std::min(MAX_HEADS, c.kv_heads);
     while (a.heads > 1 && slots * 2 * ((c.kv_heads + a.heads - 1) / a.heads) < 512) a.heads = (a.heads + 1) / 2;
     a.kv_blocks = (int)(slots * 2 * ((c.kv_heads + a.heads - 1) / a.heads));
     a.q_rows = rows_a_block(std::max(1, a.q_heads), c.head_dim, wide ? 8 : 1);

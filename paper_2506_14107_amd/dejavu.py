@@ -670,7 +670,8 @@ class TokenCache:
                 workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
                 ws = workspace.data_ptr()
         else:
-            if workspace.get_device() != index or workspace.dtype is not torch.uint8:
+            if (workspace.get_device() != index or workspace.dtype is not torch.uint8
+                    or not workspace.is_contiguous()):
                 _misfit("workspace", workspace)
             ws, size = workspace.data_ptr(), workspace.numel()
         dv_cache_attention(self.address, n, t, tp, o, at, dtype, q.data_ptr(), qs, rows, heads,
