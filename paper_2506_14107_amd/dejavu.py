@@ -460,6 +460,13 @@ def _rows(name, t, shape, dtype, index):
     return _stride(name, t)
 
 
+def _like(t, stride, wide):
+    """New rows like those of t, side by side."""
+    if stride == wide:
+        return torch.empty_like(t)   # the cheaper call
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _ints(name, t, index, shape):
     if (t.dtype is not torch.int32 or t.get_device() != index or t.shape != shape
             or not t.is_contiguous()):
@@ -523,8 +530,8 @@ def rotary(x, positions, rot, out=None, stream=None):
     dtype = _dtype(x)
     xs = _stride("x", x)
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
         os = h * d
+        out = _like(x, xs, os)
     else:
         os = xs if out is x else _rows("out", out, shape, x.dtype, index)
     dv_rotary(rot.address, dtype, x.data_ptr(), xs, n, h, d,
@@ -604,7 +611,7 @@ class TokenCache:
             shape = (rows, heads, self.head_dim)
             qs = _rows("q", q, shape, dt, index)
             if q_out is None:
-                q_out = torch.empty(shape, dtype=dt, device=q.device)
+                q_out = _like(q, qs, heads * self.head_dim)
             qos = _rows("q_out", q_out, shape, dt, index)
             qp, qop = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
@@ -653,8 +660,8 @@ class TokenCache:
         qs = _rows("q", q, shape, q.dtype, index)
         dtype = _dtype(q)
         if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=q.device)
             os = heads * d
+            out = _like(q, qs, os)
         else:
             os = _rows("out", out, shape, q.dtype, index)
         ws = size = 0
