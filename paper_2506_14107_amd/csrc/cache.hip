@@ -227,7 +227,9 @@ __device__ __forceinline__ float inverse(float s) {
 }
 // The part of a page that slot u stands for.
 __device__ __forceinline__ PagePart page_part(const SeqArgs& q, int pt, int pages, int u) {
-    return part_at(q, pt, pages, q.offsets ? find_seq(q, 1, page_shift(pt), 2, u) : seq_of(q, q.one ? 0 : u), u);
+    const int shift = page_shift(pt);
+    const Seq s = q.offsets ? find_seq(q, [&](const Seq& x) { return part_count(x, shift); }, u) : seq_of(q, q.one ? 0 : u);
+    return part_at(q, pt, pages, s, u);
 }
 
 // ---- write -----------------------------------------------------------------------------------------

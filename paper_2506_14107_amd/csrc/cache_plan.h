@@ -41,30 +41,37 @@ __host__ __device__ inline int page_from(const SeqArgs& q, int pages, int entry,
 // sequence s has row s (or the call's one sequence has them all).
 struct Seq {
     int s;          // -1: none
-    int off;        // its first row as the call says
     int row0, n;    // its rows
     int at;         // q.at[s]
+    int slot0;      // its first slot (with offsets)
 };
 __host__ __device__ inline Seq seq_from(const SeqArgs& q, int s, int off, int next, int at) {
     const int a = off < 0 ? 0 : off, b = next < q.rows ? next : q.rows;
-    return {s, off, a, b > a ? b - a : 0, at};
+    return {s, a, b > a ? b - a : 0, at, 0};
 }
+// ... without offsets
 __host__ __device__ inline Seq seq_of(const SeqArgs& q, int s) {
     if (s < 0 || s >= q.n_seqs) return {-1, 0, 0, 0, 0};
-    if (q.one) return {s, 0, 0, q.rows, q.at[s]};
-    if (!q.offsets) return {s, s, s, s < q.rows ? 1 : 0, q.at[s]};
-    return seq_from(q, s, q.offsets[s], q.offsets[s + 1], q.at[s]);
+    if (q.one) return {s, 0, q.rows, q.at[s], 0};
+    return {s, s, s < q.rows ? 1 : 0, q.at[s], 0};
 }
 
-// Kernels deal blocks to slots: sequence s owns the slots from slot_base(s), and a slot finds its
-// sequence by comparing bases, so that a ragged batch needs no list made on the host.
-//   pages that n rows touch, from any start: at most n / pt + 2 (floor), so base = offset / pt + 2 s
-//   tiles of R packed rows (row x query heads of a key head, `mul`): at most n mul / R + 1 (floor)
-__host__ __device__ inline long long slot_base(int offset, int mul, int shift, int add, int s) {
-    return ((long long)offset * mul >> shift) + (long long)add * s;
+// Kernels deal blocks to slots.  With offsets a sequence owns as many as it has pages or tiles, one sequence after the
+// other; a block finds the sequence of its slot by summing those numbers (find_seq), so that a ragged batch needs
+// no list made on the host.  The host, which does not know the offsets, launches as many slots as there can be:
+//   pages that n rows touch, from any start: at most n / pt + 2 (floor)
+//   tiles of R packed rows (rows x query heads of a key head): at most n group / R + 1 (floor)
+// The slots that nobody owns are the last ones.  (Left between the sequences instead, one in two, they met the
+// rotation of blocks over the chip's engines and left half of those idle: one query of 16 heads a key head over 64
+// sequences of up to 12,000 keys 224 us, so 177.)
+__host__ __device__ inline int part_count(const Seq& s, int shift) {
+    return s.n == 0 || s.at < 0 ? 0 : (int)(((long long)s.at + s.n - 1) >> shift) - (s.at >> shift) + 1;
+}
+__host__ __device__ inline int tile_count(const Seq& s, int group, int shift) {
+    return (int)(((long long)s.n * group + (1 << shift) - 1) >> shift);
 }
 __host__ __device__ inline long long page_slots(bool offsets, int n_seqs, int rows, int shift) {
-    return offsets ? slot_base(rows, 1, shift, 2, n_seqs) : n_seqs;
+    return offsets ? ((long long)rows >> shift) + 2ll * n_seqs : n_seqs;
 }
 
 // One page of one sequence that a call's rows touch.
@@ -78,7 +85,8 @@ __host__ __device__ inline PagePart part_at(const SeqArgs& q, int pt, int pages,
     PagePart p = {-1, 0, 0, 0};
     const int shift = page_shift(pt), s = sp.s, start = sp.at;
     if (s < 0 || sp.n == 0 || start < 0) return p;
-    const long long j = q.one ? u : q.offsets ? u - slot_base(sp.off, 1, shift, 2, s) : 0;
+    const long long j = q.one ? u : q.offsets ? u - sp.slot0 : 0;
+    if (j < 0) return p;
     const long long page = ((long long)start >> shift) + j;     // of the sequence
     const long long end = (long long)start + sp.n, next = (page + 1) << shift;
     const long long a = start > page << shift ? start : page << shift, b = end < next ? end : next;
@@ -101,7 +109,7 @@ struct Tile {
     int end;     // keys that the tile's last row sees
 };
 __host__ __device__ inline long long tile_slots(bool offsets, int n_seqs, int rows, int group, int shift) {
-    return offsets ? slot_base(rows, group, shift, 1, n_seqs)
+    return offsets ? ((long long)rows * group >> shift) + n_seqs
                    : (long long)n_seqs * ((group + (1 << shift) - 1) >> shift);
 }
 // ... slot u, of sequence s (without offsets: of sequence u / tiles of a row)
@@ -110,10 +118,9 @@ __host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int
     Tile t = {-1, 0, 0, 0, 0, 0, 0};
     const int s = sp.s;
     if (s < 0) return t;
-    const long long j = q.offsets ? u - slot_base(sp.off, group, shift, 1, s)
-                                  : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
+    const long long j = q.offsets ? u - sp.slot0 : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
     const long long first = j << shift, left = (long long)sp.n * group - first;
-    if (left <= 0) return t;
+    if (j < 0 || left <= 0) return t;
     t.seq = s;
     t.row0 = sp.row0;
     t.n = sp.n;
@@ -201,21 +208,45 @@ inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets
 }
 
 #ifdef __HIPCC__
-// The sequence whose slots hold slot u (every lane of a wavefront calls, with the same u).  Its offsets and
-// place are loaded along with the search: a chain of loads is what small calls wait for.
-__device__ __forceinline__ Seq find_seq(const SeqArgs& q, int mul, int shift, int add, long long u) {
-    Seq r = {-1, 0, 0, 0, 0};
-    for (int b = 0; b < q.n_seqs; b += 64) {
-        const int s = b + (threadIdx.x & 63), c = s < q.n_seqs ? s : q.n_seqs - 1;
-        const int off = q.offsets[c], next = q.offsets[c + 1], at = q.at[c];
-        const unsigned long long before = __ballot(s < q.n_seqs && slot_base(off, mul, shift, add, s) <= u);
-        if (!before) break;
-        const int k = __popcll(before) - 1;
-        r = seq_from(q, b + k, __builtin_amdgcn_readlane(off, k), __builtin_amdgcn_readlane(next, k),
-                     __builtin_amdgcn_readlane(at, k));
-        if (k < 63) break;
+// x of the lanes up to this one, summed (each step adds what lies 1, 2, 4, 8 lanes of 16 below, then the row below's last,
+// then the lower half's)
+__device__ __forceinline__ int sum_up(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+// The sequence that owns slot u (every lane of a wavefront calls, with the same u); count: the slots of one.  N times 64
+// sequences are looked at together: a chain of loads is what small calls wait for.
+template <int N, class Count>
+__device__ __forceinline__ Seq find_among(const SeqArgs& q, const Count& count, int u) {
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int b = 0; b < q.n_seqs; b += 64 * N) {
+        Seq sp[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int s = b + i * 64 + lane, c = s < q.n_seqs ? s : q.n_seqs - 1;
+            sp[i] = seq_from(q, s, q.offsets[c], q.offsets[c + 1], q.at[c]);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int n = sp[i].s < q.n_seqs ? count(sp[i]) : 0, upto = base + sum_up(n);
+            const int k = __popcll(__ballot(upto <= u));
+            if (k < 64)
+                return {b + i * 64 + k, __builtin_amdgcn_readlane(sp[i].row0, k), __builtin_amdgcn_readlane(sp[i].n, k),
+                        __builtin_amdgcn_readlane(sp[i].at, k), __builtin_amdgcn_readlane(upto - n, k)};
+            base = __builtin_amdgcn_readlane(upto, 63);
+        }
     }
-    return r;
+    return {-1, 0, 0, 0, 0};
+}
+template <class Count>
+__device__ __forceinline__ Seq find_seq(const SeqArgs& q, const Count& count, int u) {
+    return q.n_seqs <= 64 ? find_among<1>(q, count, u) : find_among<4>(q, count, u);
 }
 #endif
 

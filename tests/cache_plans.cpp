@@ -4,20 +4,31 @@
 
 using namespace dv;
 
+// The sequence that owns slot u: the first whose slots reach past it (count: the slots of one).
+template <class Count>
+static Seq owner(const SeqArgs& q, const Count& count, int u) {
+    int base = 0;
+    for (int s = 0; s < q.n_seqs; ++s) {
+        Seq sp = seq_from(q, s, q.offsets[s], q.offsets[s + 1], q.at[s]);
+        sp.slot0 = base;
+        base += count(sp);
+        if (u < base) return sp;
+    }
+    return {-1, 0, 0, 0, 0};
+}
+
 extern "C" {
 
 // For every slot of a write or read: sequence, page, first row, first place, places (5 ints a slot).
-// Returns the slots; the sequence of a slot is the last whose base is not above it.
+// Returns the slots.
 int t_page_parts(const int* table, int table_pages, int pages, const int* offsets, int n_seqs, int rows,
                  const int* starts, int pt, int* out) {
     const SeqArgs q = {n_seqs, table_pages, rows, table, offsets, starts};
     const int slots = (int)page_slots(offsets != nullptr, n_seqs, rows, page_shift(pt));
     for (int u = 0; u < slots; ++u) {
-        int s = offsets ? -1 : u;
-        if (offsets)
-            while (s + 1 < n_seqs && slot_base(offsets[s + 1], 1, page_shift(pt), 2, s + 1) <= u) ++s;
-        const PagePart p = part_at(q, pt, pages, seq_of(q, s), u);
-        const int v[] = {s, p.page, p.row0, p.slot0, p.n};
+        const Seq s = offsets ? owner(q, [&](const Seq& x) { return part_count(x, page_shift(pt)); }, u) : seq_of(q, u);
+        const PagePart p = part_at(q, pt, pages, s, u);
+        const int v[] = {s.s, p.page, p.row0, p.slot0, p.n};
         for (int i = 0; i < 5; ++i) out[5 * u + i] = v[i];
     }
     return slots;
@@ -30,10 +41,9 @@ int t_tiles(int table_pages, const int* offsets, int n_seqs, int rows, const int
     const SeqArgs q = {n_seqs, table_pages, rows, nullptr, offsets, lengths};
     const int slots = (int)tile_slots(offsets != nullptr, n_seqs, rows, group, shift);
     for (int u = 0; u < slots; ++u) {
-        int s = offsets ? -1 : u / ((group + (1 << shift) - 1) >> shift);
-        if (offsets)
-            while (s + 1 < n_seqs && slot_base(offsets[s + 1], group, shift, 1, s + 1) <= u) ++s;
-        const Tile t = tile_of(q, pt, group, shift, causal != 0, seq_of(q, s), u);
+        const Seq s = offsets ? owner(q, [&](const Seq& x) { return tile_count(x, group, shift); }, u)
+                              : seq_of(q, u / ((group + (1 << shift) - 1) >> shift));
+        const Tile t = tile_of(q, pt, group, shift, causal != 0, s, u);
         const int v[] = {t.seq, t.row0, t.first, t.rows, t.len, t.end};
         for (int i = 0; i < 6; ++i) out[6 * u + i] = v[i];
     }
