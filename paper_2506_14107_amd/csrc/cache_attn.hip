@@ -133,7 +133,7 @@ template <int SHIFT>
 __device__ __forceinline__ Tile tile_at(const CacheAttnArgs& a, long long u) {
     const int G = a.q_heads / a.c.kv_heads;
     // a mixed batch: short sequences go to the kernel of single tokens, the others to that of tiles
-    auto other = [&](const Seq& s) { return a.route == ATTN_BOTH && ((long long)s.n * G > FEW) != (SHIFT == LS); };
+    auto other = [&](const Seq& s) { return a.route == ATTN_BOTH && ((long long)s.n * G > few_rows(a.c.head_dim)) != (SHIFT == LS); };
     const Seq s = a.seq.offsets ? find_seq(a.seq, [&](const Seq& x) { return other(x) ? 0 : tile_count(x, G, SHIFT); }, (int)u)
                                 : seq_of(a.seq, (int)(u / ((G + (1 << SHIFT) - 1) >> SHIFT)));
     Tile t = tile_of(a.seq, a.c.page_tokens, G, SHIFT, a.causal != 0, s, u);

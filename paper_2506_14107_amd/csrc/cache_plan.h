@@ -154,7 +154,10 @@ inline long long cache_write_threads(int pt, int dh, int kv_heads, int n_seqs, i
 
 // ---- how an attention call is cut ----------------------------------------------------------------
 constexpr int TS = 4, LS = 7;      // small tiles of 16 packed rows, large ones of 128
-constexpr int FEW = 64;            // packed rows of a sequence up to which small tiles take it
+// Blocks of small tiles that a compute unit holds at least (their registers grow with the head), and packed rows of a
+// sequence up to which they take it where both kernels run.
+__host__ __device__ inline int small_resident(int head_dim) { return head_dim > 85 ? 2 : head_dim > 64 ? 3 : 4; }
+__host__ __device__ inline int few_rows(int head_dim) { return small_resident(head_dim) << TS; }
 constexpr int MAX_SPLITS = 512;
 
 // partial results: per tile of R rows, head and split R rows of dh fp32, R maxima, R sums
@@ -168,16 +171,17 @@ inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets
     const long long keys = (long long)table_pages * page_tokens;   // at most 2^30
     const long long most_rows = std::min<long long>(rows, !offsets ? 1 : max_rows > 0 ? max_rows : rows);
     // Large tiles (bf16) decode a key once for 128 rows and give the matrix units long products; small ones read
-    // keys at the memory's rate and have four times the blocks.  Large ones take sequences of more than FEW
-    // packed rows of batches whose small tiles would not all be resident at once.  us, small / large, 32 sequences
-    // of 2048 keys (8 heads of 128, 4 queries each): 64 packed rows 52 / 69, 96 84 / 72, 512 360 / 165; 64 of
-    // 8192: 16 rows 269 / 230, 64 429 / 379, 512 2750 / 1245; 4 of 700 (16 heads of 80): 128 rows 12 / 30; one of
-    // 4096: 512 rows 28 / 34.
+    // keys at the memory's rate and have eight times the blocks.  Large ones take sequences of more than few_rows
+    // packed rows of batches whose small tiles would be more than twice as many as are resident at once.  us, small /
+    // large: 8 heads of 128 with 4 queries each, 32 sequences of 2048 keys: 32 packed rows 29 / 50, 64 50 / 51, 96 73 /
+    // 54, 512 364 / 159; 64 of 8192: 16 rows 214 / 208, 32 261 / 210, 64 426 / 270, 512 2763 / 1177; 4 of 4096: 128
+    // rows 33 / 36, 256 58 / 53, 512 106 / 75; one of 4096: 512 rows 27 / 33; 16 heads of 64, 32 of 2048: 64 rows 41 /
+    // 55, 128 80 / 60; 16 of 80, 4 of 700: 128 rows 10 / 27.
     // Where some sequences may have fewer, both kernels run, each on its own: they need not if there is one
     // sequence, or if all have as many rows as the longest.
     const long long small_blocks = tile_slots(offsets, n_seqs, rows, G, TS) * kv_heads;
     const bool alike = n_seqs == 1 || (max_rows > 0 && (long long)n_seqs * max_rows == rows);
-    p.route = !bf || most_rows * G <= FEW || small_blocks <= 2 * unit ? ATTN_FEW : alike ? ATTN_MANY : ATTN_BOTH;
+    p.route = !bf || most_rows * G <= few_rows(head_dim) || small_blocks <= 2 * small_resident(head_dim) * unit ? ATTN_FEW : alike ? ATTN_MANY : ATTN_BOTH;
 
     // Splits of equal length.  One sequence: as many as are resident at once, two blocks a compute unit (one
     // query over 200,001 keys of 8 heads of 128, us with 32 / 64 / 98 / 126 splits: 85 / 77 / 87 / 82).
@@ -185,9 +189,11 @@ inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets
     // spread over the chip (64 sequences of 1 to 12,000 keys, us with splits of 1024 / 2048 / 3136 /
     // 6272 / 12,032 keys: 171 / 161 / 167 / 180 / 182) unless there are many tiles anyway -- but not into more
     // than 64 blocks a compute unit, most of them empty where tables are far longer than sequences (the same
-    // 64 with tables of 131,072 / 524,288 places: 169 / 179 with that bound, 212 / 411 without).  512 keys and
-    // fewer are not split: the join costs more.
-    auto cut = [&](CacheAttnCut& c, int shift, long long cap) {
+    // 64 with tables of 131,072 / 524,288 places: 169 / 179 with that bound, 212 / 411 without).  What takes no
+    // longer than the join's launch is not split (`whole` keys and fewer, and into no less than 512; us of one call, whole /
+    // split, one query: 1000 / 2000 keys of 128 channels 9.4 / 12.4, 14.6 / 12.4; 2000 of 64 9.0 / 12.5; a large tile of
+    // 700 keys takes 27).
+    auto cut = [&](CacheAttnCut& c, int shift, long long cap, long long whole) {
         c.slots = tile_slots(offsets, n_seqs, rows, G, shift);
         const long long units = std::max(1ll, c.slots * kv_heads);
         const long long most = std::min<long long>(MAX_SPLITS, std::max(1ll, 2 * unit / units));
@@ -195,14 +201,15 @@ inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets
         if (n_seqs > 1 && units < 16 * unit) chunk = std::min(chunk, cap);
         const long long splits = std::min<long long>(MAX_SPLITS, std::max(1ll, 64 * unit / units));
         chunk = std::max({chunk, 512ll, (keys + splits - 1) / splits});
+        if (keys <= whole) chunk = std::max(chunk, keys);
         c.chunk = (int)((chunk + 255) / 256 * 256);
         c.splits = (int)std::max(1ll, (keys + c.chunk - 1) / c.chunk);
         c.tile_rows = (int)std::min<long long>(1 << shift, std::max(1ll, most_rows * G));
         return c.splits > 1 ? (size_t)c.slots * kv_heads * c.splits * part_floats(1 << shift, head_dim) : 0;
     };
-    if (p.route != ATTN_MANY) p.few_floats = cut(p.few, TS, 2048);
+    if (p.route != ATTN_MANY) p.few_floats = cut(p.few, TS, 2048, (bf ? 1 << 17 : 1 << 16) / head_dim);
     size_t many = 0;
-    if (p.route != ATTN_FEW) many = cut(p.many, LS, keys);
+    if (p.route != ATTN_FEW) many = cut(p.many, LS, keys, 512);
     p.bytes = (p.few_floats + many) * sizeof(float);
     return p;
 }

@@ -336,6 +336,7 @@ def test_attention_routes_of_the_gpu_tests(lib):
                     assert p[0] == MANY, name
                 split |= {(w, p[i] > 1) for w, i in (("few", 2), ("many", 5)) if p[i]}
             assert plan(lib, 0, len(counts), sum(counts) + pad, 1, 0, tp, pt, heads, heads * group, dh)[0] == FEW
+    assert plan(lib, 1, 3, 240, 1, 0, 10, 16, 64, 128, 64)[0] == BOTH      # of test_attention_extremes
     assert split == {(w, s) for w in ("few", "many") for s in (False, True)}, split
 
 
