@@ -10,10 +10,11 @@
 // g = l / 16 ends up with the scores of the 16 keys 16 g .. 16 g + 15: the order in which the value
 // product contracts them, and 16 bytes of one channel's row of a page.
 // Codes become bf16 exactly (3 fraction bits, power-of-two scales) by v_cvt_scalef32_pk_bf16_fp8, which
-// applies the scale.  The softmax is one pass with a running maximum and sum in fp32; probabilities are
-// rounded to bf16 for the value product, a relative 2^-9 each, as in the encoder.  fp32 queries are three
-// bf16 terms (24 bits), and so are their probabilities: K and V being exact in bf16, three products
-// give fp32 results at the bf16 matrix rate.
+// applies the scale.  The softmax is one pass with a running maximum and sum in fp32; probabilities
+// are rounded to bf16 for the value product of large tiles, at most a relative 2^-8 each, as in the encoder; small ones,
+// whose time the memory sets, take them as two bf16 terms (16 bits, the same times: outputs of bf16 0.0016 off, which
+// is their own rounding, where one term gives 0.0019).  fp32 queries are three bf16 terms (24 bits), and so are
+// their probabilities: K and V being exact in bf16, three products give fp32 results at the bf16 matrix rate.
 // Single tokens are bound by the cache's bytes: one query over 200,001 keys of 8 heads of 128 72 us (5.7 TB/s of
 // the 6.2 that plain reads reach), one of each of 64 sequences of 1 to 12,000 keys 147 (5.2; the longest end last);
 // joining the splits adds 6 to 8.  Questions of some rows over short caches are bound by the latency of a
@@ -156,7 +157,8 @@ __device__ __forceinline__ void store4(void* out, size_t at, f32x4 x) {
 // join their results through LDS.
 template <int DH, bool BF>
 __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
-    constexpr int NT = BF ? 1 : 3;             // bf16 terms of queries and probabilities
+    constexpr int NT = BF ? 1 : 3;             // bf16 terms of queries
+    constexpr int PT = BF ? 2 : 3;             // ... of probabilities
     constexpr int KS = (DH + 31) / 32;         // 32-channel steps of S^T
     constexpr int CT = DH / 16;                // 16-channel tiles of O^T
     constexpr bool WIDE = DH % 64 == 0;        // 16-byte key loads
@@ -330,16 +332,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
             p[e >> 3][e & 7] = __builtin_amdgcn_exp2f(fmaf(sc[e], sl2, off));
             l += p[e >> 3][e & 7];
         }
-        bf16x8 pf[2][NT];
-        split8<NT>(p[0], pf[0]);
-        split8<NT>(p[1], pf[1]);
+        bf16x8 pf[2][PT];
+        split8<PT>(p[0], pf[0]);
+        split8<PT>(p[1], pf[1]);
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const bf16x8 vf = decode8(vw[c][2 * k], vw[c][2 * k + 1], vs);
 #pragma unroll
-                for (int n = NT - 1; n >= 0; --n)
+                for (int n = PT - 1; n >= 0; --n)
                     o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k][n], o[c], 0, 0, 0);
             }
         __builtin_amdgcn_sched_barrier(0);
