@@ -61,9 +61,9 @@ __host__ __device__ inline Seq seq_of(const SeqArgs& q, int s) {
 // no list made on the host.  The host, which does not know the offsets, launches as many slots as there can be:
 //   pages that n rows touch, from any start: at most n / pt + 2 (floor)
 //   tiles of R packed rows (rows x query heads of a key head): at most n group / R + 1 (floor)
-// The slots that nobody owns are the last ones.  (Left between the sequences instead, one in two, they met the
-// rotation of blocks over the chip's engines and left half of those idle: one query of 16 heads a key head over 64
-// sequences of up to 12,000 keys 224 us, so 177.)
+// The slots that nobody owns are the last ones.  (Between the sequences instead, every second one empty, one query
+// of 16 heads a key head over 64 sequences of up to 12,000 keys takes 224 us, so 177: presumably blocks are dealt to
+// the chip's engines in rotation, and the empty ones all went to the same.)
 __host__ __device__ inline int part_count(const Seq& s, int shift) {
     return s.n == 0 || s.at < 0 ? 0 : (int)(((long long)s.at + s.n - 1) >> shift) - (s.at >> shift) + 1;
 }
