@@ -68,11 +68,11 @@ __device__ __forceinline__ bf16x8 decode8(uint32_t lo, uint32_t hi, float scale)
     const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     return (bf16x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// the largest of three, a NaN aside (without the quieting of its operands that fmaxf asks for)
+// The largest of three (v_maximum3_f32, a NaN if one is: fmaxf would quiet every operand first).  Left to the
+// compiler because the operands are products of the matrix units: it keeps the 8 or 12 wait states behind those, and
+// would not for inline assembly.
 __device__ __forceinline__ float max3(float a, float b, float c) {
-    float d;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-    return d;
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 // x as T bf16 terms: the first its rounding, each next the rounding of what is left
 template <int T>
