@@ -809,7 +809,7 @@ int encode_impl(dv_handle* h, const float* frames, int n, int G, float tau, cons
 // completes, in stream order: the held ones, then its own up to its last anchor.  Each batch
 // starts at a group boundary: the frames before the first one computed are carried over (the
 // last of them, the anchor of the first computed frame, from the cache), and ends on an anchor,
-// which is cached for the next batch.
+// which is cached for the next batch or call.
 int stream_reorder_impl(dv_handle* h, const float* frames, int n, int G, int mode, float tau,
                         const uint8_t* masks, float* emb, uint8_t* om, float* tokens,
                         hipStream_t s, bool flush) {
@@ -831,10 +831,19 @@ int stream_reorder_impl(dv_handle* h, const float* frames, int n, int G, int mod
             lead = (int)(u - (u - 1) / G * G);
         }
         long long cnt = std::min<long long>(d.B - lead, last - u + 1);
-        if (u + cnt - 1 < last) cnt = (u + cnt - 1) / 4 * 4 - u + 1;   // end on an anchor
+        // An 8-bit cache would round what this call's next frames attend to: a batch that is not the call's
+        // last ends ahead of a group instead, whose first frame is computed along with it and again,
+        // identically, by the next batch (as in encode_batches).
+        int ahead = 0;
+        if (u + cnt - 1 < last && d.cache8) {
+            cnt = (u + cnt) / G * G - u;
+            ahead = 1;
+        } else if (u + cnt - 1 < last) {
+            cnt = (u + cnt - 1) / 4 * 4 - u + 1;
+        }
         if (cnt < 1) return fail(DV_EINVAL, "internal: empty stream batch");
         const long long e = u + cnt - 1;
-        const int F = lead + (int)cnt;
+        const int F = lead + (int)cnt + ahead;
         const int npend = (int)std::max<long long>(0, std::min(st, e + 1) - u);
         const float* pend = npend ? h->w.hold + (size_t)(u - done) * img : nullptr;
         const float* fr = frames ? frames + (size_t)std::max<long long>(0, u - st) * img : nullptr;
@@ -843,8 +852,8 @@ int stream_reorder_impl(dv_handle* h, const float* frames, int n, int G, int mod
             if (npend) {   // held frames' maps, then the call's own
                 HIP_TRY(hipMemcpyAsync(h->w.injs, h->w.holdm + (size_t)(u - done) * ml, npend * ml,
                                        hipMemcpyDeviceToDevice, s));
-                if (cnt > npend)
-                    HIP_TRY(hipMemcpyAsync(h->w.injs + npend * ml, masks, (cnt - npend) * ml,
+                if (cnt + ahead > npend)
+                    HIP_TRY(hipMemcpyAsync(h->w.injs + npend * ml, masks, (cnt + ahead - npend) * ml,
                                            hipMemcpyDeviceToDevice, s));
                 inj = h->w.injs;
             } else {
@@ -852,7 +861,7 @@ int stream_reorder_impl(dv_handle* h, const float* frames, int n, int G, int mod
             }
         }
         const size_t k = (size_t)(u - done);
-        const int fill = flush ? -1 : F - 1;
+        const int fill = flush || ahead ? -1 : F - 1;
         int rc = run_batch(h, h->w, fr, F, G, mode, tau, inj, emb + k * D,
                            om ? om + k * ml : nullptr,
                            tokens ? tokens + k * N * D : nullptr, s, lead, fill,
