@@ -74,6 +74,23 @@ __device__ __forceinline__ bf16x8 decode8(uint32_t lo, uint32_t hi, float scale)
 __device__ __forceinline__ float max3(float a, float b, float c) {
     return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
+// Scores are kept as products; exponents of 2 are (score - maximum) times this.  (Where the factor itself passes fp32, the
+// largest number stands for it: a difference of one unit is past any exponent long before.)
+__device__ __forceinline__ float exponent_factor(float scale) {
+    return fminf(scale * 1.4426950408889634f, 3.4028235e38f);
+}
+// An exponent is one fma, score * factor + off with off = -maximum * factor, whose rounding a row's probabilities share.
+// At 2^31 that rounding would be as large as exponents get, so rows whose |off| passes FAR have their maximum taken off
+// the scores first (take_off).  Up to FAR it is at most 2^-15, and the largest probability a 1 in bf16.
+constexpr float FAR = 1024.f;
+template <class TakeOff>
+__device__ __forceinline__ float offset_of(float m, float factor, TakeOff take_off) {
+    const float off = m == -INFINITY ? 0.f : -m * factor;      // no key seen yet: all probabilities 0
+    const bool far = fabsf(off) > FAR;
+    if (!__any(far)) return off;
+    take_off(far ? m : 0.f);
+    return far ? 0.f : off;
+}
 // x as T bf16 terms: the first its rounding, each next the rounding of what is left
 template <int T>
 __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&t)[T]) {
@@ -174,7 +191,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     if (blockIdx.y > 0 && k0 >= k1) return;    // the first split also writes rows that see no key
     const int G = a.q_heads / H;
     const int g = lane >> 4, c16 = lane & 15;
-    const float sl2 = a.scale * 1.4426950408889634f;
+    const float sl2 = exponent_factor(a.scale);
 
     // the lane's query: packed row first + c16 (rows past the tile repeat its last one)
     const int r = t.first + min(c16, t.rows - 1), qi = r / G;
@@ -325,7 +342,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
 #pragma unroll
             for (int c = 0; c < CT; ++c) o[c] *= alpha;
         }
-        const float off = m == -INFINITY ? 0.f : -m * sl2;      // no key seen yet: all probabilities 0
+        const float off = offset_of(m, sl2, [&](float top) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[e] -= top;
+        });
         float p[2][8];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -436,7 +456,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
     const int k0 = blockIdx.y * a.many.chunk, k1 = min(t.end, k0 + a.many.chunk);
     if (blockIdx.y > 0 && k0 >= k1) return;
     const int G = a.q_heads / H;
-    const float sl2 = a.scale * 1.4426950408889634f;
+    const float sl2 = exponent_factor(a.scale);
 
     const int mine = t.first + wave * 32;                    // the wavefront's first packed row
     const int r = min(mine + lr, t.first + t.rows - 1), qi = r / G;
@@ -608,7 +628,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[c][e] *= alpha;
         }
-        const float off = m == -INFINITY ? 0.f : -m * sl2;
+        const float off = offset_of(m, sl2, [&](float top) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[b][e] -= top;
+        });
         bf16x8 pf[4];
         // (sums of the rounded probabilities, two a v_dot2_f32_bf16, take as long)
         float sum[16];
@@ -702,7 +727,7 @@ __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {
     const Tile t = tile_at<SHIFT>(a, u);
     if (t.seq < 0 || t.end <= cut.chunk) return;
     const int splits = (t.end + cut.chunk - 1) / cut.chunk;
-    const float sl2 = a.scale * 1.4426950408889634f;
+    const float sl2 = exponent_factor(a.scale);
     const size_t per = part_floats(R, DH);
     const float* part = cut.part + (((size_t)u * H + h) * cut.splits) * per;
     const int lanes = DH / 4, groups = 64 / lanes;        // of a wavefront
