@@ -118,33 +118,53 @@ __device__ __forceinline__ void settle(bf16x8 (&q)[K]) {
 #pragma unroll
     for (int k = 0; k < K; ++k) asm volatile("" : "+v"(q[k]));
 }
-// bytes of w that are NaN codes, as 0xFF
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-    return (((w & 0x7F7F7F7Fu) + 0x01010101u & 0x80808080u) >> 7) * 255u;
+// Codes that decode to NaN (magnitude 0x7F) or, where the scale is 2^120 and more, to infinity: 256 times 2^120 is 2^128,
+// and each doubling of the scale takes in another exponent (8 codes).  odd_codes: what, added to the magnitude, carries
+// into the sign's bit for these codes, in every byte; odd_bytes: the bytes of w that hold one, as 0xFF.
+__device__ __forceinline__ uint32_t odd_codes(float scale) {
+    const int over = (int)(__builtin_bit_cast(uint32_t, scale) >> 23 & 255) - (127 + 119);
+    return 0x01010101u * (uint32_t)max(1, 8 * over);
 }
+__device__ __forceinline__ uint32_t odd_bytes(uint32_t w, uint32_t odd) {
+    return (((w & 0x7F7F7F7Fu) + odd & 0x80808080u) >> 7) * 255u;
+}
+constexpr uint32_t HUGE_SCALE = (127 + 120) << 23;   // bits of the scale from which on a page may hold infinities
 
-// A NaN among values that only some rows of a tile see: its products with the other rows' zero
-// probabilities would be NaN too.  Steps that not all rows see in full take such codes as 0 and say so; if
-// one did, each lane looks through the values that its row sees in those steps.  (Products of indicators on
-// the matrix units instead, within the step, cost every step registers.)
+// A NaN or infinity among values that only some rows of a tile see: its products with the other rows' zero
+// probabilities would be NaN too.  Steps that not all rows see in full take such codes as 0 and say so; if there was one,
+// each lane looks through the values that its row sees in those steps and adds what it finds to its sums.  (Products of
+// indicators on the matrix units instead, within the step, cost every step registers.)  Small tiles do the same with all
+// pages that may hold infinities: a probability's second term can be 0, its product with an infinity NaN.
 // Keys first .. last - 1 of sequence s, key/value head h: bit i tells of the lane's i-th channel, base +
 // stride (i / 4) + i % 4 (those below DH).
-__device__ __forceinline__ uint64_t find_nan(const CacheAttnArgs& a, int s, int h, int first, int last, int stride,
-                                             int base) {
+struct Odd {
+    uint64_t nan, up, down;
+    __device__ __forceinline__ float add_to(float x, int i) const {
+        if (nan >> i & 1) return __builtin_nanf("");
+        if (up >> i & 1) x += INFINITY;
+        if (down >> i & 1) x -= INFINITY;
+        return x;
+    }
+};
+__device__ __forceinline__ void find_odd(Odd& f, const CacheAttnArgs& a, int s, int h, int first, int last, int stride,
+                                         int base) {
     const int pt = a.c.page_tokens, shift = page_shift(pt), DH = a.c.head_dim;
-    uint64_t found = 0;
 #pragma unroll 1
     for (int key = first; key < last; ++key) {
         const int page = page_of(a.seq.table, a.seq.table_pages, a.c.pages, s, key >> shift);
         if (page < 0) continue;
-        const uint8_t* v = a.c.v + ((size_t)page * a.c.kv_heads + h) * DH * pt + (key & (pt - 1));
+        const size_t at = (size_t)page * a.c.kv_heads + h;
+        const uint8_t* v = a.c.v + at * DH * pt + (key & (pt - 1));
+        const uint32_t odd = odd_codes(a.c.v_scale[at]) & 255;
 #pragma unroll 1
         for (int i = 0; i < 64; ++i) {
             const int ch = base + stride * (i >> 2) + (i & 3);
-            if (ch < DH && (v[(size_t)ch * pt] & 0x7F) == 0x7F) found |= 1ull << i;
+            if (ch >= DH) continue;
+            const uint32_t w = v[(size_t)ch * pt];
+            if ((w & 0x7F) == 0x7F) f.nan |= 1ull << i;
+            else if ((w & 0x7F) + odd >= 0x80) (w & 0x80 ? f.down : f.up) |= 1ull << i;
         }
     }
-    return found;
 }
 
 template <int SHIFT>
@@ -270,7 +290,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
     // are computed, those of its values when their product is; the pages of the step after that are
     // asked for between the two, because loads are waited for in order.
     constexpr int NEXT = WAVES * STEP;
-    uint32_t nans = 0;
+    uint32_t odds = 0;
     int kb = k0 + wave * STEP;
     Pages next = pages(kb);
     if (kb < k1) {   // in the order of the loop, whose waits count on it
@@ -308,7 +328,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
         // keys kv .. kv + 15 belong to the lane; those it does not see, and those of pages that are
         // not there, get -inf
         const int live = present ? min(sees, k1) - kv : 0;
-        const bool some = __any(live < 16);
+        const bool some = __any(live < 16 || __builtin_bit_cast(uint32_t, vs) >= HUGE_SCALE);
         if (some) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[e] = e < live ? sc[e] : -INFINITY;
@@ -316,14 +336,15 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
             // that has none else: 0
             const int there = present ? k1 - kv : 0;
             if (there <= 0) vs = 1.f;
+            const uint32_t odd = odd_codes(vs);
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int b = there - 4 * w;
                     vw[c][w] &= b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << 8 * b) - 1;
-                    const uint32_t bad = nan_bytes(vw[c][w]);
-                    nans |= bad;
+                    const uint32_t bad = odd_bytes(vw[c][w], odd);
+                    odds |= bad;
                     vw[c][w] &= ~bad;
                 }
         }
@@ -374,14 +395,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
         step(std::true_type());
     }
 
-    if (__any(nans != 0)) {
-        uint64_t found = 0;
+    if (__any(odds != 0)) {
+        Odd found{};
         for (kb = k0 + wave * STEP; kb < k1; kb += NEXT)
-            found |= find_nan(a, t.seq, h, kb, min(min(kb + STEP, k1), sees), 16, g * 4);
+            find_odd(found, a, t.seq, h, kb, min(min(kb + STEP, k1), sees), 16, g * 4);
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[c][e] = found >> (c * 4 + e) & 1 ? __builtin_nanf("") : o[c][e];
+            for (int e = 0; e < 4; ++e) o[c][e] = found.add_to(o[c][e], c * 4 + e);
     }
 
     // join the wavefronts
@@ -435,7 +456,7 @@ struct Lds {
     uint8_t k[2][STEP * KLD];
     uint8_t v[2][DH * VLD];
     uint8_t there[2][4];   // whether a step's four 16-key groups have a page
-    int nan;               // a step that not all rows see holds a NaN value
+    int odd;               // first key of the first step that held a value taken as 0 (find_odd), or more
 };
 
 // ONE: a step lies in one page (64 or 128 tokens), whose address is scalar then.
@@ -547,16 +568,17 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
             k[0] = __builtin_bit_cast(u32x4, decode8(kc[n][0], kc[n][1], ksc[n]));
             k[1] = __builtin_bit_cast(u32x4, decode8(kc[n][2], kc[n][3], ksc[n]));
             if (kb + STEP > min(ball, k1) || !vin) {
+                const uint32_t odd = odd_codes(vsc);
                 uint32_t bad = 0;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int b = there - 4 * w;
                     vc[n][w] &= b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << 8 * b) - 1;
-                    const uint32_t x = nan_bytes(vc[n][w]);
+                    const uint32_t x = odd_bytes(vc[n][w], odd);
                     bad |= x;
                     vc[n][w] &= ~x;
                 }
-                if (bad) lds.nan = 1;
+                if (bad) atomicMin(&lds.odd, kb);   // (the order does not matter)
             }
             u32x4* v = (u32x4*)(lds.v[buf] + i / 4 * Lds<DH>::VLD + i % 4 * 32);
             v[0] = __builtin_bit_cast(u32x4, decode8(vc[n][0], vc[n][1], vsc));
@@ -663,7 +685,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
                 o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at(c, j), pf[j], o[c], 0, 0, 0);
     };
 
-    if (tid == 0) lds.nan = 0;
+    if (tid == 0) lds.odd = k1;
     Pages next = pages(k0);
     if (k0 < k1) load(k0, next);
     next = pages(k0 + STEP);
@@ -683,13 +705,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
     }
     if (kb < wend) step(kb, buf);
 
-    if (lds.nan) {
-        const int first = max(k0, k0 + (min(ball, k1) - k0) / STEP * STEP);   // the first step not seen in full
-        const uint64_t found = find_nan(a, t.seq, h, first, min(sees, k1), 8, hl * 4);
+    if (lds.odd < k1) {
+        Odd found{};
+        find_odd(found, a, t.seq, h, lds.odd, min(sees, k1), 8, hl * 4);
 #pragma unroll
         for (int c = 0; c < CB; ++c)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[c][e] = found >> (c * 16 + e) & 1 ? __builtin_nanf("") : o[c][e];
+            for (int e = 0; e < 16; ++e) o[c][e] = found.add_to(o[c][e], c * 16 + e);
     }
     l = across<5>(l, [](float x, float y) { return x + y; });
     const int row = mine + lr - t.first;
