@@ -557,7 +557,8 @@ class TokenCache:
                   (pages, kv_heads), (pages, kv_heads)]
         types = [torch.float8_e4m3fn, torch.float8_e4m3fn, torch.float32, torch.float32]
         if buffers is None:
-            device = device or torch.device("cuda", torch.cuda.current_device())
+            if device is None:
+                device = torch.device("cuda", torch.cuda.current_device())
             buffers = [torch.empty(s, dtype=t, device=device) for s, t in zip(shapes, types)]
         for b, s, t in zip(buffers, shapes, types):
             if (tuple(b.shape) != s or b.dtype is not t or not b.is_contiguous()
