@@ -479,7 +479,11 @@ def _elsewhere(index, stream):
     device or stream current, so that what it allocates belongs there (_Away)."""
     if index < 0:
         raise ValueError("tensors must be on a HIP device")
-    return stream is not None or torch.cuda.current_device() != index
+    if stream is None:
+        return torch.cuda.current_device() != index
+    if stream.device.index != index:
+        raise ValueError(f"a stream of {stream.device} for tensors on device {index}")
+    return True
 
 
 class _Away:

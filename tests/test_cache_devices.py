@@ -1,4 +1,7 @@
 """Which device and stream the operators on token rows take, with devices stood in for."""
+import types
+
+import pytest
 import torch
 
 from paper_2506_14107_amd import dejavu as dj
@@ -14,3 +17,19 @@ def test_device_zero_is_a_device(monkeypatch):
     seen.clear()
     dj.TokenCache(4, 2, 64, 16)
     assert seen == [torch.device("cuda", 1)] * 4
+
+
+def test_streams_of_another_device_are_refused(monkeypatch):
+    """Work asked for on a stream that is not of the tensors' device would run on another than the one given."""
+    rot = dj.Rotary((8, 12, 12))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    x = types.SimpleNamespace(get_device=lambda: 0)
+    stream = types.SimpleNamespace(device=torch.device("cuda", 1))
+    with pytest.raises(ValueError, match="cuda:1"):
+        dj.rotary(x, x, rot, stream=stream)
+    c = dj.TokenCache(4, 2, 64, 16, device="cpu")
+    c.index = 0
+    for call in (lambda: c.write(x, x, x, stream=stream), lambda: c.read(x, stream=stream),
+                 lambda: c.attention(x, x, stream=stream)):
+        with pytest.raises(ValueError, match="cuda:1"):
+            call()
