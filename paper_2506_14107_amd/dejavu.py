@@ -444,9 +444,14 @@ def _misfit(name, t):
                      "do not fit the other arguments")
 
 
+_INT_MAX = 2 ** 31 - 1   # counts are C ints, to which ctypes cuts what is larger
+
+
 def _stride(name, t):
     """Row stride of a tensor [rows, heads, head_dim] whose heads lie side by side."""
     n, h, d = t.shape
+    if n > _INT_MAX:
+        raise ValueError(f"{name} has {n} rows: too many for one call")
     sr, sh, sd = t.stride()
     if (sd != 1 and d > 1) or (sh != d and h > 1):
         raise ValueError(f"the heads of a row of {name} must lie side by side")
@@ -581,6 +586,8 @@ class TokenCache:
         """(n_seqs, table, table_pages, offsets, at) as the entry points take them."""
         index = self.index
         n = at.shape[0] if at.dim() == 1 else -1
+        if n > _INT_MAX:
+            raise ValueError(f"{name} has {n} sequences: too many for one call")
         if table is None:
             t, tp = 0, self.pages // max(n, 1)
         else:
