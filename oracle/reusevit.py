@@ -323,12 +323,12 @@ def finish_rows(x_rows, o_rows, P):
     return z + h @ P["W_2"].T + P["b_2"]
 
 
-def reordered_layer(x, P, cfg, G, l, tau, masks, sources, t_cls, rec):
+def reordered_layer(x, P, cfg, G, l, tau, masks, sources, t_cls, rec, cached8=None):
     """One layer over all frames with the reordered referencing; returns the layer output and
     the class-token attention weights of every frame (for the next layer's decision cue).
     rec: the per-(frame, layer, token) records (masks, cos, cos_past, cos_fut, src, dec, t) to
     fill.  sources (injection mode, optional): replaces the choice of reference of reused
-    tokens (nonzero = the future one)."""
+    tokens (nonzero = the future one).  cached8: see encode."""
     F, N, D = x.shape
     H = cfg["heads"]
     decide = bool(cfg.get("decision"))
@@ -373,6 +373,9 @@ def reordered_layer(x, P, cfg, G, l, tau, masks, sources, t_cls, rec):
         k_t, v_t = np.empty((N, D)), np.empty((N, D))
         k_t[C], v_t[C] = k_c, v_c                           # fresh keys/values ...
         k_t[R], v_t[R] = k_eff[src, R], v_eff[src, R]       # ... and the reference's
+        if cached8 is not None and cached8[f]:              # ... the past one's as the 8-bit cache holds them
+            old = R[src == past]
+            k_t[old], v_t[old] = eight_bits(k_eff[past], H)[old], eight_bits(v_eff[past], H)[old]
         o_c, t_next[f] = attention(q_c, k_t, v_t, H, first_probs=True)
         y[f, C] = finish_rows(x[f, C], o_c, P)
         y[f, R] = y[src, R]                                 # reused rows: the reference's output
@@ -400,8 +403,8 @@ def encode(frames, blob, cfg, group_size, tau=None, masks=None, dtype=np.float64
       tokens [F, N, D]   output of the last layer
       layers (optional)  list of the L+1 token buffers x^0..x^L
 
-    cached8 (optional, bool [F], not with cfg["reorder"]): frames whose reference came in an earlier
-    call of a stream that holds its keys and values in 8 bits.
+    cached8 (optional, bool [F]): frames whose reference (with cfg["reorder"] their past one) came in an
+    earlier call of a stream that holds its keys and values in 8 bits.
     """
     if (tau is None) == (masks is None):
         raise ValueError("give exactly one of tau (gate mode) and masks (injection mode)")
@@ -433,7 +436,7 @@ def encode(frames, blob, cfg, group_size, tau=None, masks=None, dtype=np.float64
             rec = {"masks": out_m, "cos": out_c, "cos_past": out_cp, "cos_fut": out_cf,
                    "src": out_s, "dec": out_d, "t": out_t}
             x, t_cls = reordered_layer(x, P, cfg, G, l, tau, masks, sources,
-                                       t_cls if decide else np.full((F, N), 1.0 / N), rec)
+                                       t_cls if decide else np.full((F, N), 1.0 / N), rec, cached8)
             if return_layers:
                 hist.append(x.copy())
             continue

@@ -4,10 +4,12 @@ import dataclasses
 import numpy as np
 import pytest
 
+import oracle
 import synth
+from oracle import reusevit
 
-from .gpu_util import dev, encoder, host, require_gpu
-from .test_gpu_encoder_options import MID, frames
+from .gpu_util import check_close, dev, encoder, host, require_gpu
+from .test_gpu_encoder_options import CARRIED, CUT, H80, MID, SMALL_F32, frames
 
 gpu = pytest.mark.gpu
 
@@ -58,3 +60,85 @@ def test_reordered_calls_of_many_batches(kw, batch, injected):
         assert np.array_equal(b, c)
         assert np.array_equal(a[np.r_[:5, 8:29]], c[np.r_[:5, 8:29]])
     assert not np.array_equal(want[2][5:8], got[2][5:8])
+
+
+# ---- what frames that meet the cache take from it ---------------------------------------------------
+# frames, group, calls and which frames reference one of an earlier call; reordered: the first call ends on anchor
+# 4, the past reference of frames 5, 6 and 8
+STAR = (11, 4, CUT, CARRIED)
+REORDERED = (17, 16, (7, 10), np.isin(np.arange(17), (5, 6, 8)))
+# fp32 cases, with a seed whose cached keys and values keep clear of the 8-bit format's ties
+F32 = {"rotary": (dict(rotary=True), STAR, 94), "restore": (dict(restore=True), STAR, 92),
+       "all": (dict(restore=True, decision=True, rotary=True), STAR, 108), "reorder": (dict(reorder=True), REORDERED, 87),
+       "reorder-restore-rotary": (dict(reorder=True, restore=True, rotary=True), REORDERED, 86)}
+
+
+def case(kw, form, seed, model):
+    m = dataclasses.replace(model, cache8=True, **kw)
+    blob = synth.make_blob(m, seed, perturb_ln=True)
+    n = form[0]
+    masks = (np.random.default_rng(seed).random((n, m.depth, m.n_tokens)) < 0.7).astype(np.uint8)
+    return m, blob, frames(m, n, seed), masks
+
+
+@pytest.mark.parametrize("name", F32)
+def test_seeds_keep_clear_of_ties(name):
+    """No cached value is within 2^-20 of its size and 2^-22 of its row's largest of a border between codes or
+    scales (an fp32 row's error: sums of 64 products and a turn, each 2^-24 of their terms)."""
+    kw, form, seed = F32[name]
+    m, blob, fr, masks = case(kw, form, seed, SMALL_F32)
+    seen, keep = [], reusevit.eight_bits
+
+    def watch(rows, heads):
+        out = keep(rows, heads)
+        far = 2.0 ** -20 * np.abs(rows) + 2.0 ** -22 * np.abs(rows).max(1, keepdims=True)
+        seen.append(np.array_equal(keep(rows + far, heads), out) and np.array_equal(keep(rows - far, heads), out))
+        return out
+
+    reusevit.eight_bits = watch
+    try:
+        oracle.encode(fr, blob, m.as_dict(), form[1], masks=masks, cached8=form[3])
+    finally:
+        reusevit.eight_bits = keep
+    assert seen and all(seen)
+
+
+@gpu
+@pytest.mark.parametrize("name", F32)
+def test_cached_values_against_the_oracle_f32(name):
+    """Injected maps, fp32: every frame within the parity bar of the oracle that quantises what it carries over, and
+    the frames that meet it outside the bar of the one that does not."""
+    require_gpu()
+    kw, form, seed = F32[name]
+    m, blob, fr, masks = case(kw, form, seed, SMALL_F32)
+    n, group, cut, carried = form
+    emb, out, toks = stream(m, blob, fr, 17, group, cut, masks)
+    assert len(emb) == n
+    sources = out == 2 if m.reorder else None
+    r = oracle.encode(fr, blob, m.as_dict(), group, masks=masks, sources=sources, cached8=carried)
+    assert np.array_equal(out, r["masks"])
+    check_close(emb, r["emb"], "f32", "embeddings")
+    check_close(toks, r["tokens"], "f32", "tokens")
+    plain = oracle.encode(fr, blob, m.as_dict(), group, masks=masks, sources=sources)
+    for f in np.flatnonzero(carried):
+        with pytest.raises(AssertionError):
+            check_close(toks[f:f + 1], plain["tokens"][f:f + 1], "f32", "unquantised")
+
+
+@gpu
+@pytest.mark.parametrize("kw", [dict(), dict(restore=True), dict(decision=True), dict(reorder=True),
+                                dict(reorder=True, restore=True, decision=True, rotary=True)],
+                         ids=["plain", "restore", "decision", "reorder", "all"])
+@pytest.mark.parametrize("model", [MID, H80], ids=["bf16", "dh80"])
+def test_cached_values_against_the_oracle_bf16(model, kw):
+    """Gate mode, bf16: with the decisions that were made, every frame within the parity bar of the quantising
+    oracle (a key of bf16 may fall on the other side of a code's border; the bar holds all the same)."""
+    require_gpu()
+    form = REORDERED if kw.get("reorder") else STAR
+    m, blob, fr, _ = case(kw, form, 77, model)
+    n, group, cut, carried = form
+    emb, out, toks = stream(m, blob, fr, 17, group, cut, None, 0.0 if m.decision else 0.9)
+    assert len(emb) == n and (out[carried] != 0).any()
+    r = oracle.encode(fr, blob, m.as_dict(), group, masks=out, sources=out == 2 if m.reorder else None, cached8=carried)
+    check_close(emb, r["emb"], "bf16", "embeddings")
+    check_close(toks, r["tokens"], "bf16", "tokens")
