@@ -40,6 +40,7 @@
 // the decision MLP a reused token may be recomputed later (its other cues change): its cosine
 // is still exactly 1, and when the MLP recomputes it the gate first copies the reference's
 // row into it.
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -612,6 +613,7 @@ int run_batch(dv_handle* h, Work& wk, const float* frames, int F, int G, int mod
             wa.v = (const char*)wk.qkv + (size_t)2 * D * el;
             wa.k_stride = wa.v_stride = 3ll * D;
             wa.row_idx = pos + (size_t)fill * N;
+            wa.cus = h->cus;
             launch_cache_write(bf, wa, s);
         } else if (fill >= 0) {
             launch_copy_ref_kv(wk.qkv, pos, fill, N, D, (int)el,
@@ -1031,11 +1033,14 @@ CacheView view_of(const dv_cache* c) {
     return {c->k, c->v, c->k_scale, c->v_scale, c->pages, c->page_tokens, c->kv_heads, c->head_dim};
 }
 
+// Compute units of the current device, asked for once a device (0: unknown, planned as for 256).
 int device_cus() {
+    static std::atomic<int> known[64];
     int dev = 0, cus = 0;
-    if (hipGetDevice(&dev) != hipSuccess ||
-        hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
-        cus = 0;   // planned as for 256
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 0;
+    if (dev < 64 && (cus = known[dev].load(std::memory_order_relaxed)) > 0) return cus;
+    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
+    if (dev < 64) known[dev].store(cus, std::memory_order_relaxed);
     return cus;
 }
 
@@ -1495,6 +1500,7 @@ int dv_cache_write(const dv_cache* cache, int n_seqs, const int32_t* table, int 
     a.q_heads = q ? q_heads : 0;
     a.pos = positions;
     a.rot = kernel_plan(plan);
+    a.cus = device_cus();
     launch_cache_write(dtype == DV_BF16, a, stream);
     HIP_TRY(hipGetLastError());
     return DV_OK;

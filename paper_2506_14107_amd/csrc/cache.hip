@@ -238,14 +238,13 @@ __device__ __forceinline__ PagePart page_part(const SeqArgs& q, int pt, int page
 // thread, at five or six wavefronts a SIMD instead of four, is 20 % slower: more passes, each a chain of the page's
 // table entry, rows, scale and codes).  Further blocks turn the query rows.
 constexpr int MAX_ITEMS = 2;                    // items of 16 channels a thread and pass
-constexpr int MAX_HEADS = 16;                   // heads of a block
 // WT threads a block (write_threads).
 template <bool BF, int V, int WT>
 __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
     constexpr int PASS = MAX_ITEMS * WT;      // items of a pass: one head's, or more heads'
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    __shared__ uint32_t s_most[MAX_HEADS];
-    __shared__ float s_scale[MAX_HEADS], s_old[MAX_HEADS];
+    __shared__ uint32_t s_most[WRITE_HEADS];
+    __shared__ float s_scale[WRITE_HEADS], s_old[WRITE_HEADS];
     const int tid = threadIdx.x;
     const int dh = a.c.head_dim, pt = a.c.page_tokens, H = a.c.kv_heads;
     if (blockIdx.x >= (unsigned)a.kv_blocks) {   // queries
@@ -551,13 +550,9 @@ void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
     bool wide = a.rot.dim % 16 == 0 && aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el);
     if (a.q) wide = wide && aligned16(a.q, a.q_stride, el) && aligned16(a.q_out, a.qo_stride, el);
     const int threads = write_threads(c.page_tokens, c.head_dim), pass = MAX_ITEMS * threads;
-    // heads of a block: as many as leave two blocks a compute unit, which share the angles of their tokens and the
-    // search for their page (us, with the heads that fill the block's threads once / as many as that: 9232 tokens of
-    // 16 heads of 64 28.5 / 22.7, 100,000 of 8 heads of 128 607 / 425; 9232 with one block a unit 30)
     const bool ragged = a.seq.offsets || a.seq.one;
     const long long slots = page_slots(ragged, a.seq.n_seqs, a.seq.rows, page_shift(c.page_tokens));
-    a.heads = std::min(MAX_HEADS, c.kv_heads);
-    while (a.heads > 1 && slots * 2 * ((c.kv_heads + a.heads - 1) / a.heads) < 512) a.heads = (a.heads + 1) / 2;
+    a.heads = write_heads(slots, c.kv_heads, a.cus);
     a.kv_blocks = (int)(slots * 2 * ((c.kv_heads + a.heads - 1) / a.heads));
     a.q_rows = rows_a_block(std::max(1, a.q_heads), c.head_dim, wide ? 8 : 1);
     const dim3 grid((unsigned)(a.kv_blocks + (a.q ? ((long long)a.seq.rows + a.q_rows - 1) / a.q_rows : 0)));

@@ -145,6 +145,16 @@ inline int rows_a_block(int heads, int dh, int vec) {
 // A block of a write has 512 threads where a page and head have more than 512 items of 16 channels (more than
 // 64 tokens of 128 channels), else 256.
 inline int write_threads(int pt, int dh) { return pt * (dh / 16) <= 512 ? 256 : 512; }
+constexpr int WRITE_HEADS = 16;   // heads a block of a write quantises at most
+// Heads of such a block: as many as leave two blocks a compute unit, which share the angles of their tokens and the
+// search for their page (us on 256 units, with the heads that fill the block's threads once / as many as that: 9232
+// tokens of 16 heads of 64 28.5 / 22.7, 100,000 of 8 heads of 128 607 / 425; 9232 with one block a unit 30).
+inline int write_heads(long long slots, int kv_heads, int cus) {
+    const long long least = 2ll * (cus > 0 ? cus : 256);
+    int heads = std::min(WRITE_HEADS, kv_heads);
+    while (heads > 1 && slots * 2 * ((kv_heads + heads - 1) / heads) < least) heads = (heads + 1) / 2;
+    return heads;
+}
 // Threads that a write launches at most: a block per page, head and keys or values, and those of the queries.
 inline long long cache_write_threads(int pt, int dh, int kv_heads, int n_seqs, int rows, bool offsets, int q_heads) {
     const int per = q_heads ? rows_a_block(q_heads, dh, 1) : 1;

@@ -320,6 +320,7 @@ struct WriteArgs {
     const int* pos;            // [rows, 3]; unused where rot.dim is 0
     const int* row_idx;        // row r of the call is row row_idx[r] of k and v (nullptr: r)
     RotaryPlan rot;
+    int cus;                   // compute units of the device (0: planned as for 256)
     int heads, kv_blocks, q_rows;   // set by the launcher
     uint32_t by_tok;
 };
