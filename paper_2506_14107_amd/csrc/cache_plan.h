@@ -164,8 +164,8 @@ inline long long cache_write_threads(int pt, int dh, int kv_heads, int n_seqs, i
 
 // ---- how an attention call is cut ----------------------------------------------------------------
 constexpr int TS = 4, LS = 7;      // small tiles of 16 packed rows, large ones of 128
-// Blocks of small tiles that a compute unit holds at least (their registers grow with the head), and packed rows of a
-// sequence up to which they take it where both kernels run.
+// Blocks of small bf16 tiles that a compute unit holds at least (their registers grow with the head; at 96 and 112 channels
+// it holds three, counted as two), and packed rows of a sequence up to which they take it where both kernels run.
 __host__ __device__ inline int small_resident(int head_dim) { return head_dim > 85 ? 2 : head_dim > 64 ? 3 : 4; }
 __host__ __device__ inline int few_rows(int head_dim) { return small_resident(head_dim) << TS; }
 constexpr int MAX_SPLITS = 512;

@@ -6,6 +6,8 @@ import re
 import shutil
 import subprocess
 
+from .test_kernel_resources import kernels, of  # noqa: F401 (a fixture)
+
 CSRC = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "paper_2506_14107_amd", "csrc")
 
 
@@ -40,3 +42,21 @@ def test_heads_of_a_writes_blocks_follow_the_chip(tmp_path):
                 assert blocks[n - 1] >= 2 * cus or n == 1
                 assert 2 * n > min(16, kv_heads) or blocks[min(2 * n, len(blocks)) - 1] < 2 * cus
     assert heads(ctypes.c_longlong(150), 16, 0) == heads(ctypes.c_longlong(150), 16, 256) != heads(ctypes.c_longlong(150), 16, 32)
+
+
+def test_resident_blocks_of_the_attention_kernels(kernels):
+    """Blocks of four wavefronts, one a SIMD of 512 registers a lane (in steps of 8), 160 KB of LDS a compute unit: small
+    bf16 tiles have at least the blocks there that the choice of tiles counts, every kernel the two that splits count."""
+    def resident(name, lds=None):
+        k, = of(kernels, name)
+        return min(512 // (-(-k["vgpr_count"] // 8) * 8), (160 << 10) // (lds or k["group_segment_fixed_size"]))
+
+    with open(os.path.join(CSRC, "cache_plan.h")) as f:
+        rule = re.search(r"small_resident\(int head_dim\) \{ return head_dim > (\d+) \? (\d) : head_dim > (\d+) \? (\d) : (\d); \}", f.read())
+    a, few, b, some, many = (int(x) for x in rule.groups())
+    for dh in range(16, 129, 16):
+        assert resident(f"cache_attn_kILi{dh}ELb1E") >= (few if dh > a else some if dh > b else many), dh
+        assert resident(f"cache_attn_kILi{dh}ELb0E") >= 2
+        lds = 2 * 64 * (2 * dh + 16) + 2 * dh * (2 * 64 + 16) + 16
+        for one in (0, 1):
+            assert resident(f"cache_attn_tile_kILi{dh}ELb{one}E", lds) >= 2
