@@ -135,11 +135,13 @@ typedef struct dv_config {
 #define DV_ROTARY_BASE 100.0
 
 /* The stream's cached reference holds its keys and values in 8 bits, as dv_cache_write quantises
- * them (pages of 64 tokens), for half (bf16) or a quarter (fp32) of their memory: a server holds one
- * handle per stream (Section 5.2's memory compaction).  Frames whose reference came in an earlier call
- * attend to the quantised keys and values of their reused tokens; the others are not affected, so a
- * stream's results depend on where its calls are cut, by the rounding to 8 bits.  Encode calls
- * outside streams do not change. */
+ * them (pages of 64 tokens), for half (bf16) or a quarter (fp32) of their memory: a server holds
+ * one handle per stream (Section 5.2's memory compaction).  Frames whose reference (with
+ * DV_FLAG_REORDER: whose past one) came in an earlier call attend to the quantised keys and values
+ * of their reused tokens, and under reordering so do the frames of their group that reuse tokens
+ * from them; the others are not affected, so a stream's results depend on where its calls are cut,
+ * by the rounding to 8 bits, and not on max_batch_frames.  Encode calls outside streams do not
+ * change. */
 #define DV_FLAG_CACHE8 32u
 
 typedef struct dv_handle dv_handle;
@@ -341,11 +343,12 @@ int dv_rotary(const dv_rotary_plan* plan, int dtype, const void* x, long long x_
               int heads, int head_dim, const int32_t* positions, void* out, long long out_stride,
               hipStream_t stream);
 
-/* A paged cache of keys and values (device buffers of the caller, 16-byte aligned codes).
- * Codes are OCP e4m3 bytes; a page and head has one scale for its keys and one for its values.
- * Keys lie [pages, kv_heads, page_tokens, head_dim], values [pages, kv_heads, head_dim,
- * page_tokens], scales [pages, kv_heads]; a value is its code times its scale.  Neither codes nor
- * scales need initialising: a page is defined by the first write to its first place. */
+/* A paged cache of keys and values (device buffers of the caller, 16-byte aligned codes). Codes are
+ * OCP e4m3 bytes; a page and head has one scale for its keys and one for its values. Keys lie
+ * [pages, kv_heads, page_tokens, head_dim], values [pages, kv_heads, head_dim, page_tokens], scales
+ * [pages, kv_heads], powers of two (those of a caller's own too); a value is its code times its
+ * scale, from 2^128 on an infinity.  Neither codes nor scales need initialising: a page is defined
+ * by the first write to its first place. */
 typedef struct dv_cache {
     uint8_t* k;
     uint8_t* v;
@@ -370,14 +373,15 @@ typedef struct dv_cache {
  * pointers may be NULL then. */
 
 /* Writes rows of keys and values to places starts[s] .. of each sequence (device int32 [n_seqs]; a
- * sequence with a negative start is passed over).  A page and head takes the least power of two
- * >= 2^-126 of which its largest magnitude is at most 448 times; codes are rounded to nearest
- * even.  Writing a page's first place starts the page anew; writing further places keeps the
- * tokens before them and lets the scale grow, which rescales those tokens' codes (each rounded again
- * only where it falls below 2^-6 of the scale).  Infinities and NaN are stored as NaN and do not
- * count for the scale; what rounds past fp32 (above 1.9375 * 2^127) reads as infinity.  Places after the last one written are undefined.  With `plan`, keys are
- * turned by positions[row] (device int32 [rows, 3]) before they are quantised, and q rows (q_heads
- * heads; NULL for none) are turned into q_out, which may be q with the same stride: one launch for a
+ * sequence with a negative start is passed over; its q rows are turned all the same).  A page and
+ * head takes the least power of two >= 2^-126 of which its largest magnitude is at most 448 times;
+ * codes are rounded to nearest even.  Writing a page's first place starts the page anew; writing
+ * further places keeps the tokens before them and lets the scale grow, which rescales those tokens'
+ * codes (each rounded again only where it falls below 2^-6 of the scale).  Infinities and NaN are
+ * stored as NaN and do not count for the scale; what rounds past fp32 (above 1.9375 * 2^127) reads
+ * as infinity.  Places after the last one written are undefined.  With `plan`, keys are turned by
+ * positions[row] (device int32 [rows, 3]) before they are quantised, and q rows (q_heads heads;
+ * NULL for none) are turned into q_out, which may be q with the same stride: one launch for a
  * decoding step.  No two sequences of a call may write the same page.  (The memory compaction of
  * Section 5.2, applied to what is kept between calls.)
  * Errors: the common ones, and DV_EINVAL for q without plan or q_out, q_heads < 1, plan without
@@ -396,20 +400,25 @@ int dv_cache_read(const dv_cache* cache, int n_seqs, const int32_t* table, int t
                   const int32_t* offsets, const int32_t* starts, int dtype, void* k,
                   long long k_stride, void* v, long long v_stride, int rows, hipStream_t stream);
 
-/* Attention of q_heads heads per row over each sequence's first lengths[s] places (device int32; cut
- * to the table, negative means 0): out = softmax(scale q k) v in fp32 arithmetic, q_heads a
- * multiple of kv_heads, query head i reading key/value head i / (q_heads / kv_heads).  causal != 0:
- * the rows are the sequence's last places, and each sees those up to its own (the i-th of n rows
- * the first lengths[s] - n + i + 1).  A row that sees nothing gets zeros.  What a row does not see, NaN
- * and infinities among it, does not reach it.  max_rows: an upper bound of the rows of any sequence, 0 if
- * unknown; it serves the choice of kernel only.  workspace: device scratch of
- * dv_cache_attention_workspace bytes for the same arguments (16-byte aligned; NULL where that is 0),
- * of this call alone until it has run.  out may be q with the same stride (in place), and must not
- * overlap it otherwise.  (The attention of Section 2.3 for a query engine's reads of
- * cached tokens.)  Errors: the common ones, and DV_EINVAL for q_heads no multiple of kv_heads,
- * q_heads * rows >= 2^31, a scale that is not finite and positive, max_rows < 0, out rows that do not
- * start on four elements, q and out the same with different strides, a workspace that is too small or
- * misaligned. */
+/* Attention of q_heads heads per row over each sequence's first lengths[s] places (device int32;
+ * cut to the table, negative means 0): out = softmax(scale q k) v, with scores, maxima, sums and
+ * outputs in fp32, q_heads a multiple of kv_heads, query head i reading key/value head i / (q_heads
+ * / kv_heads).  causal != 0: the rows are the sequence's last places, and each sees those up to its
+ * own (the i-th of n rows the first lengths[s] - n + i + 1).  A row that sees nothing gets zeros.
+ * What a row does not see, NaN and infinities among it, does not reach it.  A value that is
+ * infinite makes its channel infinite in the rows that see it (NaN with one of the other sign, a
+ * NaN, or a probability that rounds to 0); rows that see infinite or NaN keys may be NaN.
+ * Probabilities are taken to 24 bits for fp32 rows; for bf16 rows to 16 bits, or in batches with
+ * many rows (tiles of 128) to 8, which the sizes of the whole call decide: outputs are then off by
+ * 0.0020 of their size where their own rounding is 0.0016.  max_rows: an upper bound of the rows of
+ * any sequence, 0 if unknown; it serves the choice of kernel and of splits only (outputs differ by
+ * their roundings).  workspace: device scratch of dv_cache_attention_workspace bytes for the same
+ * arguments (16-byte aligned; NULL where that is 0), of this call alone until it has run.  out may
+ * be q with the same stride (in place), and must not overlap it otherwise.  (The attention of
+ * Section 2.3 for a query engine's reads of cached tokens.)  Errors: the common ones, and DV_EINVAL
+ * for q_heads no multiple of kv_heads, q_heads * rows >= 2^31, a scale that is not finite and
+ * positive, max_rows < 0, out rows that do not start on four elements, q and out the same with
+ * different strides, a workspace that is too small or misaligned. */
 int dv_cache_attention_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets,
                                  int dtype, int rows, int q_heads, int max_rows, size_t* bytes);
 int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,

@@ -16,9 +16,10 @@
 // is their own rounding, where one term gives 0.0019).  fp32 queries are three bf16 terms (24 bits), and so are
 // their probabilities: K and V being exact in bf16, three products give fp32 results at the bf16 matrix rate.
 // Single tokens are bound by the cache's bytes: one query over 200,001 keys of 8 heads of 128 72 us (5.7 TB/s of
-// the 6.2 that plain reads reach), one of each of 64 sequences of 1 to 12,000 keys 147 (5.2; the longest end last);
+// the 6.2 that plain reads reach), one of each of 64 sequences of 1 to 12,000 keys 144 (5.3; the longest end last);
 // joining the splits adds 6 to 8.  Questions of some rows over short caches are bound by the latency of a
-// tile's steps (fp32, 333 rows of 16 heads of 80 over up to 1801 keys: 21 us).
+// tile's steps (fp32, 333 rows of 16 heads of 80 over up to 1801 keys: 21 us; matrix units 8 % busy, 0.6 wavefronts a
+// SIMD).
 #include <type_traits>
 
 #include "cache_plan.h"
@@ -443,10 +444,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
 // 128 packed rows per block, 32 per wavefront (MFMA 32x32x16, queries in registers); the 64 keys of a step are
 // decoded to bf16 once per block into one of two LDS buffers, while the other is read: a
 // wavefront's matrix work on a step (1024 clocks of a SIMD at 128 channels) needs 32 KB of it.
-// 4096 rows of two sequences of 5000 to 6144 keys, 32 heads of 128 on 8: 342 us, 985 TFLOP/s (a large library
-// product: 1210).  A step of the two wavefronts on a SIMD takes 2048 clocks of its matrix unit, 2400 of
-// vector instructions (32 exponentials, each at a quarter of the rate, and some 150 others a wavefront) and the CU
-// 2560 of LDS (fragments read by four wavefronts each, decoded codes written); they overlap in part.
+// 4096 rows of two sequences of 5000 to 6144 keys, 32 heads of 128 on 8: 348 us, 968 TFLOP/s (a large library
+// product: 1210).  By the counters matrix units are busy 42 % of the time, vector units 49 (59 with exponentials at a
+// quarter of the rate), LDS 37 (fragments read by four wavefronts each, decoded codes written), at 1.75 wavefronts a
+// SIMD: they overlap in part.
 // Row m of a 32-key score block is key m with bits 2 and 3 exchanged, so that lane half hl ends up with
 // keys 16 j + 8 hl .. + 7 of each 16: the order in which the value product takes them.  Keys
 // lie in LDS at the exchanged rows.
