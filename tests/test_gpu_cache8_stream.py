@@ -62,6 +62,28 @@ def test_reordered_calls_of_many_batches(kw, batch, injected):
     assert not np.array_equal(want[2][5:8], got[2][5:8])
 
 
+@gpu
+@pytest.mark.parametrize("cut", [(30,), (7, 23), (2, 1, 27), (17, 13)])
+@pytest.mark.parametrize("batch", [9, 10, 16])
+def test_reordered_calls_without_reuse_and_with_all(batch, cut):
+    """Reuse off: no frame meets the cache, wherever calls are cut and batches end.  All reused: as at any threshold."""
+    m = dataclasses.replace(MID, reorder=True)
+    m8 = dataclasses.replace(m, cache8=True)
+    blob = synth.make_blob(m, 78, perturb_ln=True)
+    fr = frames(m, 30)
+    want = stream(m, blob, fr, 32, 8, (30,), None, float("-inf"))
+    got = stream(m8, blob, fr, batch, 8, cut, None, float("-inf"))
+    assert all(np.array_equal(a, b) for a, b in zip(want, got))
+    want, whole = [stream(x, blob, fr, 32, 8, c, None, float("inf")) for x, c in ((m, (30,)), (m8, cut))]
+    got = stream(m8, blob, fr, batch, 8, cut, None, float("inf"))
+    own = np.ones(30, bool)                     # frames behind a call's last anchor, to the end of their group
+    for end in np.cumsum(cut):
+        anchor = (end - 1) // 4 * 4
+        own[anchor + 1:anchor // 8 * 8 + 8] = False
+    for a, b, c in zip(want, whole, got):
+        assert np.array_equal(b, c) and np.array_equal(a[own], c[own])
+
+
 # ---- what frames that meet the cache take from it ---------------------------------------------------
 # frames, group, calls and which frames reference one of an earlier call; reordered: the first call ends on anchor
 # 4, the past reference of frames 5, 6 and 8
