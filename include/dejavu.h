@@ -343,6 +343,24 @@ int dv_rotary(const dv_rotary_plan* plan, int dtype, const void* x, long long x_
               int heads, int head_dim, const int32_t* positions, void* out, long long out_stride,
               hipStream_t stream);
 
+/* A norm of heads (host data, held by the caller): channel c of head h becomes x * weight[c] / sqrt(mean
+ * of the head's x^2 + eps).  weight: device, of the rows' type, [head_dim], or with per_head != 0
+ * [heads, head_dim]; NULL: ones. */
+typedef struct dv_head_norm {
+    const void* weight;
+    int per_head;
+    float eps;          /* finite and positive */
+} dv_head_norm;
+
+/* Norms every head of `rows` rows and then, with a plan, turns it as dv_rotary does (plan NULL: the norm
+ * alone, positions are not read): one pass over the rows, computed in fp32 and rounded once.  Sums of
+ * squares are fp32: a head whose channels are all zeros stays zeros, one with an infinity or a NaN, or with
+ * magnitudes past 2^60, has no defined result (and no effect on others).  Queries and keys of Section 2.3's attention.
+ * Errors: those of dv_rotary, and DV_EINVAL for norm NULL or an eps that is not finite and positive. */
+int dv_norm_rotary(const dv_head_norm* norm, const dv_rotary_plan* plan, int dtype, const void* x,
+                   long long x_stride, int rows, int heads, int head_dim, const int32_t* positions,
+                   void* out, long long out_stride, hipStream_t stream);
+
 /* A paged cache of keys and values (device buffers of the caller, 16-byte aligned codes). Codes are
  * OCP e4m3 bytes; a page and head has one scale for its keys and one for its values. Keys lie
  * [pages, kv_heads, page_tokens, head_dim], values [pages, kv_heads, head_dim, page_tokens], scales
@@ -372,6 +390,32 @@ typedef struct dv_cache {
  * dtype, stride too small, sizes past one launch's 2^32 threads), DV_EHIP.  rows = 0 does nothing, and row
  * pointers may be NULL then. */
 
+/* The next rows of a batch: hands out the pages that hold them, takes back those of sequences that
+ * end, and says where each row goes.  Sequence s holds lengths[s] places (below 0 means 0) and gets counts[s] more rows;
+ * counts[s] < 0: it ends.  Rows lie one sequence behind the other: offsets [n_seqs + 1] (sum of counts below
+ * 2^31).  ring [pages] holds the numbers of free pages, cursor (device int64) how many were taken from it
+ * so far and how many given to it: those between stand at their count modulo `pages`.  Pages that new places
+ * need are taken from it in the order of sequences and places, and entered in `table` [n_seqs, table_pages];
+ * the pages of sequences that end (entries that are pages of the cache) are given to it in the same
+ * order, for later calls to take.  From the first sequence on that the ring does not hold enough pages
+ * for, those that need any get none; nor does a sequence whose new places pass its table.  Such a sequence is not
+ * extended: starts[s] = -1 (dv_cache_write passes it over), lengths_out[s] = lengths[s].  The others have
+ * starts[s] = lengths[s] and lengths_out[s] = lengths[s] + counts[s]; those that end -1 and 0.  cursor_out:
+ * taken, given, and the pages that were lacking (0: every sequence that its table holds was
+ * extended).  For a row at place p of its sequence positions [rows, 3] become (p, p, p) (NULL: not wanted) and slots
+ * [rows] page * page_tokens + p % page_tokens, or -1 where its sequence was not extended or has no page there (NULL:
+ * not wanted); those of rows past the last sequence's stay as they are, and rows from `rows` on have none.
+ * lengths_out and cursor_out must not overlap lengths, counts and cursor (a loop alternates two
+ * buffers of each); entries of a table that are not new stay as they are.  (For a query engine's batches over
+ * the memory of Section 5.2.)  Errors: DV_EINVAL (NULL pointer, n_seqs or table_pages < 1, n_seqs *
+ * table_pages >= 2^31, pages outside [1, 2^30], rows < 0, page_tokens out of range, table_pages *
+ * page_tokens > 2^30, an output that is an input), DV_EHIP. */
+int dv_cache_extend(int n_seqs, int32_t* table, int table_pages, int page_tokens,
+                    const int32_t* lengths, const int32_t* counts, int32_t* ring, int pages,
+                    const int64_t* cursor, int rows, int32_t* offsets, int32_t* starts,
+                    int32_t* lengths_out, int64_t* cursor_out, int32_t* positions, int64_t* slots,
+                    hipStream_t stream);
+
 /* Writes rows of keys and values to places starts[s] .. of each sequence (device int32 [n_seqs]; a
  * sequence with a negative start is passed over; its q rows are turned all the same).  A page and
  * head takes the least power of two >= 2^-126 of which its largest magnitude is at most 448 times;
@@ -392,6 +436,17 @@ int dv_cache_write(const dv_cache* cache, int n_seqs, const int32_t* table, int 
                    const dv_rotary_plan* plan, const int32_t* positions, const void* q,
                    long long q_stride, int q_heads, void* q_out, long long q_out_stride,
                    hipStream_t stream);
+
+/* dv_cache_write with norms: keys are normed (k_norm; NULL: not) before they are turned and quantised, q
+ * rows (q_norm) before they are turned into q_out, both without a rounding in between.  q may come
+ * without a plan if q_norm is there.  One launch for a decoding step, as without norms (Section 5.2).
+ * Errors: those of dv_cache_write, and DV_EINVAL for an eps that is not finite and positive, and q_norm without q. */
+int dv_cache_write_norm(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
+                        const int32_t* offsets, const int32_t* starts, int dtype, const void* k,
+                        long long k_stride, const void* v, long long v_stride, int rows,
+                        const dv_rotary_plan* plan, const int32_t* positions, const void* q,
+                        long long q_stride, int q_heads, void* q_out, long long q_out_stride,
+                        const dv_head_norm* k_norm, const dv_head_norm* q_norm, hipStream_t stream);
 
 /* Reads places starts[s] .. of each sequence into rows of keys and values (code times scale; exact,
  * in bf16 below 2^-126 aside), the inverse of dv_cache_write's layout (Section 5.2).  Errors: the common

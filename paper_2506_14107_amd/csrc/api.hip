@@ -991,6 +991,16 @@ RotaryPlan kernel_plan(const dv_rotary_plan* p) {
     return r;
 }
 
+int check_norm(const dv_head_norm* n) {
+    if (!(n->eps > 0) || std::isinf(n->eps)) return fail(DV_EINVAL, "a norm's eps must be finite and positive");
+    return DV_OK;
+}
+
+NormArgs kernel_norm(const dv_head_norm* n) {
+    if (!n) return {};
+    return {n->weight, 1, n->per_head != 0, n->eps};
+}
+
 int check_dtype(int dtype) {
     return dtype == DV_F32 || dtype == DV_BF16 ? DV_OK : fail(DV_EINVAL, "unknown dtype %d", dtype);
 }
@@ -1430,21 +1440,25 @@ int dv_rotary_init(dv_rotary_plan* plan, const int section[3], int layout, int p
     return DV_OK;
 }
 
-int dv_rotary(const dv_rotary_plan* plan, int dtype, const void* x, long long x_stride, int rows, int heads,
-              int head_dim, const int32_t* positions, void* out, long long out_stride, hipStream_t stream) {
-    int rc = check_plan(plan);
-    if (rc || (rc = check_dtype(dtype))) return rc;
-    if (rows > 0 && (!x || !positions || !out)) return fail(DV_EINVAL, "NULL argument");
+static int check_heads(const dv_rotary_plan* plan, int dtype, const void* x, long long x_stride, int rows, int heads,
+                       int head_dim, const int32_t* positions, const void* out, long long out_stride) {
+    int rc = check_dtype(dtype);
+    if (rc) return rc;
+    if (rows > 0 && (!x || (plan && !positions) || !out)) return fail(DV_EINVAL, "NULL argument");
     if (rows < 0 || heads < 1 || head_dim < 1) return fail(DV_EINVAL, "rows must be >= 0, heads and head_dim >= 1");
-    if (plan->dim > head_dim || head_dim % 2)
-        return fail(DV_EINVAL, "head dim %d must be even and hold the %d turned channels", head_dim, plan->dim);
+    const int dim = plan ? plan->dim : 0;
+    if (dim > head_dim || head_dim % 2)
+        return fail(DV_EINVAL, "head dim %d must be even and hold the %d turned channels", head_dim, dim);
     const long long wide = (long long)heads * head_dim;
     if (wide > (1 << 24) || rows * wide >= (1ll << 33) || rows > (1 << 27))   // blocks of up to 16 rows, 256 threads
         return fail(DV_EINVAL, "%d rows of %lld channels: too many for one call", rows, wide);
     if ((rc = check_stride("x", x_stride, wide)) || (rc = check_stride("out", out_stride, wide))) return rc;
     if (x && x == out && x_stride != out_stride) return fail(DV_EINVAL, "in place the strides must be the same");
-    if (rows == 0) return DV_OK;
-    RotaryArgs a{};
+    return DV_OK;
+}
+
+static void set_rows(RotaryArgs& a, const dv_rotary_plan* plan, const void* x, long long x_stride, int rows, int heads,
+                     int head_dim, const int32_t* positions, void* out, long long out_stride) {
     a.x = x;
     a.out = out;
     a.x_stride = x_stride;
@@ -1454,7 +1468,32 @@ int dv_rotary(const dv_rotary_plan* plan, int dtype, const void* x, long long x_
     a.dh = head_dim;
     a.pos = positions;
     a.rot = kernel_plan(plan);
+}
+
+int dv_rotary(const dv_rotary_plan* plan, int dtype, const void* x, long long x_stride, int rows, int heads,
+              int head_dim, const int32_t* positions, void* out, long long out_stride, hipStream_t stream) {
+    int rc = check_plan(plan);
+    if (rc || (rc = check_heads(plan, dtype, x, x_stride, rows, heads, head_dim, positions, out, out_stride))) return rc;
+    if (rows == 0) return DV_OK;
+    RotaryArgs a{};
+    set_rows(a, plan, x, x_stride, rows, heads, head_dim, positions, out, out_stride);
     launch_rotary(dtype == DV_BF16, a, stream);
+    HIP_TRY(hipGetLastError());
+    return DV_OK;
+}
+
+int dv_norm_rotary(const dv_head_norm* norm, const dv_rotary_plan* plan, int dtype, const void* x, long long x_stride,
+                   int rows, int heads, int head_dim, const int32_t* positions, void* out, long long out_stride,
+                   hipStream_t stream) {
+    int rc = DV_OK;
+    if (!norm) return fail(DV_EINVAL, "norm is NULL");
+    if ((rc = check_norm(norm)) || (plan && (rc = check_plan(plan)))) return rc;
+    if ((rc = check_heads(plan, dtype, x, x_stride, rows, heads, head_dim, positions, out, out_stride))) return rc;
+    if (rows == 0) return DV_OK;
+    NormRotaryArgs a{};
+    set_rows(a, plan, x, x_stride, rows, heads, head_dim, positions, out, out_stride);
+    a.norm = kernel_norm(norm);
+    launch_norm_rotary(dtype == DV_BF16, a, stream);
     HIP_TRY(hipGetLastError());
     return DV_OK;
 }
@@ -1463,6 +1502,15 @@ int dv_cache_write(const dv_cache* cache, int n_seqs, const int32_t* table, int 
                    const int32_t* starts, int dtype, const void* k, long long k_stride, const void* v,
                    long long v_stride, int rows, const dv_rotary_plan* plan, const int32_t* positions, const void* q,
                    long long q_stride, int q_heads, void* q_out, long long q_out_stride, hipStream_t stream) {
+    return dv_cache_write_norm(cache, n_seqs, table, table_pages, offsets, starts, dtype, k, k_stride, v, v_stride, rows,
+                               plan, positions, q, q_stride, q_heads, q_out, q_out_stride, nullptr, nullptr, stream);
+}
+
+int dv_cache_write_norm(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages, const int32_t* offsets,
+                        const int32_t* starts, int dtype, const void* k, long long k_stride, const void* v,
+                        long long v_stride, int rows, const dv_rotary_plan* plan, const int32_t* positions, const void* q,
+                        long long q_stride, int q_heads, void* q_out, long long q_out_stride, const dv_head_norm* k_norm,
+                        const dv_head_norm* q_norm, hipStream_t stream) {
     int rc = check_cache(cache, n_seqs, table, table_pages, offsets != nullptr, rows);
     if (rc || (rc = check_dtype(dtype))) return rc;
     if (!starts || (rows > 0 && (!k || !v))) return fail(DV_EINVAL, "NULL argument");
@@ -1474,8 +1522,11 @@ int dv_cache_write(const dv_cache* cache, int n_seqs, const int32_t* table, int 
         if (plan->dim > cache->head_dim)
             return fail(DV_EINVAL, "head dim %d does not hold the %d turned channels", cache->head_dim, plan->dim);
     }
+    if ((k_norm && (rc = check_norm(k_norm))) || (q_norm && (rc = check_norm(q_norm)))) return rc;
+    if (q_norm && !q && rows > 0) return fail(DV_EINVAL, "a norm of queries, but no queries");
     if (q) {
-        if (!plan || !q_out) return fail(DV_EINVAL, "q is there to be turned: it needs a rotary plan and q_out");
+        if ((!plan && !q_norm) || !q_out)
+            return fail(DV_EINVAL, "q is there to be normed or turned: it needs a norm or a rotary plan, and q_out");
         if (q_heads < 1 || (long long)rows * q_heads * cache->head_dim >= (1ll << 32))
             return fail(DV_EINVAL, "%d rows of %d query heads are too few or too many for one call", rows, q_heads);
         const long long q_wide = (long long)q_heads * cache->head_dim;
@@ -1500,6 +1551,8 @@ int dv_cache_write(const dv_cache* cache, int n_seqs, const int32_t* table, int 
     a.q_heads = q ? q_heads : 0;
     a.pos = positions;
     a.rot = kernel_plan(plan);
+    a.k_norm = kernel_norm(k_norm);
+    a.q_norm = kernel_norm(q_norm);
     a.cus = device_cus();
     launch_cache_write(dtype == DV_BF16, a, stream);
     HIP_TRY(hipGetLastError());
@@ -1570,6 +1623,45 @@ int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, 
     a.scale = scale;
     a.causal = causal;
     launch_cache_attention(dtype == DV_BF16, a, p, (float*)workspace, stream);
+    HIP_TRY(hipGetLastError());
+    return DV_OK;
+}
+
+int dv_cache_extend(int n_seqs, int32_t* table, int table_pages, int page_tokens, const int32_t* lengths,
+                    const int32_t* counts, int32_t* ring, int pages, const int64_t* cursor, int rows, int32_t* offsets,
+                    int32_t* starts, int32_t* lengths_out, int64_t* cursor_out, int32_t* positions, int64_t* slots,
+                    hipStream_t stream) {
+    if (!table || !lengths || !counts || !ring || !cursor || !offsets || !starts || !lengths_out || !cursor_out)
+        return fail(DV_EINVAL, "NULL argument");
+    if (n_seqs < 1 || table_pages < 1 || pages < 1) return fail(DV_EINVAL, "n_seqs, table_pages and pages must be >= 1");
+    if (rows < 0) return fail(DV_EINVAL, "rows must be >= 0 (got %d)", rows);
+    if (!page_tokens_ok(page_tokens))
+        return fail(DV_EINVAL, "page_tokens must be 16, 32, 64 or 128 (got %d)", page_tokens);
+    if ((long long)table_pages * page_tokens > (1ll << 30))
+        return fail(DV_EINVAL, "table_pages %d: more than 2^30 tokens a sequence", table_pages);
+    if (pages > (1 << 30)) return fail(DV_EINVAL, "%d pages are too many", pages);
+    if ((long long)n_seqs * table_pages >= (1ll << 31))
+        return fail(DV_EINVAL, "%d sequences of %d pages are too many for one call", n_seqs, table_pages);
+    if (lengths_out == lengths || lengths_out == counts || cursor_out == cursor)
+        return fail(DV_EINVAL, "lengths and cursor are read and written: each needs a buffer of its own for either");
+    ExtendArgs a{};
+    a.n_seqs = n_seqs;
+    a.table_pages = table_pages;
+    a.shift = page_shift(page_tokens);
+    a.rows = rows;
+    a.pages = pages;
+    a.table = table;
+    a.lengths = lengths;
+    a.counts = counts;
+    a.ring = ring;
+    a.cursor = (const long long*)cursor;
+    a.offsets = offsets;
+    a.starts = starts;
+    a.lengths_out = lengths_out;
+    a.cursor_out = (long long*)cursor_out;
+    a.positions = positions;
+    a.slots = (long long*)slots;
+    launch_cache_extend(a, stream);
     HIP_TRY(hipGetLastError());
     return DV_OK;
 }

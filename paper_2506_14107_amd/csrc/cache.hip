@@ -198,6 +198,162 @@ __global__ __launch_bounds__(256) void rotary_k(RotaryArgs a) {
     if (n > 0) turn_rows<BF, V, 256>(a, a.rot, row0, min(n, a.per_block), lds);
 }
 
+// ---- norms of heads --------------------------------------------------------------------------------
+// A head x of dh channels becomes x w / sqrt(mean x^2 + eps), and is then turned: the sum of squares, the factor
+// and the products are fp32, rounded once with the turned value.  A thread holds 16 channels of a head, of which the
+// rotation mixes only those (item_at); the head's threads leave their sums of squares in LDS, side by side, and
+// each adds them in the same order.
+
+// Channels of chunk c of a head (16 of them): x[e V + f] is channel o0 + f of item e, x[8 + e V + f] channel o1 + f.
+template <bool BF, int V>
+__device__ __forceinline__ void load_chunk(const void* base, size_t at, int dim, bool pairs, int c, float (&x)[16]) {
+#pragma unroll
+    for (int e = 0; e < 8 / V; ++e) {
+        const Item it = item_at<V>(dim, pairs, c * (8 / V) + e);
+        float u[V], w[V];
+        load_ch<BF, V>(base, at + it.o0, u);
+        load_ch<BF, V>(base, at + it.o1, w);
+#pragma unroll
+        for (int f = 0; f < V; ++f) x[e * V + f] = u[f], x[8 + e * V + f] = w[f];
+    }
+}
+template <bool BF, int V>
+__device__ __forceinline__ void store_chunk(void* base, size_t at, int dim, bool pairs, int c, const float (&x)[16]) {
+#pragma unroll
+    for (int e = 0; e < 8 / V; ++e) {
+        const Item it = item_at<V>(dim, pairs, c * (8 / V) + e);
+        float u[V], w[V];
+#pragma unroll
+        for (int f = 0; f < V; ++f) u[f] = x[e * V + f], w[f] = x[8 + e * V + f];
+        store_ch<BF, V>(base, at + it.o0, u);
+        store_ch<BF, V>(base, at + it.o1, w);
+    }
+}
+// ... turned where it is; cos and sin of its row
+template <int V>
+__device__ __forceinline__ void turn_chunk(int dim, bool pairs, int c, const float* cos, const float* sin, float (&x)[16]) {
+#pragma unroll
+    for (int e = 0; e < 8 / V; ++e) {
+        const int i = c * (8 / V) + e;
+        if (i * 2 * V >= dim) continue;
+        float u[V], w[V];
+#pragma unroll
+        for (int f = 0; f < V; ++f) u[f] = x[e * V + f], w[f] = x[8 + e * V + f];
+        turn_item<V>(pairs, cos + i * V, sin + i * V, u, w);
+#pragma unroll
+        for (int f = 0; f < V; ++f) x[e * V + f] = u[f], x[8 + e * V + f] = w[f];
+    }
+}
+__device__ __forceinline__ float sum_squares(const float (&x)[16]) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s = fmaf(x[e], x[e], s);
+    return s;
+}
+// ... normed; part: the sums of squares of the head's dh / 16 chunks, head h of the weight
+template <bool BF, int V>
+__device__ __forceinline__ void norm_chunk(const NormArgs& nm, const float* part, int dh, int h, int dim, bool pairs, int c,
+                                           float (&x)[16]) {
+    float sum = 0.f;
+    for (int i = 0; i < dh / 16; ++i) sum += part[i];
+    const float f = rsqrtf(sum / (float)dh + nm.eps);
+    float w[16];
+    if (nm.weight) {
+        load_chunk<BF, V>(nm.weight, nm.per_head ? (size_t)h * dh : 0, dim, pairs, c, w);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = 1.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = x[e] * f * w[e];
+}
+
+// Rows row0 .. row0 + n - 1 of x (n at most ROT_ROWS), heads of a multiple of 16 channels normed and turned, to out (a block
+// of NT threads).  lds: ROT_LDS floats and NORM_ITEMS NT more.
+constexpr int NORM_ITEMS = 4;   // chunks of a thread at once
+template <bool BF, int V, int NT>
+__device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& rot, const NormArgs& nm, int row0, int n,
+                                          float* lds) {
+    const int tid = threadIdx.x, ld = (rot.dim / 2 + 3) & ~3;
+    float *cos = lds, *sin = lds + ROT_ROWS * 64, *part = lds + ROT_LDS;
+    if (rot.dim) angles_of<NT>(rot, n, cos, sin, ld, [&](int r) { return a.pos + (size_t)(row0 + r) * 3; });
+    const int per_head = a.dh / 16, per_row = per_head * a.heads, total = n * per_row;
+    const int batch = NORM_ITEMS * NT / per_head * per_head;   // whole heads
+    for (int first = 0; first < total; first += batch) {
+        const int end = min(batch, total - first);
+        float x[NORM_ITEMS][16];
+        int rr[NORM_ITEMS], hh[NORM_ITEMS], cc[NORM_ITEMS];
+#pragma unroll
+        for (int k = 0; k < NORM_ITEMS; ++k) {
+            const int i = tid + k * NT;
+            if (i >= end) continue;
+            const int rest = (first + i) % per_row;
+            rr[k] = (first + i) / per_row, hh[k] = rest / per_head, cc[k] = rest % per_head;
+            load_chunk<BF, V>(a.x, (size_t)(row0 + rr[k]) * a.x_stride + (size_t)hh[k] * a.dh, rot.dim, rot.pairs, cc[k], x[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < NORM_ITEMS; ++k)
+            if (tid + k * NT < end) part[tid + k * NT] = sum_squares(x[k]);
+        __syncthreads();   // (the angles are there too)
+#pragma unroll
+        for (int k = 0; k < NORM_ITEMS; ++k) {
+            const int i = tid + k * NT;
+            if (i >= end) continue;
+            norm_chunk<BF, V>(nm, part + i - cc[k], a.dh, hh[k], rot.dim, rot.pairs, cc[k], x[k]);
+            turn_chunk<V>(rot.dim, rot.pairs, cc[k], cos + rr[k] * ld, sin + rr[k] * ld, x[k]);
+            store_chunk<BF, V>(a.out, (size_t)(row0 + rr[k]) * a.out_stride + (size_t)hh[k] * a.dh, rot.dim, rot.pairs, cc[k],
+                               x[k]);
+        }
+        __syncthreads();   // the next batch takes the sums' places
+    }
+}
+// The same for heads of any even number of channels: a wavefront goes over a head twice.
+template <bool BF, int NT>
+__device__ __forceinline__ void norm_rows_any(const RowsArgs& a, const RotaryPlan& rot, const NormArgs& nm, int row0, int n,
+                                              float* lds) {
+    const int lane = threadIdx.x & 63, ld = (rot.dim / 2 + 3) & ~3;
+    float *cos = lds, *sin = lds + ROT_ROWS * 64;
+    if (rot.dim) angles_of<NT>(rot, n, cos, sin, ld, [&](int r) { return a.pos + (size_t)(row0 + r) * 3; });
+    __syncthreads();
+    for (int i = threadIdx.x >> 6; i < n * a.heads; i += NT / 64) {
+        const int r = i / a.heads, h = i % a.heads;
+        const size_t at = (size_t)(row0 + r) * a.x_stride + (size_t)h * a.dh;
+        const size_t to = (size_t)(row0 + r) * a.out_stride + (size_t)h * a.dh, wat = nm.per_head ? (size_t)h * a.dh : 0;
+        float sum = 0.f;
+        for (int c = lane; c < a.dh; c += 64) {
+            float x[1];
+            load_ch<BF, 1>(a.x, at + c, x);
+            sum = fmaf(x[0], x[0], sum);
+        }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        const float f = rsqrtf(sum / (float)a.dh + nm.eps);
+        for (int p = lane; p < a.dh / 2; p += 64) {
+            const Item it = item_at<1>(rot.dim, rot.pairs, p);
+            float x[1], y[1], u[1] = {1.f}, w[1] = {1.f};
+            load_ch<BF, 1>(a.x, at + it.o0, x);
+            load_ch<BF, 1>(a.x, at + it.o1, y);
+            if (nm.weight) {
+                load_ch<BF, 1>(nm.weight, wat + it.o0, u);
+                load_ch<BF, 1>(nm.weight, wat + it.o1, w);
+            }
+            x[0] = x[0] * f * u[0], y[0] = y[0] * f * w[0];
+            if (it.turned) turn_item<1>(rot.pairs, cos + r * ld + p, sin + r * ld + p, x, y);
+            store_ch<BF, 1>(a.out, to + it.o0, x);
+            store_ch<BF, 1>(a.out, to + it.o1, y);
+        }
+    }
+}
+
+// V = 0: heads of any even number of channels.
+template <bool BF, int V>
+__global__ __launch_bounds__(256) void norm_rotary_k(NormRotaryArgs a) {
+    __shared__ __attribute__((aligned(16))) float lds[ROT_LDS + (V ? NORM_ITEMS * 256 : 0)];
+    const int row0 = blockIdx.x * a.per_block, n = min(a.rows - row0, a.per_block);
+    if constexpr (V > 0) norm_rows<BF, V, 256>(a, a.rot, a.norm, row0, n, lds);
+    else norm_rows_any<BF, 256>(a, a.rot, a.norm, row0, n, lds);
+}
+
 // ---- codes -----------------------------------------------------------------------------------------
 // e4m3 codes of four floats already divided by the scale
 __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
@@ -238,8 +394,8 @@ __device__ __forceinline__ PagePart page_part(const SeqArgs& q, int pt, int page
 // thread, at five or six wavefronts a SIMD instead of four, is 20 % slower: more passes, each a chain of the page's
 // table entry, rows, scale and codes).  Further blocks turn the query rows.
 constexpr int MAX_ITEMS = 2;                    // items of 16 channels a thread and pass
-// WT threads a block (write_threads).
-template <bool BF, int V, int WT>
+// WT threads a block (write_threads).  NORM: keys, queries or both are normed first.
+template <bool BF, int V, int WT, bool NORM>
 __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
     constexpr int PASS = MAX_ITEMS * WT;      // items of a pass: one head's, or more heads'
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -253,7 +409,9 @@ __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
         const int row0 = a.seq.offsets ? max(a.seq.offsets[0], b) : b;   // rows before it are no sequence's
         const int live = a.seq.offsets ? min(a.seq.offsets[a.seq.n_seqs], a.seq.rows) : min(a.seq.n_seqs, a.seq.rows);
         const int n = min(live, b + a.q_rows) - row0;
-        if (n > 0) turn_rows<BF, V, WT>(q, a.rot, row0, n, (float*)lds);
+        if (n <= 0) return;
+        if (NORM && a.q_norm.on) norm_rows<BF, V, WT>(q, a.rot, a.q_norm, row0, n, (float*)lds);
+        else turn_rows<BF, V, WT>(q, a.rot, row0, n, (float*)lds);
         return;
     }
     const int groups = (H + a.heads - 1) / a.heads, hg = blockIdx.x % groups;
@@ -265,9 +423,10 @@ __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
     const int dim = values ? 0 : a.rot.dim;   // channels that are turned
     const int per_tok = dh / 16, per_head = p.n * per_tok, keep = p.slot0;
     const int end = min(H, (hg + 1) * a.heads);
-    // keys: cosines and sines [token][pair], once for all heads; values: codes [head][token][channel + 4]
+    // keys: cosines and sines [token][pair], once for all heads, and sums of squares of the pass's items; values: codes
+    // [head][token][channel + 4]
     const int ald = (dim / 2 + 3) & ~3, ld = dh + 4;
-    float *cos = (float*)lds, *sin = cos + p.n * ald;
+    float *cos = (float*)lds, *sin = cos + p.n * ald, *part = sin + p.n * ald;
     uint8_t* tile = lds;
     if (dim) angles_of<WT>(a.rot, p.n, cos, sin, ald, [&](int r) { return a.pos + (size_t)(p.row0 + r) * 3; });
     // i / per_head for i < 2^10, per_head <= 2^10 (the error of the factor, below per_head, times i is below 2^20)
@@ -294,31 +453,21 @@ __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
             if (hh[k] >= hn) continue;
             const int row = p.row0 + tt[k];
             const size_t at = (size_t)(a.row_idx ? a.row_idx[row] : row) * stride + (size_t)(h0 + hh[k]) * dh;
-#pragma unroll
-            for (int e = 0; e < 8 / V; ++e) {
-                const Item it = item_at<V>(dim, a.rot.pairs, cc[k] * (8 / V) + e);
-                float u[V], w[V];
-                load_ch<BF, V>(src, at + it.o0, u);
-                load_ch<BF, V>(src, at + it.o1, w);
-#pragma unroll
-                for (int f = 0; f < V; ++f) x[k][e * V + f] = u[f], x[k][8 + e * V + f] = w[f];
-            }
+            load_chunk<BF, V>(src, at, dim, a.rot.pairs, cc[k], x[k]);
         }
-        __syncthreads();   // s_most is cleared, the angles are there
+        const bool normed = NORM && !values && a.k_norm.on;
+        if (normed) {
+#pragma unroll
+            for (int k = 0; k < MAX_ITEMS; ++k)
+                if (hh[k] < hn) part[tid + k * WT] = sum_squares(x[k]);
+        }
+        __syncthreads();   // s_most is cleared, the angles and the sums are there
 #pragma unroll
         for (int k = 0; k < MAX_ITEMS; ++k) {
             if (hh[k] >= hn) continue;
-#pragma unroll
-            for (int e = 0; e < 8 / V; ++e) {
-                const int c = cc[k] * (8 / V) + e, at = tt[k] * ald + c * V;
-                if (c * 2 * V >= dim) continue;
-                float u[V], w[V];
-#pragma unroll
-                for (int f = 0; f < V; ++f) u[f] = x[k][e * V + f], w[f] = x[k][8 + e * V + f];
-                turn_item<V>(a.rot.pairs, cos + at, sin + at, u, w);
-#pragma unroll
-                for (int f = 0; f < V; ++f) x[k][e * V + f] = u[f], x[k][8 + e * V + f] = w[f];
-            }
+            if (normed)
+                norm_chunk<BF, V>(a.k_norm, part + tid + k * WT - cc[k], dh, h0 + hh[k], dim, a.rot.pairs, cc[k], x[k]);
+            turn_chunk<V>(dim, a.rot.pairs, cc[k], cos + tt[k] * ald, sin + tt[k] * ald, x[k]);
             float most = 0.f;   // a NaN does not count
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf(x[k][e]));
@@ -544,33 +693,50 @@ void launch_rotary(bool bf, RotaryArgs a, hipStream_t s) {
     else rotary_k<false, 1><<<grid, 256, 0, s>>>(a);
 }
 
+void launch_norm_rotary(bool bf, NormRotaryArgs a, hipStream_t s) {
+    const size_t el = bf ? 2 : 4;
+    const bool chunks = a.dh % 16 == 0 && a.dh <= 16 * NORM_ITEMS * 256;
+    const bool wide = chunks && a.rot.dim % 16 == 0 && aligned16(a.x, a.x_stride, el) &&
+                      aligned16(a.out, a.out_stride, el) && (uintptr_t)a.norm.weight % 16 == 0;
+    a.per_block = rows_a_block(a.heads, a.dh, chunks ? 8 : 1);
+    const dim3 grid((unsigned)(((long long)a.rows + a.per_block - 1) / a.per_block));
+    if (wide) bf ? norm_rotary_k<true, 8><<<grid, 256, 0, s>>>(a) : norm_rotary_k<false, 8><<<grid, 256, 0, s>>>(a);
+    else if (chunks) bf ? norm_rotary_k<true, 1><<<grid, 256, 0, s>>>(a) : norm_rotary_k<false, 1><<<grid, 256, 0, s>>>(a);
+    else bf ? norm_rotary_k<true, 0><<<grid, 256, 0, s>>>(a) : norm_rotary_k<false, 0><<<grid, 256, 0, s>>>(a);
+}
+
 void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
     const size_t el = bf ? 2 : 4;
     const CacheView& c = a.c;
-    bool wide = a.rot.dim % 16 == 0 && aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el);
+    const bool norm = a.k_norm.on || a.q_norm.on;
+    bool wide = a.rot.dim % 16 == 0 && aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el) &&
+                (uintptr_t)a.k_norm.weight % 16 == 0 && (uintptr_t)a.q_norm.weight % 16 == 0;
     if (a.q) wide = wide && aligned16(a.q, a.q_stride, el) && aligned16(a.q_out, a.qo_stride, el);
     const int threads = write_threads(c.page_tokens, c.head_dim), pass = MAX_ITEMS * threads;
     const bool ragged = a.seq.offsets || a.seq.one;
     const long long slots = page_slots(ragged, a.seq.n_seqs, a.seq.rows, page_shift(c.page_tokens));
     a.heads = write_heads(slots, c.kv_heads, a.cus);
     a.kv_blocks = (int)(slots * 2 * ((c.kv_heads + a.heads - 1) / a.heads));
-    a.q_rows = rows_a_block(std::max(1, a.q_heads), c.head_dim, wide ? 8 : 1);
+    a.q_rows = rows_a_block(std::max(1, a.q_heads), c.head_dim, wide || a.q_norm.on ? 8 : 1);
     const dim3 grid((unsigned)(a.kv_blocks + (a.q ? ((long long)a.seq.rows + a.q_rows - 1) / a.q_rows : 0)));
     a.by_tok = div_magic(c.head_dim / 16);
-    // a pass's codes, rows padded by 4 bytes (16 channels: a row an item); the angles of a page, or of q_rows rows
-    const size_t lds = std::max({(size_t)pass * 20, (size_t)c.page_tokens * ((a.rot.dim / 2 + 3) & ~3) * 2 * sizeof(float),
-                                 ROT_LDS * sizeof(float)});   // 64 KB at most
-    auto go = [&](auto f, auto v) {
-        constexpr bool B = decltype(f)::value;
+    // a pass's codes, rows padded by 4 bytes (16 channels: a row an item); the angles of a page, or of q_rows rows, and
+    // sums of squares
+    const size_t lds = std::max({(size_t)pass * 20,
+                                 ((size_t)c.page_tokens * ((a.rot.dim / 2 + 3) & ~3) * 2 + (norm ? pass : 0)) * sizeof(float),
+                                 (ROT_LDS + (norm ? NORM_ITEMS * threads : 0)) * sizeof(float)});   // 64 KB, 68 at most
+    auto launch = [&](auto f, auto v, auto normed) {
+        constexpr bool B = decltype(f)::value, N = decltype(normed)::value;
         constexpr int V = decltype(v)::value;
         if (threads == 256) {
-            cache_write_k<B, V, 256><<<grid, 256, lds, s>>>(a);
+            cache_write_k<B, V, 256, N><<<grid, 256, lds, s>>>(a);
         } else {   // 64 KB beside the kernel's own
-            static const bool ok = allow_lds((const void*)cache_write_k<B, V, 512>, 64 << 10);
+            static const bool ok = allow_lds((const void*)cache_write_k<B, V, 512, N>, N ? 68 << 10 : 64 << 10);
             (void)ok;
-            cache_write_k<B, V, 512><<<grid, 512, lds, s>>>(a);
+            cache_write_k<B, V, 512, N><<<grid, 512, lds, s>>>(a);
         }
     };
+    auto go = [&](auto f, auto v) { norm ? launch(f, v, std::true_type()) : launch(f, v, std::false_type()); };
     using W8 = std::integral_constant<int, 8>;
     using W1 = std::integral_constant<int, 1>;
     if (bf && wide) go(std::true_type(), W8());

@@ -297,6 +297,16 @@ struct RotaryArgs : RowsArgs {
     int per_block;           // set by the launcher
 };
 void launch_rotary(bool bf16, RotaryArgs a, hipStream_t s);
+// Norm of heads: x / sqrt(mean x^2 + eps) * weight.
+struct NormArgs {
+    const void* weight;      // [dh] or (per_head) [heads, dh], of the rows' type (nullptr: ones)
+    int on, per_head;
+    float eps;
+};
+struct NormRotaryArgs : RotaryArgs {
+    NormArgs norm;           // on
+};
+void launch_norm_rotary(bool bf16, NormRotaryArgs a, hipStream_t s);   // rot.dim = 0: not turned
 
 struct CacheView {
     uint8_t *k, *v;            // e4m3 codes: [pages, heads, tokens, channels], [pages, heads, channels, tokens]
@@ -320,6 +330,7 @@ struct WriteArgs {
     const int* pos;            // [rows, 3]; unused where rot.dim is 0
     const int* row_idx;        // row r of the call is row row_idx[r] of k and v (nullptr: r)
     RotaryPlan rot;
+    NormArgs k_norm, q_norm;   // of keys and queries, before they are turned
     int cus;                   // compute units of the device (0: planned as for 256)
     int heads, kv_blocks, q_rows;   // set by the launcher
     uint32_t by_tok;
@@ -333,6 +344,21 @@ struct ReadArgs {
     uint32_t by_oct;           // set by the launcher
 };
 void launch_cache_read(bool bf16, ReadArgs a, hipStream_t s);
+
+// The next rows of a batch and the pages that hold them.
+struct ExtendArgs {
+    int n_seqs, table_pages, shift, rows, pages;   // shift: of a page's tokens; pages: of the cache, and places of the ring
+    int* table;                    // [n_seqs, table_pages]
+    const int *lengths, *counts;   // [n_seqs] places held, new rows (below 0: the sequence ends)
+    int* ring;
+    const long long* cursor;       // pages taken so far, given so far
+    int *offsets, *starts, *lengths_out;
+    long long* cursor_out;         // ... and pages that were lacking
+    int* positions;                // [rows, 3] or nullptr
+    long long* slots;              // [rows] or nullptr
+    int row_blocks, back_blocks;   // set by the launcher
+};
+void launch_cache_extend(ExtendArgs a, hipStream_t s);
 
 // How a call's tiles of one size are cut: splits of `chunk` keys, `splits` of them for the longest
 // sequence the table holds, `slots` row tiles dealt, of at most tile_rows packed rows; part: the partial

@@ -44,6 +44,10 @@ class dv_cache(ctypes.Structure):
                 ("head_dim", ctypes.c_int)]
 
 
+class dv_head_norm(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("per_head", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
 class dv_config(ctypes.Structure):
     _fields_ = [("image_size", ctypes.c_int), ("patch", ctypes.c_int), ("depth", ctypes.c_int),
                 ("width", ctypes.c_int), ("heads", ctypes.c_int), ("mlp", ctypes.c_int),
@@ -94,6 +98,11 @@ def load(path=None):
         "dv_cache_write": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P, ctypes.c_int,
                                           _P, _I64, _P, _I64, ctypes.c_int, _P, _P, _P, _I64,
                                           ctypes.c_int, _P, _I64, _P]),
+        "dv_norm_rotary": (ctypes.c_int, [_P, _P, ctypes.c_int, _P, _I64, ctypes.c_int,
+                                          ctypes.c_int, ctypes.c_int, _P, _P, _I64, _P]),
+        "dv_cache_write_norm": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P,
+                                               ctypes.c_int, _P, _I64, _P, _I64, ctypes.c_int, _P,
+                                               _P, _P, _I64, ctypes.c_int, _P, _I64, _P, _P, _P]),
         "dv_cache_read": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P, ctypes.c_int,
                                          _P, _I64, _P, _I64, ctypes.c_int, _P]),
         "dv_cache_attention_workspace": (ctypes.c_int, [_P, ctypes.c_int, ctypes.c_int,
@@ -104,6 +113,9 @@ def load(path=None):
                                               ctypes.c_int, _P, _I64, ctypes.c_int, ctypes.c_int,
                                               ctypes.c_int, ctypes.c_float, ctypes.c_int, _P, _I64,
                                               _P, ctypes.c_size_t, _P]),
+        "dv_cache_extend": (ctypes.c_int, [ctypes.c_int, _P, ctypes.c_int, ctypes.c_int, _P, _P, _P,
+                                           ctypes.c_int, _P, ctypes.c_int, _P, _P, _P, _P, _P, _P,
+                                           _P]),
         "dv_mfma_probe": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, _P,
                                          ctypes.POINTER(ctypes.c_double), _P]),
         "dv_profile": (ctypes.c_int, [_P, ctypes.c_uint]),
@@ -229,6 +241,20 @@ def dv_cache_write(cache, n_seqs, table, table_pages, offsets, starts, dtype, k,
                                  q_heads, q_out, q_out_stride, stream))
 
 
+def dv_norm_rotary(norm, plan, dtype, x, x_stride, rows, heads, head_dim, positions, out, out_stride,
+                   stream):
+    _check(load().dv_norm_rotary(norm, plan, dtype, x, x_stride, rows, heads, head_dim, positions,
+                                 out, out_stride, stream))
+
+
+def dv_cache_write_norm(cache, n_seqs, table, table_pages, offsets, starts, dtype, k, k_stride, v,
+                        v_stride, rows, plan, positions, q, q_stride, q_heads, q_out, q_out_stride,
+                        k_norm, q_norm, stream):
+    _check(load().dv_cache_write_norm(cache, n_seqs, table, table_pages, offsets, starts, dtype, k,
+                                      k_stride, v, v_stride, rows, plan, positions, q, q_stride,
+                                      q_heads, q_out, q_out_stride, k_norm, q_norm, stream))
+
+
 def dv_cache_read(cache, n_seqs, table, table_pages, offsets, starts, dtype, k, k_stride, v,
                   v_stride, rows, stream):
     _check(load().dv_cache_read(cache, n_seqs, table, table_pages, offsets, starts, dtype, k,
@@ -249,6 +275,13 @@ def dv_cache_attention(cache, n_seqs, table, table_pages, offsets, lengths, dtyp
     _check(load().dv_cache_attention(cache, n_seqs, table, table_pages, offsets, lengths, dtype, q,
                                      q_stride, rows, q_heads, max_rows, scale, int(causal), out,
                                      out_stride, workspace, workspace_bytes, stream))
+
+
+def dv_cache_extend(n_seqs, table, table_pages, page_tokens, lengths, counts, ring, pages, cursor, rows,
+                    offsets, starts, lengths_out, cursor_out, positions, slots, stream):
+    _check(load().dv_cache_extend(n_seqs, table, table_pages, page_tokens, lengths, counts, ring,
+                                  pages, cursor, rows, offsets, starts, lengths_out, cursor_out,
+                                  positions, slots, stream))
 
 
 def dv_mfma_probe(blocks, iters, sink, stream):
@@ -548,6 +581,102 @@ def rotary(x, positions, rot, out=None, stream=None):
     return out
 
 
+def _norm(name, weight, eps, heads, d, dtype, index):
+    """dv_head_norm of a weight [d] or [heads, d] (None: ones)."""
+    if weight is None:
+        return dv_head_norm(0, 0, eps)
+    shape = weight.shape
+    per_head = len(shape) == 2
+    if (shape != ((heads, d) if per_head else (d,)) or weight.dtype is not dtype
+            or weight.get_device() != index or not weight.is_contiguous()):
+        _misfit(name, weight)
+    return dv_head_norm(weight.data_ptr(), per_head, eps)
+
+
+def norm_rotary(x, weight=None, eps=1e-6, positions=None, rot=None, out=None, stream=None):
+    """Rows x [rows, heads, head_dim] with their heads normed, x weight / sqrt(mean x^2 + eps), and then
+    turned by `positions` at the rates of `rot` (both None: not turned), into `out` (which may be x) or a
+    new tensor.  weight: [head_dim], or [heads, head_dim], of x's type; None: ones."""
+    _need_torch()
+    index = x.get_device()
+    if _elsewhere(index, stream):
+        with _Away(index, stream):
+            return norm_rotary(x, weight, eps, positions, rot, out)
+    shape = x.shape
+    if len(shape) != 3:
+        _misfit("x", x)
+    n, h, d = shape
+    dt = x.dtype
+    dtype = _dtype(x)
+    xs = _stride("x", x)
+    if out is None:
+        os = h * d
+        out = _like(x, xs, os)
+    else:
+        os = xs if out is x else _rows("out", out, shape, dt, index)
+    plan = pos = 0
+    if rot is not None and positions is not None:
+        plan, pos = rot.address, _ints("positions", positions, index, (n, 3))
+    elif rot is not None or positions is not None:
+        raise ValueError("rot and positions come together")
+    norm = _norm("weight", weight, eps, h, d, dt, index)
+    dv_norm_rotary(ctypes.addressof(norm), plan, dtype, x.data_ptr(), xs, n, h, d, pos,
+                   out.data_ptr(), os, _raw_stream(index))
+    return out
+
+
+def _longs(name, t, index, shape):
+    if (t.dtype is not torch.int64 or t.get_device() != index or t.shape != shape
+            or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int64 tensor {list(shape)} on device {index}")
+    return t.data_ptr()
+
+
+def extend(table, lengths, counts, ring, cursor, page_tokens, rows, out=None, stream=None):
+    """The next rows of a batch: hands out the pages that hold them and says where each row goes.
+
+    Sequence s holds lengths[s] places and gets counts[s] more rows (int32 [n_seqs]; fewer than 0: it
+    ends).  ring (int32 [pages]) holds the numbers of free pages, cursor (int64 [3]) how many were
+    taken from it so far and how many given to it.  New pages are entered in `table` (int32 [n_seqs,
+    table_pages]), those of sequences that end go back to the ring, both in place.  Returns, or fills
+    `out` with, (offsets [n_seqs + 1], starts [n_seqs], lengths [n_seqs], cursor [3], positions
+    [rows, 3], slots [rows]): int32, cursor and slots int64, positions and slots None if `out` says so.
+    offsets, starts and lengths are what TokenCache.write and attention take; starts is -1 for
+    sequences that end and for those that there were not enough pages for, which keep their length;
+    cursor[2] is how many pages were lacking.  The lengths and cursor returned are buffers of their
+    own: a loop passes them to its next call.  Entries of positions and slots past the last row are
+    undefined in new tensors and left as they were in those of `out`."""
+    _need_torch()
+    index = table.get_device()
+    if _elsewhere(index, stream):
+        with _Away(index, stream):
+            return extend(table, lengths, counts, ring, cursor, page_tokens, rows, out)
+    if table.dim() != 2 or ring.dim() != 1:
+        raise ValueError("table must have two dimensions and ring one")
+    (n, tp), pages = table.shape, ring.shape[0]
+    if max(n, tp, pages, rows) > _INT_MAX:
+        raise ValueError("too many sequences, pages or rows for one call")
+    if out is None:
+        new = torch.empty
+        dev = table.device
+        out = (new(n + 1, dtype=torch.int32, device=dev), new(n, dtype=torch.int32, device=dev),
+               new(n, dtype=torch.int32, device=dev), new(3, dtype=torch.int64, device=dev),
+               new((rows, 3), dtype=torch.int32, device=dev),
+               new(rows, dtype=torch.int64, device=dev))
+    offsets, starts, after, cursor_out, positions, slots = out
+    dv_cache_extend(n, _ints("table", table, index, (n, tp)), tp, page_tokens,
+                    _ints("lengths", lengths, index, (n,)), _ints("counts", counts, index, (n,)),
+                    _ints("ring", ring, index, (pages,)), pages,
+                    _longs("cursor", cursor, index, (3,)), rows,
+                    _ints("offsets", offsets, index, (n + 1,)),
+                    _ints("starts", starts, index, (n,)), _ints("lengths", after, index, (n,)),
+                    _longs("cursor", cursor_out, index, (3,)),
+                    0 if positions is None else _ints("positions", positions, index, (rows, 3)),
+                    0 if slots is None else _longs("slots", slots, index, (rows,)),
+                    _raw_stream(index))
+    return out
+
+
 class TokenCache:
     """A paged cache of keys and values in 8 bits (float8_e4m3fn codes, a power-of-two scale for each
     page and head): `pages` pages of `page_tokens` tokens of `kv_heads` heads.
@@ -597,14 +726,18 @@ class TokenCache:
         return n, t, tp, o, _ints(name, at, index, (n,))
 
     def write(self, k, v, starts, offsets=None, table=None, rotary=None, positions=None, q=None,
-              q_out=None, stream=None):
+              q_out=None, stream=None, k_norm=None, q_norm=None, eps=1e-6):
         """Quantises rows k and v [rows, kv_heads, head_dim] into places starts[s] .. of each
         sequence.  With `rotary` and `positions` the keys are turned first, and the rows of q
-        [rows, heads, head_dim] into `q_out` (which may be q) or a new tensor, which is returned."""
+        [rows, heads, head_dim] into `q_out` (which may be q) or a new tensor, which is returned.
+        k_norm, q_norm: weights of norms of the heads of keys and queries ([head_dim] or [heads,
+        head_dim]; True: ones) with `eps`, which come before the turn; q may then come without
+        `rotary`."""
         index = self.index
         if _elsewhere(index, stream):
             with _Away(index, stream):
-                return self.write(k, v, starts, offsets, table, rotary, positions, q, q_out)
+                return self.write(k, v, starts, offsets, table, rotary, positions, q, q_out, None,
+                                  k_norm, q_norm, eps)
         n, t, tp, o, at = self._seqs(starts, "starts", offsets, table)
         rows, dt = k.shape[0], k.dtype
         dtype = _dtype(k)
@@ -628,8 +761,22 @@ class TokenCache:
             qp, qop = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise ValueError("q_out without q")
-        dv_cache_write(self.address, n, t, tp, o, at, dtype, k.data_ptr(), ks, v.data_ptr(), vs, rows,
-                       plan, pos, qp, qs, heads, qop, qos, _raw_stream(index))
+        if k_norm is None and q_norm is None:
+            dv_cache_write(self.address, n, t, tp, o, at, dtype, k.data_ptr(), ks, v.data_ptr(), vs,
+                           rows, plan, pos, qp, qs, heads, qop, qos, _raw_stream(index))
+            return q_out
+        kn = qn = 0
+        d = self.head_dim
+        if k_norm is not None:
+            k_norm = _norm("k_norm", None if k_norm is True else k_norm, eps, self.kv_heads, d, dt, index)
+            kn = ctypes.addressof(k_norm)
+        if q_norm is not None:
+            if q is None:
+                raise ValueError("q_norm without q")
+            q_norm = _norm("q_norm", None if q_norm is True else q_norm, eps, heads, d, dt, index)
+            qn = ctypes.addressof(q_norm)
+        dv_cache_write_norm(self.address, n, t, tp, o, at, dtype, k.data_ptr(), ks, v.data_ptr(), vs,
+                            rows, plan, pos, qp, qs, heads, qop, qos, kn, qn, _raw_stream(index))
         return q_out
 
     def read(self, starts, offsets=None, table=None, rows=None, dtype=None, out=None, stream=None):
