@@ -482,6 +482,42 @@ int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, 
                        int causal, void* out, long long out_stride, void* workspace,
                        size_t workspace_bytes, hipStream_t stream);
 
+/* dv_cache_attention with a window: of the places that a row would see there, the first e of its
+ * sequence, it sees those from e - window on, and the first `sinks`.  Pages between that no row of a call sees are not
+ * read, and need not be there (a table entry that is no page): the keys that a call takes time for are the
+ * window's and the sinks', whatever the sequences' lengths.  A window of 2^30 and more sees all (Section 2.3's attention over
+ * the memory of Section 5.2, bounded for streams that do not end).  Errors: those of
+ * dv_cache_attention, and DV_EINVAL for window < 1, sinks < 0.  The workspace's size depends on both. */
+int dv_cache_attention_window_workspace(const dv_cache* cache, int n_seqs, int table_pages,
+                                        int with_offsets, int dtype, int rows, int q_heads,
+                                        int max_rows, int window, int sinks, size_t* bytes);
+int dv_cache_attention_window(const dv_cache* cache, int n_seqs, const int32_t* table,
+                              int table_pages, const int32_t* offsets, const int32_t* lengths,
+                              int dtype, const void* q, long long q_stride, int rows, int q_heads,
+                              int max_rows, float scale, int causal, int window, int sinks, void* out,
+                              long long out_stride, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream);
+
+/* dv_cache_attention for sequences behind prefixes that groups of them share: rows of sequences
+ * groups[g] .. groups[g + 1] - 1 (device int32 [n_groups + 1], not descending, within 0 .. n_seqs; NULL with
+ * n_groups = 1: all) see the first prefix_lengths[g] places (device int32, cut to the table, negative means 0)
+ * of prefix g, which lie in the pages of its row of prefix_table [n_groups, prefix_table_pages], all of
+ * them, and then their own sequence's as in dv_cache_attention (table, lengths and causal are about
+ * those).  Sequences of no group see their own places only.  A prefix is read once for all rows of its group.  (Questions
+ * about one video, Section 2.1's query engine.)  Errors: those of dv_cache_attention, and DV_EINVAL for
+ * n_groups or prefix_table_pages < 1, prefix_table_pages * page_tokens > 2^30, prefix_table or prefix_lengths
+ * NULL, groups NULL with n_groups > 1. */
+int dv_cache_attention_shared_workspace(const dv_cache* cache, int n_seqs, int table_pages,
+                                        int with_offsets, int n_groups, int prefix_table_pages,
+                                        int dtype, int rows, int q_heads, int max_rows, size_t* bytes);
+int dv_cache_attention_shared(const dv_cache* cache, int n_seqs, const int32_t* table,
+                              int table_pages, const int32_t* offsets, const int32_t* lengths,
+                              int n_groups, const int32_t* groups, const int32_t* prefix_table,
+                              int prefix_table_pages, const int32_t* prefix_lengths, int dtype,
+                              const void* q, long long q_stride, int rows, int q_heads, int max_rows,
+                              float scale, int causal, void* out, long long out_stride,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* Stage timing (measurement support; the stages are the steps of Sections 2.3 and 3.3) with
  * HIP events recorded on the encode stream around every
  * launch of the selected stages.  stage_mask: bit s selects stage s (0 = off,

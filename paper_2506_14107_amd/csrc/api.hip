@@ -1580,22 +1580,10 @@ int dv_cache_read(const dv_cache* cache, int n_seqs, const int32_t* table, int t
     return DV_OK;
 }
 
-int dv_cache_attention_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets, int dtype,
-                                 int rows, int q_heads, int max_rows, size_t* bytes) {
-    if (!bytes) return fail(DV_EINVAL, "bytes is NULL");
-    *bytes = 0;
-    static const int32_t some = 0;   // the size does not depend on what a table holds
-    int rc = check_cache(cache, n_seqs, &some, table_pages, with_offsets != 0, rows);
-    if (rc || (rc = check_dtype(dtype)) || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows))) return rc;
-    *bytes = cache_attn_plan(dtype == DV_BF16, n_seqs, rows, with_offsets != 0, max_rows, table_pages,
-                             cache->page_tokens, cache->kv_heads, q_heads, cache->head_dim, device_cus()).bytes;
-    return DV_OK;
-}
-
-int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
-                       const int32_t* offsets, const int32_t* lengths, int dtype, const void* q, long long q_stride,
-                       int rows, int q_heads, int max_rows, float scale, int causal, void* out, long long out_stride,
-                       void* workspace, size_t workspace_bytes, hipStream_t stream) {
+// What the attention calls have in common, without their sequences' plans.
+static int check_attention(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages, const int32_t* offsets,
+                           const int32_t* lengths, int dtype, const void* q, long long q_stride, int rows, int q_heads,
+                           int max_rows, float scale, const void* out, long long out_stride) {
     int rc = check_cache(cache, n_seqs, table, table_pages, offsets != nullptr, rows);
     if (rc || (rc = check_dtype(dtype)) || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows))) return rc;
     if (!lengths || (rows > 0 && (!q || !out))) return fail(DV_EINVAL, "NULL argument");
@@ -1605,13 +1593,19 @@ int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, 
     if (q && q == out && q_stride != out_stride) return fail(DV_EINVAL, "in place the strides must be the same");
     if ((uintptr_t)out % (dtype == DV_BF16 ? 8 : 16) || out_stride % 4)
         return fail(DV_EINVAL, "out rows must start on four elements");
-    const CacheAttnPlan p = cache_attn_plan(dtype == DV_BF16, n_seqs, rows, offsets != nullptr, max_rows, table_pages,
-                                            cache->page_tokens, cache->kv_heads, q_heads, cache->head_dim,
-                                            device_cus());
-    if (p.bytes && (!workspace || workspace_bytes < p.bytes || (uintptr_t)workspace % 16))
-        return fail(DV_EINVAL, "the call needs a 16-byte aligned workspace of %zu bytes (got %zu)", p.bytes,
-                    workspace ? workspace_bytes : 0);
-    if (rows == 0) return DV_OK;
+    return DV_OK;
+}
+
+static int check_workspace(size_t need, const void* workspace, size_t bytes) {
+    if (need && (!workspace || bytes < need || (uintptr_t)workspace % 16))
+        return fail(DV_EINVAL, "the call needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
+                    workspace ? bytes : 0);
+    return DV_OK;
+}
+
+static CacheAttnArgs attention_args(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
+                                    const int32_t* offsets, const int32_t* lengths, const void* q, long long q_stride,
+                                    int rows, int q_heads, float scale, int causal, void* out, long long out_stride) {
     CacheAttnArgs a{};
     a.c = view_of(cache);
     a.seq = {n_seqs, table_pages, rows, table, offsets, lengths};
@@ -1622,7 +1616,133 @@ int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, 
     a.q_heads = q_heads;
     a.scale = scale;
     a.causal = causal;
-    launch_cache_attention(dtype == DV_BF16, a, p, (float*)workspace, stream);
+    return a;
+}
+
+static CacheAttnPlan plan_of(const dv_cache* c, int n_seqs, int table_pages, bool offsets, int dtype, int rows, int q_heads,
+                             int max_rows, int window = 0, int sinks = 0, bool part = false) {
+    return cache_attn_plan(dtype == DV_BF16, n_seqs, rows, offsets, max_rows, table_pages, c->page_tokens, c->kv_heads,
+                           q_heads, c->head_dim, device_cus(), window, sinks, part);
+}
+
+static const int32_t SOME_TABLE = 0;   // a workspace's size does not depend on what a table holds
+
+int dv_cache_attention_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets, int dtype,
+                                 int rows, int q_heads, int max_rows, size_t* bytes) {
+    if (!bytes) return fail(DV_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    int rc = check_cache(cache, n_seqs, &SOME_TABLE, table_pages, with_offsets != 0, rows);
+    if (rc || (rc = check_dtype(dtype)) || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows))) return rc;
+    *bytes = plan_of(cache, n_seqs, table_pages, with_offsets != 0, dtype, rows, q_heads, max_rows).bytes;
+    return DV_OK;
+}
+
+int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
+                       const int32_t* offsets, const int32_t* lengths, int dtype, const void* q, long long q_stride,
+                       int rows, int q_heads, int max_rows, float scale, int causal, void* out, long long out_stride,
+                       void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    int rc = check_attention(cache, n_seqs, table, table_pages, offsets, lengths, dtype, q, q_stride, rows, q_heads, max_rows,
+                             scale, out, out_stride);
+    if (rc) return rc;
+    const CacheAttnPlan p = plan_of(cache, n_seqs, table_pages, offsets != nullptr, dtype, rows, q_heads, max_rows);
+    if ((rc = check_workspace(p.bytes, workspace, workspace_bytes))) return rc;
+    if (rows == 0) return DV_OK;
+    launch_cache_attention(dtype == DV_BF16,
+                           attention_args(cache, n_seqs, table, table_pages, offsets, lengths, q, q_stride, rows, q_heads,
+                                          scale, causal, out, out_stride),
+                           p, (float*)workspace, stream);
+    HIP_TRY(hipGetLastError());
+    return DV_OK;
+}
+
+static int check_window(int window, int sinks) {
+    if (window < 1 || sinks < 0) return fail(DV_EINVAL, "window must be >= 1, sinks >= 0 (got %d, %d)", window, sinks);
+    return DV_OK;
+}
+static int held_by(int x) { return std::min(x, 1 << 30); }   // no sequence has more keys
+
+int dv_cache_attention_window_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets, int dtype,
+                                        int rows, int q_heads, int max_rows, int window, int sinks, size_t* bytes) {
+    if (!bytes) return fail(DV_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    int rc = check_cache(cache, n_seqs, &SOME_TABLE, table_pages, with_offsets != 0, rows);
+    if (rc || (rc = check_dtype(dtype)) || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows)) ||
+        (rc = check_window(window, sinks)))
+        return rc;
+    *bytes = plan_of(cache, n_seqs, table_pages, with_offsets != 0, dtype, rows, q_heads, max_rows, held_by(window),
+                     held_by(sinks)).bytes;
+    return DV_OK;
+}
+
+int dv_cache_attention_window(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
+                              const int32_t* offsets, const int32_t* lengths, int dtype, const void* q,
+                              long long q_stride, int rows, int q_heads, int max_rows, float scale, int causal,
+                              int window, int sinks, void* out, long long out_stride, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream) {
+    int rc = check_attention(cache, n_seqs, table, table_pages, offsets, lengths, dtype, q, q_stride, rows, q_heads, max_rows,
+                             scale, out, out_stride);
+    if (rc || (rc = check_window(window, sinks))) return rc;
+    const CacheAttnPlan p = plan_of(cache, n_seqs, table_pages, offsets != nullptr, dtype, rows, q_heads, max_rows,
+                                    held_by(window), held_by(sinks));
+    if ((rc = check_workspace(p.bytes, workspace, workspace_bytes))) return rc;
+    if (rows == 0) return DV_OK;
+    CacheAttnArgs a = attention_args(cache, n_seqs, table, table_pages, offsets, lengths, q, q_stride, rows, q_heads, scale,
+                                     causal, out, out_stride);
+    a.window = held_by(window);
+    a.sinks = held_by(sinks);
+    launch_cache_window(dtype == DV_BF16, a, p, (float*)workspace, stream);
+    HIP_TRY(hipGetLastError());
+    return DV_OK;
+}
+
+// Groups of a call and their prefixes.
+static int check_groups(const dv_cache* cache, int n_groups, int prefix_table_pages, int rows, int q_heads) {
+    if (n_groups < 1 || prefix_table_pages < 1) return fail(DV_EINVAL, "n_groups and prefix_table_pages must be >= 1");
+    if ((long long)prefix_table_pages * cache->page_tokens > (1ll << 30))
+        return fail(DV_EINVAL, "prefix_table_pages %d: more than 2^30 tokens a prefix", prefix_table_pages);
+    return check_queries(cache, n_groups, rows, q_heads, 0);
+}
+static CacheAttnPlan prefix_plan(const dv_cache* c, int n_groups, int table_pages, int dtype, int rows, int q_heads) {
+    return plan_of(c, n_groups, table_pages, true, dtype, rows, q_heads, n_groups == 1 ? rows : 0, 0, 0, true);
+}
+
+int dv_cache_attention_shared_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets, int n_groups,
+                                        int prefix_table_pages, int dtype, int rows, int q_heads, int max_rows,
+                                        size_t* bytes) {
+    if (!bytes) return fail(DV_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    int rc = check_cache(cache, n_seqs, &SOME_TABLE, table_pages, with_offsets != 0, rows);
+    if (rc || (rc = check_dtype(dtype)) || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows)) ||
+        (rc = check_groups(cache, n_groups, prefix_table_pages, rows, q_heads)))
+        return rc;
+    *bytes = plan_of(cache, n_seqs, table_pages, with_offsets != 0, dtype, rows, q_heads, max_rows, 0, 0, true).bytes +
+             prefix_plan(cache, n_groups, prefix_table_pages, dtype, rows, q_heads).bytes;
+    return DV_OK;
+}
+
+int dv_cache_attention_shared(const dv_cache* cache, int n_seqs, const int32_t* table, int table_pages,
+                              const int32_t* offsets, const int32_t* lengths, int n_groups, const int32_t* groups,
+                              const int32_t* prefix_table, int prefix_table_pages, const int32_t* prefix_lengths,
+                              int dtype, const void* q, long long q_stride, int rows, int q_heads, int max_rows,
+                              float scale, int causal, void* out, long long out_stride, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream) {
+    int rc = check_attention(cache, n_seqs, table, table_pages, offsets, lengths, dtype, q, q_stride, rows, q_heads, max_rows,
+                             scale, out, out_stride);
+    if (rc || (rc = check_groups(cache, n_groups, prefix_table_pages, rows, q_heads))) return rc;
+    if (!prefix_table || !prefix_lengths) return fail(DV_EINVAL, "NULL argument");
+    if (!groups && n_groups != 1) return fail(DV_EINVAL, "groups is NULL: that is one group, not %d", n_groups);
+    const CacheAttnPlan p = plan_of(cache, n_seqs, table_pages, offsets != nullptr, dtype, rows, q_heads, max_rows, 0, 0, true);
+    const CacheAttnPlan pre = prefix_plan(cache, n_groups, prefix_table_pages, dtype, rows, q_heads);
+    if ((rc = check_workspace(p.bytes + pre.bytes, workspace, workspace_bytes))) return rc;
+    if (rows == 0) return DV_OK;
+    SeqArgs prefix = {n_groups, prefix_table_pages, rows, prefix_table, offsets, prefix_lengths};
+    prefix.by_group = 1;
+    prefix.grouped = n_seqs;
+    prefix.groups = groups;
+    launch_cache_shared(dtype == DV_BF16,
+                        attention_args(cache, n_seqs, table, table_pages, offsets, lengths, q, q_stride, rows, q_heads, scale,
+                                       causal, out, out_stride),
+                        prefix, p, pre, (float*)workspace, stream);
     HIP_TRY(hipGetLastError());
     return DV_OK;
 }

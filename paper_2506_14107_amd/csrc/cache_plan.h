@@ -107,6 +107,7 @@ struct Tile {
     int rows;    // packed rows of the tile
     int len;     // keys of the sequence
     int end;     // keys that the tile's last row sees
+    int skip0, left_out;   // keys skip0 .. skip0 + left_out - 1, whole steps of 64, which no row of it sees
 };
 __host__ __device__ inline long long tile_slots(bool offsets, int n_seqs, int rows, int group, int shift) {
     return offsets ? ((long long)rows * group >> shift) + n_seqs
@@ -115,10 +116,10 @@ __host__ __device__ inline long long tile_slots(bool offsets, int n_seqs, int ro
 // ... slot u, of sequence s (without offsets: of sequence u / tiles of a row)
 __host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int shift, bool causal, const Seq& sp,
                                         long long u) {
-    Tile t = {-1, 0, 0, 0, 0, 0, 0};
+    Tile t = {-1, 0, 0, 0, 0, 0, 0, 0, 0};
     const int s = sp.s;
     if (s < 0) return t;
-    const long long j = q.offsets ? u - sp.slot0 : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
+    const long long j = q.offsets || q.by_group ? u - sp.slot0 : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
     const long long first = j << shift, left = (long long)sp.n * group - first;
     if (j < 0 || left <= 0) return t;
     t.seq = s;
@@ -134,6 +135,15 @@ __host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int
         t.end = e > 0 ? (int)e : 0;
     }
     return t;
+}
+
+// With a window: a row that sees the keys below e without one sees those from e - window on, and the first `sinks`.
+__host__ __device__ inline void leave_out(Tile& t, int group, bool causal, int window, int sinks) {
+    const int first = causal ? t.len - t.n + t.first / group + 1 : t.len;   // what the tile's first row sees without a window
+    const int low = (first > window ? first - window : 0) & ~63, high = ((sinks < t.end ? sinks : t.end) + 63) & ~63;
+    if (t.seq < 0 || high >= low) return;
+    t.skip0 = high;
+    t.left_out = low - high;
 }
 
 // ---- launches of rotary positions and of a write --------------------------------------------------
@@ -173,12 +183,20 @@ constexpr int MAX_SPLITS = 512;
 // partial results: per tile of R rows, head and split R rows of dh fp32, R maxima, R sums
 __host__ __device__ inline size_t part_floats(int R, int dh) { return (size_t)R * (dh + 2); }
 
+// window > 0: rows see at most that many keys before their own place and `sinks` first ones.  part: every result is left as a
+// partial one.
 inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets, int max_rows, int table_pages,
-                                     int page_tokens, int kv_heads, int q_heads, int head_dim, int cus) {
+                                     int page_tokens, int kv_heads, int q_heads, int head_dim, int cus, int window = 0,
+                                     int sinks = 0, bool part = false) {
     CacheAttnPlan p{};
     const int G = q_heads / kv_heads;
     const long long unit = cus > 0 ? cus : 256;
-    const long long keys = (long long)table_pages * page_tokens;   // at most 2^30
+    const long long held = (long long)table_pages * page_tokens;   // at most 2^30
+    // keys that a tile takes at most (leave_out): the rows of a tile, which lie side by side, move its window's end
+    auto keys_of = [&](int shift) {
+        const long long more = std::min<long long>(rows, (1 << shift) / G + 1);
+        return window ? std::min(held, (std::min<long long>(held, sinks) + 63) / 64 * 64 + window + more + 63) : held;
+    };
     const long long most_rows = std::min<long long>(rows, !offsets ? 1 : max_rows > 0 ? max_rows : rows);
     // Large tiles (bf16) decode a key once for 128 rows and give the matrix units long products; small ones read
     // keys at the memory's rate and have eight times the blocks.  Large ones take sequences of more than few_rows
@@ -204,6 +222,7 @@ inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets
     // split, one query: 1000 / 2000 keys of 128 channels 9.4 / 12.4, 14.6 / 12.4; 2000 of 64 9.0 / 12.5; a large tile of
     // 700 keys takes 27).
     auto cut = [&](CacheAttnCut& c, int shift, long long cap, long long whole) {
+        const long long keys = keys_of(shift);
         c.slots = tile_slots(offsets, n_seqs, rows, G, shift);
         const long long units = std::max(1ll, c.slots * kv_heads);
         const long long most = std::min<long long>(MAX_SPLITS, std::max(1ll, 2 * unit / units));
@@ -215,11 +234,11 @@ inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets
         c.chunk = (int)((chunk + 255) / 256 * 256);
         c.splits = (int)std::max(1ll, (keys + c.chunk - 1) / c.chunk);
         c.tile_rows = (int)std::min<long long>(1 << shift, std::max(1ll, most_rows * G));
-        return c.splits > 1 ? (size_t)c.slots * kv_heads * c.splits * part_floats(1 << shift, head_dim) : 0;
+        return c.splits > 1 || part ? (size_t)c.slots * kv_heads * c.splits * part_floats(1 << shift, head_dim) : 0;
     };
     if (p.route != ATTN_MANY) p.few_floats = cut(p.few, TS, 2048, (bf ? 1 << 17 : 1 << 16) / head_dim);
     size_t many = 0;
-    if (p.route != ATTN_FEW) many = cut(p.many, LS, keys, 512);
+    if (p.route != ATTN_FEW) many = cut(p.many, LS, held, 512);
     p.bytes = (p.few_floats + many) * sizeof(float);
     return p;
 }
@@ -238,7 +257,15 @@ __device__ __forceinline__ int sum_up(int x) {
 }
 // The sequence that owns slot u (every lane of a wavefront calls, with the same u); count: the slots of one.  N times 64
 // sequences are looked at together: a chain of loads is what small calls wait for.
-template <int N, class Count>
+// GROUPS: of the groups of sequences, whose rows lie together.
+__device__ __forceinline__ Seq group_from(const SeqArgs& q, int g) {
+    auto first = [&](int i) {   // row of sequence groups[i]
+        const int s = q.groups ? max(0, min(q.groups[i], q.grouped)) : i ? q.grouped : 0;
+        return q.offsets ? q.offsets[s] : s;
+    };
+    return seq_from(q, g, first(g), first(g + 1), q.at[g]);
+}
+template <int N, bool GROUPS, class Count>
 __device__ __forceinline__ Seq find_among(const SeqArgs& q, const Count& count, int u) {
     const int lane = threadIdx.x & 63;
     int base = 0;
@@ -247,7 +274,8 @@ __device__ __forceinline__ Seq find_among(const SeqArgs& q, const Count& count, 
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int s = b + i * 64 + lane, c = s < q.n_seqs ? s : q.n_seqs - 1;
-            sp[i] = seq_from(q, s, q.offsets[c], q.offsets[c + 1], q.at[c]);
+            if (GROUPS) sp[i] = group_from(q, c), sp[i].s = s;
+            else sp[i] = seq_from(q, s, q.offsets[c], q.offsets[c + 1], q.at[c]);
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -261,9 +289,9 @@ __device__ __forceinline__ Seq find_among(const SeqArgs& q, const Count& count, 
     }
     return {-1, 0, 0, 0, 0};
 }
-template <class Count>
+template <bool GROUPS = false, class Count>
 __device__ __forceinline__ Seq find_seq(const SeqArgs& q, const Count& count, int u) {
-    return q.n_seqs <= 64 ? find_among<1>(q, count, u) : find_among<4>(q, count, u);
+    return q.n_seqs <= 64 ? find_among<1, GROUPS>(q, count, u) : find_among<4, GROUPS>(q, count, u);
 }
 #endif
 

@@ -319,6 +319,9 @@ struct SeqArgs {
     const int* offsets;    // [n_seqs + 1] first row of each sequence (nullptr: one row each)
     const int* at;         // [n_seqs] write, read: place of the first row; attention: keys
     int one;               // one sequence that all rows belong to (offsets nullptr)
+    int by_group;          // attention: the sequences are groups of a call's `grouped` ones, groups[i] .. groups[i + 1] - 1 (nullptr:
+    int grouped;           // one of all); offsets are those ones'
+    const int* groups;
 };
 struct WriteArgs {
     CacheView c;
@@ -378,6 +381,7 @@ struct CacheAttnArgs {
     int q_heads;
     float scale;
     int causal;
+    int window, sinks;   // of a call with a window
     // set by the launcher
     int route;
     CacheAttnCut few, many;
@@ -390,5 +394,10 @@ struct CacheAttnPlan {
     size_t bytes;
 };
 void launch_cache_attention(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);
+void launch_cache_window(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);   // a.window, a.sinks
+// Sequences behind prefixes that groups of them share: `prefix` has the prefixes' table, lengths and groups, the parts'
+// results meet in the workspace (p's, then pre's).
+void launch_cache_shared(bool bf16, CacheAttnArgs a, const SeqArgs& prefix, const CacheAttnPlan& p, const CacheAttnPlan& pre,
+                         float* workspace, hipStream_t s);
 
 }  // namespace dv

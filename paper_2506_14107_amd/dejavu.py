@@ -113,6 +113,21 @@ def load(path=None):
                                               ctypes.c_int, _P, _I64, ctypes.c_int, ctypes.c_int,
                                               ctypes.c_int, ctypes.c_float, ctypes.c_int, _P, _I64,
                                               _P, ctypes.c_size_t, _P]),
+        "dv_cache_attention_window_workspace": (ctypes.c_int, [_P] + [ctypes.c_int] * 9 +
+                                                [ctypes.POINTER(ctypes.c_size_t)]),
+        "dv_cache_attention_window": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P,
+                                                     ctypes.c_int, _P, _I64, ctypes.c_int,
+                                                     ctypes.c_int, ctypes.c_int, ctypes.c_float,
+                                                     ctypes.c_int, ctypes.c_int, ctypes.c_int, _P,
+                                                     _I64, _P, ctypes.c_size_t, _P]),
+        "dv_cache_attention_shared_workspace": (ctypes.c_int, [_P] + [ctypes.c_int] * 9 +
+                                                [ctypes.POINTER(ctypes.c_size_t)]),
+        "dv_cache_attention_shared": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P,
+                                                     ctypes.c_int, _P, _P, ctypes.c_int, _P,
+                                                     ctypes.c_int, _P, _I64, ctypes.c_int,
+                                                     ctypes.c_int, ctypes.c_int, ctypes.c_float,
+                                                     ctypes.c_int, _P, _I64, _P, ctypes.c_size_t,
+                                                     _P]),
         "dv_cache_extend": (ctypes.c_int, [ctypes.c_int, _P, ctypes.c_int, ctypes.c_int, _P, _P, _P,
                                            ctypes.c_int, _P, ctypes.c_int, _P, _P, _P, _P, _P, _P,
                                            _P]),
@@ -275,6 +290,44 @@ def dv_cache_attention(cache, n_seqs, table, table_pages, offsets, lengths, dtyp
     _check(load().dv_cache_attention(cache, n_seqs, table, table_pages, offsets, lengths, dtype, q,
                                      q_stride, rows, q_heads, max_rows, scale, int(causal), out,
                                      out_stride, workspace, workspace_bytes, stream))
+
+
+def dv_cache_attention_window_workspace(cache, n_seqs, table_pages, with_offsets, dtype, rows, q_heads,
+                                        max_rows, window, sinks):
+    n = ctypes.c_size_t()
+    _check(load().dv_cache_attention_window_workspace(cache, n_seqs, table_pages, int(with_offsets),
+                                                      dtype, rows, q_heads, max_rows, window, sinks,
+                                                      ctypes.byref(n)))
+    return n.value
+
+
+def dv_cache_attention_window(cache, n_seqs, table, table_pages, offsets, lengths, dtype, q, q_stride,
+                              rows, q_heads, max_rows, scale, causal, window, sinks, out, out_stride,
+                              workspace, workspace_bytes, stream):
+    _check(load().dv_cache_attention_window(cache, n_seqs, table, table_pages, offsets, lengths, dtype,
+                                            q, q_stride, rows, q_heads, max_rows, scale, int(causal),
+                                            window, sinks, out, out_stride, workspace,
+                                            workspace_bytes, stream))
+
+
+def dv_cache_attention_shared_workspace(cache, n_seqs, table_pages, with_offsets, n_groups,
+                                        prefix_table_pages, dtype, rows, q_heads, max_rows):
+    n = ctypes.c_size_t()
+    _check(load().dv_cache_attention_shared_workspace(cache, n_seqs, table_pages, int(with_offsets),
+                                                      n_groups, prefix_table_pages, dtype, rows,
+                                                      q_heads, max_rows, ctypes.byref(n)))
+    return n.value
+
+
+def dv_cache_attention_shared(cache, n_seqs, table, table_pages, offsets, lengths, n_groups, groups,
+                              prefix_table, prefix_table_pages, prefix_lengths, dtype, q, q_stride,
+                              rows, q_heads, max_rows, scale, causal, out, out_stride, workspace,
+                              workspace_bytes, stream):
+    _check(load().dv_cache_attention_shared(cache, n_seqs, table, table_pages, offsets, lengths,
+                                            n_groups, groups, prefix_table, prefix_table_pages,
+                                            prefix_lengths, dtype, q, q_stride, rows, q_heads,
+                                            max_rows, scale, int(causal), out, out_stride, workspace,
+                                            workspace_bytes, stream))
 
 
 def dv_cache_extend(n_seqs, table, table_pages, page_tokens, lengths, counts, ring, pages, cursor, rows,
@@ -625,6 +678,13 @@ def norm_rotary(x, weight=None, eps=1e-6, positions=None, rot=None, out=None, st
     return out
 
 
+def _window(window, sinks):
+    """Window and sinks as the entry points take them (no sequence has more than 2^30 places)."""
+    if window < 1 or sinks < 0:
+        raise ValueError(f"window must be >= 1 and sinks >= 0 (got {window}, {sinks})")
+    return min(window, 1 << 30), min(sinks, 1 << 30)
+
+
 def _longs(name, t, index, shape):
     if (t.dtype is not torch.int64 or t.get_device() != index or t.shape != shape
             or not t.is_contiguous()):
@@ -801,16 +861,18 @@ class TokenCache:
         return out
 
     def attention(self, q, lengths, offsets=None, table=None, causal=True, scale=None, max_rows=0,
-                  out=None, workspace=None, stream=None):
+                  out=None, workspace=None, stream=None, window=0, sinks=0):
         """Attention of rows q [rows, heads, head_dim] over the first lengths[s] places of their
         sequences, into `out` or a new tensor.  causal: the rows are the sequence's last places and
         see no later ones.  max_rows: an upper bound of any sequence's rows, if known.  workspace: a
-        uint8 tensor to use (see attention_workspace) instead of one of the call's own."""
+        uint8 tensor to use (see attention_workspace) instead of one of the call's own.
+        window > 0: of the e places that a row would see it sees those from e - window on and the
+        first `sinks`; pages between need not be there."""
         index = self.index
         if _elsewhere(index, stream):
             with _Away(index, stream):
                 return self.attention(q, lengths, offsets, table, causal, scale, max_rows, out,
-                                      workspace)
+                                      workspace, None, window, sinks)
         n, t, tp, o, at = self._seqs(lengths, "lengths", offsets, table)
         if q.dim() != 3:
             _misfit("q", q)
@@ -823,32 +885,114 @@ class TokenCache:
             out = _like(q, qs, os)
         else:
             os = _rows("out", out, shape, q.dtype, index)
+        if window or sinks:
+            window, sinks = _window(window, sinks)
         ws = size = 0
         if workspace is None:
             key = (n, tp, o != 0, dtype, rows, heads, max_rows)
-            size = self.scratch.get(key)
-            if size is None:
-                size = dv_cache_attention_workspace(self.address, *key)
-                if len(self.scratch) >= 1024:
-                    self.scratch.clear()
-                self.scratch[key] = size
+            need = dv_cache_attention_workspace
+            if window:
+                key += (window, sinks)
+                need = dv_cache_attention_window_workspace
+            size = self._scratch(need, key)
             if size:
                 workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
                 ws = workspace.data_ptr()
         else:
-            if (workspace.get_device() != index or workspace.dtype is not torch.uint8
-                    or not workspace.is_contiguous()):
-                _misfit("workspace", workspace)
-            ws, size = workspace.data_ptr(), workspace.numel()
-        dv_cache_attention(self.address, n, t, tp, o, at, dtype, q.data_ptr(), qs, rows, heads,
-                           max_rows, d ** -0.5 if scale is None else scale, causal, out.data_ptr(), os,
-                           ws, size, _raw_stream(index))
+            ws, size = self._given(workspace)
+        scale = d ** -0.5 if scale is None else scale
+        if window:
+            dv_cache_attention_window(self.address, n, t, tp, o, at, dtype, q.data_ptr(), qs, rows,
+                                      heads, max_rows, scale, causal, window, sinks, out.data_ptr(),
+                                      os, ws, size, _raw_stream(index))
+        else:
+            dv_cache_attention(self.address, n, t, tp, o, at, dtype, q.data_ptr(), qs, rows, heads,
+                               max_rows, scale, causal, out.data_ptr(), os, ws, size,
+                               _raw_stream(index))
         return out
 
+    def attention_shared(self, q, lengths, prefix_lengths, prefix_table, offsets=None, table=None,
+                         groups=None, causal=True, scale=None, max_rows=0, out=None, workspace=None,
+                         stream=None):
+        """Attention of rows q [rows, heads, head_dim] over the first prefix_lengths[g] places of the
+        prefix that their sequence's group g shares, and then over the first lengths[s] places of
+        their own (causal: the rows are the last of these, and see all of the prefix).  Prefix g lies
+        in the pages of its row of `prefix_table` (int32 [n_groups, prefix_table_pages]); `groups`
+        (int32 [n_groups + 1]) cuts the sequences into groups, None: all are one group.  The rest as
+        in `attention`; workspace: see attention_shared_workspace."""
+        index = self.index
+        if _elsewhere(index, stream):
+            with _Away(index, stream):
+                return self.attention_shared(q, lengths, prefix_lengths, prefix_table, offsets, table,
+                                             groups, causal, scale, max_rows, out, workspace)
+        n, t, tp, o, at = self._seqs(lengths, "lengths", offsets, table)
+        if q.dim() != 3:
+            _misfit("q", q)
+        if prefix_lengths.dim() != 1 or prefix_table.dim() != 2:
+            raise ValueError("prefix_lengths must have one dimension and prefix_table two")
+        ng, ptp = prefix_table.shape
+        if max(ng, ptp) > _INT_MAX:
+            raise ValueError("prefix_table has too many entries for one call")
+        pt, pat = _ints("prefix_table", prefix_table, index, (ng, ptp)), \
+            _ints("prefix_lengths", prefix_lengths, index, (ng,))
+        if groups is None and ng != 1:
+            raise ValueError(f"{ng} prefixes without groups")
+        gr = 0 if groups is None else _ints("groups", groups, index, (ng + 1,))
+        rows, heads, d = q.shape
+        shape = (rows, heads, self.head_dim)
+        qs = _rows("q", q, shape, q.dtype, index)
+        dtype = _dtype(q)
+        if out is None:
+            os = heads * d
+            out = _like(q, qs, os)
+        else:
+            os = _rows("out", out, shape, q.dtype, index)
+        if workspace is None:
+            size = self._scratch(dv_cache_attention_shared_workspace,
+                                 (n, tp, o != 0, ng, ptp, dtype, rows, heads, max_rows, 0))
+            workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+            ws = workspace.data_ptr()
+        else:
+            ws, size = self._given(workspace)
+        dv_cache_attention_shared(self.address, n, t, tp, o, at, ng, gr, pt, ptp, pat, dtype,
+                                  q.data_ptr(), qs, rows, heads, max_rows,
+                                  d ** -0.5 if scale is None else scale, causal, out.data_ptr(), os,
+                                  ws, size, _raw_stream(index))
+        return out
+
+    def _scratch(self, need, key):
+        """Workspace bytes of a call of these sizes (the length of the key tells the calls apart)."""
+        size = self.scratch.get(key)
+        if size is None:
+            size = need(self.address, *key[:9])
+            if len(self.scratch) >= 1024:
+                self.scratch.clear()
+            self.scratch[key] = size
+        return size
+
+    def _given(self, workspace):
+        if (workspace.get_device() != self.index or workspace.dtype is not torch.uint8
+                or not workspace.is_contiguous()):
+            _misfit("workspace", workspace)
+        return workspace.data_ptr(), workspace.numel()
+
     def attention_workspace(self, n_seqs, rows, heads, table_pages=None, with_offsets=True,
-                            max_rows=0, dtype=None):
+                            max_rows=0, dtype=None, window=0, sinks=0):
         """Bytes of scratch that `attention` needs for such a call (of rows of `dtype`; bf16)."""
         tp = self.pages // max(n_seqs, 1) if table_pages is None else table_pages
-        return dv_cache_attention_workspace(self.address, n_seqs, tp, with_offsets,
-                                            DV_F32 if dtype is torch.float32 else DV_BF16, rows,
+        dtype = DV_F32 if dtype is torch.float32 else DV_BF16
+        if window or sinks:
+            window, sinks = _window(window, sinks)
+            return dv_cache_attention_window_workspace(self.address, n_seqs, tp, with_offsets, dtype,
+                                                       rows, heads, max_rows, window, sinks)
+        return dv_cache_attention_workspace(self.address, n_seqs, tp, with_offsets, dtype, rows,
                                             heads, max_rows)
+
+    def attention_shared_workspace(self, n_seqs, rows, heads, prefix_table_pages, n_groups=1,
+                                   table_pages=None, with_offsets=True, max_rows=0, dtype=None):
+        """Bytes of scratch that `attention_shared` needs for such a call (of rows of `dtype`; bf16)."""
+        tp = self.pages // max(n_seqs, 1) if table_pages is None else table_pages
+        return dv_cache_attention_shared_workspace(self.address, n_seqs, tp, with_offsets, n_groups,
+                                                   prefix_table_pages,
+                                                   DV_F32 if dtype is torch.float32 else DV_BF16,
+                                                   rows, heads, max_rows)
