@@ -1620,9 +1620,9 @@ static CacheAttnArgs attention_args(const dv_cache* cache, int n_seqs, const int
 }
 
 static CacheAttnPlan plan_of(const dv_cache* c, int n_seqs, int table_pages, bool offsets, int dtype, int rows, int q_heads,
-                             int max_rows, int window = 0, int sinks = 0, bool part = false) {
+                             int max_rows, int window = 0, int sinks = 0) {
     return cache_attn_plan(dtype == DV_BF16, n_seqs, rows, offsets, max_rows, table_pages, c->page_tokens, c->kv_heads,
-                           q_heads, c->head_dim, device_cus(), window, sinks, part);
+                           q_heads, c->head_dim, device_cus(), window, sinks);
 }
 
 static const int32_t SOME_TABLE = 0;   // a workspace's size does not depend on what a table holds
@@ -1702,8 +1702,14 @@ static int check_groups(const dv_cache* cache, int n_groups, int prefix_table_pa
         return fail(DV_EINVAL, "prefix_table_pages %d: more than 2^30 tokens a prefix", prefix_table_pages);
     return check_queries(cache, n_groups, rows, q_heads, 0);
 }
-static CacheAttnPlan prefix_plan(const dv_cache* c, int n_groups, int table_pages, int dtype, int rows, int q_heads) {
-    return plan_of(c, n_groups, table_pages, true, dtype, rows, q_heads, n_groups == 1 ? rows : 0, 0, 0, true);
+static int shared_plan(const dv_cache* c, int n_seqs, int table_pages, bool offsets, int n_groups, int prefix_table_pages, int dtype,
+                       int rows, int q_heads, int max_rows, CacheSharedPlan* p) {
+    *p = cache_shared_plan(dtype == DV_BF16, n_seqs, rows, offsets, max_rows, table_pages, n_groups, prefix_table_pages,
+                           c->page_tokens, c->kv_heads, q_heads, c->head_dim, device_cus());
+    if (p->blocks * 256 > MAX_THREADS)
+        return fail(DV_EINVAL, "%d rows of %d heads in %d sequences and %d groups are too many for one call", rows, q_heads, n_seqs,
+                    n_groups);
+    return DV_OK;
 }
 
 int dv_cache_attention_shared_workspace(const dv_cache* cache, int n_seqs, int table_pages, int with_offsets, int n_groups,
@@ -1715,8 +1721,11 @@ int dv_cache_attention_shared_workspace(const dv_cache* cache, int n_seqs, int t
     if (rc || (rc = check_dtype(dtype)) || (rc = check_queries(cache, n_seqs, rows, q_heads, max_rows)) ||
         (rc = check_groups(cache, n_groups, prefix_table_pages, rows, q_heads)))
         return rc;
-    *bytes = plan_of(cache, n_seqs, table_pages, with_offsets != 0, dtype, rows, q_heads, max_rows, 0, 0, true).bytes +
-             prefix_plan(cache, n_groups, prefix_table_pages, dtype, rows, q_heads).bytes;
+    CacheSharedPlan p;
+    if ((rc = shared_plan(cache, n_seqs, table_pages, with_offsets != 0, n_groups, prefix_table_pages, dtype, rows, q_heads,
+                          max_rows, &p)))
+        return rc;
+    *bytes = p.bytes;
     return DV_OK;
 }
 
@@ -1731,9 +1740,11 @@ int dv_cache_attention_shared(const dv_cache* cache, int n_seqs, const int32_t* 
     if (rc || (rc = check_groups(cache, n_groups, prefix_table_pages, rows, q_heads))) return rc;
     if (!prefix_table || !prefix_lengths) return fail(DV_EINVAL, "NULL argument");
     if (!groups && n_groups != 1) return fail(DV_EINVAL, "groups is NULL: that is one group, not %d", n_groups);
-    const CacheAttnPlan p = plan_of(cache, n_seqs, table_pages, offsets != nullptr, dtype, rows, q_heads, max_rows, 0, 0, true);
-    const CacheAttnPlan pre = prefix_plan(cache, n_groups, prefix_table_pages, dtype, rows, q_heads);
-    if ((rc = check_workspace(p.bytes + pre.bytes, workspace, workspace_bytes))) return rc;
+    CacheSharedPlan p;
+    if ((rc = shared_plan(cache, n_seqs, table_pages, offsets != nullptr, n_groups, prefix_table_pages, dtype, rows, q_heads,
+                          max_rows, &p)) ||
+        (rc = check_workspace(p.bytes, workspace, workspace_bytes)))
+        return rc;
     if (rows == 0) return DV_OK;
     SeqArgs prefix = {n_groups, prefix_table_pages, rows, prefix_table, offsets, prefix_lengths};
     prefix.by_group = 1;
@@ -1742,7 +1753,7 @@ int dv_cache_attention_shared(const dv_cache* cache, int n_seqs, const int32_t* 
     launch_cache_shared(dtype == DV_BF16,
                         attention_args(cache, n_seqs, table, table_pages, offsets, lengths, q, q_stride, rows, q_heads, scale,
                                        causal, out, out_stride),
-                        prefix, p, pre, (float*)workspace, stream);
+                        prefix, p.own, p.prefix, (float*)workspace, stream);
     HIP_TRY(hipGetLastError());
     return DV_OK;
 }

@@ -217,23 +217,26 @@ __device__ __forceinline__ void store4(void* out, size_t at, f32x4 x) {
 
 // One tile, head and split of the keys per block; its wavefronts take the steps of the split in turn and
 // join their results through LDS.
+template <int DH>
+struct Small {
+    float o[WAVES][TR][DH + 4], m[WAVES][TR], l[WAVES][TR];
+};
+// Block bx of a split's, by: the split.
 template <int DH, bool BF, int KEYS>
-__device__ __forceinline__ void attend_small(const CacheAttnArgs& a) {
+__device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& lds, unsigned bx, unsigned by) {
     constexpr int NT = BF ? 1 : 3;             // bf16 terms of queries
     constexpr int PT = BF ? 2 : 3;             // ... of probabilities
     constexpr int KS = (DH + 31) / 32;         // 32-channel steps of S^T
     constexpr int CT = DH / 16;                // 16-channel tiles of O^T
     constexpr bool WIDE = DH % 64 == 0;        // 16-byte key loads
-    __shared__ float s_o[WAVES][TR][DH + 4];
-    __shared__ float s_m[WAVES][TR], s_l[WAVES][TR];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int H = a.c.kv_heads, pt = a.c.page_tokens, shift = page_shift(pt);
-    const int h = blockIdx.x % H;
-    const long long u = blockIdx.x / H;
+    const int h = bx % H;
+    const long long u = bx / H;
     const Tile t = tile_at<TS, KEYS>(a, u);
     if (t.seq < 0) return;
-    const int k0 = blockIdx.y * a.few.chunk, k1 = min(t.end - t.left_out, k0 + a.few.chunk);
-    if (blockIdx.y > 0 && k0 >= k1) return;    // the first split also writes rows that see no key
+    const int k0 = by * a.few.chunk, k1 = min(t.end - t.left_out, k0 + a.few.chunk);
+    if (by > 0 && k0 >= k1) return;    // the first split also writes rows that see no key
     const int kend = KEYS == WINDOW ? t.end : k1;   // (splits end with a step)
     const int G = a.q_heads / H;
     const int g = lane >> 4, c16 = lane & 15;
@@ -443,26 +446,26 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a) {
 
     // join the wavefronts
     l = group_sum(l);
-    if (g == 0) s_m[wave][c16] = m, s_l[wave][c16] = l;
+    if (g == 0) lds.m[wave][c16] = m, lds.l[wave][c16] = l;
 #pragma unroll
-    for (int c = 0; c < CT; ++c) *(f32x4*)&s_o[wave][c16][c * 16 + g * 4] = o[c];
+    for (int c = 0; c < CT; ++c) *(f32x4*)&lds.o[wave][c16][c * 16 + g * 4] = o[c];
     __syncthreads();
     const bool whole = KEYS != PART && t.end - t.left_out <= a.few.chunk;      // no other split has keys
-    float* part = a.few.part + (((size_t)u * H + h) * a.few.splits + blockIdx.y) * part_floats(TR, DH);
+    float* part = a.few.part + (((size_t)u * H + h) * a.few.splits + by) * part_floats(TR, DH);
     for (int i = tid; i < TR * (DH / 4); i += 256) {
         const int row = i / (DH / 4), ch = i % (DH / 4) * 4;
         if (row >= t.rows) break;
-        float top = s_m[0][row];
+        float top = lds.m[0][row];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_m[w][row]);
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, lds.m[w][row]);
         const float ref = top == -INFINITY ? 0.f : top;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float f = __builtin_amdgcn_exp2f((s_m[w][row] - ref) * sl2);
-            sum += s_l[w][row] * f;
-            x += *(const f32x4*)&s_o[w][row][ch] * f;
+            const float f = __builtin_amdgcn_exp2f((lds.m[w][row] - ref) * sl2);
+            sum += lds.l[w][row] * f;
+            x += *(const f32x4*)&lds.o[w][row][ch] * f;
         }
         if (whole) {
             const int pr = t.first + row;
@@ -497,21 +500,19 @@ struct Lds {
 
 // ONE: a step lies in one page (64 or 128 tokens), whose address is scalar then.
 template <int DH, bool ONE, int KEYS>
-__device__ __forceinline__ void attend_large(const CacheAttnArgs& a) {
+__device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& lds, unsigned bx, unsigned by) {
     constexpr int KS = DH / 16;                      // 16-channel steps of S^T
     constexpr int CB = (DH + 31) / 32;               // 32-channel blocks of O^T
     constexpr int PARTS = DH / 16;                   // 16-byte parts of a key
     constexpr int NL = (STEP * PARTS + 255) / 256;   // parts a thread copies of each of keys and values
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    Lds<DH>& lds = *(Lds<DH>*)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hl = lane >> 5, lr = lane & 31;
     const int H = a.c.kv_heads, pt = a.c.page_tokens, shift = page_shift(pt);
-    const int h = blockIdx.x % H;
-    const long long u = a.many.slots - 1 - blockIdx.x / H;   // a sequence's last rows, with the most keys, first
+    const int h = bx % H;
+    const long long u = a.many.slots - 1 - bx / H;   // a sequence's last rows, with the most keys, first
     const Tile t = tile_at<LS, KEYS>(a, u);
     if (t.seq < 0) return;
-    const int k0 = blockIdx.y * a.many.chunk, k1 = min(t.end - t.left_out, k0 + a.many.chunk);
-    if (blockIdx.y > 0 && k0 >= k1) return;
+    const int k0 = by * a.many.chunk, k1 = min(t.end - t.left_out, k0 + a.many.chunk);
+    if (by > 0 && k0 >= k1) return;
     const int kend = KEYS == WINDOW ? t.end : k1;
     const int G = a.q_heads / H;
     const float sl2 = exponent_factor(a.scale);
@@ -780,7 +781,7 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a) {
     const int row = mine + lr - t.first;
     if (row >= t.rows) return;
     const bool whole = KEYS != PART && t.end - t.left_out <= a.many.chunk;
-    float* part = a.many.part + (((size_t)u * H + h) * a.many.splits + blockIdx.y) * part_floats(LR, DH);
+    float* part = a.many.part + (((size_t)u * H + h) * a.many.splits + by) * part_floats(LR, DH);
     const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
 #pragma unroll
     for (int c = 0; c < CB; ++c)

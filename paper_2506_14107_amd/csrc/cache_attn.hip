@@ -7,11 +7,13 @@ namespace {
 
 template <int DH, bool BF>
 __global__ __launch_bounds__(256, 2) void cache_attn_k(CacheAttnArgs a) {
-    attend_small<DH, BF, ALL>(a);
+    __shared__ Small<DH> lds;
+    attend_small<DH, BF, ALL>(a, lds, blockIdx.x, blockIdx.y);
 }
 template <int DH, bool ONE>
 __global__ __launch_bounds__(256, 2) void cache_attn_tile_k(CacheAttnArgs a) {
-    attend_large<DH, ONE, ALL>(a);
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    attend_large<DH, ONE, ALL>(a, *(Lds<DH>*)smem, blockIdx.x, blockIdx.y);
 }
 template <bool BF, int SHIFT, int W>
 __global__ __launch_bounds__(256) void cache_join_k(CacheAttnArgs a) {

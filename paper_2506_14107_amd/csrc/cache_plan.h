@@ -183,11 +183,10 @@ constexpr int MAX_SPLITS = 512;
 // partial results: per tile of R rows, head and split R rows of dh fp32, R maxima, R sums
 __host__ __device__ inline size_t part_floats(int R, int dh) { return (size_t)R * (dh + 2); }
 
-// window > 0: rows see at most that many keys before their own place and `sinks` first ones.  part: every result is left as a
-// partial one.
+// window > 0: rows see at most that many keys before their own place and `sinks` first ones.
 inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets, int max_rows, int table_pages,
                                      int page_tokens, int kv_heads, int q_heads, int head_dim, int cus, int window = 0,
-                                     int sinks = 0, bool part = false) {
+                                     int sinks = 0) {
     CacheAttnPlan p{};
     const int G = q_heads / kv_heads;
     const long long unit = cus > 0 ? cus : 256;
@@ -234,12 +233,58 @@ inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets
         c.chunk = (int)((chunk + 255) / 256 * 256);
         c.splits = (int)std::max(1ll, (keys + c.chunk - 1) / c.chunk);
         c.tile_rows = (int)std::min<long long>(1 << shift, std::max(1ll, most_rows * G));
-        return c.splits > 1 || part ? (size_t)c.slots * kv_heads * c.splits * part_floats(1 << shift, head_dim) : 0;
+        return c.splits > 1 ? (size_t)c.slots * kv_heads * c.splits * part_floats(1 << shift, head_dim) : 0;
     };
     if (p.route != ATTN_MANY) p.few_floats = cut(p.few, TS, 2048, (bf ? 1 << 17 : 1 << 16) / head_dim);
     size_t many = 0;
     if (p.route != ATTN_FEW) many = cut(p.many, LS, held, 512);
     p.bytes = (p.few_floats + many) * sizeof(float);
+    return p;
+}
+
+// Two plans of a call with shared prefixes: its sequences' own keys, taken as without prefixes, and the prefixes', whose
+// sequences are the groups (rows: all of the call's).  Every result is left as a partial one for the join, so that more
+// splits cost no launch.
+struct CacheSharedPlan {
+    CacheAttnPlan own, prefix;
+    size_t bytes;
+    long long blocks;   // of the launch that takes both
+};
+inline CacheSharedPlan cache_shared_plan(bool bf, int n_seqs, int rows, bool offsets, int max_rows, int table_pages,
+                                         int n_groups, int prefix_table_pages, int page_tokens, int kv_heads, int q_heads,
+                                         int head_dim, int cus) {
+    CacheSharedPlan p{};
+    const int G = q_heads / kv_heads;
+    const long long unit = cus > 0 ? cus : 256;
+    p.own = cache_attn_plan(bf, n_seqs, rows, offsets, max_rows, table_pages, page_tokens, kv_heads, q_heads, head_dim, cus);
+    // Large tiles take prefixes of many rows and keys: us of a call, small / large, one group of 64, 96, 128, 256, 1024 packed rows; 8
+    // heads of 128, 65,536 keys 59 / 52, 84 / 56, 99 / 61, 186 / 99, 709 / 305, 16,384 28 / 31, 33 / 34, 37 / 37, 60 / 49, 202 /
+    // 112, 4096 19 / 18, 20 / 20, 21 / 22, 29 / 31, 81 / 63; 8 of 80, 65,536 42 / 50, 60 / 55, 69 / 60, 123 / 98, 427 / 259, 16,384
+    // 22 / 29, 28 / 34, 33 / 39, 53 / 58, 126 / 98.  Where groups differ each goes to its kernel (few_rows).
+    const long long packed = (long long)rows * G, keys = (long long)prefix_table_pages * page_tokens;
+    const bool large = bf && packed >= 64ll * n_groups && (double)packed * keys * kv_heads * head_dim >= 3e9;
+    p.prefix.route = !large ? ATTN_FEW : n_groups == 1 ? ATTN_MANY : ATTN_BOTH;
+    // `most` blocks fill the chip; splits end with a step of 64 keys and hold four of them at least
+    auto cut = [&](CacheAttnCut& c, int shift, int n, long long held, bool ragged, long long row_most, long long most) {
+        c.slots = tile_slots(ragged, n, rows, G, shift);
+        if (ragged && n == 1) c.slots = std::max(1ll, (packed + (1 << shift) - 1) >> shift);   // rows lie side by side
+        const long long units = std::max(1ll, c.slots * kv_heads), splits = std::min<long long>(MAX_SPLITS, std::max(1ll, most / units));
+        c.chunk = (int)((std::max((held + splits - 1) / splits, 256ll) + 63) / 64 * 64);
+        c.splits = (int)std::max(1ll, (held + c.chunk - 1) / c.chunk);
+        c.tile_rows = (int)std::min<long long>(1 << shift, std::max(1ll, row_most * G));
+        p.blocks += units * c.splits;
+        return (size_t)units * c.splits * part_floats(1 << shift, head_dim);
+    };
+    auto both = [&](CacheAttnPlan& x, int n, long long held, bool ragged, long long row_most) {
+        // groups or sequences of different lengths leave some of their splits empty (12 questions about three clips of up to
+        // 2056 keys in fp32: 16.7 us with two blocks a unit, 13.4 with four; one group of 32 packed rows over 100,003 keys 52, 57)
+        x.few_floats = x.route == ATTN_MANY ? 0 : cut(x.few, TS, n, held, ragged, row_most, (n > 1 ? 4 : 2) * unit);
+        const size_t many = x.route == ATTN_FEW ? 0 : cut(x.many, LS, n, held, ragged, row_most, 2 * unit);
+        x.bytes = (x.few_floats + many) * sizeof(float);
+        p.bytes += x.bytes;
+    };
+    both(p.own, n_seqs, (long long)table_pages * page_tokens, offsets, !offsets ? 1 : max_rows > 0 ? std::min(max_rows, rows) : rows);
+    both(p.prefix, n_groups, keys, true, rows);
     return p;
 }
 

@@ -7,27 +7,41 @@ namespace dv {
 
 namespace {
 
-template <int DH, bool BF>
-__global__ __launch_bounds__(256, 2) void cache_part_k(CacheAttnArgs a) {
-    attend_small<DH, BF, PART>(a);
+// Both parts of a call in one launch: blocks of the prefixes' tiles, then of the sequences' own, large ones first.
+struct SharedArgs {
+    CacheAttnArgs part[2];   // the sequences' own keys, the prefixes'
+    unsigned first[4];       // first block behind the prefixes' large tiles, their small ones, the sequences' large ones, all
+};
+struct Block {
+    int part;
+    bool large;
+    unsigned bx, by;
+};
+__device__ __forceinline__ Block block_of(const SharedArgs& a) {
+    const unsigned b = blockIdx.x;
+    const int i = (b >= a.first[0]) + (b >= a.first[1]) + (b >= a.first[2]);
+    const bool large = i % 2 == 0;
+    const CacheAttnArgs& x = a.part[i < 2];
+    const unsigned r = i ? b - a.first[i - 1] : b, wide = (unsigned)((large ? x.many.slots : x.few.slots) * x.c.kv_heads);
+    return {i < 2, large, r % wide, r / wide};
 }
 template <int DH, bool ONE>
-__global__ __launch_bounds__(256, 2) void cache_part_tile_k(CacheAttnArgs a) {
-    attend_large<DH, ONE, PART>(a);
+__global__ __launch_bounds__(256, 2) void cache_shared_k(SharedArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    const Block b = block_of(a);
+    const CacheAttnArgs& x = a.part[b.part];
+    if (b.large) attend_large<DH, ONE, PART>(x, *(Lds<DH>*)smem, b.bx, b.by);
+    else attend_small<DH, true, PART>(x, *(Small<DH>*)smem, b.bx, b.by);
 }
-struct PartKeys {
-    template <int DH, bool BF>
-    static constexpr auto small() { return cache_part_k<DH, BF>; }
-    template <int DH, bool ONE>
-    static constexpr auto large() { return cache_part_tile_k<DH, ONE>; }
-};
+template <int DH>
+__global__ __launch_bounds__(256, 2) void cache_shared_small_k(SharedArgs a, int f32) {
+    __shared__ Small<DH> lds;
+    const Block b = block_of(a);
+    const CacheAttnArgs& x = a.part[b.part];
+    if (f32) attend_small<DH, false, PART>(x, lds, b.bx, b.by);
+    else attend_small<DH, true, PART>(x, lds, b.bx, b.by);
+}
 
-// A tile's partial results in the splits of its cut.
-struct Splits {
-    const float* part;   // of the first split, this head's
-    size_t per;
-    int n, row, rows;    // splits, the row in the tile, the tile's rows
-};
 // Where a row's partial results over its prefix lie: group g has the row's sequence.
 struct Prefix {
     int g, row0, n, len, few0, many0;   // (its first slots of small and large tiles)
@@ -53,101 +67,221 @@ __device__ __forceinline__ Prefix prefix_of(const SeqArgs& q, int seq, int G, in
     return {-1, 0, 0, 0, 0, 0};
 }
 
-// Joins a tile's rows: the splits of their own keys (a) and of their group's prefix (pre).  A wavefront takes a row.
-template <bool BF, int SHIFT>
-__global__ __launch_bounds__(256) void cache_shared_join_k(CacheAttnArgs a, CacheAttnArgs pre) {
-    constexpr int R = 1 << SHIFT;
-    __shared__ f32x4 s_x[256];
+// The partial results of a tile's rows over their own keys and over their group's prefix, one list of splits.
+struct Parts {
+    const float *own, *pre;      // of the tile and head; of the head in the prefix's tiles
+    size_t per0, per1, tiles1;   // floats of a split, of a prefix's tile of all heads
+    int n0, n1, R, shift;
+    long long at0, slots;        // the tile's first packed row in its group (below 0: none), tiles of prefixes
+    int slot0, dh;
+    // of packed row `row` of the tile: where split s has its output and its maximum, how many splits there are
+    __device__ __forceinline__ bool behind(int row) const { return at0 >= 0 && slot0 + ((at0 + row) >> shift) < slots; }
+    __device__ __forceinline__ int splits(int row) const { return n0 + (behind(row) ? n1 : 0); }
+    __device__ __forceinline__ const float* split(int s, int row) const {
+        return s < n0 ? own + s * per0 : pre + (slot0 + ((at0 + row) >> shift)) * tiles1 + (s - n0) * per1;
+    }
+    __device__ __forceinline__ const float* output(int s, int row) const {
+        return split(s, row) + (s < n0 ? row : (int)((at0 + row) & ((1 << shift) - 1))) * dh;
+    }
+    __device__ __forceinline__ const float* maximum(int s, int row) const {   // the sum lies `rows(s)` floats behind
+        return split(s, row) + (s < n0 ? R * dh + row : (dh << shift) + (int)((at0 + row) & ((1 << shift) - 1)));
+    }
+    __device__ __forceinline__ int rows(int s) const { return s < n0 ? R : 1 << shift; }
+};
+template <int SHIFT>
+__device__ __forceinline__ Parts parts_of(const CacheAttnArgs& a, const CacheAttnArgs& pre, const Tile& t, long long u, int h) {
+    const int H = a.c.kv_heads, DH = a.c.head_dim, G = a.q_heads / H, limit = few_rows(DH);
     const CacheAttnCut& cut = SHIFT == TS ? a.few : a.many;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int H = a.c.kv_heads, DH = a.c.head_dim, G = a.q_heads / H;
-    const int h = blockIdx.x % H;
+    const Prefix p = prefix_of(pre.seq, t.seq, G, limit, pre.route);
+    const bool small = pre.route == ATTN_FEW || (pre.route == ATTN_BOTH && (long long)p.n * G <= limit);
+    const CacheAttnCut& pc = small ? pre.few : pre.many;
+    const int len = (int)min((long long)max(p.len, 0), (long long)pre.seq.table_pages * a.c.page_tokens);
+    Parts x;
+    x.shift = small ? TS : LS;
+    x.R = 1 << SHIFT;
+    x.dh = DH;
+    x.per0 = part_floats(x.R, DH), x.per1 = part_floats(1 << x.shift, DH);
+    x.own = cut.part + ((size_t)u * H + h) * cut.splits * x.per0;
+    x.tiles1 = (size_t)H * pc.splits * x.per1;
+    x.pre = pc.part + (size_t)h * pc.splits * x.per1;
+    x.n0 = max(1, (t.end + cut.chunk - 1) / cut.chunk);
+    x.n1 = max(1, (len + pc.chunk - 1) / pc.chunk);
+    x.at0 = p.g < 0 ? -1 : ((long long)t.row0 - p.row0) * G + t.first;
+    x.slots = pc.slots;
+    x.slot0 = small ? p.few0 : p.many0;
+    return x;
+}
+template <bool BF>
+__device__ __forceinline__ void store_row(const CacheAttnArgs& a, const Tile& t, int h, int row, int ch, f32x4 x, float sum) {
+    const int pr = t.first + row, G = a.q_heads / a.c.kv_heads;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    store4<BF>(a.out, (size_t)(t.row0 + pr / G) * a.o_stride + (size_t)(h * G + pr % G) * a.c.head_dim + ch, x * inv);
+}
+
+// Joins a tile's rows where no row has more than FEW splits: dh / 4 lanes take a row and hold all of it.
+constexpr int FEW = 8;
+template <bool BF, int SHIFT>
+__global__ __launch_bounds__(256) void cache_shared_join_few_k(SharedArgs args) {
+    const CacheAttnArgs &a = args.part[0], &pre = args.part[1];
+    const int tid = threadIdx.x, lane = tid & 63, H = a.c.kv_heads, h = blockIdx.x % H;
     const long long u = blockIdx.x / H;
     const Tile t = tile_at<SHIFT, PART>(a, u);
     if (t.seq < 0) return;
     const float sl2 = exponent_factor(a.scale);
-    const int limit = few_rows(DH);
-    const Prefix p = prefix_of(pre.seq, t.seq, G, limit, pre.route);
-    const bool small = pre.route == ATTN_FEW || (pre.route == ATTN_BOTH && (long long)p.n * G <= limit);
-    const int lanes = DH / 4, groups = 64 / lanes;        // of a wavefront
-    const int ch = lane % lanes * 4, grp = lane / lanes;
-    for (int row0 = blockIdx.y * 4; row0 < t.rows; row0 += gridDim.y * 4) {
-        const int row = min(row0 + wave, t.rows - 1), pr = t.first + row;
-        Splits list[2];
-        list[0] = {cut.part + ((size_t)u * H + h) * cut.splits * part_floats(R, DH), part_floats(R, DH),
-                   max(1, (t.end + cut.chunk - 1) / cut.chunk), row, R};
-        list[1] = {nullptr, 0, 0, 0, 0};
-        if (p.g >= 0) {
-            const CacheAttnCut& pc = small ? pre.few : pre.many;
-            const int shift = small ? TS : LS;
-            const long long at = ((long long)t.row0 + pr / G - p.row0) * G + pr % G, slot = (small ? p.few0 : p.many0) + (at >> shift);
-            const int len = (int)min((long long)max(p.len, 0), (long long)pre.seq.table_pages * a.c.page_tokens);
-            const size_t per = part_floats(1 << shift, DH);
-            if (at >= 0 && slot < pc.slots)
-                list[1] = {pc.part + ((size_t)slot * H + h) * pc.splits * per, per, max(1, (len + pc.chunk - 1) / pc.chunk),
-                           (int)(at & ((1 << shift) - 1)), 1 << shift};
-        }
-        float top = -INFINITY;
+    const Parts p = parts_of<SHIFT>(a, pre, t, u, h);
+    const int lanes = a.c.head_dim / 4, groups = 64 / lanes, ch = lane % lanes * 4, rows = 4 * groups;   // of a block
+    if (lane / lanes >= groups) return;
+    for (int row = blockIdx.y * rows + (tid >> 6) * groups + lane / lanes; row < t.rows; row += gridDim.y * rows) {
+        const int total = min(p.splits(row), FEW);
+        f32x4 y[FEW];
+        float m[FEW], l[FEW], top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 2; ++w)
-            for (int s = lane; s < list[w].n; s += 64)
-                top = fmaxf(top, list[w].part[s * list[w].per + list[w].rows * DH + list[w].row]);
+        for (int s = 0; s < FEW; ++s) {
+            if (s >= total) continue;
+            const float* at = p.maximum(s, row);
+            m[s] = at[0], l[s] = at[p.rows(s)];
+            y[s] = *(const f32x4*)(p.output(s, row) + ch);
+        }
+#pragma unroll
+        for (int s = 0; s < FEW; ++s) top = s < total ? fmaxf(top, m[s]) : top;
+        const float ref = top == -INFINITY ? 0.f : top;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int s = 0; s < FEW; ++s) {
+            if (s >= total) continue;
+            const float w = __builtin_amdgcn_exp2f((m[s] - ref) * sl2);
+            sum += l[s] * w;
+            x += y[s] * w;
+        }
+        store_row<BF>(a, t, h, row, ch, x, sum);
+    }
+}
+
+// ... any number of splits: a row takes W wavefronts of a block; every lane weighs one split in 64, then lanes go over the channels
+// and groups of lanes over the splits.
+template <bool BF, int SHIFT, int W>
+__global__ __launch_bounds__(256) void cache_shared_join_k(SharedArgs args) {
+    constexpr int ROWS = 4 / W, AHEAD = 8;   // loads asked for together
+    __shared__ f32x4 s_x[256];
+    const CacheAttnArgs &a = args.part[0], &pre = args.part[1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, H = a.c.kv_heads, h = blockIdx.x % H;
+    const long long u = blockIdx.x / H;
+    const Tile t = tile_at<SHIFT, PART>(a, u);
+    if (t.seq < 0) return;
+    const float sl2 = exponent_factor(a.scale);
+    const Parts p = parts_of<SHIFT>(a, pre, t, u, h);
+    const int lanes = a.c.head_dim / 4, groups = 64 / lanes;        // of a wavefront
+    const int ch = lane % lanes * 4, grp = lane / lanes;
+    // one round, unless a sequence has more rows than it was said to have
+    for (int row0 = blockIdx.y * ROWS; row0 < t.rows; row0 += gridDim.y * ROWS) {
+        const int row = min(row0 + wave / W, t.rows - 1), total = p.splits(row);
+        // the first splits' results are asked for before their weights are known
+        const int s1 = min(lane, total - 1), step = W * groups;
+        const float *m1 = p.maximum(s1, row), m = lane < total ? m1[0] : -INFINITY, l = m1[p.rows(s1)];
+        f32x4 y[AHEAD];
+        auto ask = [&](int i) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) y[k] = *(const f32x4*)(p.output(min(i + k * step, total - 1), row) + ch);
+        };
+        const int mine = wave % W * groups + grp;   // the lane's first split
+        ask(mine);
+        float top = m;
+        for (int s = lane + 64; s < total; s += 64) top = fmaxf(top, *p.maximum(s, row));
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
         const float ref = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f, w = lane < total ? __builtin_amdgcn_exp2f((m - ref) * sl2) : 0.f;
+        if (lane < total) sum = l * w;
+        for (int s0 = 0;;) {
+            const int n = min(64, total - s0);
+            for (int i = wave % W * groups; i < n; i += step * AHEAD) {
+                if (s0 + i > wave % W * groups) ask(s0 + i + grp);
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-            const Splits& l = list[v];
-            for (int s0 = 0; s0 < l.n; s0 += 64) {
-                const int s = s0 + lane, n = min(64, l.n - s0);
-                float w = 0.f;
-                if (s < l.n) {
-                    const float* ml = l.part + s * l.per + l.rows * DH + l.row;
-                    w = __builtin_amdgcn_exp2f((ml[0] - ref) * sl2);
-                    sum += ml[l.rows] * w;
-                }
-                const float* from = l.part + s0 * l.per + l.row * DH + ch;
-                for (int i = 0; i < n; i += groups) {
-                    const int j = i + grp;
+                for (int k = 0; k < AHEAD; ++k) {
+                    const int j = i + k * step + grp;
                     const float wj = __shfl(w, j & 63, 64);
-                    if (grp < groups && j < n) x += *(const f32x4*)(from + j * l.per) * wj;
+                    if (grp < groups && j < n) x += y[k] * wj;
                 }
             }
+            if ((s0 += 64) >= total) break;
+            const int s = min(s0 + lane, total - 1);
+            const float* at = p.maximum(s, row);
+            w = s0 + lane < total ? __builtin_amdgcn_exp2f((at[0] - ref) * sl2) : 0.f;
+            if (s0 + lane < total) sum += at[p.rows(s)] * w;
         }
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
         s_x[tid] = x;
         __syncthreads();
-        if (grp == 0 && row0 + wave < t.rows) {
-            for (int k = 1; k < groups; ++k) x += s_x[wave * 64 + k * lanes + lane];
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            store4<BF>(a.out, (size_t)(t.row0 + pr / G) * a.o_stride + (size_t)(h * G + pr % G) * DH + ch, x * inv);
+        if (wave % W == 0 && grp == 0 && row0 + wave / W < t.rows) {
+            for (int v = 0; v < W; ++v)
+                for (int k = v == 0; k < groups; ++k) x += s_x[(wave + v) * 64 + k * lanes + lane];
+            store_row<BF>(a, t, h, row, ch, x, sum);
         }
         __syncthreads();
     }
 }
 
 template <bool BF, int SHIFT>
-void launch_shared_join(const CacheAttnArgs& a, const CacheAttnArgs& pre, const CacheAttnCut& c, hipStream_t s) {
-    const dim3 grid((unsigned)(c.slots * a.c.kv_heads), (unsigned)((c.tile_rows + 3) / 4));
-    cache_shared_join_k<BF, SHIFT><<<grid, 256, 0, s>>>(a, pre);
+void launch_shared_join(const SharedArgs& a, const CacheAttnCut& c, hipStream_t s) {
+    const CacheAttnArgs& pre = a.part[1];
+    const int splits = c.splits + std::max(pre.route == ATTN_MANY ? 1 : pre.few.splits, pre.route == ATTN_FEW ? 1 : pre.many.splits);
+    const unsigned tiles = (unsigned)(c.slots * a.part[0].c.kv_heads);
+    const int rows = 4 * (64 / (a.part[0].c.head_dim / 4));
+    if (splits <= FEW) cache_shared_join_few_k<BF, SHIFT><<<dim3(tiles, (c.tile_rows + rows - 1) / rows), 256, 0, s>>>(a);
+    // us of 640 tiles of 4 rows in 33 splits: 11 with one wavefront a row, 17 with four; of 80 in 33: 8, 7
+    else if (splits <= 64) cache_shared_join_k<BF, SHIFT, 1><<<dim3(tiles, (c.tile_rows + 3) / 4), 256, 0, s>>>(a);
+    else cache_shared_join_k<BF, SHIFT, 4><<<dim3(tiles, c.tile_rows), 256, 0, s>>>(a);
+}
+
+template <int DH>
+void launch_shared(bool bf, const SharedArgs& a, hipStream_t s) {
+    const dim3 grid(a.first[3]);
+    if (a.part[0].route == ATTN_FEW && a.part[1].route == ATTN_FEW) {
+        cache_shared_small_k<DH><<<grid, 256, 0, s>>>(a, !bf);
+        return;
+    }
+    constexpr size_t lds = sizeof(Lds<DH>) > sizeof(Small<DH>) ? sizeof(Lds<DH>) : sizeof(Small<DH>);
+    auto go = [&](auto one) {
+        constexpr auto k = cache_shared_k<DH, decltype(one)::value>;
+        static const bool ok = allow_lds((const void*)k, lds);
+        (void)ok;
+        k<<<grid, 256, lds, s>>>(a);
+    };
+    if (a.part[0].c.page_tokens >= STEP) go(std::true_type());
+    else go(std::false_type());
 }
 
 }  // namespace
 
 void launch_cache_shared(bool bf, CacheAttnArgs a, const SeqArgs& prefix, const CacheAttnPlan& p, const CacheAttnPlan& pre,
                          float* workspace, hipStream_t s) {
-    CacheAttnArgs b = a;
-    b.seq = prefix;
-    b.causal = 0;
-    set_plan(a, p, workspace);
-    set_plan(b, pre, workspace + p.bytes / sizeof(float));
-    launch_parts<PartKeys>(bf, b, s);
-    launch_parts<PartKeys>(bf, a, s);
-    if (a.route != ATTN_MANY) bf ? launch_shared_join<true, TS>(a, b, a.few, s) : launch_shared_join<false, TS>(a, b, a.few, s);
-    if (a.route != ATTN_FEW) launch_shared_join<true, LS>(a, b, a.many, s);
+    SharedArgs x{{a, a}, {}};
+    x.part[1].seq = prefix;
+    x.part[1].causal = 0;
+    set_plan(x.part[0], p, workspace);
+    set_plan(x.part[1], pre, workspace + p.bytes / sizeof(float));
+    unsigned first = 0;
+    for (int i = 0; i < 4; ++i) {
+        const CacheAttnArgs& y = x.part[i < 2];
+        const CacheAttnCut& c = i % 2 ? y.few : y.many;
+        if (y.route != (i % 2 ? ATTN_MANY : ATTN_FEW)) first += (unsigned)(c.slots * y.c.kv_heads * c.splits);
+        x.first[i] = first;
+    }
+    switch (a.c.head_dim) {
+        case 16: launch_shared<16>(bf, x, s); break;
+        case 32: launch_shared<32>(bf, x, s); break;
+        case 48: launch_shared<48>(bf, x, s); break;
+        case 64: launch_shared<64>(bf, x, s); break;
+        case 80: launch_shared<80>(bf, x, s); break;
+        case 96: launch_shared<96>(bf, x, s); break;
+        case 112: launch_shared<112>(bf, x, s); break;
+        default: launch_shared<128>(bf, x, s); break;
+    }
+    if (p.route != ATTN_MANY) bf ? launch_shared_join<true, TS>(x, p.few, s) : launch_shared_join<false, TS>(x, p.few, s);
+    if (p.route != ATTN_FEW) launch_shared_join<true, LS>(x, p.many, s);
 }
 
 }  // namespace dv

@@ -51,7 +51,7 @@ def test_tiles_take_every_key_that_a_row_sees(lib, shift):
         window, sinks = rng.choice([1, 2, 63, 64, 65, 200, 1000, big]), rng.choice([0, 1, 63, 64, 65, 300, 5000, big])
         tp, pt = rng.choice([1, 30, 200]), 16
         length = min(length, tp * pt)
-        p = plan(lib, 1, 1, n, 1, rng.choice([0, 1, n]), tp, pt, 2, 2 * group, 64, 256, window, sinks, 0)
+        p = plan(lib, 1, 1, n, 1, rng.choice([0, 1, n]), tp, pt, 2, 2 * group, 64, 256, window, sinks)
         for first, rows, end, skip0, left_out in tiles(lib, n, length, tp, pt, group, shift, causal, window, sinks):
             assert skip0 % 64 == 0 and left_out % 64 == 0 and (left_out == 0 or skip0 + left_out < end)
             for i in range(first // group, (first + rows - 1) // group + 1):
@@ -66,28 +66,47 @@ def test_tiles_take_every_key_that_a_row_sees(lib, shift):
 
 def test_windows_are_cut_by_what_they_see(lib):
     """Splits and workspaces follow the window, not the table."""
-    short = plan(lib, 1, 64, 64, 1, 1, 200, 64, 8, 32, 128, 256, 2048, 257, 0)
-    long = plan(lib, 1, 64, 64, 1, 1, 200000, 64, 8, 32, 128, 256, 2048, 257, 0)
+    short = plan(lib, 1, 64, 64, 1, 1, 200, 64, 8, 32, 128, 256, 2048, 257)
+    long = plan(lib, 1, 64, 64, 1, 1, 200000, 64, 8, 32, 128, 256, 2048, 257)
     assert short == long
-    assert plan(lib, 1, 64, 64, 1, 1, 200, 64, 8, 32, 128, 256, 1 << 30, 0, 0) == \
-        plan(lib, 1, 64, 64, 1, 1, 200, 64, 8, 32, 128, 256, 0, 0, 0)
+    assert plan(lib, 1, 64, 64, 1, 1, 200, 64, 8, 32, 128, 256, 1 << 30, 0) == \
+        plan(lib, 1, 64, 64, 1, 1, 200, 64, 8, 32, 128, 256, 0, 0)
 
 
 @pytest.mark.parametrize("bf16", [0, 1])
-def test_partial_results_have_room(lib, bf16):
-    """Calls whose results are joined with others' leave them in the workspace, in one split or more."""
+def test_shared_calls_are_cut(lib, bf16):
+    """Splits cover every key that a table can hold, slots every row whichever way it falls into groups, the workspace a
+    partial result for every tile, head and split."""
     rng = random.Random(5)
-    for _ in range(2000):
+    for _ in range(3000):
         n, heads, group = rng.choice([1, 2, 64, 300]), rng.choice([1, 2, 8, 40]), rng.choice([1, 4, 16])
-        pt, dh = rng.choice([16, 64, 128]), rng.choice([16, 64, 128])
-        tp = min((1 << 30) // pt, int(2 ** rng.uniform(0, 22)))
-        rows = rng.choice([n, 5 * n, int(2 ** rng.uniform(0, 16))])
-        p = plan(lib, bf16, n, rows, 1, rng.choice([0, rows]), tp, pt, heads, heads * group, dh, 256, 0, 0, 1)
-        need = 0
-        for chunk, splits, slots, tile in ((*p[1:4], 16), (*p[4:7], 128)):
-            assert not splits or chunk * splits >= tp * pt
-            need += slots * heads * splits * tile * (dh + 2) * 4
-        assert p[7] == need
+        pt, dh, ng = rng.choice([16, 64, 128]), rng.choice([16, 64, 128]), rng.choice([1, 1, 2, 30])
+        tables = [min((1 << 30) // pt, int(2 ** rng.uniform(0, 22))) for _ in range(2)]
+        offsets = rng.random() < 0.7
+        rows = rng.choice([n, 5 * n, int(2 ** rng.uniform(0, 16))]) if offsets else n
+        out = (ctypes.c_longlong * 18)()
+        lib.t_shared_plan(bf16, n, rows, int(offsets), rng.choice([0, rows]), tables[0], ng, tables[1], pt, heads, heads * group, dh,
+                          256, out)
+        total = blocks = 0
+        for i, (k, seqs) in enumerate(((tables[0], n), (tables[1], ng))):
+            route, *cuts, size = out[8 * i:8 * i + 8]
+            need = 0
+            for (chunk, splits, slots), tile, off in ((cuts[:3], 16, 1), (cuts[3:], 128, 0)):
+                assert bool(splits) == (route != off) and (bf16 or tile == 16 or not splits)
+                if not splits:
+                    continue
+                assert chunk % 64 == 0 and chunk * splits >= k * pt > chunk * (splits - 1) and splits <= 512
+                if seqs == 1:
+                    assert slots >= -(-rows * group // tile)
+                elif i or offsets:      # each sequence may end with a part of a tile
+                    assert slots >= rows * group // tile + min(seqs, rows * group % tile + rows * group // tile)
+                else:
+                    assert slots == seqs * -(-group // tile)
+                need += slots * heads * splits * tile * (dh + 2) * 4
+                blocks += slots * heads * splits
+            assert size == need
+            total += need
+        assert out[16] == total and out[17] == blocks
 
 
 # ---- refusals ------------------------------------------------------------------------------------------

@@ -24,12 +24,26 @@ int t_window_tiles(int n, int length, int table_pages, int pt, int group, int sh
 
 // route; out: small tiles' chunk, splits, slots, large ones', workspace bytes
 int t_window_plan(int bf16, int n_seqs, int rows, int offsets, int max_rows, int table_pages, int page_tokens, int kv_heads,
-                  int q_heads, int head_dim, int cus, int window, int sinks, int part, long long* out) {
+                  int q_heads, int head_dim, int cus, int window, int sinks, long long* out) {
     const CacheAttnPlan p = cache_attn_plan(bf16 != 0, n_seqs, rows, offsets != 0, max_rows, table_pages, page_tokens, kv_heads,
-                                            q_heads, head_dim, cus, window, sinks, part != 0);
+                                            q_heads, head_dim, cus, window, sinks);
     const long long v[] = {p.few.chunk, p.few.splits, p.few.slots, p.many.chunk, p.many.splits, p.many.slots, (long long)p.bytes};
     for (int i = 0; i < 7; ++i) out[i] = v[i];
     return p.route;
+}
+
+// The plans of a call with shared prefixes, one after the other; then the bytes and blocks of both.
+void t_shared_plan(int bf16, int n_seqs, int rows, int offsets, int max_rows, int table_pages, int n_groups, int prefix_table_pages,
+                   int page_tokens, int kv_heads, int q_heads, int head_dim, int cus, long long* out) {
+    const CacheSharedPlan p = cache_shared_plan(bf16 != 0, n_seqs, rows, offsets != 0, max_rows, table_pages, n_groups,
+                                                prefix_table_pages, page_tokens, kv_heads, q_heads, head_dim, cus);
+    for (const CacheAttnPlan* x : {&p.own, &p.prefix}) {
+        const long long v[] = {x->route, x->few.chunk, x->few.splits, x->few.slots, x->many.chunk, x->many.splits, x->many.slots,
+                               (long long)x->bytes};
+        for (long long y : v) *out++ = y;
+    }
+    out[0] = (long long)p.bytes;
+    out[1] = p.blocks;
 }
 
 }  // extern "C"
