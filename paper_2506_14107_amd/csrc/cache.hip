@@ -24,9 +24,11 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // ---- rows ------------------------------------------------------------------------------------------
@@ -39,7 +41,7 @@ struct Elem<true> {
     using T = uint16_t;
 };
 
-// V consecutive channels as fp32 (V = 8: 16 or 32 bytes at once; V = 1: one element)
+// V consecutive channels as fp32 (V = 8 and 4: 16 or 8 bytes at once, or 16; V = 1: one element)
 template <bool BF, int V>
 __device__ __forceinline__ void load_ch(const void* base, size_t at, float (&x)[V]) {
     if constexpr (V == 8 && BF) {
@@ -51,6 +53,14 @@ __device__ __forceinline__ void load_ch(const void* base, size_t at, float (&x)[
         const f32x4 a = p[0], b = p[1];
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+    } else if constexpr (V == 4 && BF) {
+        const bf16x4 r = *(const bf16x4*)((const uint16_t*)base + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (float)r[i];
+    } else if constexpr (V == 4) {
+        const f32x4 r = *(const f32x4*)((const float*)base + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = r[i];
     } else if constexpr (BF) {
         x[0] = bf16_to_f32(((const uint16_t*)base)[at]);
     } else {
@@ -68,6 +78,10 @@ __device__ __forceinline__ void store_ch(void* base, size_t at, const float (&x)
         f32x4* p = (f32x4*)((float*)base + at);
         p[0] = (f32x4){x[0], x[1], x[2], x[3]};
         p[1] = (f32x4){x[4], x[5], x[6], x[7]};
+    } else if constexpr (V == 4 && BF) {
+        *(bf16x4*)((uint16_t*)base + at) = (bf16x4){(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+    } else if constexpr (V == 4) {
+        *(f32x4*)((float*)base + at) = (f32x4){x[0], x[1], x[2], x[3]};
     } else if constexpr (BF) {
         ((__bf16*)base)[at] = (__bf16)x[0];
     } else {
@@ -104,7 +118,7 @@ __device__ __forceinline__ void turn_cos_sin(int pos, uint64_t turn, float& c, f
 
 // An item is two groups of V channels of one row and head that the rotation mixes (or, past the turned
 // channels, leaves): items of the `dim` turned channels first.
-//   halves: channels o .. o + V - 1 with o + dim/2 ..; pairs (V = 8): 16 channels in a row, (V = 1): 2
+//   halves: channels o .. o + V - 1 with o + dim/2 ..; pairs: 2 V channels in a row
 // Either way the i-th item turns the V pairs from V i on.
 struct Item {
     int o0, o1;
@@ -119,9 +133,9 @@ __device__ __forceinline__ Item item_at(int dim, bool pairs, int i) {
 template <int V>
 __device__ __forceinline__ void turn_item(bool pairs, const float* cos, const float* sin, float (&a)[V], float (&b)[V]) {
     float c[V], s[V];
-    if constexpr (V == 8) {
+    if constexpr (V > 1) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < V / 4; ++i) {
             const f32x4 x = *(const f32x4*)(cos + 4 * i), y = *(const f32x4*)(sin + 4 * i);
 #pragma unroll
             for (int e = 0; e < 4; ++e) c[4 * i + e] = x[e], s[4 * i + e] = y[e];
@@ -229,6 +243,36 @@ __device__ __forceinline__ void store_chunk(void* base, size_t at, int dim, bool
         store_ch<BF, V>(base, at + it.o1, w);
     }
 }
+// The same in two steps, for loads that are asked for well before they are needed: the chunk as it lies in memory, and x.
+template <bool BF, int V>
+struct Raw {
+    using T = std::conditional_t<BF, std::conditional_t<V == 8, bf16x8, std::conditional_t<V == 4, bf16x4, __bf16>>,
+                                 std::conditional_t<V == 8, f32x8, std::conditional_t<V == 4, f32x4, float>>>;
+    T v[16 / V];   // item e's two groups at 2 e and 2 e + 1
+};
+template <bool BF, int V>
+__device__ __forceinline__ void load_raw(const void* base, size_t at, int dim, bool pairs, int c, Raw<BF, V>& r) {
+    using T = typename Raw<BF, V>::T;
+    const typename Elem<BF>::T* p = (const typename Elem<BF>::T*)base + at;
+#pragma unroll
+    for (int e = 0; e < 8 / V; ++e) {
+        const Item it = item_at<V>(dim, pairs, c * (8 / V) + e);
+        r.v[2 * e] = *(const T*)(p + it.o0);
+        r.v[2 * e + 1] = *(const T*)(p + it.o1);
+    }
+}
+template <bool BF, int V>
+__device__ __forceinline__ void unpack(const Raw<BF, V>& r, float (&x)[16]) {
+#pragma unroll
+    for (int e = 0; e < 16 / V; ++e)
+#pragma unroll
+        for (int f = 0; f < V; ++f) {
+            float y;
+            if constexpr (V > 1) y = (float)r.v[e][f];
+            else y = (float)r.v[e];
+            x[e % 2 * 8 + e / 2 * V + f] = y;
+        }
+}
 // ... turned where it is; cos and sin of its row
 template <int V>
 __device__ __forceinline__ void turn_chunk(int dim, bool pairs, int c, const float* cos, const float* sin, float (&x)[16]) {
@@ -250,27 +294,33 @@ __device__ __forceinline__ float sum_squares(const float (&x)[16]) {
     for (int e = 0; e < 16; ++e) s = fmaf(x[e], x[e], s);
     return s;
 }
-// ... normed; part: the sums of squares of the head's dh / 16 chunks, head h of the weight
+// ... normed; part: the sums of squares of the head's dh / 16 chunks; w: the weight's chunk, where there is one
 template <bool BF, int V>
-__device__ __forceinline__ void norm_chunk(const NormArgs& nm, const float* part, int dh, int h, int dim, bool pairs, int c,
-                                           float (&x)[16]) {
+__device__ __forceinline__ void load_weight(const NormArgs& nm, int dh, int h, int dim, bool pairs, int c, Raw<BF, V>& w) {
+    if (nm.weight) load_raw<BF, V>(nm.weight, nm.per_head ? (size_t)h * dh : 0, dim, pairs, c, w);
+}
+template <bool BF, int V>
+__device__ __forceinline__ void norm_chunk(const NormArgs& nm, const float* part, int dh, const Raw<BF, V>& w, float (&x)[16]) {
+    const int n = dh / 16;
     float sum = 0.f;
-    for (int i = 0; i < dh / 16; ++i) sum += part[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += i < n ? part[i] : 0.f;
+    for (int i = 8; i < n; ++i) sum += part[i];
     const float f = rsqrtf(sum / (float)dh + nm.eps);
-    float w[16];
     if (nm.weight) {
-        load_chunk<BF, V>(nm.weight, nm.per_head ? (size_t)h * dh : 0, dim, pairs, c, w);
+        float y[16];
+        unpack(w, y);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = x[e] * f * y[e];
     } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = 1.f;
+        for (int e = 0; e < 16; ++e) x[e] = x[e] * f;
     }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = x[e] * f * w[e];
 }
 
 // Rows row0 .. row0 + n - 1 of x (n at most ROT_ROWS), heads of a multiple of 16 channels normed and turned, to out (a block
 // of NT threads).  lds: ROT_LDS floats and NORM_ITEMS NT more.
-constexpr int NORM_ITEMS = 4;   // chunks of a thread at once
+constexpr int NORM_ITEMS = 2;   // chunks of a thread at once
 template <bool BF, int V, int NT>
 __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& rot, const NormArgs& nm, int row0, int n,
                                           float* lds) {
@@ -282,6 +332,7 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& r
     for (int first = 0; first < total; first += batch) {
         const int end = min(batch, total - first);
         float x[NORM_ITEMS][16];
+        Raw<BF, V> r[NORM_ITEMS], w[BF ? NORM_ITEMS : 1];   // (fp32 has no registers for weights ahead)
         int rr[NORM_ITEMS], hh[NORM_ITEMS], cc[NORM_ITEMS];
 #pragma unroll
         for (int k = 0; k < NORM_ITEMS; ++k) {
@@ -289,17 +340,23 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& r
             if (i >= end) continue;
             const int rest = (first + i) % per_row;
             rr[k] = (first + i) / per_row, hh[k] = rest / per_head, cc[k] = rest % per_head;
-            load_chunk<BF, V>(a.x, (size_t)(row0 + rr[k]) * a.x_stride + (size_t)hh[k] * a.dh, rot.dim, rot.pairs, cc[k], x[k]);
+            load_raw<BF, V>(a.x, (size_t)(row0 + rr[k]) * a.x_stride + (size_t)hh[k] * a.dh, rot.dim, rot.pairs, cc[k], r[k]);
+            if constexpr (BF) load_weight<BF, V>(nm, a.dh, hh[k], rot.dim, rot.pairs, cc[k], w[k]);
         }
 #pragma unroll
-        for (int k = 0; k < NORM_ITEMS; ++k)
-            if (tid + k * NT < end) part[tid + k * NT] = sum_squares(x[k]);
+        for (int k = 0; k < NORM_ITEMS; ++k) {
+            if (tid + k * NT >= end) continue;
+            unpack(r[k], x[k]);
+            part[tid + k * NT] = sum_squares(x[k]);
+        }
         __syncthreads();   // (the angles are there too)
 #pragma unroll
         for (int k = 0; k < NORM_ITEMS; ++k) {
             const int i = tid + k * NT;
             if (i >= end) continue;
-            norm_chunk<BF, V>(nm, part + i - cc[k], a.dh, hh[k], rot.dim, rot.pairs, cc[k], x[k]);
+            Raw<BF, V>& wk = w[BF ? k : 0];
+            if constexpr (!BF) load_weight<BF, V>(nm, a.dh, hh[k], rot.dim, rot.pairs, cc[k], wk);
+            norm_chunk<BF, V>(nm, part + i - cc[k], a.dh, wk, x[k]);
             turn_chunk<V>(rot.dim, rot.pairs, cc[k], cos + rr[k] * ld, sin + rr[k] * ld, x[k]);
             store_chunk<BF, V>(a.out, (size_t)(row0 + rr[k]) * a.out_stride + (size_t)hh[k] * a.dh, rot.dim, rot.pairs, cc[k],
                                x[k]);
@@ -396,8 +453,9 @@ __device__ __forceinline__ PagePart page_part(const SeqArgs& q, int pt, int page
 constexpr int MAX_ITEMS = 2;                    // items of 16 channels a thread and pass
 // WT threads a block (write_threads).  NORM: keys, queries or both are normed first.
 template <bool BF, int V, int WT, bool NORM>
-__global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
+__global__ __launch_bounds__(WT, NORM ? 3 : 4) void cache_write_k(WriteArgs a) {
     constexpr int PASS = MAX_ITEMS * WT;      // items of a pass: one head's, or more heads'
+    constexpr bool AHEAD = V > 1 && BF;   // (the others have no registers for it)
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ uint32_t s_most[WRITE_HEADS];
     __shared__ float s_scale[WRITE_HEADS], s_old[WRITE_HEADS];
@@ -432,41 +490,75 @@ __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
     // i / per_head for i < 2^10, per_head <= 2^10 (the error of the factor, below per_head, times i is below 2^20)
     const uint32_t by_head = ((1u << 20) + per_head - 1) / per_head;
 
+    // the thread's items of a pass: head, token, chunk
+    int hh[MAX_ITEMS], tt[MAX_ITEMS], cc[MAX_ITEMS];
+    auto place = [&](int k) {
+        const int i = tid + k * WT;
+        hh[k] = (int)(i * by_head >> 20);
+        const int rest = i - hh[k] * per_head;
+        tt[k] = div_by(rest, a.by_tok), cc[k] = rest - tt[k] * per_tok;
+    };
+    auto row_at = [&](int k, int h0) {
+        const int row = p.row0 + tt[k];
+        return (size_t)(a.row_idx ? a.row_idx[row] : row) * stride + (size_t)(h0 + hh[k]) * dh;
+    };
+    auto heads_from = [&](int h0) { return max(1, min(end - h0, PASS / per_head)); };
+    auto scale_of = [&](int h0, int hn) {
+        return keep > 0 && tid < hn ? (values ? a.c.v_scale : a.c.k_scale)[(size_t)p.page * H + h0 + tid] : 0.f;
+    };
+    // AHEAD: the rows and scales of a pass are asked for while the one before is computed
+    Raw<BF, V> raw[AHEAD ? MAX_ITEMS : 1];
+    float next = 0.f;
+    auto ask = [&](int h0) {
+        const int hn = heads_from(h0);
+        next = scale_of(h0, hn);
+#pragma unroll
+        for (int k = 0; k < MAX_ITEMS; ++k)
+            if (hh[k] < hn) load_raw<BF, V>(src, row_at(k, h0), dim, a.rot.pairs, cc[k], raw[k]);
+    };
+    if constexpr (AHEAD) {
+#pragma unroll
+        for (int k = 0; k < MAX_ITEMS; ++k) place(k);
+        ask(hg * a.heads);
+    }
     for (int h0 = hg * a.heads, hn; h0 < end; h0 += hn) {
-        hn = max(1, min(end - h0, PASS / per_head));
+        hn = heads_from(h0);
         float* scales = (values ? a.c.v_scale : a.c.k_scale) + (size_t)p.page * H + h0;
         uint8_t* codes = (values ? a.c.v : a.c.k) + ((size_t)p.page * H + h0) * pt * dh;
-        float old = 0.f;
-        if (tid < hn) {
-            s_most[tid] = 0;
-            if (keep > 0) old = scales[tid];
-        }
+        if (tid < hn) s_most[tid] = 0;
         // the pass's new values in registers
+        const float old = AHEAD ? next : scale_of(h0, hn);
         float x[MAX_ITEMS][16];
-        int hh[MAX_ITEMS], tt[MAX_ITEMS], cc[MAX_ITEMS];
 #pragma unroll
         for (int k = 0; k < MAX_ITEMS; ++k) {
-            const int i = tid + k * WT;
-            hh[k] = (int)(i * by_head >> 20);
-            const int rest = i - hh[k] * per_head;
-            tt[k] = div_by(rest, a.by_tok), cc[k] = rest - tt[k] * per_tok;
-            if (hh[k] >= hn) continue;
-            const int row = p.row0 + tt[k];
-            const size_t at = (size_t)(a.row_idx ? a.row_idx[row] : row) * stride + (size_t)(h0 + hh[k]) * dh;
-            load_chunk<BF, V>(src, at, dim, a.rot.pairs, cc[k], x[k]);
+            if constexpr (AHEAD) {
+                if (hh[k] < hn) unpack(raw[k], x[k]);
+            } else {
+                place(k);
+                if (hh[k] < hn) load_chunk<BF, V>(src, row_at(k, h0), dim, a.rot.pairs, cc[k], x[k]);
+            }
         }
+        if constexpr (AHEAD)
+            if (h0 + hn < end) ask(h0 + hn);
         const bool normed = NORM && !values && a.k_norm.on;
+        Raw<BF, V> weight[AHEAD ? MAX_ITEMS : 1];
         if (normed) {
 #pragma unroll
-            for (int k = 0; k < MAX_ITEMS; ++k)
-                if (hh[k] < hn) part[tid + k * WT] = sum_squares(x[k]);
+            for (int k = 0; k < MAX_ITEMS; ++k) {
+                if (hh[k] >= hn) continue;
+                if constexpr (AHEAD) load_weight<BF, V>(a.k_norm, dh, h0 + hh[k], dim, a.rot.pairs, cc[k], weight[k]);
+                part[tid + k * WT] = sum_squares(x[k]);
+            }
         }
         __syncthreads();   // s_most is cleared, the angles and the sums are there
 #pragma unroll
         for (int k = 0; k < MAX_ITEMS; ++k) {
             if (hh[k] >= hn) continue;
-            if (normed)
-                norm_chunk<BF, V>(a.k_norm, part + tid + k * WT - cc[k], dh, h0 + hh[k], dim, a.rot.pairs, cc[k], x[k]);
+            if (normed) {
+                Raw<BF, V>& w = weight[AHEAD ? k : 0];
+                if constexpr (!AHEAD) load_weight<BF, V>(a.k_norm, dh, h0 + hh[k], dim, a.rot.pairs, cc[k], w);
+                norm_chunk<BF, V>(a.k_norm, part + tid + k * WT - cc[k], dh, w, x[k]);
+            }
             turn_chunk<V>(dim, a.rot.pairs, cc[k], cos + tt[k] * ald, sin + tt[k] * ald, x[k]);
             float most = 0.f;   // a NaN does not count
 #pragma unroll
@@ -519,7 +611,16 @@ __global__ __launch_bounds__(WT, 4) void cache_write_k(WriteArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 w[e] = code4(x[k][4 * e] * inv, x[k][4 * e + 1] * inv, x[k][4 * e + 2] * inv, x[k][4 * e + 3] * inv);
-            if constexpr (V == 8) {
+            if constexpr (V == 4) {   // w[e] is group e / 2 of item e % 2
+                uint8_t* to = values ? tile + (hh[k] * p.n + tt[k]) * ld
+                                     : codes + ((size_t)hh[k] * pt + p.slot0 + tt[k]) * dh;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const Item it = item_at<4>(dim, a.rot.pairs, cc[k] * 2 + e);
+                    *(uint32_t*)(to + it.o0) = w[e];
+                    *(uint32_t*)(to + it.o1) = w[2 + e];
+                }
+            } else if constexpr (V == 8) {
                 const Item it = item_at<8>(dim, a.rot.pairs, cc[k]);
                 if (values) {
                     uint32_t* to = (uint32_t*)(tile + (hh[k] * p.n + tt[k]) * ld + it.o0);   // (o1 = o0 + 8)
@@ -676,7 +777,8 @@ __global__ __launch_bounds__(256) void cache_read_k(ReadArgs a) {
     }
 }
 
-bool aligned16(const void* p, size_t stride, size_t el) { return (uintptr_t)p % 16 == 0 && stride * el % 16 == 0; }
+bool aligned(size_t to, const void* p, size_t stride, size_t el) { return (uintptr_t)p % to == 0 && stride * el % to == 0; }
+bool aligned16(const void* p, size_t stride, size_t el) { return aligned(16, p, stride, el); }
 
 }  // namespace
 
@@ -696,22 +798,32 @@ void launch_rotary(bool bf, RotaryArgs a, hipStream_t s) {
 void launch_norm_rotary(bool bf, NormRotaryArgs a, hipStream_t s) {
     const size_t el = bf ? 2 : 4;
     const bool chunks = a.dh % 16 == 0 && a.dh <= 16 * NORM_ITEMS * 256;
-    const bool wide = chunks && a.rot.dim % 16 == 0 && aligned16(a.x, a.x_stride, el) &&
-                      aligned16(a.out, a.out_stride, el) && (uintptr_t)a.norm.weight % 16 == 0;
+    auto fits = [&](int v, size_t to) {   // v channels at once, loads of `to` bytes
+        return chunks && a.rot.dim % (2 * v) == 0 && aligned(to, a.x, a.x_stride, el) && aligned(to, a.out, a.out_stride, el) &&
+               (uintptr_t)a.norm.weight % to == 0;
+    };
     a.per_block = rows_a_block(a.heads, a.dh, chunks ? 8 : 1);
     const dim3 grid((unsigned)(((long long)a.rows + a.per_block - 1) / a.per_block));
-    if (wide) bf ? norm_rotary_k<true, 8><<<grid, 256, 0, s>>>(a) : norm_rotary_k<false, 8><<<grid, 256, 0, s>>>(a);
-    else if (chunks) bf ? norm_rotary_k<true, 1><<<grid, 256, 0, s>>>(a) : norm_rotary_k<false, 1><<<grid, 256, 0, s>>>(a);
-    else bf ? norm_rotary_k<true, 0><<<grid, 256, 0, s>>>(a) : norm_rotary_k<false, 0><<<grid, 256, 0, s>>>(a);
+    auto go = [&](auto v) {
+        constexpr int V = decltype(v)::value;
+        bf ? norm_rotary_k<true, V><<<grid, 256, 0, s>>>(a) : norm_rotary_k<false, V><<<grid, 256, 0, s>>>(a);
+    };
+    if (fits(8, 16)) go(std::integral_constant<int, 8>());
+    else if (fits(4, 4 * el)) go(std::integral_constant<int, 4>());
+    else if (chunks) go(std::integral_constant<int, 1>());
+    else go(std::integral_constant<int, 0>());
 }
 
 void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
     const size_t el = bf ? 2 : 4;
     const CacheView& c = a.c;
     const bool norm = a.k_norm.on || a.q_norm.on;
-    bool wide = a.rot.dim % 16 == 0 && aligned16(a.k, a.k_stride, el) && aligned16(a.v, a.v_stride, el) &&
-                (uintptr_t)a.k_norm.weight % 16 == 0 && (uintptr_t)a.q_norm.weight % 16 == 0;
-    if (a.q) wide = wide && aligned16(a.q, a.q_stride, el) && aligned16(a.q_out, a.qo_stride, el);
+    auto fits = [&](int v, size_t to) {   // v channels at once, loads of `to` bytes
+        return a.rot.dim % (2 * v) == 0 && aligned(to, a.k, a.k_stride, el) && aligned(to, a.v, a.v_stride, el) &&
+               (!a.q || (aligned(to, a.q, a.q_stride, el) && aligned(to, a.q_out, a.qo_stride, el))) &&
+               (uintptr_t)a.k_norm.weight % to == 0 && (uintptr_t)a.q_norm.weight % to == 0;
+    };
+    const bool wide = fits(8, 16);
     const int threads = write_threads(c.page_tokens, c.head_dim), pass = MAX_ITEMS * threads;
     const bool ragged = a.seq.offsets || a.seq.one;
     const long long slots = page_slots(ragged, a.seq.n_seqs, a.seq.rows, page_shift(c.page_tokens));
@@ -736,13 +848,19 @@ void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
             cache_write_k<B, V, 512, N><<<grid, 512, lds, s>>>(a);
         }
     };
-    auto go = [&](auto f, auto v) { norm ? launch(f, v, std::true_type()) : launch(f, v, std::false_type()); };
     using W8 = std::integral_constant<int, 8>;
+    using W4 = std::integral_constant<int, 4>;
     using W1 = std::integral_constant<int, 1>;
-    if (bf && wide) go(std::true_type(), W8());
-    else if (bf) go(std::true_type(), W1());
-    else if (wide) go(std::false_type(), W8());
-    else go(std::false_type(), W1());
+    auto go = [&](auto v, auto normed) { bf ? launch(std::true_type(), v, normed) : launch(std::false_type(), v, normed); };
+    if (norm) {
+        if (wide) go(W8(), std::true_type());
+        else if (fits(4, 4 * el)) go(W4(), std::true_type());
+        else go(W1(), std::true_type());
+    } else if (wide) {
+        go(W8(), std::false_type());
+    } else {
+        go(W1(), std::false_type());
+    }
 }
 
 void launch_cache_read(bool bf, ReadArgs a, hipStream_t s) {
