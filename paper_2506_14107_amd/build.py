@@ -13,7 +13,7 @@ SRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_lib")
 LIB = os.path.join(OUT_DIR, "libdejavu.so")
 SOURCES = ["api.hip", "rowops.hip", "gemm.hip", "attention.hip", "cache.hip",
-           "cache_attn.hip", "cache_window.hip", "cache_shared.hip", "cache_extend.hip", "probe.hip"]
+           "cache_attn.hip", "cache_window.hip", "cache_shared.hip", "cache_behind.hip", "cache_extend.hip", "probe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-fno-gpu-rdc",

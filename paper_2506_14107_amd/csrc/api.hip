@@ -1750,10 +1750,11 @@ int dv_cache_attention_shared(const dv_cache* cache, int n_seqs, const int32_t* 
     prefix.by_group = 1;
     prefix.grouped = n_seqs;
     prefix.groups = groups;
-    launch_cache_shared(dtype == DV_BF16,
-                        attention_args(cache, n_seqs, table, table_pages, offsets, lengths, q, q_stride, rows, q_heads, scale,
-                                       causal, out, out_stride),
-                        prefix, p.own, p.prefix, (float*)workspace, stream);
+    CacheAttnArgs a = attention_args(cache, n_seqs, table, table_pages, offsets, lengths, q, q_stride, rows, q_heads, scale,
+                                     causal, out, out_stride);
+    a.front = prefix;
+    if (p.behind) launch_cache_behind(dtype == DV_BF16, a, p.own, (float*)workspace, stream);
+    else launch_cache_shared(dtype == DV_BF16, a, prefix, p.own, p.prefix, (float*)workspace, stream);
     HIP_TRY(hipGetLastError());
     return DV_OK;
 }

@@ -38,8 +38,9 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // What the keys of a call are: all up to a row's own; those of a window and the first ones (the steps between the two are
-// left out: Tile::skip0); or a part of what the rows see, whose result is joined with another part's.
-enum Keys : int { ALL = 0, WINDOW = 1, PART = 2 };
+// left out: Tile::skip0); a part of what the rows see, whose result is joined with another part's; or those of a prefix in
+// another table and then the sequence's own.
+enum Keys : int { ALL = 0, WINDOW = 1, PART = 2, BEHIND = 3 };
 
 constexpr int TR = 1 << TS, LR = 1 << LS;   // packed rows of a tile
 constexpr int STEP = 64;                    // keys of a step
@@ -152,12 +153,12 @@ struct Odd {
         return x;
     }
 };
-__device__ __forceinline__ void find_odd(Odd& f, const CacheAttnArgs& a, int s, int h, int first, int last, int stride,
-                                         int base) {
+__device__ __forceinline__ void find_odd(Odd& f, const CacheAttnArgs& a, const SeqArgs& q, int s, int h, int first, int last,
+                                         int stride, int base) {
     const int pt = a.c.page_tokens, shift = page_shift(pt), DH = a.c.head_dim;
 #pragma unroll 1
     for (int key = first; key < last; ++key) {
-        const int page = page_of(a.seq.table, a.seq.table_pages, a.c.pages, s, key >> shift);
+        const int page = page_of(q.table, q.table_pages, a.c.pages, s, key >> shift);
         if (page < 0) continue;
         const size_t at = (size_t)page * a.c.kv_heads + h;
         const uint8_t* v = a.c.v + at * DH * pt + (key & (pt - 1));
@@ -185,23 +186,48 @@ __device__ __forceinline__ Tile tile_at(const CacheAttnArgs& a, long long u) {
     Tile t = tile_of(a.seq, a.c.page_tokens, G, SHIFT, a.causal != 0, s, u);
     if (other(s)) t.seq = -1;
     if constexpr (KEYS == WINDOW) leave_out(t, G, a.causal != 0, a.window, a.sinks);
+    if constexpr (KEYS == BEHIND) put_behind(t, a.front, a.c.page_tokens);
     return t;
 }
 // The key at place v of those that a tile takes (steps of 64 lie together).
 template <int KEYS>
 __device__ __forceinline__ int key_at(const Tile& t, int v) {
-    return KEYS == WINDOW && v >= t.skip0 ? v + t.left_out : v;
+    return (KEYS == WINDOW || KEYS == BEHIND) && v >= t.skip0 ? v + t.left_out : v;
 }
-// What the row that sees keys below `sees` sees of keys first .. last - 1 (find_odd).
+// Whether that is the prefix's.
 template <int KEYS>
-__device__ __forceinline__ void find_odd_seen(Odd& f, const CacheAttnArgs& a, int s, int h, int first, int last, int sees, int stride,
-                                              int base) {
-    last = min(last, sees);
+__device__ __forceinline__ bool in_front(const Tile& t, int v) {
+    return KEYS == BEHIND && v < t.skip0;
+}
+// Table entry and page of the key `off` places behind place v, both of one step (entry_of, page_from).
+template <int KEYS>
+__device__ __forceinline__ int entry_at(const CacheAttnArgs& a, const Tile& t, int shift, int v, int off) {
+    const int j = (key_at<KEYS>(t, v) + off) >> shift;
+    if constexpr (KEYS == BEHIND) {
+        const SeqArgs& q = a.front;
+        const int* own = a.seq.table ? a.seq.table + (long long)t.seq * a.seq.table_pages + min(j, a.seq.table_pages - 1) : a.seq.at;
+        return *(in_front<KEYS>(t, v) ? q.table + (long long)t.group * q.table_pages + min(j, q.table_pages - 1) : own);
+    }
+    return entry_of(a.seq, t.seq, j);
+}
+template <int KEYS>
+__device__ __forceinline__ int page_at(const CacheAttnArgs& a, const Tile& t, int shift, int v, int off, int entry) {
+    const int j = (key_at<KEYS>(t, v) + off) >> shift;
+    if (in_front<KEYS>(t, v)) return j < a.front.table_pages && (unsigned)entry < (unsigned)a.c.pages ? entry : -1;
+    return page_from(a.seq, a.c.pages, entry, t.seq, j);
+}
+// What the row that sees keys below `sees` sees of the step at place v, of keys before `last` (find_odd).
+template <int KEYS>
+__device__ __forceinline__ void find_odd_seen(Odd& f, const CacheAttnArgs& a, const Tile& t, int h, int v, int last, int sees,
+                                              int stride, int base) {
+    int first = key_at<KEYS>(t, v);
+    const bool front = in_front<KEYS>(t, v);
+    last = min(min(last, first + STEP), front ? t.front_len : sees);
     if constexpr (KEYS == WINDOW) {
-        find_odd(f, a, s, h, first, min(last, a.sinks), stride, base);
+        find_odd(f, a, a.seq, t.seq, h, first, min(last, a.sinks), stride, base);
         first = max(first, max(sees - a.window, a.sinks));
     }
-    find_odd(f, a, s, h, first, last, stride, base);
+    find_odd(f, a, front ? a.front : a.seq, front ? t.group : t.seq, h, first, last, stride, base);
 }
 
 template <bool BF>
@@ -237,7 +263,7 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
     if (t.seq < 0) return;
     const int k0 = by * a.few.chunk, k1 = min(t.end - t.left_out, k0 + a.few.chunk);
     if (by > 0 && k0 >= k1) return;    // the first split also writes rows that see no key
-    const int kend = KEYS == WINDOW ? t.end : k1;   // (splits end with a step)
+    const int kend = KEYS == WINDOW || KEYS == BEHIND ? t.end : k1;   // (splits end with a step)
     const int G = a.q_heads / H;
     const int g = lane >> 4, c16 = lane & 15;
     const float sl2 = exponent_factor(a.scale);
@@ -273,9 +299,7 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
         int k, v;
     };
     auto pages = [&](int v) {
-        const int kb = key_at<KEYS>(t, v);
-        return Pages{entry_of(a.seq, t.seq, (kb + (c16 >> 2) * 16) >> shift),
-                     entry_of(a.seq, t.seq, (kb + g * 16) >> shift)};
+        return Pages{entry_at<KEYS>(a, t, shift, v, (c16 >> 2) * 16), entry_at<KEYS>(a, t, shift, v, g * 16)};
     };
     uint32_t kw[4][KS][2];
     u32x4 vw[CT];
@@ -283,7 +307,7 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
     bool present = false;   // the lane's group of the step has a page
     auto load_keys = [&](int v, const Pages& pg) {
         const int kk = key_at<KEYS>(t, v) + (c16 >> 2) * 16;
-        const size_t page = (size_t)max(page_from(a.seq, a.c.pages, pg.k, t.seq, kk >> shift), 0) * H + h;
+        const size_t page = (size_t)max(page_at<KEYS>(a, t, shift, v, (c16 >> 2) * 16, pg.k), 0) * H + h;
         const uint8_t* base = a.c.k + (page * pt + (kk & (pt - 1)) + (c16 & 3)) * DH;
         ks = a.c.k_scale[page];
 #pragma unroll
@@ -308,7 +332,7 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
     };
     auto load_values = [&](int v, const Pages& pg) {
         const int kv = key_at<KEYS>(t, v) + g * 16;
-        const int p = page_from(a.seq, a.c.pages, pg.v, t.seq, kv >> shift);
+        const int p = page_at<KEYS>(a, t, shift, v, g * 16, pg.v);
         present = p >= 0;
         const size_t page = (size_t)max(p, 0) * H + h;
         const uint8_t* base = a.c.v + (page * DH + c16) * pt + (kv & (pt - 1));
@@ -358,7 +382,9 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
         __builtin_amdgcn_sched_barrier(0);
         // keys kv .. kv + 15 belong to the lane; those it does not see, and those of pages that are
         // not there, get -inf
-        const int live = present ? min(sees, kend) - kv : 0;
+        const bool front = in_front<KEYS>(t, kb);
+        const int until = front ? t.front_len : kend;
+        const int live = present ? min(front ? until : sees, until) - kv : 0;
         bool part = live < 16 || __builtin_bit_cast(uint32_t, vs) >= HUGE_SCALE;
         if constexpr (KEYS == WINDOW) part |= kv < low && kv + 16 > a.sinks;
         const bool some = __any(part);
@@ -371,7 +397,7 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
             }
             // values that no row of the tile sees may hold anything, and so may the scale of a page
             // that has none else: 0
-            const int there = present ? kend - kv : 0;
+            const int there = present ? until - kv : 0;
             if (there <= 0) vs = 1.f;
             const uint32_t odd = odd_codes(vs);
 #pragma unroll
@@ -434,10 +460,7 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
 
     if (__any(odds != 0)) {
         Odd found{};
-        for (kb = k0 + wave * STEP; kb < k1; kb += NEXT) {
-            const int key = key_at<KEYS>(t, kb);
-            find_odd_seen<KEYS>(found, a, t.seq, h, key, min(key + STEP, kend), sees, 16, g * 4);
-        }
+        for (kb = k0 + wave * STEP; kb < k1; kb += NEXT) find_odd_seen<KEYS>(found, a, t, h, kb, in_front<KEYS>(t, kb) ? t.front_len : kend, sees, 16, g * 4);
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
@@ -513,7 +536,7 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
     if (t.seq < 0) return;
     const int k0 = by * a.many.chunk, k1 = min(t.end - t.left_out, k0 + a.many.chunk);
     if (by > 0 && k0 >= k1) return;
-    const int kend = KEYS == WINDOW ? t.end : k1;
+    const int kend = KEYS == WINDOW || KEYS == BEHIND ? t.end : k1;
     const int G = a.q_heads / H;
     const float sl2 = exponent_factor(a.scale);
 
@@ -548,16 +571,14 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
         int k[NL], v;
     };
     auto pages = [&](int v) {
-        const int kb = key_at<KEYS>(t, v);
         Pages p;
         if constexpr (ONE) {
-            p.v = entry_of(a.seq, t.seq, kb >> shift);
+            p.v = entry_at<KEYS>(a, t, shift, v, 0);
             return p;
         }
 #pragma unroll
-        for (int n = 0; n < NL; ++n)
-            p.k[n] = entry_of(a.seq, t.seq, (kb + (tid + n * 256) / PARTS) >> shift);
-        p.v = entry_of(a.seq, t.seq, (kb + tid % 4 * 16) >> shift);
+        for (int n = 0; n < NL; ++n) p.k[n] = entry_at<KEYS>(a, t, shift, v, (tid + n * 256) / PARTS);
+        p.v = entry_at<KEYS>(a, t, shift, v, tid % 4 * 16);
         return p;
     };
     u32x4 kc[NL], vc[NL];
@@ -567,7 +588,7 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
     auto load = [&](int v, const Pages& p) {
         const int kb = key_at<KEYS>(t, v);
         if constexpr (ONE) {
-            const int page = page_from(a.seq, a.c.pages, __builtin_amdgcn_readfirstlane(p.v), t.seq, kb >> shift);
+            const int page = page_at<KEYS>(a, t, shift, v, 0, __builtin_amdgcn_readfirstlane(p.v));
             const size_t at = (size_t)max(page, 0) * H + h;
             const uint8_t* kbase = a.c.k + (at * pt + (kb & (pt - 1))) * DH;
             const uint8_t* vbase = a.c.v + at * DH * pt + (kb & (pt - 1));
@@ -583,7 +604,7 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
             return;
         }
         const int tok = kb + tid % 4 * 16;
-        const int vp = page_from(a.seq, a.c.pages, p.v, t.seq, tok >> shift);
+        const int vp = page_at<KEYS>(a, t, shift, v, tid % 4 * 16, p.v);
         vin = vp >= 0;
         const size_t vpage = (size_t)max(vp, 0) * H + h;
         const uint8_t* vbase = a.c.v + vpage * DH * pt + (tok & (pt - 1));
@@ -592,7 +613,7 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
         for (int n = 0; n < NL; ++n) {
             const int i = tid + n * 256;
             if (STEP * PARTS % 256 && i >= STEP * PARTS) break;
-            const size_t kpage = (size_t)max(page_from(a.seq, a.c.pages, p.k[n], t.seq, (kb + i / PARTS) >> shift), 0) * H + h;
+            const size_t kpage = (size_t)max(page_at<KEYS>(a, t, shift, v, i / PARTS, p.k[n]), 0) * H + h;
             kc[n] = *(const u32x4*)(a.c.k + (kpage * pt + ((kb + i / PARTS) & (pt - 1))) * DH + i % PARTS * 16);
             ksc[n] = a.c.k_scale[kpage];
             vc[n] = *(const u32x4*)(vbase + i / 4 * pt);
@@ -602,8 +623,10 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
         const int kb = key_at<KEYS>(t, v);
         if (tid < 4) lds.there[buf][tid] = vin;   // the four groups of the first channel
         // values past the keys that anyone sees, and of pages that are not there, are 0
-        const int there = vin ? kend - kb - tid % 4 * 16 : 0;
-        bool part = kb + STEP > min(ball, kend) || !vin;   // not all rows see all of it
+        const bool front = in_front<KEYS>(t, v);
+        const int until = front ? t.front_len : kend;
+        const int there = vin ? until - kb - tid % 4 * 16 : 0;
+        bool part = kb + STEP > min(front ? until : ball, until) || !vin;   // not all rows see all of it
         if constexpr (KEYS == WINDOW) part |= kb < blow && kb + STEP > a.sinks;
         if (there <= 0) vsc = 1.f;
 #pragma unroll
@@ -640,7 +663,8 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
         for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
     float m = -INFINITY, l = 0.f;
 
-    auto step = [&](int kb, int buf) {   // (kb: of the keys themselves)
+    auto step = [&](int v, int buf) {
+        const int kb = key_at<KEYS>(t, v);
         f32x16 sc[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -666,10 +690,12 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
         __builtin_amdgcn_sched_barrier(0);
         // element e of block b is key kb + 32 b + 16 (e / 8) + 8 hl + e % 8
         const uint32_t there = *(const uint32_t*)lds.there[buf];
-        bool some = kb + STEP > min(wall, kend) || there != 0x01010101u;
+        const bool front = in_front<KEYS>(t, v);
+        const int until = front ? t.front_len : kend;
+        bool some = kb + STEP > min(front ? until : wall, until) || there != 0x01010101u;
         if constexpr (KEYS == WINDOW) some |= kb < wlow && kb + STEP > a.sinks;
         if (some) {
-            const int live = min(sees, kend) - kb - 8 * hl;
+            const int live = min(front ? until : sees, until) - kb - 8 * hl;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -737,9 +763,9 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
 
     auto turn = [&](int v, int buf) {   // a wavefront takes the steps that some row of it sees
         const int kb = key_at<KEYS>(t, v);
-        bool any = kb < wend;
+        bool any = in_front<KEYS>(t, v) ? mine < t.first + t.rows : kb < wend;
         if constexpr (KEYS == WINDOW) any = any && (kb + STEP > wfrom || kb < a.sinks);
-        if (any) step(kb, buf);
+        if (any) step(v, buf);
     };
 
     if (tid == 0) lds.odd = k1;
@@ -764,13 +790,11 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
 
     if (lds.odd < k1) {
         Odd found{};
-        if constexpr (KEYS == WINDOW) {
-            for (int v = lds.odd; v < k1; v += STEP) {
-                const int key = key_at<KEYS>(t, v);
-                find_odd_seen<KEYS>(found, a, t.seq, h, key, min(key + STEP, kend), sees, 8, hl * 4);
-            }
+        if constexpr (KEYS == WINDOW || KEYS == BEHIND) {
+            for (int v = lds.odd; v < k1; v += STEP)
+                find_odd_seen<KEYS>(found, a, t, h, v, in_front<KEYS>(t, v) ? t.front_len : kend, sees, 8, hl * 4);
         } else {
-            find_odd(found, a, t.seq, h, lds.odd, min(sees, k1), 8, hl * 4);
+            find_odd(found, a, a.seq, t.seq, h, lds.odd, min(sees, k1), 8, hl * 4);
         }
 #pragma unroll
         for (int c = 0; c < CB; ++c)

@@ -108,6 +108,7 @@ struct Tile {
     int len;     // keys of the sequence
     int end;     // keys that the tile's last row sees
     int skip0, left_out;   // keys skip0 .. skip0 + left_out - 1, whole steps of 64, which no row of it sees
+    int group, front_len;  // behind a prefix: its group (-1: none) and the prefix's keys, in places 0 .. skip0 - 1 (left_out is -skip0)
 };
 __host__ __device__ inline long long tile_slots(bool offsets, int n_seqs, int rows, int group, int shift) {
     return offsets ? ((long long)rows * group >> shift) + n_seqs
@@ -116,7 +117,7 @@ __host__ __device__ inline long long tile_slots(bool offsets, int n_seqs, int ro
 // ... slot u, of sequence s (without offsets: of sequence u / tiles of a row)
 __host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int shift, bool causal, const Seq& sp,
                                         long long u) {
-    Tile t = {-1, 0, 0, 0, 0, 0, 0, 0, 0};
+    Tile t = {-1, 0, 0, 0, 0, 0, 0, 0, 0, -1, 0};
     const int s = sp.s;
     if (s < 0) return t;
     const long long j = q.offsets || q.by_group ? u - sp.slot0 : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
@@ -251,6 +252,7 @@ struct CacheSharedPlan {
     CacheAttnPlan own, prefix;
     size_t bytes;
     long long blocks;   // of the launch that takes both
+    bool behind;        // one plan, `own`: tiles of the sequences take the prefix's keys and then their own
 };
 inline CacheSharedPlan cache_shared_plan(bool bf, int n_seqs, int rows, bool offsets, int max_rows, int table_pages,
                                          int n_groups, int prefix_table_pages, int page_tokens, int kv_heads, int q_heads,
@@ -266,6 +268,27 @@ inline CacheSharedPlan cache_shared_plan(bool bf, int n_seqs, int rows, bool off
     const long long packed = (long long)rows * G, keys = (long long)prefix_table_pages * page_tokens;
     const bool large = bf && packed >= 64ll * n_groups && (double)packed * keys * kv_heads * head_dim >= 3e9;
     p.prefix.route = !large ? ATTN_FEW : n_groups == 1 ? ATTN_MANY : ATTN_BOTH;
+    // Tiles of the sequences take the prefix themselves where that is less than a pass of its own costs.  Estimates in us: a
+    // large tile takes its keys at 0.95 PFLOP/s; a small one 2 head_dim + 96 bytes a key at 13.7 TB/s, most of them from the
+    // caches, and in a pass of its own, whose blocks are cut to fill the chip, 2 head_dim at 14; all no faster than the memory has
+    // them once.  Two parts are 4 us and 1.2 ns a row and head of 128 channels more (partial results and their join).  us of a call, two
+    // parts / behind, 8 heads of 128 with 4 queries each, prefixes of 128, 512, 2048, 8192: 64 sequences of a row 14 / 11, 15 / 14,
+    // 21 / 35, 37 / 105; 12 of 33 29 / 16, 33 / 24, 44 / 62, 90 / 178; 64 of 40 141 / 37, 125 / 60, 191 / 158, 511 / 539; 16 heads of 64
+    // in fp32, 12 of 33 16 / 11, 18 / 12, 26 / 34, 68 / 82.
+    const double places = (double)keys * kv_heads, once = n_groups * places * 2 * head_dim / 4.5e6;
+    auto big_cost = [&](long long tiles) { return tiles * places * 128 * 4 * head_dim / 0.95e9; };
+    const long long per = ((long long)rows + n_seqs - 1) / n_seqs * G;   // packed rows of a sequence, were all alike
+    const bool big = p.own.route != ATTN_FEW && per > few_rows(head_dim);
+    const double behind = big ? big_cost(n_seqs * ((per + 127) / 128)) : n_seqs * ((per + 15) / 16) * places * (2 * head_dim + 96) / 13.7e6;
+    const double pass = large ? big_cost((packed + 127) / 128 + n_groups - 1) : ((packed + 15) / 16 + n_groups - 1) * places * 2 * head_dim / 14e6;
+    const double apart = std::max(once, pass) + 4 + 1.2e-3 * rows * q_heads * head_dim / 128;
+    if (keys < (1 << 29) && behind < apart) {
+        p.behind = true;
+        p.own = cache_attn_plan(bf, n_seqs, rows, offsets, max_rows, table_pages + (int)((keys + 63) / 64 * 64 / page_tokens),
+                                page_tokens, kv_heads, q_heads, head_dim, cus);
+        p.bytes = p.own.bytes;
+        return p;
+    }
     // `most` blocks fill the chip; splits end with a step of 64 keys and hold four of them at least
     auto cut = [&](CacheAttnCut& c, int shift, int n, long long held, bool ragged, long long row_most, long long most) {
         c.slots = tile_slots(ragged, n, rows, G, shift);
@@ -335,6 +358,26 @@ __device__ __forceinline__ Seq find_among(const SeqArgs& q, const Count& count, 
         }
     }
     return {-1, 0, 0, 0, 0};
+}
+// The group of sequence `seq` (-1: none; every lane of a wavefront calls, with the same one).
+__device__ __forceinline__ int group_of(const SeqArgs& q, int seq) {
+    if (!q.groups) return 0;
+    const int lane = threadIdx.x & 63;
+    for (int b = 0; b < q.n_seqs; b += 64) {
+        const int g = b + lane, c = g < q.n_seqs ? g : q.n_seqs - 1;
+        const uint64_t here = __ballot(g < q.n_seqs && q.groups[c] <= seq && seq < q.groups[c + 1]);
+        if (here) return b + __ffsll((unsigned long long)here) - 1;
+    }
+    return -1;
+}
+// The tile takes its group's prefix first, in whole steps.
+__device__ __forceinline__ void put_behind(Tile& t, const SeqArgs& q, int pt) {
+    if (t.seq < 0) return;
+    t.group = group_of(q, t.seq);
+    if (t.group < 0) return;
+    t.front_len = max(0, min(q.at[t.group], q.table_pages * pt));
+    t.skip0 = (t.front_len + 63) & ~63;
+    t.left_out = -t.skip0;
 }
 template <bool GROUPS = false, class Count>
 __device__ __forceinline__ Seq find_seq(const SeqArgs& q, const Count& count, int u) {

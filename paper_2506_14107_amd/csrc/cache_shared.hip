@@ -33,13 +33,12 @@ __global__ __launch_bounds__(256, 2) void cache_shared_k(SharedArgs a) {
     if (b.large) attend_large<DH, ONE, PART>(x, *(Lds<DH>*)smem, b.bx, b.by);
     else attend_small<DH, true, PART>(x, *(Small<DH>*)smem, b.bx, b.by);
 }
-template <int DH>
-__global__ __launch_bounds__(256, 2) void cache_shared_small_k(SharedArgs a, int f32) {
+template <int DH, bool BF>
+__global__ __launch_bounds__(256, 2) void cache_shared_small_k(SharedArgs a) {
     __shared__ Small<DH> lds;
     const Block b = block_of(a);
     const CacheAttnArgs& x = a.part[b.part];
-    if (f32) attend_small<DH, false, PART>(x, lds, b.bx, b.by);
-    else attend_small<DH, true, PART>(x, lds, b.bx, b.by);
+    attend_small<DH, BF, PART>(x, lds, b.bx, b.by);
 }
 
 // Where a row's partial results over its prefix lie: group g has the row's sequence.
@@ -240,7 +239,7 @@ template <int DH>
 void launch_shared(bool bf, const SharedArgs& a, hipStream_t s) {
     const dim3 grid(a.first[3]);
     if (a.part[0].route == ATTN_FEW && a.part[1].route == ATTN_FEW) {
-        cache_shared_small_k<DH><<<grid, 256, 0, s>>>(a, !bf);
+        bf ? cache_shared_small_k<DH, true><<<grid, 256, 0, s>>>(a) : cache_shared_small_k<DH, false><<<grid, 256, 0, s>>>(a);
         return;
     }
     constexpr size_t lds = sizeof(Lds<DH>) > sizeof(Small<DH>) ? sizeof(Lds<DH>) : sizeof(Small<DH>);

@@ -382,6 +382,7 @@ struct CacheAttnArgs {
     float scale;
     int causal;
     int window, sinks;   // of a call with a window
+    SeqArgs front;       // behind prefixes: their table, lengths and groups
     // set by the launcher
     int route;
     CacheAttnCut few, many;
@@ -397,6 +398,7 @@ void launch_cache_attention(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, 
 void launch_cache_window(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);   // a.window, a.sinks
 // Sequences behind prefixes that groups of them share: `prefix` has the prefixes' table, lengths and groups, the parts'
 // results meet in the workspace (p's, then pre's).
+void launch_cache_behind(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);   // a.front
 void launch_cache_shared(bool bf16, CacheAttnArgs a, const SeqArgs& prefix, const CacheAttnPlan& p, const CacheAttnPlan& pre,
                          float* workspace, hipStream_t s);
 

@@ -2,9 +2,11 @@
 import numpy as np
 import pytest
 
+from paper_2506_14107_amd import dejavu as dj
+
 from . import cache_ref as ref
 from .gpu_util import require_gpu
-from .test_gpu_cache import Pair, close, ints, normal, values
+from .test_gpu_cache import Pair, close, ints, normal, types, values
 
 pytestmark = pytest.mark.gpu
 
@@ -30,6 +32,29 @@ LARGE = {
     "mixed": (46, 4, 64, 32, [1, 120, 17, 0, 16, 3], [90, 130, 17, 4, 60, 2], [0, 2, 5, 6], [90, 150, 33], 0),
     "80": (54, 2, 80, 64, [230], [230], [0, 1], [64], 0),
     "16": (122, 1, 16, 128, [257], [300], [0, 1], [500], 0),
+}
+# ... whose tiles take the prefix and then the sequence's own keys; those above do so or not as the sizes have it
+BEHIND = {
+    "tokens": (2, 4, 128, 64, [1] * 6, [1, 64, 65, 5, 0, 130], [0, 6], [100], 0),
+    "split": (1, 4, 64, 32, [1, 2], [2500, 1], [0, 1, 2], [70, 650], 0),
+    "pages-16": (3, 5, 80, 16, [7, 1, 20, 0, 2, 1], [9, 17, 20, 3, 0, 70], [0, 2, 2, 5, 6], [90, 33, 57, 0], 3),
+    "outside": (2, 3, 96, 64, [4, 1, 2, 5], [4, 90, 2, 30], [1, 3], [63], 0),
+    "large": (56, 4, 64, 64, [141], [200], [0, 1], [100], 3),
+    "large-16": (54, 2, 80, 16, [100, 130, 100], [130, 130, 9], [0, 2, 3], [65, 40], 0),
+    "large-128": (34, 2, 128, 128, [250, 3], [250, 300], [0, 1, 1], [300, 7], 2),
+    "mixed": (46, 4, 64, 32, [1, 120, 17, 0, 160, 30], [90, 130, 17, 4, 160, 2], [0, 2, 5, 6], [90, 50, 33], 0),
+}
+APART = {
+    "tokens": (8, 4, 128, 64, [1] * 30, [9] * 30, [0, 30], [3000], 0),
+    "f32-groups": (4, 4, 64, 16, [1] * 24, [3, 50, 0] * 8, [0, 15, 24], [4000, 3000], 0),
+}
+# Prefixes so long, for so many rows, that they take large tiles: alone, beside groups that do not, under sequences that do too
+LONG = {
+    "tokens": (8, 4, 128, 64, [1] * 76, [1 + i % 90 for i in range(76)], [0, 76], [10048], 0),
+    "groups": (8, 4, 128, 64, [1] * 100, [1 + i % 9 for i in range(100)], [0, 90, 92, 100], [9024, 512, 320], 0),
+    "prompts": (8, 4, 128, 64, [40] * 64, [40 + i for i in range(64)], [0, 64], [16384], 0),
+    "prompts-16": (16, 2, 64, 16, [90, 1, 1, 30] * 16, [90, 5, 1, 200] * 16, [0, 30, 64], [8192, 6400], 3),
+    "few": (2, 4, 64, 32, [1] * 10, [40, 1, 7, 2, 3] * 2, [0, 10], [60000], 0),
 }
 
 
@@ -112,7 +137,60 @@ def test_shared_large_tiles(name, causal):
     shared_case(*LARGE[name], name, "bf16", causal)
 
 
-ALL = {**CASES, **{"large-" + k: v for k, v in LARGE.items()}}
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", BEHIND)
+def test_shared_behind(name, dtype, causal):
+    shared_case(*BEHIND[name], name, dtype, causal)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", APART)
+def test_shared_apart(name, dtype):
+    shared_case(*APART[name], name, dtype, True)
+
+
+ALL = {**CASES, **{"large-" + k: v for k, v in LARGE.items()}, **{"behind-" + k: v for k, v in BEHIND.items()},
+       **{"apart-" + k: v for k, v in APART.items()}, **{"long-" + k: v for k, v in LONG.items()}}
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", LONG)
+def test_long_prefixes(name, dtype, causal):
+    """Prefixes of whole pages, against attention over one table of both (itself tested against 64 bits): either is off by its
+    tolerance, with the most that its parts can be: the largest value, the largest |q| |k|."""
+    torch = require_gpu()
+    heads, group, dh, pt, counts, lengths, groups, prefix, pad = LONG[name]
+    rng = np.random.default_rng(26)
+    n, ng, tp, ptp = len(counts), len(prefix), max(-(-x // pt) for x in lengths), max(prefix) // pt
+    total = n * tp + ng * ptp
+    c = dj.TokenCache(total, heads, dh, pt)
+    g = torch.Generator("cuda").manual_seed(3)
+    for t in (c.k, c.v):
+        t.copy_((torch.randn(t.shape, generator=g, device="cuda") * 100).clamp(-448, 448))
+    for t in (c.k_scale, c.v_scale):
+        t.copy_(torch.exp2(torch.randint(-9, -5, t.shape, generator=g, device="cuda").float()))
+    order = rng.permutation(total)
+    table, ptable = order[:n * tp].reshape(n, tp), order[n * tp:].reshape(ng, ptp)
+    offs = np.concatenate([[0], np.cumsum(counts)])
+    q = torch.randn(int(offs[-1]) + pad, heads * group, dh, generator=g, device="cuda").to(types(torch)[dtype])
+    of = [max(i for i in range(ng) if groups[i] <= s) for s in range(n)]
+    both = np.full((n, ptp + tp), -1)
+    for s in range(n):
+        k = prefix[of[s]] // pt
+        both[s, :k], both[s, k:k + tp] = ptable[of[s], :k], table[s]
+    after = np.array(lengths) + np.array(prefix)[of]
+    got, want = torch.full_like(q, 3), torch.full_like(q, 3)
+    c.attention_shared(q, ints(lengths), ints(prefix), ints(ptable), ints(offs), ints(table), ints(groups), causal=causal, out=got)
+    c.attention(q, ints(after), ints(offs), ints(both), causal=causal, out=want)
+    v = (c.v.float().abs().amax((2, 3)) * c.v_scale).max().item()
+    kk = (c.k.float().norm(dim=3).amax(2) * c.k_scale).max().item() * q.float().norm(dim=2).max().item() * dh ** -0.5
+    one = np.ones((1, 1, 1))
+    tol = ref.attention_tolerance(0 * one, v * one, kk * np.ones((1, 1)), dtype, dh, int(after.max())).item()
+    d = (got.double() - want.double()).abs()
+    assert torch.isfinite(got).all() and d.max().item() <= 2 * tol, (d.max().item(), tol)
+    assert d.square().mean().sqrt().item() <= 0.1 * tol      # and far closer nearly everywhere
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -150,7 +228,7 @@ def test_every_key_counts_once(name, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("name", ["tokens", "groups", "large-tokens", "large-rows"])
+@pytest.mark.parametrize("name", ["tokens", "groups", "large-tokens", "large-rows", "behind-split", "behind-large-128", "behind-mixed", "apart-f32-groups"])
 def test_scores_far_apart_missing_pages_and_odd_lengths(name, dtype):
     heads, group, dh, pt, counts, lengths, groups, prefix, _ = ALL[name]
     rng = np.random.default_rng(12)
@@ -180,7 +258,7 @@ def test_scores_far_apart_missing_pages_and_odd_lengths(name, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("name", ["tokens", "groups", "large-tokens", "large-rows", "both-long"])
+@pytest.mark.parametrize("name", ["tokens", "groups", "large-tokens", "large-rows", "both-long", "behind-split", "behind-large-128", "behind-mixed", "apart-f32-groups"])
 def test_nan_and_infinite_values_of_a_prefix_reach_its_group(name, dtype):
     heads, group, dh, pt, counts, lengths, groups, prefix, _ = ALL[name]
     rng = np.random.default_rng(13)
@@ -207,7 +285,7 @@ def test_nan_and_infinite_values_of_a_prefix_reach_its_group(name, dtype):
         close(part, out, tol, f"sequence {s}")
 
 
-@pytest.mark.parametrize("name", ["groups", "both-long", "large-tokens", "large-mixed"])
+@pytest.mark.parametrize("name", ["groups", "both-long", "large-tokens", "large-mixed", "behind-split", "behind-mixed", "apart-tokens"])
 def test_in_place_on_a_stream_and_with_a_workspace(name):
     torch = require_gpu()
     heads, group, dh, pt, counts, lengths, groups, prefix, _ = ALL[name]

@@ -10,6 +10,7 @@ import torch
 
 from paper_2506_14107_amd import dejavu as dj
 
+from . import test_gpu_shared as on_gpu
 from .test_cache import ATTEND, COMMON, FAKE, cache, refused
 from .test_cache_operators import on_device
 
@@ -77,17 +78,27 @@ def test_windows_are_cut_by_what_they_see(lib):
 def test_shared_calls_are_cut(lib, bf16):
     """Splits cover every key that a table can hold, slots every row whichever way it falls into groups, the workspace a
     partial result for every tile, head and split."""
-    rng = random.Random(5)
+    rng, seen = random.Random(5), set()
     for _ in range(3000):
         n, heads, group = rng.choice([1, 2, 64, 300]), rng.choice([1, 2, 8, 40]), rng.choice([1, 4, 16])
         pt, dh, ng = rng.choice([16, 64, 128]), rng.choice([16, 64, 128]), rng.choice([1, 1, 2, 30])
         tables = [min((1 << 30) // pt, int(2 ** rng.uniform(0, 22))) for _ in range(2)]
         offsets = rng.random() < 0.7
         rows = rng.choice([n, 5 * n, int(2 ** rng.uniform(0, 16))]) if offsets else n
-        out = (ctypes.c_longlong * 18)()
+        out = (ctypes.c_longlong * 19)()
         lib.t_shared_plan(bf16, n, rows, int(offsets), rng.choice([0, rows]), tables[0], ng, tables[1], pt, heads, heads * group, dh,
                           256, out)
         total = blocks = 0
+        if out[18]:      # one plan, whose splits cover the prefix in whole steps and the sequence
+            route, *cuts, size = out[:8]
+            need = 0
+            for (chunk, splits, slots), tile in ((cuts[:3], 16), (cuts[3:], 128)):
+                assert not splits or chunk % 64 == 0 and chunk * splits >= -(-tables[1] * pt // 64) * 64 + tables[0] * pt
+                need += slots * heads * splits * tile * (dh + 2) * 4 * (splits > 1)
+            assert size == need == out[16] and chunk * splits < 1 << 31
+            seen.add("behind")
+            continue
+        seen.add("apart")
         for i, (k, seqs) in enumerate(((tables[0], n), (tables[1], ng))):
             route, *cuts, size = out[8 * i:8 * i + 8]
             need = 0
@@ -107,6 +118,23 @@ def test_shared_calls_are_cut(lib, bf16):
             assert size == need
             total += need
         assert out[16] == total and out[17] == blocks
+    assert seen == {"behind", "apart"}
+
+
+def test_shared_calls_of_the_gpu_tests(lib):
+    """Their long prefixes take large tiles, small ones or either by group, under sequences in small tiles or by sequence; the
+    short ones go with the sequences' own keys, in small tiles, large ones and either."""
+    def plans(cases):
+        out, r = (ctypes.c_longlong * 19)(), {}
+        for name, (heads, group, dh, pt, counts, lengths, groups, prefix, pad) in cases.items():
+            tp, ptp = (max(1, max(-(-x // pt) for x in y)) for y in (lengths, prefix))
+            lib.t_shared_plan(1, len(counts), sum(counts) + pad, 1, 0, tp, len(prefix), ptp, pt, heads, heads * group, dh, 256, out)
+            r[name] = ("behind", out[0]) if out[18] else (out[8], out[0])
+        return r
+
+    assert plans(on_gpu.LONG) == {"tokens": (1, 0), "groups": (2, 0), "prompts": (1, 2), "prompts-16": (2, 2), "few": (0, 0)}
+    assert set(plans(on_gpu.BEHIND).values()) == {("behind", 0), ("behind", 1), ("behind", 2)}
+    assert set(plans(on_gpu.APART).values()) == {(0, 0)}
 
 
 # ---- refusals ------------------------------------------------------------------------------------------
@@ -134,10 +162,20 @@ def test_window_refuses(kw):
 
 @pytest.mark.parametrize("kw", ATTENTION + [
     dict(n_groups=0), dict(prefix_table=None), dict(prefix_lengths=None), dict(prefix_table_pages=0),
-    dict(prefix_table_pages=(1 << 24) + 1), dict(groups=None), dict(workspace=None), dict(workspace_bytes=16),
-    dict(workspace=FAKE + 4), dict(n_groups=(1 << 31) - 1)])
+    dict(prefix_table_pages=(1 << 24) + 1), dict(groups=None), dict(n_groups=(1 << 31) - 1)])
 def test_shared_refuses(kw):
     assert refused("dv_cache_attention_shared", SHARED, kw) == EINVAL and dj.dv_last_error()
+
+
+def test_shared_refuses_a_workspace_that_is_too_small():
+    """Prefixes and sequences in one pass, whose splits meet in it, and in one each."""
+    desc = cache(pages=1 << 20)
+    for n, pages in ((4, 40), (64, 2000)):
+        need = dj.dv_cache_attention_shared_workspace(ctypes.addressof(desc), n, 1024, True, 2, pages, dj.DV_BF16, n, 16, 1)
+        assert need > 0
+        kw = dict(c=dict(pages=1 << 20), n_seqs=n, rows=n, table_pages=1024, max_rows=1, prefix_table_pages=pages)
+        for bad in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=FAKE + 4)):
+            assert refused("dv_cache_attention_shared", SHARED, dict(kw, **bad)) == EINVAL and "workspace" in dj.dv_last_error()
 
 
 def test_window_refuses_a_workspace_that_is_too_small():

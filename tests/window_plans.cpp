@@ -32,7 +32,8 @@ int t_window_plan(int bf16, int n_seqs, int rows, int offsets, int max_rows, int
     return p.route;
 }
 
-// The plans of a call with shared prefixes, one after the other; then the bytes and blocks of both.
+// The plans of a call with shared prefixes, one after the other; then the bytes and blocks of both,
+// and whether the first takes the prefixes too.
 void t_shared_plan(int bf16, int n_seqs, int rows, int offsets, int max_rows, int table_pages, int n_groups, int prefix_table_pages,
                    int page_tokens, int kv_heads, int q_heads, int head_dim, int cus, long long* out) {
     const CacheSharedPlan p = cache_shared_plan(bf16 != 0, n_seqs, rows, offsets != 0, max_rows, table_pages, n_groups,
@@ -44,6 +45,7 @@ void t_shared_plan(int bf16, int n_seqs, int rows, int offsets, int max_rows, in
     }
     out[0] = (long long)p.bytes;
     out[1] = p.blocks;
+    out[2] = p.behind;
 }
 
 }  // extern "C"
