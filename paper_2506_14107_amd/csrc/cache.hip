@@ -332,7 +332,7 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& r
     for (int first = 0; first < total; first += batch) {
         const int end = min(batch, total - first);
         float x[NORM_ITEMS][16];
-        Raw<BF, V> r[NORM_ITEMS], w[BF ? NORM_ITEMS : 1];   // (fp32 has no registers for weights ahead)
+        Raw<BF, V> r[NORM_ITEMS];
         int rr[NORM_ITEMS], hh[NORM_ITEMS], cc[NORM_ITEMS];
 #pragma unroll
         for (int k = 0; k < NORM_ITEMS; ++k) {
@@ -341,7 +341,6 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& r
             const int rest = (first + i) % per_row;
             rr[k] = (first + i) / per_row, hh[k] = rest / per_head, cc[k] = rest % per_head;
             load_raw<BF, V>(a.x, (size_t)(row0 + rr[k]) * a.x_stride + (size_t)hh[k] * a.dh, rot.dim, rot.pairs, cc[k], r[k]);
-            if constexpr (BF) load_weight<BF, V>(nm, a.dh, hh[k], rot.dim, rot.pairs, cc[k], w[k]);
         }
 #pragma unroll
         for (int k = 0; k < NORM_ITEMS; ++k) {
@@ -354,9 +353,9 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& r
         for (int k = 0; k < NORM_ITEMS; ++k) {
             const int i = tid + k * NT;
             if (i >= end) continue;
-            Raw<BF, V>& wk = w[BF ? k : 0];
-            if constexpr (!BF) load_weight<BF, V>(nm, a.dh, hh[k], rot.dim, rot.pairs, cc[k], wk);
-            norm_chunk<BF, V>(nm, part + i - cc[k], a.dh, wk, x[k]);
+            Raw<BF, V> w;
+            load_weight<BF, V>(nm, a.dh, hh[k], rot.dim, rot.pairs, cc[k], w);
+            norm_chunk<BF, V>(nm, part + i - cc[k], a.dh, w, x[k]);
             turn_chunk<V>(rot.dim, rot.pairs, cc[k], cos + rr[k] * ld, sin + rr[k] * ld, x[k]);
             store_chunk<BF, V>(a.out, (size_t)(row0 + rr[k]) * a.out_stride + (size_t)hh[k] * a.dh, rot.dim, rot.pairs, cc[k],
                                x[k]);
@@ -541,12 +540,10 @@ __global__ __launch_bounds__(WT, NORM ? 3 : 4) void cache_write_k(WriteArgs a) {
         if constexpr (AHEAD)
             if (h0 + hn < end) ask(h0 + hn);
         const bool normed = NORM && !values && a.k_norm.on;
-        Raw<BF, V> weight[AHEAD ? MAX_ITEMS : 1];
-        if (normed) {
+                if (normed) {
 #pragma unroll
             for (int k = 0; k < MAX_ITEMS; ++k) {
                 if (hh[k] >= hn) continue;
-                if constexpr (AHEAD) load_weight<BF, V>(a.k_norm, dh, h0 + hh[k], dim, a.rot.pairs, cc[k], weight[k]);
                 part[tid + k * WT] = sum_squares(x[k]);
             }
         }
@@ -555,8 +552,8 @@ __global__ __launch_bounds__(WT, NORM ? 3 : 4) void cache_write_k(WriteArgs a) {
         for (int k = 0; k < MAX_ITEMS; ++k) {
             if (hh[k] >= hn) continue;
             if (normed) {
-                Raw<BF, V>& w = weight[AHEAD ? k : 0];
-                if constexpr (!AHEAD) load_weight<BF, V>(a.k_norm, dh, h0 + hh[k], dim, a.rot.pairs, cc[k], w);
+                Raw<BF, V> w;
+                load_weight<BF, V>(a.k_norm, dh, h0 + hh[k], dim, a.rot.pairs, cc[k], w);
                 norm_chunk<BF, V>(a.k_norm, part + tid + k * WT - cc[k], dh, w, x[k]);
             }
             turn_chunk<V>(dim, a.rot.pairs, cc[k], cos + tt[k] * ald, sin + tt[k] * ald, x[k]);
