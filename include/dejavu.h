@@ -399,7 +399,8 @@ typedef struct dv_cache {
  * the pages of sequences that end (entries that are pages of the cache) are given to it in the same
  * order, for later calls to take.  From the first sequence on that the ring does not hold enough pages
  * for, those that need any get none; nor does a sequence whose new places pass its table.  Such a sequence is not
- * extended: starts[s] = -1 (dv_cache_write passes it over), lengths_out[s] = lengths[s].  The others have
+ * extended: starts[s] = -1 (dv_cache_write passes it over), lengths_out[s] = lengths[s], and what attention gives for its
+ * rows means nothing.  The others have
  * starts[s] = lengths[s] and lengths_out[s] = lengths[s] + counts[s]; those that end -1 and 0.  cursor_out:
  * taken, given, and the pages that were lacking (0: every sequence that its table holds was
  * extended).  For a row at place p of its sequence positions [rows, 3] become (p, p, p) (NULL: not wanted) and slots
@@ -407,7 +408,7 @@ typedef struct dv_cache {
  * not wanted); those of rows past the last sequence's stay as they are, and rows from `rows` on have none.
  * lengths_out and cursor_out must not overlap lengths, counts and cursor (a loop alternates two
  * buffers of each); entries of a table that are not new stay as they are.  (For a query engine's batches over
- * the memory of Section 5.2.)  Errors: DV_EINVAL (NULL pointer, n_seqs or table_pages < 1, n_seqs *
+ * the memory of Section 5.2.)  Errors: DV_EINVAL (NULL pointer, n_seqs or table_pages < 1, n_seqs > 2^30, n_seqs *
  * table_pages >= 2^31, pages outside [1, 2^30], rows < 0, page_tokens out of range, table_pages *
  * page_tokens > 2^30, an output that is an input), DV_EHIP. */
 int dv_cache_extend(int n_seqs, int32_t* table, int table_pages, int page_tokens,

@@ -1772,7 +1772,7 @@ int dv_cache_extend(int n_seqs, int32_t* table, int table_pages, int page_tokens
     if ((long long)table_pages * page_tokens > (1ll << 30))
         return fail(DV_EINVAL, "table_pages %d: more than 2^30 tokens a sequence", table_pages);
     if (pages > (1 << 30)) return fail(DV_EINVAL, "%d pages are too many", pages);
-    if ((long long)n_seqs * table_pages >= (1ll << 31))
+    if (n_seqs > (1 << 30) || (long long)n_seqs * table_pages >= (1ll << 31))
         return fail(DV_EINVAL, "%d sequences of %d pages are too many for one call", n_seqs, table_pages);
     if (lengths_out == lengths || lengths_out == counts || cursor_out == cursor)
         return fail(DV_EINVAL, "lengths and cursor are read and written: each needs a buffer of its own for either");

@@ -65,7 +65,8 @@ EXTEND = dict(n_seqs=4, table=FAKE, table_pages=8, page_tokens=64, lengths=FAKE,
 @pytest.mark.parametrize("kw", [dict([(name, None)]) for name in (
     "table", "lengths", "counts", "ring", "cursor", "offsets", "starts", "lengths_out", "cursor_out")] + [
     dict(n_seqs=0), dict(table_pages=0), dict(pages=0), dict(pages=(1 << 30) + 1), dict(rows=-1), dict(page_tokens=48),
-    dict(page_tokens=256), dict(table_pages=(1 << 24) + 1), dict(n_seqs=1 << 15, table_pages=1 << 16), dict(lengths_out=FAKE),
+    dict(page_tokens=256), dict(table_pages=(1 << 24) + 1), dict(n_seqs=1 << 15, table_pages=1 << 16),
+    dict(n_seqs=(1 << 30) + 1, table_pages=1), dict(lengths_out=FAKE),
     dict(cursor_out=FAKE)])
 def test_extend_refuses(kw):
     assert dj.load().dv_cache_extend(*dict(EXTEND, **kw).values()) == dj.DV_EINVAL and dj.dv_last_error()

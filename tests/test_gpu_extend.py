@@ -220,6 +220,65 @@ def test_serving_steps(pages):
     assert (lacked > 0) == (pages < 40)      # the smaller cache runs short
 
 
+def test_streams_and_answers_about_one_video():
+    """Used together: a video's tokens written as a shared prefix; answers whose pages come from the ring, normed, turned and written,
+    attending over the prefix and their own places; and streams that see a window of theirs.  Against attention over one table
+    of both (whole pages), and against the rows read back."""
+    torch = require_gpu()
+    heads, group, dh, pt, n, P, pages = 2, 4, 64, 16, 7, 12, 90
+    c = dj.TokenCache(pages, heads, dh, pt)
+    rot = dj.Rotary((8, 12, 12))
+    g = torch.Generator("cuda").manual_seed(2)
+    rng = np.random.default_rng(12)
+    normal = lambda rows, h: torch.randn(rows, h, dh, generator=g, device="cuda")  # noqa: E731
+    ring = torch.arange(pages, dtype=torch.int32, device="cuda")
+    table = torch.full((n + 1, P), -1, dtype=torch.int32, device="cuda")
+    lengths, cursor = torch.zeros(n + 1, dtype=torch.int32, device="cuda"), torch.tensor([0, pages, 0], device="cuda")
+    video = 9 * pt
+    kw, qw = normal(1, heads)[0], normal(1, heads * group)[0]
+
+    def step(counts):
+        nonlocal lengths, cursor
+        rows = int(np.maximum(counts, 0).sum())
+        offsets, starts, lengths, cursor, pos, _ = dj.extend(table, lengths, ints(counts), ring, cursor, pt, rows)
+        q = c.write(normal(rows, heads), normal(rows, heads), starts, offsets, table, rot, pos, normal(rows, heads * group), k_norm=kw,
+                    q_norm=qw)
+        return offsets, q
+
+    step([video] + [0] * n)                       # the video is sequence 0
+    prefix, ptable = ints([video]), table[:1].clone()
+    for k in range(9):
+        counts = np.concatenate([[0], rng.choice([0, 1, 1, 5], n)])
+        offsets, q = step(counts)
+        assert cursor[2].item() == 0
+        if not len(q):
+            continue
+        own, offs = lengths[1:].contiguous(), offsets[1:].contiguous()
+        got = c.attention_shared(q, own, prefix, ptable, offs, table[1:].contiguous())
+        both = torch.cat([ptable[:, :9].expand(n, 9), table[1:]], 1).contiguous()
+        want = c.attention(q, own + video, offs, both)
+        seen = c.attention(q, own, offs, table[1:].contiguous(), window=17, sinks=3)
+        for s in range(n):
+            a, b, length = offs[s].item(), offs[s + 1].item(), own[s].item()
+            if a == b:
+                continue
+            keys, vals = [values(x) for x in c.read(ints([0]), ints([0, video + length]), both[s:s + 1], rows=video + length,
+                                                    dtype=torch.float32)]
+            e = (length - (b - a) + np.arange(b - a) + 1)[:, None]
+            j = np.arange(length)[None]
+            q64 = values(q)[a:b]
+            sees = np.concatenate([np.ones((b - a, video), bool), j < e], 1)
+            o, mass, size = ref.attention(q64, keys, vals, sees, dh ** -0.5)
+            tol = ref.attention_tolerance(o, mass, size, "f32", dh, video + length)
+            assert (np.abs(values(got)[a:b] - o) <= tol).all() and (np.abs(values(want)[a:b] - o) <= tol).all()
+            o, mass, size = ref.attention(q64, keys[video:], vals[video:], (j < e) & ((j < 3) | (j >= e - 17)), dh ** -0.5)
+            assert (np.abs(values(seen)[a:b] - o) <= ref.attention_tolerance(o, mass, size, "f32", dh, length)).all()
+    counts = np.full(n + 1, -1)
+    counts[0] = 0
+    step(counts)                                  # all answers end: the ring holds all but the video's pages
+    assert (cursor[1] - cursor[0]).item() == pages - 9 and lengths.tolist() == [video] + [0] * n
+
+
 def test_captured_steps_replay():
     """A graph of two steps whose lengths and cursor alternate: replayed, it goes on where it stood."""
     torch = require_gpu()

@@ -136,6 +136,10 @@ WRITE = {
     "long-pages": (2, 4, 128, 128, (24, 20, 20), "halves", "all", 0),
     "long-pages-unaligned": (1, 3, 128, 128, (24, 20, 20), "pairs", "head", 1),
     "ones": (1, 16, 16, 16, (2, 3, 3), "halves", None, 0),
+    "quarters": (2, 4, 48, 16, (4, 4, 4), "halves", "head", 0),
+    "quarters-pairs": (3, 3, 112, 64, (10, 9, 9), "pairs", "all", 0),
+    "four-apart": (2, 4, 80, 32, (14, 13, 13), "halves", "head", 4),
+    "four-apart-pairs": (1, 2, 128, 128, (24, 20, 20), "pairs", "head", 4),
 }
 
 
