@@ -282,7 +282,8 @@ inline CacheSharedPlan cache_shared_plan(bool bf, int n_seqs, int rows, bool off
     const double behind = big ? big_cost(n_seqs * ((per + 127) / 128)) : n_seqs * ((per + 15) / 16) * places * (2 * head_dim + 96) / 13.7e6;
     const double pass = large ? big_cost((packed + 127) / 128 + n_groups - 1) : ((packed + 15) / 16 + n_groups - 1) * places * 2 * head_dim / 14e6;
     const double apart = std::max(once, pass) + 4 + 1.2e-3 * rows * q_heads * head_dim / 128;
-    if (keys < (1 << 29) && behind < apart) {
+    const long long places_of_both = (keys + 63) / 64 * 64 + (long long)table_pages * page_tokens;
+    if (places_of_both <= 1 << 30 && behind < apart) {   // (counted in ints)
         p.behind = true;
         p.own = cache_attn_plan(bf, n_seqs, rows, offsets, max_rows, table_pages + (int)((keys + 63) / 64 * 64 / page_tokens),
                                 page_tokens, kv_heads, q_heads, head_dim, cus);

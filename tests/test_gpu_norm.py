@@ -200,6 +200,26 @@ def test_write_norms_keys_and_queries(name, dtype):
               2.0 ** -4 * np.abs(old[0][1][i]) + 2.0 ** -9 * z[table[1][0]][:, None], "held")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_outside_the_sequences_are_left_alone(dtype):
+    """Rows before the first sequence and behind the last one: neither written nor normed, in place too."""
+    torch = require_gpu()
+    rng = np.random.default_rng(9)
+    k, v, q = (normal(rng, (30, h, 64), dtype)[0] for h in (2, 2, 4))
+    pos, rot = ints(rng.integers(0, 99, (30, 3))), dj.Rotary((8, 12, 12))
+    before = q.clone()
+    c = Pair(3, 2, 64, 16).c
+    for t in (c.k_scale, c.v_scale):
+        t.fill_(7.0)
+    assert c.write(k, v, ints([0, 3]), ints([6, 15, 21]), ints([[0], [2]]), rot, pos, q, q, k_norm=True, q_norm=True) is q
+    assert torch.equal(q[:6], before[:6]) and torch.equal(q[21:], before[21:])
+    assert torch.equal(q[6:21], dj.norm_rotary(before[6:21], None, 1e-6, pos[6:21].contiguous(), rot))
+    assert (c.k_scale[1] == 7).all() and (c.v_scale[1] == 7).all()
+    # a sequence with a negative start is passed over; its queries are normed all the same
+    c.write(k, v, ints([-1, 0]), ints([0, 15, 30]), ints([[0], [1]]), rot, pos, before.clone(), q, k_norm=True, q_norm=True)
+    assert torch.equal(q, dj.norm_rotary(before, None, 1e-6, pos, rot))
+
+
 @pytest.mark.parametrize("which", ["k", "q"])
 def test_either_norm_alone(which):
     """Only keys or only queries normed: the others as without."""

@@ -319,6 +319,21 @@ def test_one_prefix_equals_one_sequence():
     assert torch.isfinite(got).all()
 
 
+@pytest.mark.parametrize("name", ["groups", "behind-large-128", "apart-f32-groups", "apart-tokens"])
+def test_rows_before_the_first_sequence_are_left_alone(name):
+    """Offsets that start behind a few rows: those stay as they were, in `out` and in the joins' view of the groups."""
+    torch = require_gpu()
+    heads, group, dh, pt, counts, lengths, groups, prefix, _ = ALL[name]
+    rng = np.random.default_rng(27)
+    p, table, ptable = build(heads, dh, pt, lengths, prefix, rng)
+    offs = 5 + np.concatenate([[0], np.cumsum(counts)])
+    q, q64 = normal(rng, (int(offs[-1]) + 2, heads * group, dh), "bf16")
+    out = torch.full_like(q, 9)
+    p.c.attention_shared(q, ints(lengths), ints(prefix), ints(ptable), ints(offs), ints(table), ints(groups), out=out)
+    assert (out[:5] == 9).all() and (out[-2:] == 9).all()
+    check(p, table, ptable, q64[5:], counts, lengths, groups, prefix, True, "bf16", out[5:], name)
+
+
 def test_captured_steps_replay():
     """A graph of answers about one video, whose own places grow: each replay equals the eager call."""
     torch = require_gpu()

@@ -177,6 +177,27 @@ def test_nan_and_infinite_values_reach_the_rows_that_see_them(name, dtype, causa
 
 
 @pytest.mark.parametrize("name", ["prompt-mixed", "long"])
+def test_rows_before_the_first_sequence_are_left_alone(name):
+    torch = require_gpu()
+    for heads, group, dh, pt, counts, lengths, _ in (ATTENTION[name], LARGE["mixed-128"]):
+        rng = np.random.default_rng(27)
+        p, table = filled(rng, heads, dh, pt, lengths)
+        offs = 5 + np.concatenate([[0], np.cumsum(counts)])
+        q, q64 = normal(rng, (int(offs[-1]) + 2, heads * group, dh), "bf16")
+        out = torch.full_like(q, 9)
+        p.c.attention(q, ints(lengths), ints(offs), ints(table), out=out, window=70, sinks=3)
+        assert (out[:5] == 9).all() and (out[-2:] == 9).all()
+        got = values(out)
+        for s, length in enumerate(lengths):
+            a, b = offs[s], offs[s + 1]
+            if a == b:
+                continue
+            k, v, _ = p.m.history(table.tolist(), s, length)
+            want, mass, size = ref.attention(q64[a:b], k, v, seen(length, b - a, True, 70, 3), dh ** -0.5)
+            close(got[a:b], want, ref.attention_tolerance(want, mass, size, "bf16", dh, max(1, min(length, 73))), f"{name}, sequence {s}")
+
+
+@pytest.mark.parametrize("name", ["prompt-mixed", "long"])
 def test_in_place_on_a_stream_and_with_a_workspace(name):
     torch = require_gpu()
     for heads, group, dh, pt, counts, lengths, _ in (ATTENTION[name], LARGE["mixed-128"], MORE["splits"]):
