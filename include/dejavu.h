@@ -406,11 +406,11 @@ typedef struct dv_cache {
  * extended).  For a row at place p of its sequence positions [rows, 3] become (p, p, p) (NULL: not wanted) and slots
  * [rows] page * page_tokens + p % page_tokens, or -1 where its sequence was not extended or has no page there (NULL:
  * not wanted); those of rows past the last sequence's stay as they are, and rows from `rows` on have none.
- * No page may stand in two entries or in the ring as well.  lengths_out and cursor_out must not overlap lengths, counts and
- * cursor (a loop alternates two buffers of each); entries of a table that are not new stay as they are.  (For a query engine's batches over
+ * No page may stand in two entries or in the ring as well.  Outputs must not overlap lengths, counts and cursor (a
+ * loop alternates two buffers of lengths and cursor); entries of a table that are not new stay as they are.  (For a query engine's batches over
  * the memory of Section 5.2.)  Errors: DV_EINVAL (NULL pointer, n_seqs or table_pages < 1, n_seqs > 2^30, n_seqs *
  * table_pages >= 2^31, pages outside [1, 2^30], rows < 0, page_tokens out of range, table_pages *
- * page_tokens > 2^30, an output that is an input), DV_EHIP. */
+ * page_tokens > 2^30, an output that overlaps them), DV_EHIP. */
 int dv_cache_extend(int n_seqs, int32_t* table, int table_pages, int page_tokens,
                     const int32_t* lengths, const int32_t* counts, int32_t* ring, int pages,
                     const int64_t* cursor, int rows, int32_t* offsets, int32_t* starts,

@@ -1774,8 +1774,14 @@ int dv_cache_extend(int n_seqs, int32_t* table, int table_pages, int page_tokens
     if (pages > (1 << 30)) return fail(DV_EINVAL, "%d pages are too many", pages);
     if (n_seqs > (1 << 30) || (long long)n_seqs * table_pages >= (1ll << 31))
         return fail(DV_EINVAL, "%d sequences of %d pages are too many for one call", n_seqs, table_pages);
-    if (lengths_out == lengths || lengths_out == counts || cursor_out == cursor)
-        return fail(DV_EINVAL, "lengths and cursor are read and written: each needs a buffer of its own for either");
+    // every block reads the first three, at any time of the launch
+    const struct { const void* p; size_t bytes; } in[] = {{lengths, 4ull * n_seqs}, {counts, 4ull * n_seqs}, {cursor, 24}},
+        out[] = {{offsets, 4ull * n_seqs + 4}, {starts, 4ull * n_seqs}, {lengths_out, 4ull * n_seqs}, {cursor_out, 24},
+                 {positions, 12ull * rows}, {slots, 8ull * rows}};
+    for (const auto& i : in)
+        for (const auto& o : out)
+            if (o.p && (uintptr_t)o.p < (uintptr_t)i.p + i.bytes && (uintptr_t)i.p < (uintptr_t)o.p + o.bytes)
+                return fail(DV_EINVAL, "an output overlaps lengths, counts or cursor: what is read and written needs two buffers");
     ExtendArgs a{};
     a.n_seqs = n_seqs;
     a.table_pages = table_pages;

@@ -58,18 +58,25 @@ def test_write_with_norms_of_no_rows():
 
 
 # ---- pages handed out ---------------------------------------------------------------------------------
-EXTEND = dict(n_seqs=4, table=FAKE, table_pages=8, page_tokens=64, lengths=FAKE, counts=FAKE, ring=FAKE, pages=100, cursor=FAKE,
-              rows=9, offsets=FAKE, starts=FAKE, lengths_out=2 * FAKE, cursor_out=2 * FAKE, positions=None, slots=None, stream=None)
+EXTEND = dict(n_seqs=4, table=FAKE, table_pages=8, page_tokens=64, lengths=2 * FAKE, counts=3 * FAKE, ring=4 * FAKE, pages=100,
+              cursor=5 * FAKE, rows=9, offsets=6 * FAKE, starts=7 * FAKE, lengths_out=8 * FAKE, cursor_out=9 * FAKE, positions=None,
+              slots=None, stream=None)
 
 
 @pytest.mark.parametrize("kw", [dict([(name, None)]) for name in (
     "table", "lengths", "counts", "ring", "cursor", "offsets", "starts", "lengths_out", "cursor_out")] + [
     dict(n_seqs=0), dict(table_pages=0), dict(pages=0), dict(pages=(1 << 30) + 1), dict(rows=-1), dict(page_tokens=48),
     dict(page_tokens=256), dict(table_pages=(1 << 24) + 1), dict(n_seqs=1 << 15, table_pages=1 << 16),
-    dict(n_seqs=(1 << 30) + 1, table_pages=1), dict(lengths_out=FAKE),
-    dict(cursor_out=FAKE)])
+    dict(n_seqs=(1 << 30) + 1, table_pages=1)])
 def test_extend_refuses(kw):
     assert dj.load().dv_cache_extend(*dict(EXTEND, **kw).values()) == dj.DV_EINVAL and dj.dv_last_error()
+
+
+@pytest.mark.parametrize("out,at", [(out, EXTEND[x] + d) for out, size in (
+    ("offsets", 20), ("starts", 16), ("lengths_out", 16), ("cursor_out", 24), ("positions", 108), ("slots", 72))
+    for x, held in (("lengths", 16), ("counts", 16), ("cursor", 24)) for d in (0, held - 4, 4 - size)])
+def test_extend_refuses_outputs_over_what_it_reads(out, at):
+    assert dj.load().dv_cache_extend(*dict(EXTEND, **{out: at}).values()) == dj.DV_EINVAL and "overlap" in dj.dv_last_error()
 
 
 # ---- tensors -------------------------------------------------------------------------------------------
