@@ -484,9 +484,9 @@ int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, 
                        size_t workspace_bytes, hipStream_t stream);
 
 /* dv_cache_attention with a window: of the places that a row would see there, the first e of its
- * sequence, it sees those from e - window on, and the first `sinks`.  Pages between that no row of a call sees are not
- * read, and need not be there (a table entry that is no page): the keys that a call takes time for are the
- * window's and the sinks', whatever the sequences' lengths.  A window of 2^30 and more sees all (Section 2.3's attention over
+ * sequence, it sees those from e - window on, and the first `sinks`.  Pages between that no row of a call sees may hold
+ * anything, codes and scales, and need not be there (a table entry that is no page): the keys that a call takes time for
+ * are the window's and the sinks', in whole steps of 64, whatever the sequences' lengths.  A window of 2^30 and more sees all (Section 2.3's attention over
  * the memory of Section 5.2, bounded for streams that do not end).  Errors: those of
  * dv_cache_attention, and DV_EINVAL for window < 1, sinks < 0.  The workspace's size depends on both. */
 int dv_cache_attention_window_workspace(const dv_cache* cache, int n_seqs, int table_pages,

@@ -216,6 +216,12 @@ __device__ __forceinline__ int page_at(const CacheAttnArgs& a, const Tile& t, in
     if (in_front<KEYS>(t, v)) return j < a.front.table_pages && (unsigned)entry < (unsigned)a.c.pages ? entry : -1;
     return page_from(a.seq, a.c.pages, entry, t.seq, j);
 }
+// Where the window of a tile's first row starts, and whether that leaves the 16 keys from `key` on to no row of the tile: the
+// steps at either end of what is left out (leave_out) hold such keys, whole pages of them where those are of 16 or 32.
+__device__ __forceinline__ int window_start(const CacheAttnArgs& a, const Tile& t, int G) {
+    return max(a.causal ? t.len - t.n + t.first / G + 1 : t.len, 0) - a.window;
+}
+__device__ __forceinline__ bool hidden(const CacheAttnArgs& a, int tlow, int key) { return key >= a.sinks && key + 16 <= tlow; }
 // What the row that sees keys below `sees` sees of the step at place v, of keys before `last` (find_odd).
 template <int KEYS>
 __device__ __forceinline__ void find_odd_seen(Odd& f, const CacheAttnArgs& a, const Tile& t, int h, int v, int last, int sees,
@@ -272,6 +278,7 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
     const int r = t.first + min(c16, t.rows - 1), qi = r / G;
     const int sees = a.causal ? t.len - t.n + qi + 1 : t.len;
     const int low = max(sees, 0) - a.window;   // WINDOW: keys from here on, and the first `sinks`
+    const int tlow = window_start(a, t, G);    // ... of the tile's first row: no row sees keys from the first ones up to here
     const size_t qat = (size_t)(t.row0 + qi) * a.q_stride + (size_t)(h * G + r % G) * DH;
     bf16x8 qf[KS][NT];
 #pragma unroll
@@ -397,7 +404,8 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
             }
             // values that no row of the tile sees may hold anything, and so may the scale of a page
             // that has none else: 0
-            const int there = present ? until - kv : 0;
+            int there = present ? until - kv : 0;
+            if constexpr (KEYS == WINDOW) there = hidden(a, tlow, kv) ? 0 : there;
             if (there <= 0) vs = 1.f;
             const uint32_t odd = odd_codes(vs);
 #pragma unroll
@@ -551,6 +559,7 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
     // WINDOW: where the windows of the lane's row and of the last rows of the wavefront and the block start, and of the
     // wavefront's first
     const int low = max(sees, 0) - a.window, blow = t.end - a.window, wfrom = max(wall, 0) - a.window;
+    const int tlow = window_start(a, t, G);   // ... of the block's first row
     const int wlow = max(a.causal ? t.len - t.n + wlast + 1 : t.len, 0) - a.window;
     bf16x8 qf[KS];
     {
@@ -625,7 +634,8 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
         // values past the keys that anyone sees, and of pages that are not there, are 0
         const bool front = in_front<KEYS>(t, v);
         const int until = front ? t.front_len : kend;
-        const int there = vin ? until - kb - tid % 4 * 16 : 0;
+        int there = vin ? until - kb - tid % 4 * 16 : 0;
+        if constexpr (KEYS == WINDOW && !ONE) there = hidden(a, tlow, kb + tid % 4 * 16) ? 0 : there;   // (a row sees some key of every step)
         bool part = kb + STEP > min(front ? until : ball, until) || !vin;   // not all rows see all of it
         if constexpr (KEYS == WINDOW) part |= kb < blow && kb + STEP > a.sinks;
         if (there <= 0) vsc = 1.f;
