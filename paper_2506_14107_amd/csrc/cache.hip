@@ -453,13 +453,15 @@ __device__ __forceinline__ PagePart page_part(const SeqArgs& q, int pt, int page
 // table entry, rows, scale and codes).  Further blocks turn the query rows.  In bf16 the rows of the next pass are asked for while
 // one is computed (60,000 tokens of 8 heads of 128 94 us without, 80 so; fp32 would spill: 26 us, 36), and the kernels with norms
 // take three wavefronts a SIMD, whose registers hold that (9232 tokens of 16 heads of 80 with as many query heads, normed: 59 us with
-// four and no rows ahead, 74 with four and spills, 52 with three and none ahead, 48 so; 118 MB).
+// four and no rows ahead, 74 with four and spills, 52 with three and none ahead, 48 so; 118 MB).  Without norms the rows ahead spill four
+// registers, which a call of one pass would only pay for (one token a sequence of 16 heads of 80, kernels one behind the other, us with / without
+// them: 1 sequence 4.98 / 4.83, 48 6.41 / 6.25; 48 without a rotation 6.38 / 6.15): such calls take an instance without (write_in_one_pass).
 constexpr int MAX_ITEMS = 2;                    // items of 16 channels a thread and pass
-// WT threads a block (write_threads).  NORM: keys, queries or both are normed first.
-template <bool BF, int V, int WT, bool NORM>
+// WT threads a block (write_threads).  NORM: keys, queries or both are normed first.  MORE: blocks may take several passes.
+template <bool BF, int V, int WT, bool NORM, bool MORE>
 __global__ __launch_bounds__(WT, NORM ? 3 : 4) void cache_write_k(WriteArgs a) {
     constexpr int PASS = MAX_ITEMS * WT;      // items of a pass: one head's, or more heads'
-    constexpr bool AHEAD = V > 1 && BF;   // (the others have no registers for it)
+    constexpr bool AHEAD = V > 1 && BF && MORE;   // (the others have no registers for it)
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ uint32_t s_most[WRITE_HEADS];
     __shared__ float s_scale[WRITE_HEADS], s_old[WRITE_HEADS];
@@ -839,25 +841,29 @@ void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
     const size_t lds = std::max({(size_t)pass * 20,
                                  ((size_t)c.page_tokens * ((a.rot.dim / 2 + 3) & ~3) * 2 + (norm ? pass : 0)) * sizeof(float),
                                  (ROT_LDS + (norm ? NORM_ITEMS * threads : 0)) * sizeof(float)});   // 64 KB, 68 at most
-    auto launch = [&](auto f, auto v, auto normed) {
-        constexpr bool B = decltype(f)::value, N = decltype(normed)::value;
+    auto launch = [&](auto f, auto v, auto normed, auto several) {
+        constexpr bool B = decltype(f)::value, N = decltype(normed)::value, M = decltype(several)::value;
         constexpr int V = decltype(v)::value;
         if (threads == 256) {
-            cache_write_k<B, V, 256, N><<<grid, 256, lds, s>>>(a);
+            cache_write_k<B, V, 256, N, M><<<grid, 256, lds, s>>>(a);
         } else {   // 64 KB beside the kernel's own
-            static const bool ok = allow_lds((const void*)cache_write_k<B, V, 512, N>, N ? 68 << 10 : 64 << 10);
+            static const bool ok = allow_lds((const void*)cache_write_k<B, V, 512, N, M>, N ? 68 << 10 : 64 << 10);
             (void)ok;
-            cache_write_k<B, V, 512, N><<<grid, 512, lds, s>>>(a);
+            cache_write_k<B, V, 512, N, M><<<grid, 512, lds, s>>>(a);
         }
     };
     using W8 = std::integral_constant<int, 8>;
     using W4 = std::integral_constant<int, 4>;
     using W1 = std::integral_constant<int, 1>;
-    auto go = [&](auto v, auto normed) { bf ? launch(std::true_type(), v, normed) : launch(std::false_type(), v, normed); };
+    auto go = [&](auto v, auto normed) {
+        bf ? launch(std::true_type(), v, normed, std::true_type()) : launch(std::false_type(), v, normed, std::true_type());
+    };
     if (norm) {
         if (wide) go(W8(), std::true_type());
         else if (fits(4, 4 * el)) go(W4(), std::true_type());
         else go(W1(), std::true_type());
+    } else if (wide && bf && write_in_one_pass(c.page_tokens, c.head_dim, a.heads, a.seq.n_seqs, a.seq.rows)) {
+        launch(std::true_type(), W8(), std::false_type(), std::false_type());
     } else if (wide) {
         go(W8(), std::false_type());
     } else {

@@ -166,6 +166,11 @@ inline int write_heads(long long slots, int kv_heads, int cus) {
     while (heads > 1 && slots * 2 * ((kv_heads + heads - 1) / heads) < least) heads = (heads + 1) / 2;
     return heads;
 }
+// Whether a block of about the mean of the sequences' tokens takes its heads in one pass of two items a thread.
+inline bool write_in_one_pass(int pt, int dh, int heads, int n_seqs, int rows) {
+    const long long tokens = std::min<long long>(pt, ((long long)rows + n_seqs - 1) / std::max(1, n_seqs));
+    return tokens * (dh / 16) * heads <= 2 * write_threads(pt, dh);
+}
 // Threads that a write launches at most: a block per page, head and keys or values, and those of the queries.
 inline long long cache_write_threads(int pt, int dh, int kv_heads, int n_seqs, int rows, bool offsets, int q_heads) {
     const int per = q_heads ? rows_a_block(q_heads, dh, 1) : 1;
