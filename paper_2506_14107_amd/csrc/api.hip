@@ -1746,15 +1746,12 @@ int dv_cache_attention_shared(const dv_cache* cache, int n_seqs, const int32_t* 
         (rc = check_workspace(p.bytes, workspace, workspace_bytes)))
         return rc;
     if (rows == 0) return DV_OK;
-    SeqArgs prefix = {n_groups, prefix_table_pages, rows, prefix_table, offsets, prefix_lengths};
-    prefix.by_group = 1;
-    prefix.grouped = n_seqs;
-    prefix.groups = groups;
     CacheAttnArgs a = attention_args(cache, n_seqs, table, table_pages, offsets, lengths, q, q_stride, rows, q_heads, scale,
                                      causal, out, out_stride);
-    a.front = prefix;
+    a.front = {n_groups, prefix_table_pages, rows, prefix_table, offsets, prefix_lengths};
+    a.groups = {groups, n_seqs, 0};
     if (p.behind) launch_cache_behind(dtype == DV_BF16, a, p.own, (float*)workspace, stream);
-    else launch_cache_shared(dtype == DV_BF16, a, prefix, p.own, p.prefix, (float*)workspace, stream);
+    else launch_cache_shared(dtype == DV_BF16, a, p.own, p.prefix, (float*)workspace, stream);
     HIP_TRY(hipGetLastError());
     return DV_OK;
 }

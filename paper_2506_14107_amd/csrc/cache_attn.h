@@ -181,12 +181,13 @@ __device__ __forceinline__ Tile tile_at(const CacheAttnArgs& a, long long u) {
     auto other = [&](const Seq& s) { return a.route == ATTN_BOTH && ((long long)s.n * G > few_rows(a.c.head_dim)) != (SHIFT == LS); };
     auto count = [&](const Seq& x) { return other(x) ? 0 : tile_count(x, G, SHIFT); };
     Seq s;
-    if (KEYS == PART && a.seq.by_group) s = find_seq<true>(a.seq, count, (int)u);
-    else s = a.seq.offsets ? find_seq<false>(a.seq, count, (int)u) : seq_of(a.seq, (int)(u / ((G + (1 << SHIFT) - 1) >> SHIFT)));
-    Tile t = tile_of(a.seq, a.c.page_tokens, G, SHIFT, a.causal != 0, s, u);
+    const bool groups = KEYS == PART && a.groups.on;
+    if (groups) s = find_group(a.seq, a.groups, count, (int)u);
+    else s = a.seq.offsets ? find_seq(a.seq, count, (int)u) : seq_of(a.seq, (int)(u / ((G + (1 << SHIFT) - 1) >> SHIFT)));
+    Tile t = tile_of(a.seq, a.c.page_tokens, G, SHIFT, a.causal != 0, s, u, groups);
     if (other(s)) t.seq = -1;
     if constexpr (KEYS == WINDOW) leave_out(t, G, a.causal != 0, a.window, a.sinks);
-    if constexpr (KEYS == BEHIND) put_behind(t, a.front, a.c.page_tokens);
+    if constexpr (KEYS == BEHIND) put_behind(t, a.front, a.groups, a.c.page_tokens);
     return t;
 }
 // The key at place v of those that a tile takes (steps of 64 lie together).

@@ -114,13 +114,13 @@ __host__ __device__ inline long long tile_slots(bool offsets, int n_seqs, int ro
     return offsets ? ((long long)rows * group >> shift) + n_seqs
                    : (long long)n_seqs * ((group + (1 << shift) - 1) >> shift);
 }
-// ... slot u, of sequence s (without offsets: of sequence u / tiles of a row)
+// ... slot u, of sequence s (without offsets: of sequence u / tiles of a row, unless the sequences are groups)
 __host__ __device__ inline Tile tile_of(const SeqArgs& q, int pt, int group, int shift, bool causal, const Seq& sp,
-                                        long long u) {
+                                        long long u, bool groups = false) {
     Tile t = {-1, 0, 0, 0, 0, 0, 0, 0, 0, -1, 0};
     const int s = sp.s;
     if (s < 0) return t;
-    const long long j = q.offsets || q.by_group ? u - sp.slot0 : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
+    const long long j = q.offsets || groups ? u - sp.slot0 : u - (long long)s * ((group + (1 << shift) - 1) >> shift);
     const long long first = j << shift, left = (long long)sp.n * group - first;
     if (j < 0 || left <= 0) return t;
     t.seq = s;
@@ -333,16 +333,9 @@ __device__ __forceinline__ int sum_up(int x) {
 }
 // The sequence that owns slot u (every lane of a wavefront calls, with the same u); count: the slots of one.  N times 64
 // sequences are looked at together: a chain of loads is what small calls wait for.
-// GROUPS: of the groups of sequences, whose rows lie together.
-__device__ __forceinline__ Seq group_from(const SeqArgs& q, int g) {
-    auto first = [&](int i) {   // row of sequence groups[i]
-        const int s = q.groups ? max(0, min(q.groups[i], q.grouped)) : i ? q.grouped : 0;
-        return q.offsets ? q.offsets[s] : s;
-    };
-    return seq_from(q, g, first(g), first(g + 1), q.at[g]);
-}
-template <int N, bool GROUPS, class Count>
-__device__ __forceinline__ Seq find_among(const SeqArgs& q, const Count& count, int u) {
+// from(s): sequence s.
+template <int N, class From, class Count>
+__device__ __forceinline__ Seq find_among(const SeqArgs& q, const From& from, const Count& count, int u) {
     const int lane = threadIdx.x & 63;
     int base = 0;
     for (int b = 0; b < q.n_seqs; b += 64 * N) {
@@ -350,8 +343,8 @@ __device__ __forceinline__ Seq find_among(const SeqArgs& q, const Count& count, 
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int s = b + i * 64 + lane, c = s < q.n_seqs ? s : q.n_seqs - 1;
-            if (GROUPS) sp[i] = group_from(q, c), sp[i].s = s;
-            else sp[i] = seq_from(q, s, q.offsets[c], q.offsets[c + 1], q.at[c]);
+            sp[i] = from(c);
+            sp[i].s = s;
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -365,29 +358,43 @@ __device__ __forceinline__ Seq find_among(const SeqArgs& q, const Count& count, 
     }
     return {-1, 0, 0, 0, 0};
 }
+// Group g as a sequence: its sequences' rows lie together.
+__device__ __forceinline__ Seq group_from(const SeqArgs& q, const GroupArgs& by, int g) {
+    auto first = [&](int i) {   // row of its first sequence
+        const int s = by.first ? max(0, min(by.first[i], by.n)) : i ? by.n : 0;
+        return q.offsets ? q.offsets[s] : s;
+    };
+    return seq_from(q, g, first(g), first(g + 1), q.at[g]);
+}
 // The group of sequence `seq` (-1: none; every lane of a wavefront calls, with the same one).
-__device__ __forceinline__ int group_of(const SeqArgs& q, int seq) {
-    if (!q.groups) return 0;
+__device__ __forceinline__ int group_of(const SeqArgs& q, const GroupArgs& by, int seq) {
+    if (!by.first) return 0;
     const int lane = threadIdx.x & 63;
     for (int b = 0; b < q.n_seqs; b += 64) {
         const int g = b + lane, c = g < q.n_seqs ? g : q.n_seqs - 1;
-        const uint64_t here = __ballot(g < q.n_seqs && q.groups[c] <= seq && seq < q.groups[c + 1]);
+        const uint64_t here = __ballot(g < q.n_seqs && by.first[c] <= seq && seq < by.first[c + 1]);
         if (here) return b + __ffsll((unsigned long long)here) - 1;
     }
     return -1;
 }
 // The tile takes its group's prefix first, in whole steps.
-__device__ __forceinline__ void put_behind(Tile& t, const SeqArgs& q, int pt) {
+__device__ __forceinline__ void put_behind(Tile& t, const SeqArgs& q, const GroupArgs& by, int pt) {
     if (t.seq < 0) return;
-    t.group = group_of(q, t.seq);
+    t.group = group_of(q, by, t.seq);
     if (t.group < 0) return;
     t.front_len = max(0, min(q.at[t.group], q.table_pages * pt));
     t.skip0 = (t.front_len + 63) & ~63;
     t.left_out = -t.skip0;
 }
-template <bool GROUPS = false, class Count>
+template <class Count>
 __device__ __forceinline__ Seq find_seq(const SeqArgs& q, const Count& count, int u) {
-    return q.n_seqs <= 64 ? find_among<1, GROUPS>(q, count, u) : find_among<4, GROUPS>(q, count, u);
+    auto from = [&](int s) { return seq_from(q, s, q.offsets[s], q.offsets[s + 1], q.at[s]); };
+    return q.n_seqs <= 64 ? find_among<1>(q, from, count, u) : find_among<4>(q, from, count, u);
+}
+template <class Count>
+__device__ __forceinline__ Seq find_group(const SeqArgs& q, const GroupArgs& by, const Count& count, int u) {
+    auto from = [&](int g) { return group_from(q, by, g); };
+    return q.n_seqs <= 64 ? find_among<1>(q, from, count, u) : find_among<4>(q, from, count, u);
 }
 #endif
 

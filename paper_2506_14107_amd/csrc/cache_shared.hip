@@ -48,13 +48,13 @@ __global__ __launch_bounds__(256, 2) void cache_shared_small_k(SharedArgs a) {
 struct Prefix {
     int g, row0, n, len, few0, many0;   // (its first slots of small and large tiles)
 };
-__device__ __forceinline__ Prefix prefix_of(const SeqArgs& q, int seq, int G, int few_rows_, int route) {
+__device__ __forceinline__ Prefix prefix_of(const SeqArgs& q, const GroupArgs& by, int seq, int G, int few_rows_, int route) {
     const int lane = threadIdx.x & 63;
     int few = 0, many = 0;
     for (int b = 0; b < q.n_seqs; b += 64) {
         const int g = b + lane, c = min(g, q.n_seqs - 1);
-        const Seq s = group_from(q, c);
-        const int from = q.groups ? q.groups[c] : 0, to = q.groups ? q.groups[c + 1] : q.grouped;
+        const Seq s = group_from(q, by, c);
+        const int from = by.first ? by.first[c] : 0, to = by.first ? by.first[c + 1] : by.n;
         const bool small = route == ATTN_FEW || (route == ATTN_BOTH && (long long)s.n * G <= few_rows_);
         const int nf = g < q.n_seqs && small ? tile_count(s, G, TS) : 0, nm = g < q.n_seqs && !small ? tile_count(s, G, LS) : 0;
         const int uf = sum_up(nf), um = sum_up(nm);
@@ -94,7 +94,7 @@ template <int SHIFT>
 __device__ __forceinline__ Parts parts_of(const CacheAttnArgs& a, const CacheAttnArgs& pre, const Tile& t, long long u, int h) {
     const int H = a.c.kv_heads, DH = a.c.head_dim, G = a.q_heads / H, limit = few_rows(DH);
     const CacheAttnCut& cut = SHIFT == TS ? a.few : a.many;
-    const Prefix p = prefix_of(pre.seq, t.seq, G, limit, pre.route);
+    const Prefix p = prefix_of(pre.seq, pre.groups, t.seq, G, limit, pre.route);
     const bool small = pre.route == ATTN_FEW || (pre.route == ATTN_BOTH && (long long)p.n * G <= limit);
     const CacheAttnCut& pc = small ? pre.few : pre.many;
     const int len = (int)min((long long)max(p.len, 0), (long long)pre.seq.table_pages * a.c.page_tokens);
@@ -259,10 +259,11 @@ void launch_shared(bool bf, const SharedArgs& a, hipStream_t s) {
 
 }  // namespace
 
-void launch_cache_shared(bool bf, CacheAttnArgs a, const SeqArgs& prefix, const CacheAttnPlan& p, const CacheAttnPlan& pre,
-                         float* workspace, hipStream_t s) {
+void launch_cache_shared(bool bf, CacheAttnArgs a, const CacheAttnPlan& p, const CacheAttnPlan& pre, float* workspace,
+                         hipStream_t s) {
     SharedArgs x{{a, a}, {}};
-    x.part[1].seq = prefix;
+    x.part[1].seq = a.front;
+    x.part[1].groups.on = 1;
     x.part[1].causal = 0;
     set_plan(x.part[0], p, workspace);
     set_plan(x.part[1], pre, workspace + p.bytes / sizeof(float));

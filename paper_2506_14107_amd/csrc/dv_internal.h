@@ -319,9 +319,13 @@ struct SeqArgs {
     const int* offsets;    // [n_seqs + 1] first row of each sequence (nullptr: one row each)
     const int* at;         // [n_seqs] write, read: place of the first row; attention: keys
     int one;               // one sequence that all rows belong to (offsets nullptr)
-    int by_group;          // attention: the sequences are groups of a call's `grouped` ones, groups[i] .. groups[i + 1] - 1 (nullptr:
-    int grouped;           // one of all); offsets are those ones'
-    const int* groups;
+};
+// Sequences in groups: group i has sequences first[i] .. first[i + 1] - 1 of n (first nullptr: one group of all).  A SeqArgs of
+// groups has their tables and lengths, and the offsets of the sequences.
+struct GroupArgs {
+    const int* first;
+    int n;
+    int on;                // of a part of a call: its sequences are groups
 };
 struct WriteArgs {
     CacheView c;
@@ -333,10 +337,11 @@ struct WriteArgs {
     const int* pos;            // [rows, 3]; unused where rot.dim is 0
     const int* row_idx;        // row r of the call is row row_idx[r] of k and v (nullptr: r)
     RotaryPlan rot;
-    NormArgs k_norm, q_norm;   // of keys and queries, before they are turned
     int cus;                   // compute units of the device (0: planned as for 256)
     int heads, kv_blocks, q_rows;   // set by the launcher
     uint32_t by_tok;
+    // (last: a block waits for each 64 bytes of arguments that it reads)
+    NormArgs k_norm, q_norm;   // of keys and queries, before they are turned
 };
 void launch_cache_write(bool bf16, WriteArgs a, hipStream_t s);
 struct ReadArgs {
@@ -381,11 +386,14 @@ struct CacheAttnArgs {
     int q_heads;
     float scale;
     int causal;
-    int window, sinks;   // of a call with a window
-    SeqArgs front;       // behind prefixes: their table, lengths and groups
     // set by the launcher
     int route;
     CacheAttnCut few, many;
+    // last, because a block waits for each 64 bytes of arguments that it reads: with these ahead of the route, calls without
+    // them took 0.2 to 0.5 us longer (questions of 333 rows in bf16 13.1 -> 13.5)
+    int window, sinks;   // of a call with a window
+    SeqArgs front;       // behind prefixes: their table and lengths
+    GroupArgs groups;    // ... and of a shared call's part: groups
 };
 // What a call takes, from its sizes (cache_plan.h): the same rule sizes the workspace.
 struct CacheAttnPlan {
@@ -396,10 +404,10 @@ struct CacheAttnPlan {
 };
 void launch_cache_attention(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);
 void launch_cache_window(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);   // a.window, a.sinks
-// Sequences behind prefixes that groups of them share: `prefix` has the prefixes' table, lengths and groups, the parts'
-// results meet in the workspace (p's, then pre's).
-void launch_cache_behind(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);   // a.front
-void launch_cache_shared(bool bf16, CacheAttnArgs a, const SeqArgs& prefix, const CacheAttnPlan& p, const CacheAttnPlan& pre,
-                         float* workspace, hipStream_t s);
+// Sequences behind prefixes that groups of them share (a.front, a.groups); the parts' results of the second meet in the
+// workspace (p's, then pre's).
+void launch_cache_behind(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, float* workspace, hipStream_t s);
+void launch_cache_shared(bool bf16, CacheAttnArgs a, const CacheAttnPlan& p, const CacheAttnPlan& pre, float* workspace,
+                         hipStream_t s);
 
 }  // namespace dv

@@ -60,3 +60,19 @@ def test_steps_of_single_tokens_take_one_pass(tmp_path):
                     for tokens in (2, 5, 40, 200):
                         assert bool(one(pt, dh, heads, n, tokens * n)) == (min(tokens, pt) * (dh // 16) * heads <= 2 * threads)
     assert not one(64, 80, 16, 6, 9232) and not one(64, 128, 8, 4, 60000) and not one(128, 128, 8, 4, (1 << 31) - 1)
+
+
+def test_arguments_that_every_call_reads_come_first(tmp_path):
+    """A block waits for each 64 bytes of its arguments that it reads: what only windows, shared prefixes and norms need lies
+    behind what every call does, and sequences hold nothing of groups."""
+    at = host(tmp_path, """extern "C" void at(long long* o) {
+    const size_t x[] = {sizeof(SeqArgs), offsetof(CacheAttnArgs, many) + sizeof(CacheAttnCut), offsetof(CacheAttnArgs, window),
+                        offsetof(CacheAttnArgs, front), offsetof(CacheAttnArgs, groups), offsetof(WriteArgs, by_tok), offsetof(WriteArgs, k_norm)};
+    for (size_t i = 0; i < sizeof x / sizeof x[0]; ++i) o[i] = (long long)x[i];
+}
+""").at
+    o = (ctypes.c_longlong * 7)()
+    at(o)
+    seq, plain, window, front, groups, tok, norm = o
+    assert seq == 48 and plain <= min(window, front, groups) and tok < norm
+    assert plain <= 4 * 64
