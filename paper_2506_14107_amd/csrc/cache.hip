@@ -296,19 +296,27 @@ __device__ __forceinline__ float sum_squares(const float (&x)[16]) {
     for (int e = 0; e < 16; ++e) s = fmaf(x[e], x[e], s);
     return s;
 }
-// ... normed; part: the sums of squares of the head's dh / 16 chunks; w: the weight's chunk, where there is one
+// A head's squares are summed as this times their size, a power of two: channels of 2^60 each then sum to 2^127 at most, whatever
+// the head (1 up to 128 channels).  Scaled exactly, sums round as they would without.
+__device__ __forceinline__ float sum_scale(int dh) {
+    const int over = 25 - __builtin_clz(dh - 1);   // of the least 2^n >= dh over 2^7
+    return __builtin_bit_cast(float, (uint32_t)(127 - max(over, 0)) << 23);
+}
+// The weight's chunk, where there is a weight.
 template <bool BF, int V>
 __device__ __forceinline__ void load_weight(const NormArgs& nm, int dh, int h, int dim, bool pairs, int c, Raw<BF, V>& w) {
     if (nm.weight) load_raw<BF, V>(nm.weight, nm.per_head ? (size_t)h * dh : 0, dim, pairs, c, w);
 }
+// The chunk normed; part: the sums of squares of the head's dh / 16 chunks; down: sum_scale
 template <bool BF, int V>
-__device__ __forceinline__ void norm_chunk(const NormArgs& nm, const float* part, int dh, const Raw<BF, V>& w, float (&x)[16]) {
+__device__ __forceinline__ void norm_chunk(const NormArgs& nm, const float* part, int dh, float down, const Raw<BF, V>& w,
+                                           float (&x)[16]) {
     const int n = dh / 16;
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += i < n ? part[i] : 0.f;
-    for (int i = 8; i < n; ++i) sum += part[i];
-    const float f = rsqrtf(sum / (float)dh + nm.eps);
+    for (int i = 0; i < 8; ++i) sum += i < n ? part[i] * down : 0.f;
+    for (int i = 8; i < n; ++i) sum += part[i] * down;
+    const float f = rsqrtf(sum / ((float)dh * down) + nm.eps);
     if (nm.weight) {
         float y[16];
         unpack(w, y);
@@ -330,6 +338,7 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& r
     float *cos = lds, *sin = lds + ROT_ROWS * 64, *part = lds + ROT_LDS;
     if (rot.dim) angles_of<NT>(rot, n, cos, sin, ld, [&](int r) { return a.pos + (size_t)(row0 + r) * 3; });
     const int per_head = a.dh / 16, per_row = per_head * a.heads, total = n * per_row;
+    const float down = sum_scale(a.dh);
     const int batch = NORM_ITEMS * NT / per_head * per_head;   // whole heads
     for (int first = 0; first < total; first += batch) {
         const int end = min(batch, total - first);
@@ -357,7 +366,7 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& r
             if (i >= end) continue;
             Raw<BF, V> w;
             load_weight<BF, V>(nm, a.dh, hh[k], rot.dim, rot.pairs, cc[k], w);
-            norm_chunk<BF, V>(nm, part + i - cc[k], a.dh, w, x[k]);
+            norm_chunk<BF, V>(nm, part + i - cc[k], a.dh, down, w, x[k]);
             turn_chunk<V>(rot.dim, rot.pairs, cc[k], cos + rr[k] * ld, sin + rr[k] * ld, x[k]);
             store_chunk<BF, V>(a.out, (size_t)(row0 + rr[k]) * a.out_stride + (size_t)hh[k] * a.dh, rot.dim, rot.pairs, cc[k],
                                x[k]);
@@ -370,6 +379,7 @@ template <bool BF, int NT>
 __device__ __forceinline__ void norm_rows_any(const RowsArgs& a, const RotaryPlan& rot, const NormArgs& nm, int row0, int n,
                                               float* lds) {
     const int lane = threadIdx.x & 63, ld = (rot.dim / 2 + 3) & ~3;
+    const float down = sum_scale(a.dh);
     float *cos = lds, *sin = lds + ROT_ROWS * 64;
     if (rot.dim) angles_of<NT>(rot, n, cos, sin, ld, [&](int r) { return a.pos + (size_t)(row0 + r) * 3; });
     __syncthreads();
@@ -381,11 +391,11 @@ __device__ __forceinline__ void norm_rows_any(const RowsArgs& a, const RotaryPla
         for (int c = lane; c < a.dh; c += 64) {
             float x[1];
             load_ch<BF, 1>(a.x, at + c, x);
-            sum = fmaf(x[0], x[0], sum);
+            sum = fmaf(x[0] * down, x[0], sum);
         }
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        const float f = rsqrtf(sum / (float)a.dh + nm.eps);
+        const float f = rsqrtf(sum / ((float)a.dh * down) + nm.eps);
         for (int p = lane; p < a.dh / 2; p += 64) {
             const Item it = item_at<1>(rot.dim, rot.pairs, p);
             float x[1], y[1], u[1] = {1.f}, w[1] = {1.f};
@@ -547,7 +557,7 @@ __global__ __launch_bounds__(WT, NORM ? 3 : 4) void cache_write_k(WriteArgs a) {
         if constexpr (AHEAD)
             if (h0 + hn < end) ask(h0 + hn);
         const bool normed = NORM && !values && a.k_norm.on;
-                if (normed) {
+        if (normed) {
 #pragma unroll
             for (int k = 0; k < MAX_ITEMS; ++k) {
                 if (hh[k] >= hn) continue;
@@ -561,7 +571,7 @@ __global__ __launch_bounds__(WT, NORM ? 3 : 4) void cache_write_k(WriteArgs a) {
             if (normed) {
                 Raw<BF, V> w;
                 load_weight<BF, V>(a.k_norm, dh, h0 + hh[k], dim, a.rot.pairs, cc[k], w);
-                norm_chunk<BF, V>(a.k_norm, part + tid + k * WT - cc[k], dh, w, x[k]);
+                norm_chunk<BF, V>(a.k_norm, part + tid + k * WT - cc[k], dh, 1.f, w, x[k]);   // (dh <= 128)
             }
             turn_chunk<V>(dim, a.rot.pairs, cc[k], cos + tt[k] * ald, sin + tt[k] * ald, x[k]);
             float most = 0.f;   // a NaN does not count
