@@ -713,9 +713,12 @@ __device__ __forceinline__ void attend_large(const CacheAttnArgs& a, Lds<DH>& ld
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int j = 2 * b + (e >> 3), i = 16 * j + (e & 7);
-                    bool in = i < live && (there >> 8 * j & 1);
-                    if constexpr (KEYS == WINDOW) in = in && (i >= low - kb - 8 * hl || i < a.sinks - kb - 8 * hl);
-                    sc[b][e] = in ? sc[b][e] : -INFINITY;
+                    if constexpr (KEYS == WINDOW) {
+                        const bool in = i < live && (there >> 8 * j & 1) && (i >= low - kb - 8 * hl || i < a.sinks - kb - 8 * hl);
+                        sc[b][e] = in ? sc[b][e] : -INFINITY;
+                    } else {
+                        sc[b][e] = i < live && (there >> 8 * j & 1) ? sc[b][e] : -INFINITY;
+                    }
                 }
         }
         float mx[5];   // five chains
