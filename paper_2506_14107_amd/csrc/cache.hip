@@ -24,7 +24,7 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x8 __attribute__((ext_vector_type(8), aligned(16)));   // (rows start on 16 bytes, not on 32)
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -247,10 +247,24 @@ __device__ __forceinline__ void store_chunk(void* base, size_t at, int dim, bool
 }
 // The same in two steps, for loads that are asked for well before they are needed: the chunk as it lies in memory, and x.
 template <bool BF, int V>
+struct Group;   // V channels; (a type passed as a template's argument would lose its alignment)
+template <>
+struct Group<true, 8> { using T = bf16x8; };
+template <>
+struct Group<true, 4> { using T = bf16x4; };
+template <>
+struct Group<true, 1> { using T = __bf16; };
+template <>
+struct Group<false, 8> { using T = f32x8; };
+template <>
+struct Group<false, 4> { using T = f32x4; };
+template <>
+struct Group<false, 1> { using T = float; };
+template <bool BF, int V>
 struct Raw {
-    using T = std::conditional_t<BF, std::conditional_t<V == 8, bf16x8, std::conditional_t<V == 4, bf16x4, __bf16>>,
-                                 std::conditional_t<V == 8, f32x8, std::conditional_t<V == 4, f32x4, float>>>;
+    using T = typename Group<BF, V>::T;
     T v[16 / V];   // item e's two groups at 2 e and 2 e + 1
+    static_assert(alignof(T) <= 16, "rows start on 16 bytes at best");
 };
 template <bool BF, int V>
 __device__ __forceinline__ void load_raw(const void* base, size_t at, int dim, bool pairs, int c, Raw<BF, V>& r) {
