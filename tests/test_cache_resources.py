@@ -10,7 +10,7 @@ import pytest
 
 from paper_2506_14107_amd import dejavu as dj
 
-from .test_kernel_resources import LLVM
+from .test_kernel_resources import LLVM, kernels, of  # noqa: F401 (a fixture)
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "..", "paper_2506_14107_amd", "csrc")
@@ -76,3 +76,33 @@ def test_arguments_that_every_call_reads_come_first(tmp_path):
     seq, plain, window, front, groups, tok, norm = o
     assert seq == 48 and plain <= min(window, front, groups) and tok < norm
     assert plain <= 4 * 64
+
+
+@pytest.mark.parametrize("kind", ["window", "behind", "shared"])
+def test_resident_blocks_of_windows_and_shared_prefixes(kernels, kind):
+    """As of attention over all keys: what the choice of tiles and splits counts on, of registers and LDS."""
+    def resident(name, lds=None):
+        k, = of(kernels, name)
+        return min(512 // (-(-k["vgpr_count"] // 8) * 8), (160 << 10) // (lds or k["group_segment_fixed_size"]))
+
+    small, large = (f"cache_{kind}_k", f"cache_{kind}_tile_k") if kind != "shared" else ("cache_shared_small_k", "cache_shared_k")
+    for dh in range(16, 129, 16):
+        count = 2 if dh > 85 else 3 if dh > 64 else 4
+        assert resident(f"{small}ILi{dh}ELb1E") >= count and resident(f"{small}ILi{dh}ELb0E") >= 2, dh
+        lds = max(2 * 64 * (2 * dh + 16) + 2 * dh * (2 * 64 + 16) + 16, 4 * 4 * 16 * (dh + 6))   # (large tiles', or small ones' partial results)
+        for one in (0, 1):
+            assert resident(f"{large}ILi{dh}ELb{one}E", lds) >= 2, dh
+
+
+def test_what_spills(scratch):
+    """Attention and norms of rows spill nothing; writes do where a lane takes one channel, and a little in bf16 without norms with rows
+    ahead and with norms by fours."""
+    for k, v in scratch.items():
+        if re.search(r"cache_(attn|window|behind|shared|join|read|extend)|norm_rotary_k", k):
+            assert v == 0, k
+    most = {"Lb1ELi8": 20, "Lb0ELi8": 0, "Lb1ELi4": 44, "Lb0ELi4": 0}
+    writes = {k: v for k, v in scratch.items() if "cache_write_k" in k and "Li1E" not in k}
+    assert len(writes) == 14
+    for k, v in writes.items():
+        assert v <= most[re.search(r"cache_write_kI(Lb[01]ELi[48])", k).group(1)], k
+        assert v == 0 or "Li4E" in k or "ELb0ELb1E" in k, k
