@@ -275,16 +275,19 @@ inline CacheSharedPlan cache_shared_plan(bool bf, int n_seqs, int rows, bool off
     p.prefix.route = !large ? ATTN_FEW : n_groups == 1 ? ATTN_MANY : ATTN_BOTH;
     // Tiles of the sequences take the prefix themselves where that is less than a pass of its own costs.  Estimates in us: a
     // large tile takes its keys at 0.95 PFLOP/s; a small one 2 head_dim + 96 bytes a key at 13.7 TB/s, most of them from the
-    // caches, and in a pass of its own, whose blocks are cut to fill the chip, 2 head_dim at 14; all no faster than the memory has
-    // them once.  Two parts are 4 us and 1.2 ns a row and head of 128 channels more (partial results and their join).  us of a call, two
+    // caches, and in a pass of its own, whose blocks are cut to fill the chip, 2 head_dim at 14; a pass no faster than the memory has
+    // them once, tiles that repeat it no faster than that and the caches (12.8 TB/s) the rest.  Two parts are 4 us and 1.2 ns a row and head of 128 channels more (partial results and their join).  us of a call, two
     // parts / behind, 8 heads of 128 with 4 queries each, prefixes of 128, 512, 2048, 8192: 64 sequences of a row 14 / 11, 15 / 14,
     // 21 / 35, 37 / 105; 12 of 33 29 / 16, 33 / 24, 44 / 62, 90 / 178; 64 of 40 141 / 37, 125 / 60, 191 / 158, 511 / 539; 16 heads of 64
-    // in fp32, 12 of 33 16 / 11, 18 / 12, 26 / 34, 68 / 82.
+    // in fp32, 12 of 33 16 / 11, 18 / 12, 26 / 34, 68 / 82; 8 heads of 128 again, prefixes of 10,000, 40,000, 100,000: one sequence of a row
+    // 15.8 / 13.1, 26.4 / 24.8, 43.7 / 41.8, two 16.1 / 16.8, 26.6 / 27.1, 44.0 / 58.1, four of a row behind 100,000 45.4 / 92.
     const double places = (double)keys * kv_heads, once = n_groups * places * 2 * head_dim / 4.5e6;
     auto big_cost = [&](long long tiles) { return tiles * places * 128 * 4 * head_dim / 0.95e9; };
     const long long per = ((long long)rows + n_seqs - 1) / n_seqs * G;   // packed rows of a sequence, were all alike
     const bool big = p.own.route != ATTN_FEW && per > few_rows(head_dim);
-    const double behind = big ? big_cost(n_seqs * ((per + 127) / 128)) : n_seqs * ((per + 15) / 16) * places * (2 * head_dim + 96) / 13.7e6;
+    const long long tiles = n_seqs * (big ? (per + 127) / 128 : (per + 15) / 16);
+    const double behind = std::max(big ? big_cost(tiles) : tiles * places * (2 * head_dim + 96) / 13.7e6,
+                                   once + std::max(0ll, tiles - n_groups) * places * 2 * head_dim / 12.8e6);
     const double pass = large ? big_cost((packed + 127) / 128 + n_groups - 1) : ((packed + 15) / 16 + n_groups - 1) * places * 2 * head_dim / 14e6;
     const double apart = std::max(once, pass) + 4 + 1.2e-3 * rows * q_heads * head_dim / 128;
     const long long places_of_both = (keys + 63) / 64 * 64 + (long long)table_pages * page_tokens;
