@@ -321,16 +321,26 @@ template <bool BF, int V>
 __device__ __forceinline__ void load_weight(const NormArgs& nm, int dh, int h, int dim, bool pairs, int c, Raw<BF, V>& w) {
     if (nm.weight) load_raw<BF, V>(nm.weight, nm.per_head ? (size_t)h * dh : 0, dim, pairs, c, w);
 }
-// The chunk normed; part: the sums of squares of the head's dh / 16 chunks; down: sum_scale
-template <bool BF, int V>
-__device__ __forceinline__ void norm_chunk(const NormArgs& nm, const float* part, int dh, float down, const Raw<BF, V>& w,
-                                           float (&x)[16]) {
+// The mean square of a head; part: the sums of squares of its dh / 16 chunks.  WIDE: heads of more than 128 channels, in kernels of
+// their own (the scale in all heads' sums, 1 up to 128 channels, cost 0.3 us of a call, a branch a register too many in fp32).
+template <bool WIDE>
+__device__ __forceinline__ float mean_square(const float* part, int dh) {
     const int n = dh / 16;
-    float sum = 0.f;
+    float sum = 0.f, size = (float)dh;
+    if (!WIDE) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += i < n ? part[i] * down : 0.f;
-    for (int i = 8; i < n; ++i) sum += part[i] * down;
-    const float f = rsqrtf(sum / ((float)dh * down) + nm.eps);
+        for (int i = 0; i < 8; ++i) sum += i < n ? part[i] : 0.f;
+    } else {
+        const float down = sum_scale(dh);
+        for (int i = 0; i < n; ++i) sum += part[i] * down;
+        size *= down;
+    }
+    return sum / size;
+}
+// The chunk normed.
+template <bool BF, int V, bool WIDE>
+__device__ __forceinline__ void norm_chunk(const NormArgs& nm, const float* part, int dh, const Raw<BF, V>& w, float (&x)[16]) {
+    const float f = rsqrtf(mean_square<WIDE>(part, dh) + nm.eps);
     if (nm.weight) {
         float y[16];
         unpack(w, y);
@@ -345,14 +355,13 @@ __device__ __forceinline__ void norm_chunk(const NormArgs& nm, const float* part
 // Rows row0 .. row0 + n - 1 of x (n at most ROT_ROWS), heads of a multiple of 16 channels normed and turned, to out (a block
 // of NT threads).  lds: ROT_LDS floats and NORM_ITEMS NT more.
 constexpr int NORM_ITEMS = 2;   // chunks of a thread at once
-template <bool BF, int V, int NT>
+template <bool BF, int V, int NT, bool WIDE>
 __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& rot, const NormArgs& nm, int row0, int n,
                                           float* lds) {
     const int tid = threadIdx.x, ld = (rot.dim / 2 + 3) & ~3;
     float *cos = lds, *sin = lds + ROT_ROWS * 64, *part = lds + ROT_LDS;
     if (rot.dim) angles_of<NT>(rot, n, cos, sin, ld, [&](int r) { return a.pos + (size_t)(row0 + r) * 3; });
     const int per_head = a.dh / 16, per_row = per_head * a.heads, total = n * per_row;
-    const float down = sum_scale(a.dh);
     const int batch = NORM_ITEMS * NT / per_head * per_head;   // whole heads
     for (int first = 0; first < total; first += batch) {
         const int end = min(batch, total - first);
@@ -380,7 +389,7 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RotaryPlan& r
             if (i >= end) continue;
             Raw<BF, V> w;
             load_weight<BF, V>(nm, a.dh, hh[k], rot.dim, rot.pairs, cc[k], w);
-            norm_chunk<BF, V>(nm, part + i - cc[k], a.dh, down, w, x[k]);
+            norm_chunk<BF, V, WIDE>(nm, part + i - cc[k], a.dh, w, x[k]);
             turn_chunk<V>(rot.dim, rot.pairs, cc[k], cos + rr[k] * ld, sin + rr[k] * ld, x[k]);
             store_chunk<BF, V>(a.out, (size_t)(row0 + rr[k]) * a.out_stride + (size_t)hh[k] * a.dh, rot.dim, rot.pairs, cc[k],
                                x[k]);
@@ -428,11 +437,11 @@ __device__ __forceinline__ void norm_rows_any(const RowsArgs& a, const RotaryPla
 }
 
 // V = 0: heads of any even number of channels.
-template <bool BF, int V>
+template <bool BF, int V, bool WIDE>
 __global__ __launch_bounds__(256) void norm_rotary_k(NormRotaryArgs a) {
     __shared__ __attribute__((aligned(16))) float lds[ROT_LDS + (V ? NORM_ITEMS * 256 : 0)];
     const int row0 = blockIdx.x * a.per_block, n = min(a.rows - row0, a.per_block);
-    if constexpr (V > 0) norm_rows<BF, V, 256>(a, a.rot, a.norm, row0, n, lds);
+    if constexpr (V > 0) norm_rows<BF, V, 256, WIDE>(a, a.rot, a.norm, row0, n, lds);
     else norm_rows_any<BF, 256>(a, a.rot, a.norm, row0, n, lds);
 }
 
@@ -498,7 +507,7 @@ __global__ __launch_bounds__(WT, NORM ? 3 : 4) void cache_write_k(WriteArgs a) {
         const int live = a.seq.offsets ? min(a.seq.offsets[a.seq.n_seqs], a.seq.rows) : min(a.seq.n_seqs, a.seq.rows);
         const int n = min(live, b + a.q_rows) - row0;
         if (n <= 0) return;
-        if (NORM && a.q_norm.on) norm_rows<BF, V, WT>(q, a.rot, a.q_norm, row0, n, (float*)lds);
+        if (NORM && a.q_norm.on) norm_rows<BF, V, WT, false>(q, a.rot, a.q_norm, row0, n, (float*)lds);
         else turn_rows<BF, V, WT>(q, a.rot, row0, n, (float*)lds);
         return;
     }
@@ -585,7 +594,7 @@ __global__ __launch_bounds__(WT, NORM ? 3 : 4) void cache_write_k(WriteArgs a) {
             if (normed) {
                 Raw<BF, V> w;
                 load_weight<BF, V>(a.k_norm, dh, h0 + hh[k], dim, a.rot.pairs, cc[k], w);
-                norm_chunk<BF, V>(a.k_norm, part + tid + k * WT - cc[k], dh, 1.f, w, x[k]);   // (dh <= 128)
+                norm_chunk<BF, V, false>(a.k_norm, part + tid + k * WT - cc[k], dh, w, x[k]);
             }
             turn_chunk<V>(dim, a.rot.pairs, cc[k], cos + tt[k] * ald, sin + tt[k] * ald, x[k]);
             float most = 0.f;   // a NaN does not count
@@ -832,14 +841,16 @@ void launch_norm_rotary(bool bf, NormRotaryArgs a, hipStream_t s) {
     };
     a.per_block = rows_a_block(a.heads, a.dh, chunks ? 8 : 1);
     const dim3 grid((unsigned)(((long long)a.rows + a.per_block - 1) / a.per_block));
-    auto go = [&](auto v) {
+    auto launch = [&](auto v, auto wide) {
         constexpr int V = decltype(v)::value;
-        bf ? norm_rotary_k<true, V><<<grid, 256, 0, s>>>(a) : norm_rotary_k<false, V><<<grid, 256, 0, s>>>(a);
+        constexpr bool W = decltype(wide)::value;
+        bf ? norm_rotary_k<true, V, W><<<grid, 256, 0, s>>>(a) : norm_rotary_k<false, V, W><<<grid, 256, 0, s>>>(a);
     };
+    auto go = [&](auto v) { a.dh > 128 ? launch(v, std::true_type()) : launch(v, std::false_type()); };
     if (fits(8, 16)) go(std::integral_constant<int, 8>());
     else if (fits(4, 4 * el)) go(std::integral_constant<int, 4>());
     else if (chunks) go(std::integral_constant<int, 1>());
-    else go(std::integral_constant<int, 0>());
+    else launch(std::integral_constant<int, 0>(), std::true_type());
 }
 
 void launch_cache_write(bool bf, WriteArgs a, hipStream_t s) {
