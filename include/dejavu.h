@@ -403,7 +403,8 @@ typedef struct dv_cache {
  * rows means nothing.  The others have
  * starts[s] = lengths[s] and lengths_out[s] = lengths[s] + counts[s]; those that end -1 and 0.  cursor_out:
  * taken, given, and the pages that were lacking (0: every sequence that its table holds was
- * extended).  For a row at place p of its sequence positions [rows, 3] become (p, p, p) (NULL: not wanted) and slots
+ * extended).  For a row at place p of its sequence positions [rows, 3] become (p, p, p) (NULL: not wanted; p counts the
+ * sequence's own places: rows behind a shared prefix that go on from its positions need the prefix's length added) and slots
  * [rows] page * page_tokens + p % page_tokens, or -1 where its sequence was not extended or has no page there (NULL:
  * not wanted); those of rows past the last sequence's stay as they are, and rows from `rows` on have none.
  * No page may stand in two entries or in the ring as well.  Outputs must not overlap lengths, counts and cursor (a
@@ -486,9 +487,11 @@ int dv_cache_attention(const dv_cache* cache, int n_seqs, const int32_t* table, 
 /* dv_cache_attention with a window: of the places that a row would see there, the first e of its
  * sequence, it sees those from e - window on, and the first `sinks`.  Pages between that no row of a call sees may hold
  * anything, codes and scales, and need not be there (a table entry that is no page): the keys that a call takes time for
- * are the window's and the sinks', in whole steps of 64, whatever the sequences' lengths.  A window of 2^30 and more sees all (Section 2.3's attention over
- * the memory of Section 5.2, bounded for streams that do not end).  Errors: those of
- * dv_cache_attention, and DV_EINVAL for window < 1, sinks < 0.  The workspace's size depends on both. */
+ * are the window's and the sinks', in whole steps of 64, whatever the sequences' lengths.  A window of 2^30 and more sees all.  No call
+ * takes pages out of a table as they leave the window (dv_cache_extend takes back those of sequences that end): a caller
+ * that hands them out again enters no page in their place (Section 2.3's attention over the memory of Section 5.2, its time bounded
+ * for streams that do not end).  Errors: those of dv_cache_attention, and DV_EINVAL for window < 1, sinks < 0.  The workspace's size
+ * depends on both. */
 int dv_cache_attention_window_workspace(const dv_cache* cache, int n_seqs, int table_pages,
                                         int with_offsets, int dtype, int rows, int q_heads,
                                         int max_rows, int window, int sinks, size_t* bytes);
@@ -504,8 +507,11 @@ int dv_cache_attention_window(const dv_cache* cache, int n_seqs, const int32_t* 
  * n_groups = 1: all) see the first prefix_lengths[g] places (device int32, cut to the table, negative means 0)
  * of prefix g, which lie in the pages of its row of prefix_table [n_groups, prefix_table_pages], all of
  * them, and then their own sequence's as in dv_cache_attention (table, lengths and causal are about
- * those).  Sequences of no group see their own places only.  A prefix is read once for all rows of its group.  (Questions
- * about one video, Section 2.1's query engine.)  Errors: those of dv_cache_attention, and DV_EINVAL for
+ * those).  Sequences of no group see their own places only.  A prefix is stored once; its keys are loaded once for every 16 or
+ * 128 packed rows of its group (from the caches where they hold it), or, where prefixes are short, for every tile of a sequence.  Roundings
+ * follow the tiles, as in dv_cache_attention: with bf16 queries it is the rows of a group, not of a sequence, that give the prefix's
+ * keys to large tiles, whose probabilities are rounded to bf16 (outputs 0.0019 off, relative, small tiles 0.0016).  (Questions about one
+ * video, Section 2.1's query engine.)  Errors: those of dv_cache_attention, and DV_EINVAL for
  * n_groups or prefix_table_pages < 1, prefix_table_pages * page_tokens > 2^30, prefix_table or prefix_lengths
  * NULL, groups NULL with n_groups > 1. */
 int dv_cache_attention_shared_workspace(const dv_cache* cache, int n_seqs, int table_pages,

@@ -516,7 +516,7 @@ __device__ __forceinline__ void attend_small(const CacheAttnArgs& a, Small<DH>& 
 // decoded to bf16 once per block into one of two LDS buffers, while the other is read: a
 // wavefront's matrix work on a step (1024 clocks of a SIMD at 128 channels) needs 32 KB of it.
 // 4096 rows of two sequences of 5000 to 6144 keys, 32 heads of 128 on 8: 348 us, 968 TFLOP/s (a large library
-// product: 1210).  By the counters matrix units are busy 42 % of the time, vector units 49 (59 with exponentials at a
+// product: 1210 to 1360, by the card).  By the counters matrix units are busy 42 % of the time, vector units 49 (59 with exponentials at a
 // quarter of the rate), LDS 37 (fragments read by four wavefronts each, decoded codes written), at 1.75 wavefronts a
 // SIMD: they overlap in part.
 // Row m of a 32-key score block is key m with bits 2 and 3 exchanged, so that lane half hl ends up with

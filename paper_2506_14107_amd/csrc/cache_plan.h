@@ -231,7 +231,10 @@ inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets
         const long long keys = keys_of(shift);
         c.slots = tile_slots(offsets, n_seqs, rows, G, shift);
         const long long units = std::max(1ll, c.slots * kv_heads);
-        // (windows bound all sequences' keys alike: 64 of up to 2433 keys of 8 heads of 128 in one split 55 us, in two 58 and a join)
+        // Windows shorter than most sequences leave all of them as many keys: resident blocks (two a unit) are counted to the nearest split
+        // of a tile and head, and the cap does not hold.  Streams of 1 to 12,000 places of 8 heads of 128, us one split / in splits of 2048 / without a window: 64 with windows of 1024 31.7
+        // / 32.2 / 138, 2048 48.6 / 55.6, 4096 87 / 94; 70 with 2048 60.5 / 62.3 / 180, 100 92 / 96 / 251, 128 122 / 130 / 344.  Windows that
+        // hold most of the sequences leave them uneven, and lose by it: 64 with 8192 140 / 130 / 138, 11,900 158 / 139 / 139.
         const long long most = std::min<long long>(MAX_SPLITS, std::max(1ll, (2 * unit + (window ? units / 2 : 0)) / units));
         long long chunk = (keys + most - 1) / most;
         if (n_seqs > 1 && units < 16 * unit && !window) chunk = std::min(chunk, cap);

@@ -3,7 +3,7 @@
 // rows; a row's outputs are joined from the splits of both.  One launch takes both parts (two, one behind the other: 208 us of a call
 // with small tiles, 64 answers of up to 700 own keys behind 50,001, 8 heads of 128 with 4 queries each); with large tiles 91: the
 // matrix work on the prefix 51, starting, own keys and 34 MB of partial results the rest of 85, the join 11.  8 answers behind
-// 100,003 keys read the prefix at 4 TB/s (51 us and 8): two small tiles of 16 rows share it in a cache.
+// 100,003 keys read the prefix at 4 TB/s (51 us and 8), two small tiles of 16 rows sharing it in a cache; one sequence's tiles read at 5.7.
 #include "cache_attn.h"
 
 namespace dv {

@@ -704,7 +704,8 @@ def extend(table, lengths, counts, ring, cursor, page_tokens, rows, out=None, st
     offsets, starts and lengths are what TokenCache.write and attention take; starts is -1 for
     sequences that end and for those that there were not enough pages for, which keep their length;
     cursor[2] is how many pages were lacking.  The lengths and cursor returned are buffers of their
-    own: a loop passes them to its next call.  Entries of positions and slots past the last row are
+    own: a loop passes them to its next call.  Positions count a sequence's own places: behind a prefix
+    that it shares the caller adds the prefix's length.  Entries of positions and slots past the last row are
     undefined in new tensors and left as they were in those of `out`."""
     _need_torch()
     index = table.get_device()
@@ -867,7 +868,8 @@ class TokenCache:
         see no later ones.  max_rows: an upper bound of any sequence's rows, if known.  workspace: a
         uint8 tensor to use (see attention_workspace) instead of one of the call's own.
         window > 0: of the e places that a row would see it sees those from e - window on and the
-        first `sinks`; pages between need not be there."""
+        first `sinks`; pages between may hold anything and need not be there (the table is the
+        caller's: nothing takes them out of it)."""
         index = self.index
         if _elsewhere(index, stream):
             with _Away(index, stream):
