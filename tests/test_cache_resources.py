@@ -100,7 +100,7 @@ def test_what_spills(scratch):
     for k, v in scratch.items():
         if re.search(r"cache_(attn|window|behind|shared|join|read|extend)|norm_rotary_k", k):
             assert v == 0, k
-    most = {"Lb1ELi8": 20, "Lb0ELi8": 0, "Lb1ELi4": 44, "Lb0ELi4": 0}
+    most = {"Lb1ELi8": 20, "Lb0ELi8": 0, "Lb1ELi4": 28, "Lb0ELi4": 0}
     writes = {k: v for k, v in scratch.items() if "cache_write_k" in k and "Li1E" not in k}
     assert len(writes) == 14
     for k, v in writes.items():

@@ -6,7 +6,7 @@ from paper_2506_14107_amd import dejavu as dj
 
 from .gpu_util import require_gpu
 from .test_gpu_cache import Pair, close, ints, normal
-from .test_gpu_norm import norm, rounded
+from .test_gpu_norm import norm, rounded, turned
 
 pytestmark = pytest.mark.gpu
 
@@ -25,6 +25,23 @@ def test_heads_of_the_largest_magnitudes(dh, dtype):
     for weight, weight64 in ((None, None), (w, w64)):
         want, err = norm(x64, weight64, 1e-6, dh)
         close(dj.norm_rotary(x, weight), want, rounded(want, err, dtype), f"{dh} channels")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sec,layout,first", [((8, 12, 12), "halves", 0), ((4, 4, 4), "pairs", 0), ((5, 3, 3), "halves", 0), ((8, 12, 12), "pairs", 4),
+                                              ((8, 12, 12), "halves", 1), (None, "halves", 0)])
+@pytest.mark.parametrize("dh", [144, 256, 1040])
+def test_wide_heads_normed_and_turned(dh, sec, layout, first, dtype):
+    """Heads of more than 128 channels by eights, fours and ones, rows aligned and not."""
+    rng = np.random.default_rng(6)
+    flat, flat64 = normal(rng, first + 9 * 3 * dh, dtype, 3.0)
+    x, x64 = flat[first:].view(9, 3, dh), flat64[first:].reshape(9, 3, dh)
+    w, w64 = normal(rng, (3, dh), dtype)
+    pos = rng.integers(-1000, 1000, (9, 3))
+    y, err = norm(x64, w64, 1e-6, dh)
+    want, err = turned(y, err, pos, sec, layout, 1000)
+    got = dj.norm_rotary(x, w, 1e-6, *((ints(pos), dj.Rotary(sec, layout)) if sec else ()))
+    close(got, want, rounded(want, err, dtype), f"{dh} {sec}")
 
 
 @pytest.mark.parametrize("eps", [1e-6, 1e-37, 1e-40, 2.0 ** -149])

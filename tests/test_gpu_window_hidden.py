@@ -20,10 +20,13 @@ CASES = {
 }
 
 
-@pytest.mark.parametrize("what", [float("nan"), float("inf"), 3e38, -1.0])
-@pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("name", CASES)
+NAN, INF = float("nan"), float("inf")
+# (fp32 takes small tiles alone; scales that are numbers tell less than those that are none)
+RUNS = [(name, dtype, causal, what) for name in CASES for dtype in (("bf16",) if CASES[name][0] > 2 else ("f32", "bf16"))
+        for causal in (True, False) for what in ((NAN, INF, 3e38, -1.0) if name == "rows-32" else (NAN, INF))]
+
+
+@pytest.mark.parametrize("name,dtype,causal,what", RUNS)
 def test_pages_that_no_row_sees_may_hold_anything(name, dtype, causal, what):
     torch = require_gpu()
     heads, group, dh, pt, counts, lengths = CASES[name]
