@@ -232,9 +232,10 @@ inline CacheAttnPlan cache_attn_plan(bool bf, int n_seqs, int rows, bool offsets
         c.slots = tile_slots(offsets, n_seqs, rows, G, shift);
         const long long units = std::max(1ll, c.slots * kv_heads);
         // Windows shorter than most sequences leave all of them as many keys: resident blocks (two a unit) are counted to the nearest split
-        // of a tile and head, and the cap does not hold.  Streams of 1 to 12,000 places of 8 heads of 128, us one split / in splits of 2048 / without a window: 64 with windows of 1024 31.7
-        // / 32.2 / 138, 2048 48.6 / 55.6, 4096 87 / 94; 70 with 2048 60.5 / 62.3 / 180, 100 92 / 96 / 251, 128 122 / 130 / 344.  Windows that
-        // hold most of the sequences leave them uneven, and lose by it: 64 with 8192 140 / 130 / 138, 11,900 158 / 139 / 139.
+        // of a tile and head, and the cap does not hold.  Streams of 1 to 12,000 places of 8 heads of 128, us one split / in splits of
+        // 2048 / without a window: 64 with windows of 1024 31.7 / 32.2 / 138, 2048 48.6 / 55.6, 4096 87 / 94; 70 with 2048 60.5 / 62.3
+        // / 180, 100 92 / 96 / 251, 128 122 / 130 / 344.  Windows that hold most of the sequences leave them uneven, and lose by it: 64
+        // with 8192 140 / 130 / 138, 11,900 158 / 139 / 139.
         const long long most = std::min<long long>(MAX_SPLITS, std::max(1ll, (2 * unit + (window ? units / 2 : 0)) / units));
         long long chunk = (keys + most - 1) / most;
         if (n_seqs > 1 && units < 16 * unit && !window) chunk = std::min(chunk, cap);
@@ -278,12 +279,13 @@ inline CacheSharedPlan cache_shared_plan(bool bf, int n_seqs, int rows, bool off
     p.prefix.route = !large ? ATTN_FEW : n_groups == 1 ? ATTN_MANY : ATTN_BOTH;
     // Tiles of the sequences take the prefix themselves where that is less than a pass of its own costs.  Estimates in us: a
     // large tile takes its keys at 0.95 PFLOP/s; a small one 2 head_dim + 96 bytes a key at 13.7 TB/s, most of them from the
-    // caches, and in a pass of its own, whose blocks are cut to fill the chip, 2 head_dim at 14; a pass no faster than the memory has
-    // them once, tiles that repeat it no faster than that and the caches (12.8 TB/s) the rest.  Two parts are 4 us and 1.2 ns a row and head of 128 channels more (partial results and their join).  us of a call, two
-    // parts / behind, 8 heads of 128 with 4 queries each, prefixes of 128, 512, 2048, 8192: 64 sequences of a row 14 / 11, 15 / 14,
-    // 21 / 35, 37 / 105; 12 of 33 29 / 16, 33 / 24, 44 / 62, 90 / 178; 64 of 40 141 / 37, 125 / 60, 191 / 158, 511 / 539; 16 heads of 64
-    // in fp32, 12 of 33 16 / 11, 18 / 12, 26 / 34, 68 / 82; 8 heads of 128 again, prefixes of 10,000, 40,000, 100,000: one sequence of a row
-    // 15.8 / 13.1, 26.4 / 24.8, 43.7 / 41.8, two 16.1 / 16.8, 26.6 / 27.1, 44.0 / 58.1, four of a row behind 100,000 45.4 / 92.
+    // caches, and in a pass of its own, whose blocks are cut to fill the chip, 2 head_dim at 14; a pass no faster than the memory
+    // has them once, tiles that repeat it no faster than that and the caches (12.8 TB/s) the rest.  Two parts are 4 us and 1.2 ns
+    // a row and head of 128 channels more (partial results and their join).  us of a call, two parts / behind, 8 heads of 128
+    // with 4 queries each, prefixes of 128, 512, 2048, 8192: 64 sequences of a row 14 / 11, 15 / 14, 21 / 35, 37 / 105; 12 of 33
+    // 29 / 16, 33 / 24, 44 / 62, 90 / 178; 64 of 40 141 / 37, 125 / 60, 191 / 158, 511 / 539; 16 heads of 64 in fp32, 12 of 33 16
+    // / 11, 18 / 12, 26 / 34, 68 / 82; 8 heads of 128 again, prefixes of 10,000, 40,000, 100,000: one sequence of a row 15.8 /
+    // 13.1, 26.4 / 24.8, 43.7 / 41.8, two 16.1 / 16.8, 26.6 / 27.1, 44.0 / 58.1, four of a row behind 100,000 45.4 / 92.
     const double places = (double)keys * kv_heads, once = n_groups * places * 2 * head_dim / 4.5e6;
     auto big_cost = [&](long long tiles) { return tiles * places * 128 * 4 * head_dim / 0.95e9; };
     const long long per = ((long long)rows + n_seqs - 1) / n_seqs * G;   // packed rows of a sequence, were all alike
